@@ -441,6 +441,122 @@ int32_t ssa_decode_attn_blockmask(const ssa_attn_desc* desc, const void* q, cons
                                   void* stream);
 
 /*
+ * Attention of a request's newest tokens, each over its own past (outside the
+ * paper, whose kernel serves one token per step and leaves prompts to others,
+ * Sec. "Token generation"): prompt chunks, drafted tokens, single tokens.  The
+ * request's last q_lens[b] positions are the step's tokens, their K/V already
+ * in the cache; token t of them sits at position pos = ctx_lens[b] -
+ * q_lens[b] + t and attends to
+ *     { j <= pos :  j > pos - window  or  j < sinks }
+ * that is to the newest `window` positions, its own included (0: to all), and to
+ * the first `sinks` positions whatever the window.  Each row is an instance of
+ * the Background equations over that mask; out and lse as in
+ * ssa_decode_attn_sparse.  Row t of head h of q is at q + b*q_stride_b +
+ * h*q_stride_h + t*q_stride_t, of out likewise, its lse at
+ * lse[(b*H + h)*n_q + t].  Rows t >= q_lens[b] are neither read nor written.
+ * A token whose position is negative (q_lens[b] > ctx_lens[b]) has a zero row
+ * and lse = -inf, and so has one whose every score is -inf.  What lies in
+ * positions that no token sees is not used, whatever it is; a NaN or an
+ * infinity in a row of K or V reaches the tokens that see the row only.
+ *   desc     host; max_ctx rows of cache per request.  All its types: F16,
+ *            BF16, FP8_E4M3; H_kv dividing H
+ *   window   host; n_q >= 1 query rows are laid out per head and request,
+ *            H*n_q <= 2^24
+ *   q_lens   dev int32 [B], 0 <= q_lens[b] <= n_q, or NULL: n_q tokens each.
+ *            Larger values and ctx_lens[b] > max_ctx are clamped
+ *            (SSA_DEV_BAD_COUNT)
+ *   paging   host or NULL (a contiguous cache); as for the paged calls: the
+ *            cache pointers are then the pools, positions on pages outside
+ *            [0, n_pages) are skipped (SSA_DEV_BAD_INDEX) where a token sees
+ *            them, and table entries of positions that none sees are not used
+ *   workspace  dev, 16-byte aligned, >= ssa_attn_window_workspace_bytes(desc,
+ *            window) (0: invalid arguments); needs no initialisation
+ * Few rows per K/V head (tokens x grouped heads) split a long context over the
+ * GPU and join the parts in a second launch.
+ * Errors: SSA_ERR_NULL, SSA_ERR_SHAPE, SSA_ERR_DTYPE, SSA_ERR_ALIGN,
+ * SSA_ERR_WORKSPACE, SSA_ERR_UNSUPPORTED, SSA_ERR_CUDA.
+ */
+typedef struct {
+  int32_t n_q;                 /* query rows laid out per head and request        */
+  int32_t window;              /* newest positions a token sees; 0: no limit      */
+  int32_t sinks;               /* first positions that every token sees           */
+  int64_t q_stride_t, o_stride_t;
+  const int32_t* q_lens;       /* dev [B] or NULL                                 */
+  const ssa_paging* paging;    /* host or NULL                                    */
+} ssa_window;
+
+size_t ssa_attn_window_workspace_bytes(const ssa_attn_desc* desc, const ssa_window* window);
+int32_t ssa_attn_window(const ssa_attn_desc* desc, const ssa_window* window, const void* q, const void* k_cache,
+                        const void* v_cache, const int32_t* ctx_lens, void* out, float* lse, void* workspace,
+                        size_t workspace_bytes, uint32_t* dev_status, void* stream);
+
+/*
+ * ssa_attn_window, and how much weight every cached position was given (outside
+ * the paper: a measured counterpart to the spans that its model names):
+ *   mass_out[b*mass_stride + j] = decay * mass_in[b*mass_stride + j]
+ *                               + sum_{h,t} exp(s[h,t,j] - lse[h,t])
+ * for 0 <= j < ctx_lens[b], the sum over the request's heads and tokens that
+ * see j; the first term is 0 for the step's own positions (j >= ctx_lens[b] -
+ * q_lens[b]), whatever mass_in holds there, and everywhere where mass_in is
+ * NULL.  Entries from ctx_lens[b] on are left as they are.  mass_in and
+ * mass_out may be the same array (dev float, rows mass_stride >= max_ctx
+ * apart).  The sums are fp32 in a fixed order: the same inputs give the same
+ * bits.  H*n_q <= SSA_MASS_MAX_ROWS, else SSA_ERR_SHAPE.
+ * Workspace: ssa_attn_mass_workspace_bytes; it holds all the scores of the
+ * step, 4*B*H*n_q*max_ctx bytes and some.  The rest as for ssa_attn_window.
+ */
+#define SSA_MASS_MAX_ROWS 1024
+size_t ssa_attn_mass_workspace_bytes(const ssa_attn_desc* desc, const ssa_window* window);
+int32_t ssa_attn_mass(const ssa_attn_desc* desc, const ssa_window* window, const void* q, const void* k_cache,
+                      const void* v_cache, const int32_t* ctx_lens, void* out, float* lse, const float* mass_in,
+                      float* mass_out, int64_t mass_stride, float decay, void* workspace, size_t workspace_bytes,
+                      uint32_t* dev_status, void* stream);
+
+/*
+ * The positions that a budget keeps, as index lists: the selection that the
+ * sparse calls attend to and that ssa_cache_compact moves, made from the sums
+ * of ssa_attn_mass (or any other score) instead of from spans.  With n =
+ * ctx_lens[b]: all positions where n <= budget; else the first `sinks`, the
+ * last `recent`, and of those between the budget - sinks - recent with the
+ * largest mass, of equal ones the lowest positions (-0 equals 0; NaN ranks
+ * below everything).  index[b*index_stride ..] ascends as ssa_spans_to_index
+ * writes it, counts[b] = min(n, budget); entries past it are left untouched.
+ *   mass       dev float, rows of max_ctx entries mass_stride apart
+ *   ctx_lens   dev int32 [B]; above max_ctx: clamped (SSA_DEV_BAD_COUNT)
+ *   index      dev int32 [B * index_stride]; counts dev int32 [B] (written)
+ * Errors: SSA_ERR_NULL, SSA_ERR_SHAPE (B, max_ctx, index_stride, mass_stride <
+ * max_ctx), SSA_ERR_CAPACITY (budget <= 0 or above index_stride; sinks or
+ * recent negative or together above the budget), SSA_ERR_CUDA.
+ */
+int32_t ssa_mass_to_index(const float* mass, int64_t mass_stride, const int32_t* ctx_lens, int32_t B, int32_t max_ctx,
+                          int32_t budget, int32_t sinks, int32_t recent, int32_t* index, int32_t index_stride,
+                          int32_t* counts, uint32_t* dev_status, void* stream);
+
+/*
+ * Moves the kept rows of a cache to its front, in place: for every request, K/V
+ * head and i < counts[b], row index[b*index_stride + i] of K and of V becomes
+ * row i, and entry i of mass (dev float, rows mass_stride >= max_ctx apart, or
+ * NULL) likewise.  Afterwards counts[b] is the request's context length.  Rows
+ * from counts[b] on keep what they held.  The lists must ascend strictly
+ * within [0, ctx_lens[b]), as ssa_mass_to_index and ssa_spans_to_index write
+ * them; an entry outside that range moves nothing (SSA_DEV_BAD_INDEX), and
+ * lists in another order leave unspecified rows.  counts[b] above max_selected
+ * or ctx_lens[b] is clamped (SSA_DEV_BAD_COUNT).
+ * Paged caches (paging non-NULL, strides as for the paged calls): rows move
+ * between the request's own pages; afterwards the pages behind counts[b] are
+ * free.  A row that stays in its place is not written, so requests may share
+ * pages that hold such rows only; other pages must belong to one request.
+ * A row whose page, or whose new row's page, does not exist is not moved
+ * (SSA_DEV_BAD_INDEX).
+ *   desc   host; the fields of q and out are checked but not used
+ * Errors: SSA_ERR_NULL, SSA_ERR_SHAPE, SSA_ERR_DTYPE, SSA_ERR_ALIGN,
+ * SSA_ERR_CAPACITY, SSA_ERR_UNSUPPORTED, SSA_ERR_CUDA.
+ */
+int32_t ssa_cache_compact(const ssa_attn_desc* desc, const ssa_paging* paging, void* k_cache, void* v_cache,
+                          const int32_t* ctx_lens, const int32_t* index, int32_t index_stride, const int32_t* counts,
+                          int32_t max_selected, float* mass, int64_t mass_stride, uint32_t* dev_status, void* stream);
+
+/*
  * One decode step of the method in one call (Sec. "Self-selected attention
  * span", Inference: token generation restricted to the selected spans):
  * ssa_spans_to_index followed by ssa_decode_attn_sparse on `stream`, with the

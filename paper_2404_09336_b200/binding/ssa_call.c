@@ -17,13 +17,15 @@
 #define ENTRY_POINTS(X)                                                                                              \
   X(spans_to_index) X(decode_attn_sparse) X(decode_attn_spans) X(decode_attn_sparse_multiq) X(decode_attn_dense_multiq) \
   X(spans_to_blockmask) X(decode_attn_blockmask) X(decode_attn_sparse_paged) X(decode_attn_dense_paged)               \
-  X(refs_to_index) X(refs_to_spans) X(decode_step) X(decode_attn_sparse_noalloc) X(decode_attn_dense)
+  X(refs_to_index) X(refs_to_spans) X(decode_step) X(decode_attn_sparse_noalloc) X(decode_attn_dense)                 \
+  X(attn_window) X(attn_mass) X(mass_to_index) X(cache_compact)
 
 /* Structures that a caller fills.  Only instances of the class that bind() was given for one are taken (without a class:
  * buffers of its exact size), so that no other structure and no other buffer is read as sizes and strides. */
-enum { kDesc, kStep, kPaging, kStructures };
-static const char* const structure_name[kStructures] = {"ssa_attn_desc", "ssa_step", "ssa_paging"};
-static const size_t structure_size[kStructures] = {sizeof(ssa_attn_desc), sizeof(ssa_step), sizeof(ssa_paging)};
+enum { kDesc, kStep, kPaging, kWindow, kStructures };
+static const char* const structure_name[kStructures] = {"ssa_attn_desc", "ssa_step", "ssa_paging", "ssa_window"};
+static const size_t structure_size[kStructures] = {sizeof(ssa_attn_desc), sizeof(ssa_step), sizeof(ssa_paging),
+                                                     sizeof(ssa_window)};
 
 typedef struct {
 #define X(name) __typeof__(&ssa_##name) name;
@@ -37,7 +39,7 @@ typedef struct {
 enum { kMost = 24 };
 typedef struct {
   void* p[kMost];          /* addresses in the order of the format's D, t, r and w */
-  int64_t v[kMost];        /* integers in the order of its i, n, r (row stride) and w (bytes) */
+  int64_t v[kMost];        /* integers in the order of its i, n, r (row stride) and w (bytes), the bits of its f */
   Py_buffer held[4];
   int n_held;
 } Args;
@@ -102,7 +104,7 @@ static int structure(const State* st, int which, PyObject* o, Py_buffer* held) {
   return -1;
 }
 
-/* format: D ssa_attn_desc, S ssa_step, P ssa_paging or None, t tensor or None, r tensor or None and its row stride,
+/* format: D ssa_attn_desc, S ssa_step, P ssa_paging or None, Q ssa_window, f number as a float, t tensor or None, r tensor or None and its row stride,
  * w tensor or None and its bytes, i integer, n tensor and its number of elements. */
 static int parse(const State* st, Args* x, const char* name, const char* format, PyObject* const* a, Py_ssize_t n) {
   int np = 0, nv = 0;
@@ -119,9 +121,17 @@ static int parse(const State* st, Args* x, const char* name, const char* format,
         if (o == Py_None) { x->p[np++] = NULL; break; }  /* fall through */
       case 'D':
       case 'S':
-        if (structure(st, format[i] == 'D' ? kDesc : format[i] == 'S' ? kStep : kPaging, o, &x->held[x->n_held]) < 0) goto bad;
+      case 'Q':
+        if (structure(st, format[i] == 'D' ? kDesc : format[i] == 'S' ? kStep : format[i] == 'Q' ? kWindow : kPaging, o, &x->held[x->n_held]) < 0) goto bad;
         x->p[np++] = x->held[x->n_held++].buf;
         break;
+      case 'f': {
+        const float f = (float)PyFloat_AsDouble(o);
+        if (PyErr_Occurred()) goto bad;
+        x->v[nv] = 0;
+        memcpy(&x->v[nv++], &f, sizeof f);
+        break;
+      }
       case 't':
         if (address(st, o, &x->p[np++]) < 0) goto bad;
         break;
@@ -158,7 +168,7 @@ bad:
     const State* st = (const State*)PyModule_GetState(self);                                         \
     Args x;                                                                                          \
     int32_t rc;                                                                                      \
-    if (!st->name) { PyErr_SetString(PyExc_RuntimeError, "no library bound"); return NULL; }         \
+    if (!st->name) { PyErr_SetString(PyExc_RuntimeError, "no library bound that has it"); return NULL; }         \
     if (parse(st, &x, #name, format, a, n) < 0) return NULL;                                   \
     void** const p = x.p;                                                                            \
     const int64_t* const v = x.v;                                                                    \
@@ -169,6 +179,11 @@ bad:
     release(&x);                                                                                     \
     return PyLong_FromLong(rc);                                                                      \
   }
+static float number(const int64_t* v) {
+  float f;
+  memcpy(&f, v, sizeof f);
+  return f;
+}
 #define I(k) ((int32_t)v[k])
 #define STREAM(k) ((void*)(uintptr_t)v[k])
 
@@ -196,6 +211,15 @@ CALL(decode_attn_sparse_noalloc, "Dtttt" "rtitt" "ti",
 CALL(decode_attn_dense, "Dtttt" "tt" "wti",
      (p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], (size_t)v[0], p[8], STREAM(1)))
 
+CALL(attn_window, "DQtttt" "tt" "wti",
+     (p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], (size_t)v[0], p[9], STREAM(1)))
+CALL(attn_mass, "DQtttt" "tttrf" "wti",
+     (p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], v[0], number(&v[1]), p[10], (size_t)v[2], p[11], STREAM(3)))
+CALL(mass_to_index, "rniiii" "rtti",
+     (p[0], v[0], p[1], I(1), I(2), I(3), I(4), I(5), p[2], I(6), p[3], p[4], STREAM(7)))
+CALL(cache_compact, "DPtttrti" "rti",
+     (p[0], p[1], p[2], p[3], p[4], p[5], I(0), p[6], I(1), p[7], v[2], p[8], STREAM(3)))
+
 static ssa_anchor_tables tables(void* const* p) {
   ssa_anchor_tables t;
   memset(&t, 0, sizeof t);
@@ -214,9 +238,15 @@ static PyObject* bind_library(PyObject* self, PyObject* addresses) {
   {                                                                                 \
     PyObject* o = PyMapping_GetItemString(addresses, "ssa_" #name);                 \
     int64_t at = 0;                                                                 \
-    if (!o) return NULL;                                                            \
-    const int rc = integer(o, &at);                                                 \
-    Py_DECREF(o);                                                                   \
+    int rc = 0;                                                                     \
+    if (o) {                                                                        \
+      rc = integer(o, &at);                                                         \
+      Py_DECREF(o);                                                                 \
+    } else if (PyErr_ExceptionMatches(PyExc_KeyError)) {                            \
+      PyErr_Clear(); /* a library without it: its call raises */                    \
+    } else {                                                                        \
+      rc = -1;                                                                      \
+    }                                                                               \
     if (rc < 0) return NULL;                                                        \
     st->name = (__typeof__(st->name))(uintptr_t)at;                                 \
   }

@@ -922,9 +922,7 @@ static bool make_plan_blockmask(const ssa_attn_desc* d, int block_size, int max_
   return true;
 }
 
-static bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
-
-static int32_t check_desc(const ssa_attn_desc* d) {
+int32_t check_desc(const ssa_attn_desc* d) {
   if (d->B <= 0 || d->H <= 0 || d->max_ctx <= 0 || d->B > 65535 || d->H > 65535) return SSA_ERR_SHAPE;
   if (d->D != 64 && d->D != 128) return SSA_ERR_UNSUPPORTED;
   if (d->H_kv <= 0 || d->H % d->H_kv != 0) return SSA_ERR_UNSUPPORTED;

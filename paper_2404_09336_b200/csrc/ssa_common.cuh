@@ -16,6 +16,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 // Per-thread bookkeeping shared by the entry points (defined in ssa_api.cu).
 void note_launches(int n);
 void take_kernel_events(cudaEvent_t* begin, cudaEvent_t* end);
+int32_t check_desc(const ssa_attn_desc* d);   // status of a descriptor (defined in decode_attn.cu)
+int32_t check_paging(const ssa_paging* pg, int32_t max_ctx);   // status of a paged cache (defined in window_attn.cu)
 int sm_count();   // multiprocessors of the current device (cached; no synchronisation)
 // Bytes from p to the end of the allocation it lies in, as far as that is device memory mapped as a whole; else 0.  Reading
 // these is safe whatever offsets said that they are a list.  `known`: an allocation asked for before, which may hold p too.
@@ -26,6 +28,8 @@ inline int32_t readable_entries(const void* p, Allocation* known) {
   const size_t n = readable_bytes(p, known) / sizeof(Entry);
   return n < 0x7fffffff ? (int32_t)n : 0x7fffffff;
 }
+
+inline bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 // Programmatic dependent launch.  Every kernel of the library is launched
 // with the programmatic-serialization attribute: its blocks may become

@@ -1,0 +1,71 @@
+// What the kernels of the window attention share: parameters, and which positions a run of query rows sees.
+#pragma once
+#include "ssa_common.cuh"
+
+namespace ssa {
+
+struct WindowParams {
+  const void *q, *k, *v;
+  void* out;
+  float* lse;
+  const int32_t *ctx_lens, *q_lens, *page_table;
+  float2* ws_ml;            // [B][H][n_q][n_splits]: running maximum (log2 units) and sum of a split
+  float* ws_acc;            // [B][H][n_q][n_splits][D]
+  float* ws_s;              // [B][H][n_q][s_pitch]: scores in log2 units, for the kernel that adds the weights up
+  const float* mass_in;
+  float* mass_out;
+  uint32_t* status;
+  int64_t q_sb, q_sh, q_st, o_sb, o_sh, o_st, k_sb, k_sh, v_sb, v_sh, mass_stride;
+  int k_st, v_st;
+  int B, H, H_kv, group, n_q, max_ctx, window, sinks, n_splits, s_pitch;
+  int page_table_stride, page_shift, n_pages, out_f32;
+  float scale_log2, decay;
+};
+
+// Context length and new tokens of a request, clamped to what the call allows.
+__device__ __forceinline__ void window_sizes(const WindowParams& p, int b, int& ctx, int& n_new, uint32_t& flags) {
+  ctx = p.ctx_lens[b];
+  n_new = p.q_lens ? p.q_lens[b] : p.n_q;
+  if (ctx > p.max_ctx || n_new > p.n_q) flags |= SSA_DEV_BAD_COUNT;
+  ctx = max(0, min(ctx, p.max_ctx));
+  n_new = max(0, min(n_new, p.n_q));
+}
+
+// The positions that tokens t0..t1 of a request see between them, as tiles of kTile positions: `front` tiles from 0 (the
+// sinks), then those from w0 on.  Where the two meet there is one run, from 0.  Token t sits at position first + t.
+template <int kTile>
+struct Seen {
+  int front, w0, tiles;
+  __device__ __forceinline__ Seen(const WindowParams& p, int first, int t0, int t1) {
+    const int lo = first + t0, hi = first + t1;            // the first token's position may be negative: it sees nothing
+    front = w0 = tiles = 0;
+    if (t1 < t0 || hi < 0) return;
+    const int from = p.window == 0 ? 0 : max(0, lo - p.window + 1);
+    const int sinks = min(p.sinks, hi + 1);
+    w0 = from / kTile * kTile;
+    front = (sinks + kTile - 1) / kTile;
+    if (front * kTile >= w0) front = w0 = 0;
+    tiles = front + (hi - w0) / kTile + 1;
+  }
+  __device__ __forceinline__ int position(int tile) const { return tile < front ? tile * kTile : w0 + (tile - front) * kTile; }
+};
+
+// Tiles [x, y) of split s of n.
+__device__ __forceinline__ int2 split_tiles(int tiles, int s, int n) {
+  return make_int2((int)((long long)tiles * s / n), (int)((long long)tiles * (s + 1) / n));
+}
+
+__device__ __forceinline__ bool sees(const WindowParams& p, int pos, int j) {
+  return j <= pos && (p.window == 0 || j > pos - p.window || j < p.sinks);
+}
+
+// Pool row of logical position j, -1 where its page does not exist.
+template <bool kPaged>
+__device__ __forceinline__ int64_t row_of(const WindowParams& p, const int32_t* table, int j) {
+  if constexpr (!kPaged) return j;
+  const int page = table[j >> p.page_shift];
+  if ((unsigned)page >= (unsigned)p.n_pages) return -1;
+  return ((int64_t)page << p.page_shift) + (j & ((1 << p.page_shift) - 1));
+}
+
+}  // namespace ssa

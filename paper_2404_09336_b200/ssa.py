@@ -25,6 +25,7 @@ ERR_NULL, ERR_SHAPE, ERR_DTYPE, ERR_ALIGN, ERR_CAPACITY, ERR_WORKSPACE, ERR_CUDA
 DEV_BAD_SPAN, DEV_CLIPPED, DEV_OVERFLOW, DEV_BAD_INDEX, DEV_BAD_COUNT, DEV_TOO_MANY_SPANS = 1, 2, 4, 8, 16, 32
 DEV_BAD_REF = 64
 MAX_SPANS_PER_SEQ = 2048
+MASS_MAX_ROWS = 1024
 F16, BF16, F32, FP8_E4M3 = 0, 1, 2, 3
 _DTYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32, torch.float8_e4m3fn: FP8_E4M3}
 
@@ -58,6 +59,12 @@ class Paging(C.Structure):
     """ssa_paging (see include/ssa.h)."""
     _fields_ = [("page_table", C.c_void_p), ("page_table_stride", C.c_int32), ("page_size", C.c_int32),
                 ("n_pages", C.c_int32)]
+
+
+class Window(C.Structure):
+    """ssa_window (see include/ssa.h)."""
+    _fields_ = [("n_q", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32),
+                ("q_stride_t", C.c_int64), ("o_stride_t", C.c_int64), ("q_lens", C.c_void_p), ("paging", C.POINTER(Paging))]
 
 
 class AnchorTables(C.Structure):
@@ -122,6 +129,19 @@ def _load():
                                                    vp, vp, vp, vp]
     lib.ssa_decode_attn_dense.restype = C.c_int32
     lib.ssa_decode_attn_dense.argtypes = [C.POINTER(AttnDesc), vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp, vp]
+    desc, win = C.POINTER(AttnDesc), C.POINTER(Window)
+    for name in ("ssa_attn_window_workspace_bytes", "ssa_attn_mass_workspace_bytes"):
+        getattr(lib, name).restype = C.c_size_t
+        getattr(lib, name).argtypes = [desc, win]
+    lib.ssa_attn_window.restype = C.c_int32
+    lib.ssa_attn_window.argtypes = [desc, win, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp, vp]
+    lib.ssa_attn_mass.restype = C.c_int32
+    lib.ssa_attn_mass.argtypes = [desc, win, vp, vp, vp, vp, vp, vp, vp, vp, C.c_int64, C.c_float, vp, C.c_size_t, vp, vp]
+    lib.ssa_mass_to_index.restype = C.c_int32
+    lib.ssa_mass_to_index.argtypes = [vp, C.c_int64, vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, C.c_int32,
+                                      vp, vp, vp]
+    lib.ssa_cache_compact.restype = C.c_int32
+    lib.ssa_cache_compact.argtypes = [desc, C.POINTER(Paging), vp, vp, vp, vp, C.c_int32, vp, C.c_int32, vp, C.c_int64, vp, vp]
     lib.ssa_set_kernel_events.restype = None
     lib.ssa_set_kernel_events.argtypes = [vp, vp]
     lib.ssa_launch_count.restype = C.c_uint64
@@ -136,7 +156,8 @@ def _load():
 lib = _load()
 LIBRARY_PATH = lib._name
 
-# The calls of a decode step and their arguments, as binding/ssa_call.c reads them: D, S, P structure (P: or None), i integer,
+# The calls of a decode step and their arguments, as binding/ssa_call.c reads them: D, S, P, Q structure (P: or None), i integer,
+# f number,
 # t tensor or None, r the same and its row stride (R: behind the next tensor), w and its bytes, n and its number of elements.
 _CALLS = {
     "spans_to_index": "ttnrtti",
@@ -153,6 +174,10 @@ _CALLS = {
     "decode_step": "DSi",
     "decode_attn_sparse_noalloc": "Dttttrtittti",
     "decode_attn_dense": "Dttttttwti",
+    "attn_window": "DQttttttwti",
+    "attn_mass": "DQtttttttrfwti",
+    "mass_to_index": "rniiiirtti",
+    "cache_compact": "DPtttrtirti",
 }
 
 
@@ -161,7 +186,9 @@ class _CtypesCalls:
 
     def __init__(self, library):
         for name in _CALLS:
-            setattr(self, name, functools.partial(self._call, name, getattr(library, "ssa_" + name)))
+            entry = getattr(library, "ssa_" + name, None)
+            if entry is not None:
+                setattr(self, name, functools.partial(self._call, name, entry))
 
     @staticmethod
     def _call(name, entry, *args):
@@ -171,7 +198,9 @@ class _CtypesCalls:
         for kind, a in zip(kinds, args):
             if kind == "i":
                 given.append(int(a))
-            elif kind in "DSP":
+            elif kind == "f":
+                given.append(float(a))
+            elif kind in "DSPQ":
                 given.append(None if kind == "P" and a is None else C.byref(a))
             else:
                 given.append(None if a is None else C.c_void_p(a.data_ptr()))
@@ -197,7 +226,7 @@ def _load_calls():
     spec = importlib.util.spec_from_file_location(__package__ + "._ssa_call", path)
     calls = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(calls)
-    calls.bind({"ssa_attn_desc": AttnDesc, "ssa_step": Step, "ssa_paging": Paging} |
+    calls.bind({"ssa_attn_desc": AttnDesc, "ssa_step": Step, "ssa_paging": Paging, "ssa_window": Window} |
                {"ssa_" + name: C.cast(getattr(lib, "ssa_" + name), C.c_void_p).value for name in _CALLS})
     return calls
 
@@ -386,6 +415,58 @@ def decode_attn_dense_paged(desc, q, k_pool, v_pool, paging, ctx_lens, out, lse=
     rc = _call.decode_attn_dense_paged(desc, q, k_pool, v_pool, paging, ctx_lens, out, lse, workspace, dev_status,
                                        _stream(stream))
     return _check("ssa_decode_attn_dense_paged", rc, check)
+
+
+def make_window(q, out, window: int = 0, sinks: int = 0, q_lens=None, paging: Paging | None = None) -> Window:
+    """ssa_window for q[B,H,n_q,D], out[B,H,n_q,D] (any strides; the descriptor is made from q[:, :, 0], out[:, :, 0]).  q_lens
+    (int32 [B], device) must stay alive."""
+    w = Window()
+    w.n_q, w.window, w.sinks = int(q.shape[2]), int(window), int(sinks)
+    w.q_stride_t, w.o_stride_t = int(q.stride(2)), int(out.stride(2))
+    w.q_lens = None if q_lens is None else q_lens.data_ptr()
+    if paging is not None:
+        w.paging = C.pointer(paging)
+    return w
+
+
+def attn_window_workspace_bytes(desc: AttnDesc, window: Window) -> int:
+    return int(lib.ssa_attn_window_workspace_bytes(C.byref(desc), C.byref(window)))
+
+
+def attn_window(desc, window, q, k_cache, v_cache, ctx_lens, out, lse=None, workspace=None, dev_status=None, stream=None,
+                check=True):
+    """ssa_attn_window: the newest tokens of every request over their own past; out (and lse[B,H,n_q]) are written."""
+    rc = _call.attn_window(desc, window, q, k_cache, v_cache, ctx_lens, out, lse, workspace, dev_status, _stream(stream))
+    return _check("ssa_attn_window", rc, check)
+
+
+def attn_mass_workspace_bytes(desc: AttnDesc, window: Window) -> int:
+    return int(lib.ssa_attn_mass_workspace_bytes(C.byref(desc), C.byref(window)))
+
+
+def attn_mass(desc, window, q, k_cache, v_cache, ctx_lens, out, lse, mass_in, mass_out, decay=1.0, workspace=None,
+              dev_status=None, stream=None, check=True):
+    """ssa_attn_mass: attn_window, and mass_out[B, max_ctx] = decay * mass_in + the weight of every position (mass_in: a tensor
+    of mass_out's strides, mass_out itself, or None)."""
+    if mass_in is not None and _row_stride(mass_in) != _row_stride(mass_out):
+        raise ValueError("mass_in and mass_out must have the same row stride")
+    rc = _call.attn_mass(desc, window, q, k_cache, v_cache, ctx_lens, out, lse, mass_in, mass_out, decay, workspace,
+                         dev_status, _stream(stream))
+    return _check("ssa_attn_mass", rc, check)
+
+
+def mass_to_index(mass, ctx_lens, budget, sinks, recent, index, counts, dev_status=None, stream=None, check=True):
+    """ssa_mass_to_index: the positions of mass[B, max_ctx] that the budget keeps -> index[B, index_stride], counts[B]."""
+    rc = _call.mass_to_index(mass, ctx_lens, mass.shape[1], budget, sinks, recent, index, counts, dev_status, _stream(stream))
+    return _check("ssa_mass_to_index", rc, check)
+
+
+def cache_compact(desc, k_cache, v_cache, ctx_lens, index, counts, max_selected, mass=None, paging=None, dev_status=None,
+                  stream=None, check=True):
+    """ssa_cache_compact: listed rows of K and V (and entries of mass[B, max_ctx]) to the front, in place."""
+    rc = _call.cache_compact(desc, paging, k_cache, v_cache, ctx_lens, index, counts, max_selected, mass, dev_status,
+                             _stream(stream))
+    return _check("ssa_cache_compact", rc, check)
 
 
 def refs_to_index(line_offsets, lines, anchor_offsets, anchor_line, ref_offsets, refs, prefix_len, line_start,
