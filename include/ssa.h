@@ -62,8 +62,10 @@ enum {
                               clamped                                              */
   SSA_DEV_TOO_MANY_SPANS = 32, /* a request had more than SSA_MAX_SPANS_PER_SEQ
                               spans; the surplus was ignored                       */
-  SSA_DEV_BAD_REF = 64     /* a reference named an anchor or line that does not
+  SSA_DEV_BAD_REF = 64,    /* a reference named an anchor or line that does not
                               exist, or was malformed: skipped                     */
+  SSA_DEV_GAVE_UP = 128    /* a kernel waited seconds for its own copies and went
+                              on without them: the call's results are void         */
 };
 
 #define SSA_MAX_SPANS_PER_SEQ 2048

@@ -19,6 +19,7 @@ struct WindowParams {
   int k_st, v_st;
   int B, H, H_kv, group, n_q, max_ctx, window, sinks, n_splits, s_pitch;
   int page_table_stride, page_shift, n_pages, out_f32;
+  int block_rows, tile_keys, split_tiles;    // of the kernel that runs: query rows of a block, positions of a tile, see splits_used
   float scale_log2, decay;
 };
 
@@ -31,24 +32,28 @@ __device__ __forceinline__ void window_sizes(const WindowParams& p, int b, int& 
   n_new = max(0, min(n_new, p.n_q));
 }
 
-// The positions that tokens t0..t1 of a request see between them, as tiles of kTile positions: `front` tiles from 0 (the
+// The positions that tokens t0..t1 of a request see between them, as tiles of `size` positions: `front` tiles from 0 (the
 // sinks), then those from w0 on.  Where the two meet there is one run, from 0.  Token t sits at position first + t.
-template <int kTile>
 struct Seen {
-  int front, w0, tiles;
-  __device__ __forceinline__ Seen(const WindowParams& p, int first, int t0, int t1) {
+  int size, front, w0, tiles;
+  __device__ __forceinline__ Seen(const WindowParams& p, int size_, int first, int t0, int t1) : size(size_) {
     const int lo = first + t0, hi = first + t1;            // the first token's position may be negative: it sees nothing
     front = w0 = tiles = 0;
     if (t1 < t0 || hi < 0) return;
     const int from = p.window == 0 ? 0 : max(0, lo - p.window + 1);
     const int sinks = min(p.sinks, hi + 1);
-    w0 = from / kTile * kTile;
-    front = (sinks + kTile - 1) / kTile;
-    if (front * kTile >= w0) front = w0 = 0;
-    tiles = front + (hi - w0) / kTile + 1;
+    w0 = from / size * size;
+    front = (sinks + size - 1) / size;
+    if (front * size >= w0) front = w0 = 0;
+    tiles = front + (hi - w0) / size + 1;
   }
-  __device__ __forceinline__ int position(int tile) const { return tile < front ? tile * kTile : w0 + (tile - front) * kTile; }
+  __device__ __forceinline__ int position(int tile) const { return tile < front ? tile * size : w0 + (tile - front) * size; }
 };
+
+// A split works on at least split_tiles tiles, whatever the launch has room for.
+__device__ __forceinline__ int splits_used(const WindowParams& p, int tiles) {
+  return max(1, min(p.n_splits, tiles / p.split_tiles));
+}
 
 // Tiles [x, y) of split s of n.
 __device__ __forceinline__ int2 split_tiles(int tiles, int s, int n) {
@@ -66,6 +71,13 @@ __device__ __forceinline__ int64_t row_of(const WindowParams& p, const int32_t* 
   const int page = table[j >> p.page_shift];
   if ((unsigned)page >= (unsigned)p.n_pages) return -1;
   return ((int64_t)page << p.page_shift) + (j & ((1 << p.page_shift) - 1));
+}
+
+template <typename TQ>
+__device__ __forceinline__ void store_window_value(const WindowParams& p, int b, int h, int t, int d, float x) {
+  const int64_t o = (int64_t)b * p.o_sb + (int64_t)h * p.o_sh + (int64_t)t * p.o_st + d;
+  if (p.out_f32) reinterpret_cast<float*>(p.out)[o] = x;
+  else reinterpret_cast<TQ*>(p.out)[o] = from_float<TQ>(x);
 }
 
 }  // namespace ssa

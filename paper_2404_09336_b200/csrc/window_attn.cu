@@ -7,10 +7,11 @@
 //
 // window_rows_kernel serves few query rows per K/V head (decode steps, drafted tokens): all of a K/V head's query heads and
 // tokens are rows of one warp-level m16n8k16 tile, so a cached row is read once for sixteen of them.  HBM bounds it.
+// window_tile_kernel (window_tile.cuh) serves many: prompt chunks.  The tensor cores bound it.
 #include <algorithm>
 
 #include "mma.cuh"
-#include "window.cuh"
+#include "window_tile.cuh"
 
 namespace ssa {
 
@@ -66,18 +67,6 @@ template <> __device__ __forceinline__ bool pair_not_finite<__half>(uint32_t w) 
   return (w & 0x7c00u) == 0x7c00u || (w & 0x7c000000u) == 0x7c000000u;
 }
 
-template <typename TQ>
-__device__ __forceinline__ void store_window_value(const WindowParams& p, int b, int h, int t, int d, float x) {
-  const int64_t o = (int64_t)b * p.o_sb + (int64_t)h * p.o_sh + (int64_t)t * p.o_st + d;
-  if (p.out_f32) reinterpret_cast<float*>(p.out)[o] = x;
-  else reinterpret_cast<TQ*>(p.out)[o] = from_float<TQ>(x);
-}
-
-// A split works on at least kSplitTiles tiles, whatever the launch has room for.
-__device__ __forceinline__ int splits_used(const WindowParams& p, int tiles) {
-  return max(1, min(p.n_splits, tiles / kSplitTiles));
-}
-
 // grid (splits x row tiles, H_kv, B).  Fragments come straight from global memory: with the lane layout below, a load
 // instruction takes whole 32-byte sectors, and no value passes through shared memory before the warps' results are joined.
 //   S[16 rows, 8 keys] += Q . K^T   lane 4g+c holds key g's pieces c, c+4, ... ; step s of the contraction takes four of
@@ -107,7 +96,7 @@ window_rows_kernel(const WindowParams p) {
   const int rows = min(kRows, n_new * p.group - row0);       // rows of tokens that exist
   if (rows <= 0) return;
   const int first = ctx - n_new;
-  const Seen<kKeys> seen(p, first, row0 / p.group, (row0 + rows - 1) / p.group);
+  const Seen seen(p, kKeys, first, row0 / p.group, (row0 + rows - 1) / p.group);
   const int n_splits = splits_used(p, seen.tiles);
   if (split >= n_splits) return;
   const int2 range = split_tiles(seen.tiles, split, n_splits);
@@ -407,8 +396,8 @@ __device__ void join_row(const WindowParams& p, int b, int h, int t) {
   int ctx, n_new;
   window_sizes(p, b, ctx, n_new, flags);
   if (t >= n_new) return;
-  const int row0 = (t * p.group + h % p.group) / kRows * kRows, rows = min(kRows, n_new * p.group - row0);
-  const Seen<kKeys> seen(p, ctx - n_new, row0 / p.group, (row0 + rows - 1) / p.group);
+  const int row0 = (t * p.group + h % p.group) / p.block_rows * p.block_rows, rows = min(p.block_rows, n_new * p.group - row0);
+  const Seen seen(p, p.tile_keys, ctx - n_new, row0 / p.group, (row0 + rows - 1) / p.group);
   const int n = splits_used(p, seen.tiles), d = threadIdx.x;
   if (n == 1 || d >= D) return;
   const int64_t at = ((int64_t)b * p.H + h) * p.n_q + t, slot = at * p.n_splits;
@@ -459,7 +448,7 @@ window_mass_kernel(const WindowParams p, const int mass_blocks) {
     const int h = i / p.n_q, t = i % p.n_q, lane = threadIdx.x % 32;
     if (t >= n_new) continue;
     const int row0 = (t * p.group + h % p.group) / kRows * kRows, rows = min(kRows, n_new * p.group - row0);
-    const Seen<kKeys> seen(p, first, row0 / p.group, (row0 + rows - 1) / p.group);
+    const Seen seen(p, kKeys, first, row0 / p.group, (row0 + rows - 1) / p.group);
     const int n = splits_used(p, seen.tiles);
     const float2* ml = p.ws_ml + (((int64_t)b * p.H + h) * p.n_q + t) * p.n_splits;
     float M = neg_inf(), L = 0.f;
@@ -488,7 +477,7 @@ window_mass_kernel(const WindowParams p, const int mass_blocks) {
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
-struct WindowPlan { int n_splits, s_pitch; size_t ml_bytes, acc_bytes, s_bytes, total_bytes; };
+struct WindowPlan { bool tiles; int n_splits, s_pitch; size_t ml_bytes, acc_bytes, s_bytes, total_bytes; };
 
 int32_t check_paging(const ssa_paging* pg, int32_t max_ctx) {
   if (!pg->page_table) return SSA_ERR_NULL;
@@ -509,13 +498,21 @@ static int32_t check_window(const ssa_attn_desc* d, const ssa_window* w, bool ma
 
 static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-static bool plan_window(const ssa_attn_desc* d, const ssa_window* w, bool mass, WindowPlan* pl) {
-  const long long group = d->H / d->H_kv, row_tiles = (group * w->n_q + kRows - 1) / kRows;
-  const long long blocks = row_tiles * d->H_kv * d->B, tokens = (kRows - 1) / group + 2;
+// More than two row tiles of the kernel for few rows (which would read the cache once for each) go to the tiles of 256.
+static bool tiles_pay(const ssa_attn_desc* d, const ssa_window* w, bool mass) {
+  return !mass && d->kv_dtype != SSA_FP8_E4M3 && (long long)(d->H / d->H_kv) * w->n_q > 2 * kRows &&
+         (!w->paging || w->paging->page_size >= 8);          // (a box of a copy is eight rows at least)
+}
+
+static bool plan_window(const ssa_attn_desc* d, const ssa_window* w, bool mass, bool tiles, WindowPlan* pl) {
+  pl->tiles = tiles;
+  const int rows = tiles ? kBlockRows : kRows, keys = tiles ? kTileKeys : kKeys, fewest = tiles ? kTileSplit : kSplitTiles;
+  const long long group = d->H / d->H_kv, row_tiles = (group * w->n_q + rows - 1) / rows;
+  const long long blocks = row_tiles * d->H_kv * d->B, tokens = (rows - 1) / group + 2;
   const long long most = w->window == 0 ? d->max_ctx : std::min<long long>(d->max_ctx, (long long)w->window + w->sinks + tokens);
-  const long long tiles = (most + kKeys - 1) / kKeys + 2;
-  const long long wanted = (4ll * sm_count() + blocks - 1) / blocks;
-  pl->n_splits = (int)std::max(1ll, std::min({wanted, tiles / kSplitTiles, 256ll}));
+  const long long n_tiles = (most + keys - 1) / keys + 2;
+  const long long wanted = tiles ? sm_count() / blocks : (4ll * sm_count() + blocks - 1) / blocks;
+  pl->n_splits = (int)std::max(1ll, std::min({wanted, n_tiles / fewest, 256ll}));
   const size_t slots = (size_t)d->B * d->H * w->n_q * pl->n_splits;
   pl->ml_bytes = up256(slots * sizeof(float2));
   pl->acc_bytes = pl->n_splits > 1 ? up256(slots * d->D * sizeof(float)) : 0;
@@ -525,20 +522,42 @@ static bool plan_window(const ssa_attn_desc* d, const ssa_window* w, bool mass, 
   return row_tiles * pl->n_splits <= 0x7fffffffll;
 }
 
+// Room for either kernel: which one runs may depend on the cache's strides.
+static size_t window_bytes(const ssa_attn_desc* d, const ssa_window* w, bool mass) {
+  WindowPlan pl;
+  if (!d || !w || check_window(d, w, mass) != SSA_OK || !plan_window(d, w, mass, false, &pl)) return 0;
+  const size_t few = pl.total_bytes;
+  if (!tiles_pay(d, w, mass) || !plan_window(d, w, mass, true, &pl)) return few;
+  return std::max(few, pl.total_bytes);
+}
+
 template <typename T, int D>
-static int32_t launch_window(const WindowParams& p, bool mass, cudaStream_t st) {
+static cudaError_t launch_tiles(const WindowParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, int box_rows, cudaStream_t st) {
+  const dim3 grid((unsigned)((p.group * p.n_q + kBlockRows - 1) / kBlockRows * p.n_splits), (unsigned)p.H_kv, (unsigned)p.B);
+  auto kernel = p.page_table ? window_tile_kernel<T, D, true> : window_tile_kernel<T, D, false>;
+  constexpr int kSmem = TileShape<D>::kSmem;
+  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  if (err != cudaSuccess) return err;
+  return launch_pdl_smem(kernel, grid, dim3(kTileThreads), kSmem, st, p, k_map, v_map, box_rows);
+}
+
+template <typename T, int D>
+static int32_t launch_window(const WindowParams& p, bool mass, const CUtensorMap* maps, int box_rows, cudaStream_t st) {
   using TQ = typename Storage<T>::Query;
   const dim3 grid((unsigned)((p.group * p.n_q + kRows - 1) / kRows * p.n_splits), (unsigned)p.H_kv, (unsigned)p.B);
   cudaEvent_t begin, end;
   take_kernel_events(&begin, &end);
   if (begin) cudaEventRecord(begin, st);
-  cudaError_t err;
-  if (p.page_table)
+  cudaError_t err = cudaErrorInvalidValue;
+  if (maps) {
+    if constexpr (!kIsFp8<T>) err = launch_tiles<T, D>(p, maps[0], maps[1], box_rows, st);
+  } else if (p.page_table) {
     err = mass ? launch_pdl(window_rows_kernel<T, D, true, true>, grid, dim3(kWarps * 32), st, p)
                : launch_pdl(window_rows_kernel<T, D, true, false>, grid, dim3(kWarps * 32), st, p);
-  else
+  } else {
     err = mass ? launch_pdl(window_rows_kernel<T, D, false, true>, grid, dim3(kWarps * 32), st, p)
                : launch_pdl(window_rows_kernel<T, D, false, false>, grid, dim3(kWarps * 32), st, p);
+  }
   if (err != cudaSuccess) return SSA_ERR_CUDA;
   if (end) cudaEventRecord(end, st);
   note_launches(1);
@@ -564,11 +583,22 @@ static int32_t run_window(const ssa_attn_desc* d, const ssa_window* w, const voi
   if (rc != SSA_OK) return rc;
   if (mass && mass_stride < d->max_ctx) return SSA_ERR_SHAPE;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(ws)) return SSA_ERR_ALIGN;
-  WindowPlan pl;
-  if (!plan_window(d, w, mass, &pl)) return SSA_ERR_SHAPE;
-  if (!ws || ws_bytes < pl.total_bytes) return SSA_ERR_WORKSPACE;
+  if (!ws || ws_bytes < window_bytes(d, w, mass)) return SSA_ERR_WORKSPACE;
   const ssa_paging* pg = w->paging;
+  CUtensorMap maps[2];
+  const int box_rows = pg ? std::min(pg->page_size, kTileKeys) : kTileKeys;
+  const int64_t pool_rows = pg ? (int64_t)pg->n_pages * pg->page_size : d->max_ctx;
+  WindowPlan pl;
+  const bool tiles = tiles_pay(d, w, mass) && plan_window(d, w, mass, true, &pl) &&
+                     tile_map(&maps[0], k, d->kv_dtype, d->D, pool_rows, d->k_stride_t, d->H_kv, d->k_stride_h, pg ? 1 : d->B,
+                              d->k_stride_b, box_rows) &&
+                     tile_map(&maps[1], v, d->kv_dtype, d->D, pool_rows, d->v_stride_t, d->H_kv, d->v_stride_h, pg ? 1 : d->B,
+                              d->v_stride_b, box_rows);
+  if (!tiles && !plan_window(d, w, mass, false, &pl)) return SSA_ERR_SHAPE;
   WindowParams p;
+  p.block_rows = tiles ? kBlockRows : kRows;
+  p.tile_keys = tiles ? kTileKeys : kKeys;
+  p.split_tiles = tiles ? kTileSplit : kSplitTiles;
   p.q = q; p.k = k; p.v = v; p.out = out; p.lse = lse;
   p.ctx_lens = ctx_lens; p.q_lens = w->q_lens; p.page_table = pg ? pg->page_table : nullptr;
   char* at = static_cast<char*>(ws);
@@ -593,11 +623,13 @@ static int32_t run_window(const ssa_attn_desc* d, const ssa_window* w, const voi
   p.scale_log2 = (d->scale > 0.f ? d->scale : 1.0f / sqrtf((float)d->D)) * kLog2e;
   p.decay = decay;
   cudaStream_t st = (cudaStream_t)stream;
+  const CUtensorMap* m = tiles ? maps : nullptr;
   if (d->kv_dtype == SSA_FP8_E4M3)
-    return d->D == 128 ? launch_window<Fp8E4M3, 128>(p, mass, st) : launch_window<Fp8E4M3, 64>(p, mass, st);
+    return d->D == 128 ? launch_window<Fp8E4M3, 128>(p, mass, m, box_rows, st) : launch_window<Fp8E4M3, 64>(p, mass, m, box_rows, st);
   if (d->kv_dtype == SSA_BF16)
-    return d->D == 128 ? launch_window<__nv_bfloat16, 128>(p, mass, st) : launch_window<__nv_bfloat16, 64>(p, mass, st);
-  return d->D == 128 ? launch_window<__half, 128>(p, mass, st) : launch_window<__half, 64>(p, mass, st);
+    return d->D == 128 ? launch_window<__nv_bfloat16, 128>(p, mass, m, box_rows, st)
+                       : launch_window<__nv_bfloat16, 64>(p, mass, m, box_rows, st);
+  return d->D == 128 ? launch_window<__half, 128>(p, mass, m, box_rows, st) : launch_window<__half, 64>(p, mass, m, box_rows, st);
 }
 
 }  // namespace ssa
@@ -605,15 +637,11 @@ static int32_t run_window(const ssa_attn_desc* d, const ssa_window* w, const voi
 extern "C" {
 
 size_t ssa_attn_window_workspace_bytes(const ssa_attn_desc* desc, const ssa_window* window) {
-  ssa::WindowPlan pl;
-  if (!desc || !window || ssa::check_window(desc, window, false) != SSA_OK || !ssa::plan_window(desc, window, false, &pl)) return 0;
-  return pl.total_bytes;
+  return ssa::window_bytes(desc, window, false);
 }
 
 size_t ssa_attn_mass_workspace_bytes(const ssa_attn_desc* desc, const ssa_window* window) {
-  ssa::WindowPlan pl;
-  if (!desc || !window || ssa::check_window(desc, window, true) != SSA_OK || !ssa::plan_window(desc, window, true, &pl)) return 0;
-  return pl.total_bytes;
+  return ssa::window_bytes(desc, window, true);
 }
 
 int32_t ssa_attn_window(const ssa_attn_desc* desc, const ssa_window* window, const void* q, const void* k_cache,

@@ -1,0 +1,520 @@
+// Window attention of many query rows per K/V head (prompt chunks): tcgen05 tiles.  Included by window_attn.cu.
+//
+// A block serves 256 (token, head of the group) rows of one K/V head as two tiles of 128, and goes through the 128-position
+// tiles that they see between them.  Both contractions are tcgen05.mma of 128 x 128 x 16 steps with fp32 accumulators:
+//   S = Q . K^T   Q and K in shared memory (128-byte swizzle, K by TMA), S in TMEM
+//   O += P . V    P, the weights as 16-bit values, in TMEM over the first half of S; V in shared memory, not transposed
+// TMEM is full: 2 x (S 128 columns + O 128).  Warps 0-3 and 4-7 do the softmax of one row tile each, a thread per row; warp 8
+// issues the matrix instructions, warp 9 the copies (10 and 11 make up its group of four).  While one row tile's softmax runs, the tensor cores work on the other's.
+//
+// The running maximum that weights are relative to follows the true one only where that is more than 2^8 above it, so that O
+// is rescaled in a few tiles at the start and hardly ever after that; weights are then at most 2^8 (fp16: times 2^6, which
+// the sum divides out again, because fp16 has little range below 1), rounded once to 16 bits: the two parts that the kernel
+// for few rows takes would cost a third contraction, and the rounding is that of a 16-bit output.
+#pragma once
+#include <cuda.h>
+
+#include <type_traits>
+
+#include "mma.cuh"
+#include "window.cuh"
+
+namespace ssa {
+
+constexpr int kTileRows = 128, kBlockRows = 2 * kTileRows, kTileKeys = 128;
+constexpr int kTileThreads = 384, kTileStages = 4;
+constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;  // of a thread; 256 x 208 + 128 x 88 = 384 x 168, what the launch has
+constexpr int kTileSplit = 4;                       // fewest tiles worth a split of their own
+constexpr float kLazy = 8.f;                        // log2 of how far weights may exceed 1
+
+template <int D>
+struct TileShape {
+  static constexpr int kHalf = kTileRows * 128;                     // bytes of 128 rows of 64 elements
+  static constexpr int kTileBytes = kHalf * (D / 64);               // of a Q, K or V tile
+  static constexpr int kSmem = (2 + kTileStages) * kTileBytes + 1024;   // (1024: room to align)
+};
+
+// ---- PTX ------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(uint32_t bar, int count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, int bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok;
+}
+constexpr uint64_t kPatience = 2000000000;          // ns
+// Waits end: after two seconds the block gives up (*dead), and everything in it runs to its end without waiting.
+__device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
+  if (mbar_try(bar, parity)) return;
+  uint64_t since, now;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(since));
+  while (!mbar_try(bar, parity)) {
+    if (*dead) return;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
+    if (now - since > kPatience) { *dead = 1; return; }
+  }
+}
+__device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap* map, int x, int row, int head, int b, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+               ::"r"(to), "l"(map), "r"(x), "r"(row), "r"(head), "r"(b), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((int)add) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((int)add) : "memory");
+}
+#define SSA_R8(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]), "=r"(v[i + 4]), "=r"(v[i + 5]), "=r"(v[i + 6]), "=r"(v[i + 7])
+#define SSA_W8(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), "r"(v[i + 5]), "r"(v[i + 6]), "r"(v[i + 7])
+// 32 columns of this warp's 32 lanes: a thread has its row's.
+__device__ __forceinline__ void tc_ld32(uint32_t (&v)[32], uint32_t at) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+               "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+               : SSA_R8(v, 0), SSA_R8(v, 8), SSA_R8(v, 16), SSA_R8(v, 24) : "r"(at));
+}
+__device__ __forceinline__ void tc_st32(uint32_t at, const uint32_t (&v)[32]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+               "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+               ::SSA_W8(v, 0), SSA_W8(v, 8), SSA_W8(v, 16), SSA_W8(v, 24), "r"(at) : "memory");
+}
+#undef SSA_R8
+#undef SSA_W8
+
+// Shared-memory operand with 128-byte swizzle.  Rows of 128 bytes, groups of eight rows 1024 bytes apart; `lead`: bytes from
+// one 64-element part of the contiguous dimension to the next, where one instruction spans several (V).
+__device__ __forceinline__ uint64_t tile_desc(uint32_t at, uint32_t lead) {
+  return (uint64_t)((at & 0x3ffffu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// fp32 accumulators of 128 rows and N columns; A along its rows; B along its rows (K) or across them (V).
+template <typename T, int N, bool kAcross>
+__device__ constexpr uint32_t tile_idesc() {
+  const uint32_t type = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
+  return 1u << 4 | type << 7 | type << 10 | (kAcross ? 1u << 16 : 0u) | (uint32_t)(N / 8) << 17 | (uint32_t)(kTileRows / 16) << 24;
+}
+
+// One row again in fp32, by a warp, with the infinities and NaNs of V kept to where they are seen: lane i's dimensions i D/32 ...
+template <typename T, int D, bool kPaged>
+__device__ __noinline__ void careful_row(const WindowParams& p, const Seen& seen, int2 range, int b, int h, int t, int pos, float& m,
+                                         float& l, float (&acc)[D / 32]) {
+  constexpr int kN = D / 32;
+  const int lane = threadIdx.x % 32, hkv = h / p.group;
+  const T* q = reinterpret_cast<const T*>(p.q) + (int64_t)b * p.q_sb + (int64_t)h * p.q_sh + (int64_t)t * p.q_st + lane * kN;
+  const T* k = reinterpret_cast<const T*>(p.k) + (kPaged ? 0 : (int64_t)b * p.k_sb) + (int64_t)hkv * p.k_sh + lane * kN;
+  const T* v = reinterpret_cast<const T*>(p.v) + (kPaged ? 0 : (int64_t)b * p.v_sb) + (int64_t)hkv * p.v_sh + lane * kN;
+  const int32_t* table = kPaged ? p.page_table + (int64_t)b * p.page_table_stride : nullptr;
+  float odd[kN], qf[kN];
+  m = neg_inf();
+  l = 0.f;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) { acc[i] = odd[i] = 0.f; qf[i] = to_float(q[i]); }
+  for (int it = range.x; it < range.y; ++it)
+    for (int j = seen.position(it); j < seen.position(it) + kTileKeys; ++j) {
+      if (!sees(p, pos, j)) continue;
+      const int64_t row = row_of<kPaged>(p, table, j);
+      if (row < 0) continue;
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < kN; ++i) s = fmaf(qf[i], to_float(k[row * p.k_st + i]), s);
+#pragma unroll
+      for (int o = 16; o; o /= 2) s += __shfl_xor_sync(~0u, s, o);
+      s *= p.scale_log2;
+      const float top = fmaxf(m, s), base = top == neg_inf() ? 0.f : top, a = fast_exp2(m - base), w = fast_exp2(s - base);
+      m = top;
+      l = fmaf(l, a, w);
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        const float x = to_float(v[row * p.v_st + i]);
+        if (isfinite(x)) acc[i] = fmaf(acc[i], a, w * x);
+        else { acc[i] *= a; odd[i] += x; }
+      }
+    }
+#pragma unroll
+  for (int i = 0; i < kN; ++i) acc[i] += odd[i];
+}
+
+// grid (splits x row blocks, H_kv, B), the last row blocks first: they see most.
+template <typename T, int D, bool kPaged>
+__global__ void __launch_bounds__(kTileThreads, 1)
+window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+                   const int box_rows) {
+  using Shape = TileShape<D>;
+  constexpr float kShift = std::is_same<T, __half>::value ? 6.f : 0.f;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t s_bar[3 * kTileStages + 6];
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_dead;
+  const uint32_t base = (smem_at(smem_raw) + 1023) & ~1023u;
+  uint8_t* const smem = smem_raw + (base - smem_at(smem_raw));
+  const uint32_t full = smem_at(s_bar), empty = full + 8 * kTileStages, fixed = empty + 8 * kTileStages, s_full = fixed + 8 * kTileStages,
+                 p_full = s_full + 16, o_full = p_full + 16;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int n_blocks = gridDim.x / p.n_splits, split = blockIdx.x % p.n_splits;
+  const int row0 = (n_blocks - 1 - (int)(blockIdx.x / p.n_splits)) * kBlockRows, hkv = blockIdx.y, b = blockIdx.z;
+  uint32_t flags = 0;
+  int ctx, n_new;
+  window_sizes(p, b, ctx, n_new, flags);
+  if (flags && p.status && split == 0 && row0 == 0 && hkv == 0 && threadIdx.x == 0) atomicOr(p.status, flags);
+  const int rows = min(kBlockRows, n_new * p.group - row0);            // rows of tokens that exist
+  if (rows <= 0) return;
+  const int first = ctx - n_new;
+  const Seen seen(p, kTileKeys, first, row0 / p.group, (row0 + rows - 1) / p.group);
+  const int n_splits = splits_used(p, seen.tiles);
+  if (split >= n_splits) return;
+  const int2 range = split_tiles(seen.tiles, split, n_splits);
+  const int lo = first + row0 / p.group, hi = first + (row0 + rows - 1) / p.group;
+  // the two row tiles: positions of their first and last rows, and which of the block's tiles they take part in
+  int tile_lo[2], tile_hi[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int a = min(row0 + x * kTileRows, row0 + rows), z = min(row0 + (x + 1) * kTileRows, row0 + rows) - 1;
+    tile_lo[x] = first + a / p.group;
+    tile_hi[x] = z < a ? -1 : first + z / p.group;                     // (no rows, or none with a position: no tiles)
+  }
+  // whether the tile has positions that no token sees: their rows of V may hold anything, and are made zero
+  const int from = p.window == 0 ? 0 : max(0, lo - p.window + 1);
+  auto unseen = [&](int it) {
+    const int j0 = seen.position(it), jz = j0 + kTileKeys - 1;
+    return jz > hi || !(j0 >= from || jz < p.sinks || from <= p.sinks);
+  };
+  auto needs = [&](int x, int it) {
+    const int j0 = seen.position(it);
+    return j0 <= tile_hi[x] && (p.window == 0 || j0 < p.sinks || j0 + kTileKeys - 1 > tile_lo[x] - p.window);
+  };
+
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&s_tmem)), "n"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  if (threadIdx.x == 288) {
+    for (int i = 0; i < kTileStages; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); mbar_init(fixed + 8 * i, 32); }
+    for (int x = 0; x < 2; ++x) { mbar_init(s_full + 8 * x, 1); mbar_init(p_full + 8 * x, kTileRows); mbar_init(o_full + 8 * x, 1); }
+    s_dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp < 8) {                                                      // queries: a thread per row, 16 bytes at a time, swizzled
+    const int x = warp / 4, r = threadIdx.x % kTileRows, row = row0 + x * kTileRows + r;
+    uint8_t* to = smem + x * Shape::kTileBytes + r * 128;
+    const bool there = x * kTileRows + r < rows;
+    const int t = row / p.group, h = hkv * p.group + row % p.group;
+    const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.q) + (int64_t)b * p.q_sb + (int64_t)h * p.q_sh +
+                                                    (int64_t)t * p.q_st);
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) {
+      const uint4 w = there ? q[i] : make_uint4(0, 0, 0, 0);
+      *reinterpret_cast<uint4*>(to + i / 8 * Shape::kHalf + ((i % 8) ^ (r & 7)) * 16) = w;
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  tc_before();
+  __syncthreads();
+  tc_after();
+  const uint32_t tmem = s_tmem;
+  const uint32_t kv = base + 2 * Shape::kTileBytes;
+  const int n_tiles = range.y - range.x;
+  volatile int* dead = &s_dead;
+
+  if (warp == 9) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    // ---- copies: K(0), V(0), K(1), ... into a ring of stages ----
+    const int boxes = kTileKeys / box_rows;
+    const int32_t* table = kPaged ? p.page_table + (int64_t)b * p.page_table_stride : nullptr;
+    int waiting = -1;                                        // a tile of V with unseen rows, two loads ago
+    auto fix = [&]() {
+      const int stage = waiting % kTileStages, j0 = seen.position(range.x + waiting / 2);
+      mbar_wait(full + 8 * stage, (waiting / kTileStages) & 1, dead);
+      for (int r = lane / 8; r < kTileKeys; r += 4) {
+        const int j = j0 + r;
+        if (j <= hi && (j >= from || j < p.sinks)) continue;
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x)
+          *reinterpret_cast<uint4*>(smem + (kv - base) + stage * Shape::kTileBytes + x * Shape::kHalf + r * 128 + lane % 8 * 16) =
+              make_uint4(0, 0, 0, 0);
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      mbar_arrive(fixed + 8 * stage);
+      waiting = -1;
+    };
+    for (int i = 0; i < 2 * n_tiles; ++i) {
+      const int stage = i % kTileStages, j0 = seen.position(range.x + i / 2);
+      const bool is_v = i & 1;
+      if (i >= kTileStages) mbar_wait(empty + 8 * stage, (i / kTileStages - 1) & 1, dead);
+      if (lane == 0) mbar_expect(full + 8 * stage, Shape::kTileBytes);
+      __syncwarp();
+      if (lane < boxes) {
+        int row = j0, batch = b;
+        if constexpr (kPaged) {
+          // pages that no token sees a position of, and pages that do not exist, are read as zeros: a row behind the last
+          const int ja = j0 + lane * box_rows, jz = ja + box_rows - 1;
+          const bool used = ja <= hi && (p.window == 0 || jz > lo - p.window || ja < p.sinks);
+          const int64_t at = used ? row_of<true>(p, table, ja) : -1;
+          row = at < 0 ? p.n_pages << p.page_shift : (int)at;
+          batch = 0;
+        }
+        const uint32_t to = kv + stage * Shape::kTileBytes + lane * box_rows * 128;
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x)
+          tma_load(to + x * Shape::kHalf, is_v ? &v_map : &k_map, x * 64, row, hkv, batch, full + 8 * stage);
+      }
+      if (waiting >= 0 && i == waiting + 2) fix();
+      if (is_v && unseen(range.x + i / 2)) waiting = i;
+    }
+    if (waiting >= 0) fix();
+  } else if (warp == 8) {
+    // ---- matrix instructions, by one thread ----
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (lane == 0 && n_tiles > 0) {
+      constexpr uint32_t kIdS = tile_idesc<T, kTileKeys, false>(), kIdO = tile_idesc<T, D, true>();
+      bool begun[2] = {false, false};
+      uint32_t p_phase[2] = {0, 0}, fixes = 0;      // fixes: the phase of each stage's barrier
+      auto scores = [&](int x, uint32_t k_at) {
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+          const uint32_t off = s / 4 * Shape::kHalf + s % 4 * 32;
+          mma_ss(tmem + x * 128, tile_desc(base + x * Shape::kTileBytes + off, 16), tile_desc(k_at + off, 16), kIdS, s > 0);
+        }
+        tc_commit(s_full + 8 * x);
+      };
+      auto k_wait = [&](int it) {
+        const int i = 2 * it;
+        mbar_wait(full + 8 * (i % kTileStages), (i / kTileStages) & 1, dead);
+        tc_after();
+        return kv + i % kTileStages * Shape::kTileBytes;
+      };
+      uint32_t k_at = k_wait(0);
+      for (int x = 0; x < 2; ++x)
+        if (needs(x, range.x)) scores(x, k_at);
+      tc_commit(empty);
+      for (int it = 0; it < n_tiles; ++it) {
+        const int i = 2 * it + 1;
+        const uint32_t v_at = kv + i % kTileStages * Shape::kTileBytes;
+        mbar_wait(full + 8 * (i % kTileStages), (i / kTileStages) & 1, dead);
+        if (unseen(range.x + it)) {
+          mbar_wait(fixed + 8 * (i % kTileStages), fixes >> (i % kTileStages) & 1, dead);
+          fixes ^= 1u << (i % kTileStages);
+        }
+        tc_after();
+        if (it + 1 < n_tiles) k_at = k_wait(it + 1);
+        for (int x = 0; x < 2; ++x) {
+          if (needs(x, range.x + it)) {
+            mbar_wait(p_full + 8 * x, p_phase[x], dead);
+            p_phase[x] ^= 1;
+            tc_after();
+#pragma unroll
+            for (int s = 0; s < kTileKeys / 16; ++s)
+              mma_ts(tmem + 256 + x * 128, tmem + x * 128 + s * 8, tile_desc(v_at + s * 2048, Shape::kHalf), kIdO, begun[x] || s > 0);
+            begun[x] = true;
+          }
+          if (it + 1 < n_tiles && needs(x, range.x + it + 1)) scores(x, k_at);
+        }
+        tc_commit(empty + 8 * (i % kTileStages));
+        if (it + 1 < n_tiles) tc_commit(empty + 8 * ((i + 1) % kTileStages));
+      }
+    }
+    if (lane == 0) {
+      tc_commit(o_full);
+      tc_commit(o_full + 8);
+    }
+    __syncwarp();
+  } else if (warp < 8) {
+    // ---- softmax: a thread per row ----
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+    const int x = warp / 4, r = threadIdx.x % kTileRows, row = row0 + x * kTileRows + r;
+    const bool there = x * kTileRows + r < rows;
+    const int t = row / p.group, h = hkv * p.group + row % p.group, pos = there ? first + t : -1;
+    const uint32_t s_at = tmem + x * 128 + ((uint32_t)(warp % 4 * 32) << 16), o_at = s_at + 256;
+    const int all_lo = p.window == 0 ? 0 : tile_hi[x] - p.window + 1;  // every row of the tile sees [all_lo, tile_lo]
+    const int32_t* table = kPaged ? p.page_table + (int64_t)b * p.page_table_stride : nullptr;
+    float m = neg_inf(), l = 0.f;
+    bool begun = false;
+    uint32_t phase = 0;
+    for (int it = range.x; it < range.y; ++it) {
+      if (!needs(x, it)) continue;
+      const int j0 = seen.position(it);
+      unsigned have = ~0u;                                   // positions 4 i ... 4 i + 3 have a page
+      if constexpr (kPaged) {
+        const int j = j0 + lane * 4;
+        bool used = false;
+        for (int y = j; y < j + 4; ++y) used |= y <= hi && (p.window == 0 || y > lo - p.window || y < p.sinks);
+        const bool gone = used && row_of<true>(p, table, j) < 0;
+        have = __ballot_sync(~0u, !gone);
+        if (gone) flags |= SSA_DEV_BAD_INDEX;
+      }
+      mbar_wait(s_full + 8 * x, phase, dead);
+      phase ^= 1;
+      tc_after();
+      uint32_t s[4][32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tc_ld32(s[c], s_at + c * 32);
+      tc_wait_ld();
+      const bool whole = have == ~0u && j0 + kTileKeys - 1 <= tile_lo[x] && (j0 >= all_lo || j0 + kTileKeys <= p.sinks);
+      if (!whole) {
+#pragma unroll
+        for (int c = 0; c < 128; ++c)
+          if (!sees(p, pos, j0 + c) || !((have >> (c / 4)) & 1)) s[c / 32][c % 32] = 0xff800000u;
+      }
+      float top[4] = {neg_inf(), neg_inf(), neg_inf(), neg_inf()};
+#pragma unroll
+      for (int c = 0; c < 128; ++c) top[c % 4] = fmaxf(top[c % 4], __uint_as_float(s[c / 32][c % 32]));
+      const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale_log2;
+      const bool higher = now > m + kLazy;                   // (m = -inf: anything)
+      if (__any_sync(~0u, higher)) {
+        const float to = higher ? now : m;
+        const float a = m == to ? 1.f : fast_exp2(m - to);
+        m = to;
+        l *= a;
+        if (begun) {                                         // S is there, so the contraction before it has ended
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[32];
+            tc_ld32(o, o_at + c * 32);
+            tc_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * a);
+            tc_st32(o_at + c * 32, o);
+          }
+        }
+      }
+      begun = true;
+      const float off = (m == neg_inf() ? 0.f : -m) + kShift;
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint32_t w[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const int e = c * 64 + 2 * i;
+          const float a = fast_exp2(fmaf(__uint_as_float(s[e / 32][e % 32]), p.scale_log2, off));
+          const float z = fast_exp2(fmaf(__uint_as_float(s[e / 32][e % 32 + 1]), p.scale_log2, off));
+          sum[2 * (i & 1)] += a;
+          sum[2 * (i & 1) + 1] += z;
+          w[i] = pack2<T>(a, z);
+        }
+        tc_st32(s_at + c * 32, w);
+      }
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      tc_wait_st();
+      tc_before();
+      mbar_arrive(p_full + 8 * x);
+    }
+    mbar_wait(o_full + 8 * x, 0, dead);
+    tc_after();
+
+    // ---- the row: out, or a split's part of it ----
+    const int64_t at = ((int64_t)b * p.H + h) * p.n_q + t, slot = at * p.n_splits + split;
+    const bool finished = n_splits == 1;
+    float scale = finished ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+    bool odd = !(fabsf(l) <= 3.402823466e38f);
+    T* out16 = reinterpret_cast<T*>(p.out) + (int64_t)b * p.o_sb + (int64_t)h * p.o_sh + (int64_t)t * p.o_st;
+    float* out32 = !finished ? p.ws_acc + slot * D
+                             : reinterpret_cast<float*>(p.out) + (int64_t)b * p.o_sb + (int64_t)h * p.o_sh + (int64_t)t * p.o_st;
+#pragma unroll 1
+    for (int c = 0; c < D / 32; ++c) {
+      uint32_t o[32];
+      tc_ld32(o, o_at + c * 32);
+      tc_wait_ld();
+      float f[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        f[i] = l == 0.f ? 0.f : __uint_as_float(o[i]) * scale;
+        odd |= !(fabsf(f[i]) <= 3.402823466e38f);
+      }
+      if (!there) continue;
+      if (finished && !p.out_f32) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 8)
+          *reinterpret_cast<uint4*>(out16 + c * 32 + i) = make_uint4(pack2<T>(f[i], f[i + 1]), pack2<T>(f[i + 2], f[i + 3]),
+                                                                     pack2<T>(f[i + 4], f[i + 5]), pack2<T>(f[i + 6], f[i + 7]));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(out32 + c * 32 + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+      }
+    }
+    if (there) {
+      if (finished) {
+        if (p.lse) p.lse[at] = l == 0.f ? neg_inf() : (m - kShift + log2f(l)) * kLn2;
+      } else {
+        p.ws_ml[slot] = make_float2(m - kShift, l);
+      }
+    }
+    unsigned again = __ballot_sync(~0u, there && odd);
+    while (again) {                                          // rows that met an infinity or a NaN, or what they must not see
+      const int i = __ffs(again) - 1;
+      again &= again - 1;
+      const int rt = __shfl_sync(~0u, t, i), rh = __shfl_sync(~0u, h, i), rpos = __shfl_sync(~0u, pos, i);
+      const int64_t rat = ((int64_t)b * p.H + rh) * p.n_q + rt, rslot = rat * p.n_splits + split;
+      float rm, rl, acc[D / 32];
+      careful_row<T, D, kPaged>(p, seen, range, b, rh, rt, rpos, rm, rl, acc);
+      __syncwarp();
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) {
+        if (finished) store_window_value<T>(p, b, rh, rt, lane * (D / 32) + d, rl == 0.f ? 0.f : acc[d] / rl);
+        else p.ws_acc[rslot * D + lane * (D / 32) + d] = acc[d];
+      }
+      if (lane == 0) {
+        if (!finished) p.ws_ml[rslot] = make_float2(rm, rl);
+        else if (p.lse) p.lse[rat] = rl == 0.f ? neg_inf() : (rm + log2f(rl)) * kLn2;
+      }
+    }
+    if (kPaged && p.status && (flags & SSA_DEV_BAD_INDEX)) atomicOr(p.status, SSA_DEV_BAD_INDEX);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+  }
+  tc_before();
+  __syncthreads();
+  tc_after();
+  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512));
+  if (threadIdx.x == 0 && s_dead && p.status) atomicOr(p.status, SSA_DEV_GAVE_UP);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+// A cache or pool as (D, rows, heads, requests), read in boxes of 64 elements x box_rows rows.  False where the strides are
+// none that the copies take (the call is then left to the kernel for few rows).
+inline bool tile_map(CUtensorMap* map, const void* base, int32_t dtype, int D, int64_t rows, int64_t row_stride, int heads,
+                     int64_t head_stride, int B, int64_t b_stride, int box_rows) {
+  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static const Encode encode = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      f = nullptr;
+    }
+    return reinterpret_cast<Encode>(f);
+  }();
+  if (!encode) return false;
+  const int64_t strides[3] = {row_stride * 2, heads > 1 ? head_stride * 2 : row_stride * 2, B > 1 ? b_stride * 2 : row_stride * 2};
+  cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)rows, (cuuint64_t)heads, (cuuint64_t)B}, steps[3];
+  for (int i = 0; i < 3; ++i) {
+    if (strides[i] <= 0 || strides[i] >= 1ll << 40) return false;
+    steps[i] = (cuuint64_t)strides[i];
+  }
+  const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1}, ones[4] = {1, 1, 1, 1};
+  return encode(map, dtype == SSA_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(base),
+                dims, steps, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace ssa

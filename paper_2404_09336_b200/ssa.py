@@ -23,7 +23,7 @@ from . import build as _build
 OK = 0
 ERR_NULL, ERR_SHAPE, ERR_DTYPE, ERR_ALIGN, ERR_CAPACITY, ERR_WORKSPACE, ERR_CUDA, ERR_UNSUPPORTED = range(1, 9)
 DEV_BAD_SPAN, DEV_CLIPPED, DEV_OVERFLOW, DEV_BAD_INDEX, DEV_BAD_COUNT, DEV_TOO_MANY_SPANS = 1, 2, 4, 8, 16, 32
-DEV_BAD_REF = 64
+DEV_BAD_REF, DEV_GAVE_UP = 64, 128
 MAX_SPANS_PER_SEQ = 2048
 MASS_MAX_ROWS = 1024
 F16, BF16, F32, FP8_E4M3 = 0, 1, 2, 3

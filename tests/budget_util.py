@@ -95,7 +95,8 @@ def check(p, got, ctx, q_lens, window, sinks, out_dtype, many=False, mass_in=Non
     """Errors against fp64.  A score is a dot product of D terms in fp32: off by D 2^-24 of scale sum |q||k| at most, and so is,
     relatively, its exponential (and 2^-22 by exp2); the weight is rounded (weight_step); sums of n terms add n 2^-24.  Numerator
     and denominator both have it, each relative to sum weight |v|; the output is rounded once more."""
-    out, lse, mass, _ = got
+    out, lse, mass, status = got
+    assert not status & ssa.DEV_GAVE_UP
     q, k, v = p.values()
     q_lens = [p.n_q] * p.B if q_lens is None else q_lens
     ref = BO.attention(q, k, v, ctx, q_lens, window, sinks, p.D ** -0.5 if scale is None else scale, skipped)
