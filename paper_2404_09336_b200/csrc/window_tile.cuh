@@ -51,16 +51,14 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
                : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok;
 }
-constexpr uint64_t kPatience = 2000000000;          // ns
-// Waits end: after two seconds the block gives up (*dead), and everything in it runs to its end without waiting.
+constexpr long long kPatience = 4000000000;         // cycles
+// Waits end: after some two seconds the block gives up (*dead), and everything in it runs to its end without waiting.
 __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
   if (mbar_try(bar, parity)) return;
-  uint64_t since, now;
-  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(since));
+  const long long since = clock64();
   while (!mbar_try(bar, parity)) {
     if (*dead) return;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
-    if (now - since > kPatience) { *dead = 1; return; }
+    if (clock64() - since > kPatience) { *dead = 1; return; }
   }
 }
 __device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap* map, int x, int row, int head, int b, uint32_t bar) {
@@ -97,6 +95,21 @@ __device__ __forceinline__ void tc_st32(uint32_t at, const uint32_t (&v)[32]) {
 }
 #undef SSA_R8
 #undef SSA_W8
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 y;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(*reinterpret_cast<unsigned long long*>(&y))
+      : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
+  return y;
+}
+// The lowest n of 32 bits, for any n.
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
 
 // Shared-memory operand with 128-byte swizzle.  Rows of 128 bytes, groups of eight rows 1024 bytes apart; `lead`: bytes from
 // one 64-element part of the contiguous dimension to the next, where one instruction spans several (V).
@@ -343,6 +356,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
     const int t = row / p.group, h = hkv * p.group + row % p.group, pos = there ? first + t : -1;
     const uint32_t s_at = tmem + x * 128 + ((uint32_t)(warp % 4 * 32) << 16), o_at = s_at + 256;
     const int all_lo = p.window == 0 ? 0 : tile_hi[x] - p.window + 1;  // every row of the tile sees [all_lo, tile_lo]
+    const int window_lo = p.window == 0 ? 0 : pos - p.window + 1;
     const int32_t* table = kPaged ? p.page_table + (int64_t)b * p.page_table_stride : nullptr;
     float m = neg_inf(), l = 0.f;
     bool begun = false;
@@ -369,12 +383,24 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
       const bool whole = have == ~0u && j0 + kTileKeys - 1 <= tile_lo[x] && (j0 >= all_lo || j0 + kTileKeys <= p.sinks);
       if (!whole) {
 #pragma unroll
-        for (int c = 0; c < 128; ++c)
-          if (!sees(p, pos, j0 + c) || !((have >> (c / 4)) & 1)) s[c / 32][c % 32] = 0xff800000u;
+        for (int c = 0; c < 4; ++c) {
+          // a bit per position: up to the row's own, and from its window on or below the sinks
+          const int j = j0 + c * 32;
+          uint32_t seen_bits = bits_below(pos + 1 - j) & (~bits_below(window_lo - j) | bits_below(p.sinks - j));
+          if constexpr (kPaged) {
+#pragma unroll
+            for (int y = 0; y < 8; ++y)
+              if (!(have >> (c * 8 + y) & 1)) seen_bits &= ~(15u << (4 * y));
+          }
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (!(seen_bits >> i & 1)) s[c][i] = 0xff800000u;
+        }
       }
       float top[4] = {neg_inf(), neg_inf(), neg_inf(), neg_inf()};
 #pragma unroll
-      for (int c = 0; c < 128; ++c) top[c % 4] = fmaxf(top[c % 4], __uint_as_float(s[c / 32][c % 32]));
+      for (int c = 0; c < 128; c += 2)
+        top[c / 2 % 4] = max3(top[c / 2 % 4], __uint_as_float(s[c / 32][c % 32]), __uint_as_float(s[c / 32][c % 32 + 1]));
       const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale_log2;
       const bool higher = now > m + kLazy;                   // (m = -inf: anything)
       if (__any_sync(~0u, higher)) {
@@ -395,23 +421,24 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
         }
       }
       begun = true;
-      const float off = (m == neg_inf() ? 0.f : -m) + kShift;
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      const float off1 = (m == neg_inf() ? 0.f : -m) + kShift;
+      const float2 off = make_float2(off1, off1), by = make_float2(p.scale_log2, p.scale_log2);
+      float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         uint32_t w[32];
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
           const int e = c * 64 + 2 * i;
-          const float a = fast_exp2(fmaf(__uint_as_float(s[e / 32][e % 32]), p.scale_log2, off));
-          const float z = fast_exp2(fmaf(__uint_as_float(s[e / 32][e % 32 + 1]), p.scale_log2, off));
-          sum[2 * (i & 1)] += a;
-          sum[2 * (i & 1) + 1] += z;
-          w[i] = pack2<T>(a, z);
+          float2 x = fma2(make_float2(__uint_as_float(s[e / 32][e % 32]), __uint_as_float(s[e / 32][e % 32 + 1])), by, off);
+          x.x = fast_exp2(x.x);
+          x.y = fast_exp2(x.y);
+          sum[i & 1] = add2(sum[i & 1], x);
+          w[i] = pack2<T>(x.x, x.y);
         }
         tc_st32(s_at + c * 32, w);
       }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       tc_wait_st();
       tc_before();
       mbar_arrive(p_full + 8 * x);
