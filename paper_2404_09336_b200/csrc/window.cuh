@@ -19,6 +19,7 @@ struct WindowParams {
   int k_st, v_st;
   int B, H, H_kv, group, n_q, max_ctx, window, sinks, n_splits, s_pitch;
   int page_table_stride, page_shift, n_pages, out_f32;
+  int group_shift;                           // log2 of group, -1 where it is no power of two
   int block_rows, tile_keys, split_tiles;    // of the kernel that runs: query rows of a block, positions of a tile, see splits_used
   float scale_log2, decay;
 };
@@ -55,8 +56,14 @@ __device__ __forceinline__ int splits_used(const WindowParams& p, int tiles) {
   return max(1, min(p.n_splits, tiles / p.split_tiles));
 }
 
+// The token of a row of a K/V head: rows are ordered by token, then head of the group.
+__device__ __forceinline__ int token_of(const WindowParams& p, int row) {
+  return p.group_shift >= 0 ? row >> p.group_shift : row / p.group;
+}
+
 // Tiles [x, y) of split s of n.
 __device__ __forceinline__ int2 split_tiles(int tiles, int s, int n) {
+  if (n == 1) return make_int2(0, tiles);
   return make_int2((int)((long long)tiles * s / n), (int)((long long)tiles * (s + 1) / n));
 }
 

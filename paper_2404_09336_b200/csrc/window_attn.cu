@@ -619,6 +619,9 @@ static int32_t run_window(const ssa_attn_desc* d, const ssa_window* w, const voi
   p.n_pages = pg ? pg->n_pages : 0;
   p.page_shift = 0;
   while (pg && (1 << p.page_shift) < pg->page_size) ++p.page_shift;
+  p.group_shift = -1;
+  for (int i = 0; i < 16; ++i)
+    if (p.group == 1 << i) p.group_shift = i;
   p.out_f32 = d->out_dtype == SSA_F32;
   p.scale_log2 = (d->scale > 0.f ? d->scale : 1.0f / sqrtf((float)d->D)) * kLog2e;
   p.decay = decay;

@@ -1,16 +1,20 @@
 // Window attention of many query rows per K/V head (prompt chunks): tcgen05 tiles.  Included by window_attn.cu.
 //
-// A block serves 256 (token, head of the group) rows of one K/V head as two tiles of 128, and goes through the 128-position
-// tiles that they see between them.  Both contractions are tcgen05.mma of 128 x 128 x 16 steps with fp32 accumulators:
-//   S = Q . K^T   Q and K in shared memory (128-byte swizzle, K by TMA), S in TMEM
-//   O += P . V    P, the weights as 16-bit values, in TMEM over the first half of S; V in shared memory, not transposed
-// TMEM is full: 2 x (S 128 columns + O 128).  Warps 0-3 and 4-7 do the softmax of one row tile each, a thread per row; warp 8
-// issues the matrix instructions, warp 9 the copies (10 and 11 make up its group of four).  While one row tile's softmax runs, the tensor cores work on the other's.
+// A block serves 256 (token, head of the group) rows of one K/V head as two row tiles of 128, and goes through the tiles of 128
+// positions that they see between them.  Both contractions are tcgen05.mma in steps of 16 with fp32 accumulators:
+//   S = Q . K^T   128 x 128; Q and K in shared memory (128-byte swizzle, K by TMA), S in TMEM
+//   O += P . V    128 x D; P, the weights as 16-bit values, in TMEM over the first half of S; V in shared memory as it lies
+// TMEM is full: an S and an O for each row tile.  Warps 0-3 and 4-7 do the softmax of one row tile each, a thread per row; warp
+// 8 issues the matrix instructions, warp 9 the copies (10 and 11 make up its group of four).  While one row tile's softmax
+// runs, the tensor cores work on the other's.  (With tiles of 64 positions and two S per row tile no softmax waited for its
+// scores' chain, but an instruction of 128 x 64 takes as long as one of 128 x 128 - the 128 rows of Q are read either way -
+// and whole prompts took 524 instead of 485 us.)
 //
 // The running maximum that weights are relative to follows the true one only where that is more than 2^8 above it, so that O
 // is rescaled in a few tiles at the start and hardly ever after that; weights are then at most 2^8 (fp16: times 2^6, which
 // the sum divides out again, because fp16 has little range below 1), rounded once to 16 bits: the two parts that the kernel
-// for few rows takes would cost a third contraction, and the rounding is that of a 16-bit output.
+// for few rows takes would cost a third contraction, and the rounding is that of a 16-bit output.  (Instructions, not the special
+// function unit, bound the softmax: with a quarter of the powers on the FMA units prompts took 467 instead of 437 us.)
 #pragma once
 #include <cuda.h>
 
@@ -29,9 +33,9 @@ constexpr float kLazy = 8.f;                        // log2 of how far weights m
 
 template <int D>
 struct TileShape {
-  static constexpr int kHalf = kTileRows * 128;                     // bytes of 128 rows of 64 elements
-  static constexpr int kTileBytes = kHalf * (D / 64);               // of a Q, K or V tile
-  static constexpr int kSmem = (2 + kTileStages) * kTileBytes + 1024;   // (1024: room to align)
+  static constexpr int kQHalf = kTileRows * 128, kHalf = kTileKeys * 128;   // bytes of 64 dimensions of a Q tile, of a K or V tile
+  static constexpr int kQBytes = kQHalf * (D / 64), kTileBytes = kHalf * (D / 64);
+  static constexpr int kSmem = 2 * kQBytes + kTileStages * kTileBytes + 1024;   // (1024: room to align)
 };
 
 // ---- PTX ------------------------------------------------------------------------------------------------------------
@@ -54,7 +58,8 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
 constexpr long long kPatience = 4000000000;         // cycles
 // Waits end: after some two seconds the block gives up (*dead), and everything in it runs to its end without waiting.
 __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
-  if (mbar_try(bar, parity)) return;
+  for (int i = 0; i < 64; ++i)
+    if (mbar_try(bar, parity)) return;
   const long long since = clock64();
   while (!mbar_try(bar, parity)) {
     if (*dead) return;
@@ -64,6 +69,11 @@ __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatil
 __device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap* map, int x, int row, int head, int b, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
                ::"r"(to), "l"(map), "r"(x), "r"(row), "r"(head), "r"(b), "r"(bar) : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t is;
+  asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(is));
+  return is;
 }
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -171,18 +181,19 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
   using Shape = TileShape<D>;
   constexpr float kShift = std::is_same<T, __half>::value ? 6.f : 0.f;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t s_bar[3 * kTileStages + 6];
+  __shared__ __align__(8) uint64_t s_bar[3 * kTileStages + 8];
   __shared__ uint32_t s_tmem;
+  __shared__ int64_t s_row[2][kBlockRows];                             // where a row starts in q and in out
   __shared__ int s_dead;
   const uint32_t base = (smem_at(smem_raw) + 1023) & ~1023u;
   uint8_t* const smem = smem_raw + (base - smem_at(smem_raw));
   const uint32_t full = smem_at(s_bar), empty = full + 8 * kTileStages, fixed = empty + 8 * kTileStages, s_full = fixed + 8 * kTileStages,
-                 p_full = s_full + 16, o_full = p_full + 16;
+                 p_full = s_full + 16, o_full = p_full + 32;           // s_full, o_full: [row tile]; p_full: [row tile][half]
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   grid_dependency_wait();
   grid_launch_dependents();
-  const int n_blocks = gridDim.x / p.n_splits, split = blockIdx.x % p.n_splits;
-  const int row0 = (n_blocks - 1 - (int)(blockIdx.x / p.n_splits)) * kBlockRows, hkv = blockIdx.y, b = blockIdx.z;
+  const int block = p.n_splits == 1 ? blockIdx.x : blockIdx.x / p.n_splits, split = blockIdx.x - block * p.n_splits;
+  const int row0 = ((p.group * p.n_q - 1) / kBlockRows - block) * kBlockRows, hkv = blockIdx.y, b = blockIdx.z;
   uint32_t flags = 0;
   int ctx, n_new;
   window_sizes(p, b, ctx, n_new, flags);
@@ -190,18 +201,18 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
   const int rows = min(kBlockRows, n_new * p.group - row0);            // rows of tokens that exist
   if (rows <= 0) return;
   const int first = ctx - n_new;
-  const Seen seen(p, kTileKeys, first, row0 / p.group, (row0 + rows - 1) / p.group);
+  const int t_lo = token_of(p, row0), t_hi = token_of(p, row0 + rows - 1), lo = first + t_lo, hi = first + t_hi;
+  const Seen seen(p, kTileKeys, first, t_lo, t_hi);
   const int n_splits = splits_used(p, seen.tiles);
   if (split >= n_splits) return;
   const int2 range = split_tiles(seen.tiles, split, n_splits);
-  const int lo = first + row0 / p.group, hi = first + (row0 + rows - 1) / p.group;
   // the two row tiles: positions of their first and last rows, and which of the block's tiles they take part in
   int tile_lo[2], tile_hi[2];
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     const int a = min(row0 + x * kTileRows, row0 + rows), z = min(row0 + (x + 1) * kTileRows, row0 + rows) - 1;
-    tile_lo[x] = first + a / p.group;
-    tile_hi[x] = z < a ? -1 : first + z / p.group;                     // (no rows, or none with a position: no tiles)
+    tile_lo[x] = first + token_of(p, a);
+    tile_hi[x] = z < a ? -1 : first + token_of(p, z);                  // (no rows, or none with a position: no tiles)
   }
   // whether the tile has positions that no token sees: their rows of V may hold anything, and are made zero
   const int from = p.window == 0 ? 0 : max(0, lo - p.window + 1);
@@ -213,48 +224,38 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
     const int j0 = seen.position(it);
     return j0 <= tile_hi[x] && (p.window == 0 || j0 < p.sinks || j0 + kTileKeys - 1 > tile_lo[x] - p.window);
   };
-
-  if (warp == 8) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&s_tmem)), "n"(512) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-  }
-  if (threadIdx.x == 288) {
-    for (int i = 0; i < kTileStages; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); mbar_init(fixed + 8 * i, 32); }
-    for (int x = 0; x < 2; ++x) { mbar_init(s_full + 8 * x, 1); mbar_init(p_full + 8 * x, kTileRows); mbar_init(o_full + 8 * x, 1); }
-    s_dead = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  if (warp < 8) {                                                      // queries: a thread per row, 16 bytes at a time, swizzled
-    const int x = warp / 4, r = threadIdx.x % kTileRows, row = row0 + x * kTileRows + r;
-    uint8_t* to = smem + x * Shape::kTileBytes + r * 128;
-    const bool there = x * kTileRows + r < rows;
-    const int t = row / p.group, h = hkv * p.group + row % p.group;
-    const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.q) + (int64_t)b * p.q_sb + (int64_t)h * p.q_sh +
-                                                    (int64_t)t * p.q_st);
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
-      const uint4 w = there ? q[i] : make_uint4(0, 0, 0, 0);
-      *reinterpret_cast<uint4*>(to + i / 8 * Shape::kHalf + ((i % 8) ^ (r & 7)) * 16) = w;
-    }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  }
-  tc_before();
-  __syncthreads();
-  tc_after();
-  const uint32_t tmem = s_tmem;
-  const uint32_t kv = base + 2 * Shape::kTileBytes;
-  const int n_tiles = range.y - range.x;
+  const uint32_t kv = base + 2 * Shape::kQBytes;
+  const int n_tiles = range.y - range.x, n_loads = 2 * n_tiles;
   volatile int* dead = &s_dead;
 
-  if (warp == 9) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    // ---- copies: K(0), V(0), K(1), ... into a ring of stages ----
-    const int boxes = kTileKeys / box_rows;
-    const int32_t* table = kPaged ? p.page_table + (int64_t)b * p.page_table_stride : nullptr;
-    int waiting = -1;                                        // a tile of V with unseen rows, two loads ago
-    auto fix = [&]() {
-      const int stage = waiting % kTileStages, j0 = seen.position(range.x + waiting / 2);
-      mbar_wait(full + 8 * stage, (waiting / kTileStages) & 1, dead);
+  // ---- copies, by warp 9: K(0), V(0), K(1), ... into a ring of stages ----
+  auto load = [&](int i) {
+    const int stage = i % kTileStages, j0 = seen.position(range.x + i / 2);
+    if (lane == 0) mbar_expect(full + 8 * stage, Shape::kTileBytes);
+    __syncwarp();
+    if (lane < kTileKeys / box_rows) {
+      int row = j0, batch = b;
+      if constexpr (kPaged) {
+        // pages that no token sees a position of, and pages that do not exist, are read as zeros: a row behind the last
+        const int ja = j0 + lane * box_rows, jz = ja + box_rows - 1;
+        const bool used = ja <= hi && (jz >= from || ja < p.sinks);
+        const int64_t at = used ? row_of<true>(p, p.page_table + (int64_t)b * p.page_table_stride, ja) : -1;
+        row = at < 0 ? p.n_pages << p.page_shift : (int)at;
+        batch = 0;
+      }
+      const uint32_t to = kv + stage * Shape::kTileBytes + lane * box_rows * 128;
+#pragma unroll
+      for (int x = 0; x < D / 64; ++x)
+        tma_load(to + x * Shape::kHalf, i & 1 ? &v_map : &k_map, x * 64, row, hkv, batch, full + 8 * stage);
+    }
+  };
+  // Rows of V that no token sees become zero.  A copy's turn comes two copies after its own, so that others are on their way.
+  int settled = 1;
+  auto settle = [&](int upto) {
+    for (; settled <= upto; settled += 2) {
+      if (!unseen(range.x + settled / 2)) continue;
+      const int stage = settled % kTileStages, j0 = seen.position(range.x + settled / 2);
+      mbar_wait(full + 8 * stage, (settled / kTileStages) & 1, dead);
       for (int r = lane / 8; r < kTileKeys; r += 4) {
         const int j = j0 + r;
         if (j <= hi && (j >= from || j < p.sinks)) continue;
@@ -265,102 +266,142 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       mbar_arrive(fixed + 8 * stage);
-      waiting = -1;
-    };
-    for (int i = 0; i < 2 * n_tiles; ++i) {
-      const int stage = i % kTileStages, j0 = seen.position(range.x + i / 2);
-      const bool is_v = i & 1;
-      if (i >= kTileStages) mbar_wait(empty + 8 * stage, (i / kTileStages - 1) & 1, dead);
-      if (lane == 0) mbar_expect(full + 8 * stage, Shape::kTileBytes);
-      __syncwarp();
-      if (lane < boxes) {
-        int row = j0, batch = b;
-        if constexpr (kPaged) {
-          // pages that no token sees a position of, and pages that do not exist, are read as zeros: a row behind the last
-          const int ja = j0 + lane * box_rows, jz = ja + box_rows - 1;
-          const bool used = ja <= hi && (p.window == 0 || jz > lo - p.window || ja < p.sinks);
-          const int64_t at = used ? row_of<true>(p, table, ja) : -1;
-          row = at < 0 ? p.n_pages << p.page_shift : (int)at;
-          batch = 0;
-        }
-        const uint32_t to = kv + stage * Shape::kTileBytes + lane * box_rows * 128;
-#pragma unroll
-        for (int x = 0; x < D / 64; ++x)
-          tma_load(to + x * Shape::kHalf, is_v ? &v_map : &k_map, x * 64, row, hkv, batch, full + 8 * stage);
-      }
-      if (waiting >= 0 && i == waiting + 2) fix();
-      if (is_v && unseen(range.x + i / 2)) waiting = i;
     }
-    if (waiting >= 0) fix();
-  } else if (warp == 8) {
-    // ---- matrix instructions, by one thread ----
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (lane == 0 && n_tiles > 0) {
-      constexpr uint32_t kIdS = tile_idesc<T, kTileKeys, false>(), kIdO = tile_idesc<T, D, true>();
-      bool begun[2] = {false, false};
-      uint32_t p_phase[2] = {0, 0}, fixes = 0;      // fixes: the phase of each stage's barrier
-      auto scores = [&](int x, uint32_t k_at) {
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) {
-          const uint32_t off = s / 4 * Shape::kHalf + s % 4 * 32;
-          mma_ss(tmem + x * 128, tile_desc(base + x * Shape::kTileBytes + off, 16), tile_desc(k_at + off, 16), kIdS, s > 0);
-        }
-        tc_commit(s_full + 8 * x);
-      };
-      auto k_wait = [&](int it) {
-        const int i = 2 * it;
-        mbar_wait(full + 8 * (i % kTileStages), (i / kTileStages) & 1, dead);
-        tc_after();
-        return kv + i % kTileStages * Shape::kTileBytes;
-      };
-      uint32_t k_at = k_wait(0);
-      for (int x = 0; x < 2; ++x)
-        if (needs(x, range.x)) scores(x, k_at);
-      tc_commit(empty);
-      for (int it = 0; it < n_tiles; ++it) {
-        const int i = 2 * it + 1;
-        const uint32_t v_at = kv + i % kTileStages * Shape::kTileBytes;
-        mbar_wait(full + 8 * (i % kTileStages), (i / kTileStages) & 1, dead);
-        if (unseen(range.x + it)) {
-          mbar_wait(fixed + 8 * (i % kTileStages), fixes >> (i % kTileStages) & 1, dead);
-          fixes ^= 1u << (i % kTileStages);
-        }
-        tc_after();
-        if (it + 1 < n_tiles) k_at = k_wait(it + 1);
-        for (int x = 0; x < 2; ++x) {
-          if (needs(x, range.x + it)) {
-            mbar_wait(p_full + 8 * x, p_phase[x], dead);
-            p_phase[x] ^= 1;
-            tc_after();
-#pragma unroll
-            for (int s = 0; s < kTileKeys / 16; ++s)
-              mma_ts(tmem + 256 + x * 128, tmem + x * 128 + s * 8, tile_desc(v_at + s * 2048, Shape::kHalf), kIdO, begun[x] || s > 0);
-            begun[x] = true;
-          }
-          if (it + 1 < n_tiles && needs(x, range.x + it + 1)) scores(x, k_at);
-        }
-        tc_commit(empty + 8 * (i % kTileStages));
-        if (it + 1 < n_tiles) tc_commit(empty + 8 * ((i + 1) % kTileStages));
-      }
-    }
+  };
+  if (warp == 9) {
     if (lane == 0) {
-      tc_commit(o_full);
-      tc_commit(o_full + 8);
+      for (int i = 0; i < kTileStages; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); mbar_init(fixed + 8 * i, 32); }
+      for (int x = 0; x < 2; ++x) { mbar_init(s_full + 8 * x, 1); mbar_init(o_full + 8 * x, 1); }
+      for (int x = 0; x < 4; ++x) mbar_init(p_full + 8 * x, kTileRows);
+      s_dead = 0;
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
+    for (int i = 0; i < min(kTileStages, n_loads); ++i) load(i);
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&s_tmem)), "n"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  if (warp < 8) {                                                      // queries: a warp's 32 rows, D / 8 lanes to a row, swizzled
+    constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
+    const int i = lane % kLanes;
+    {
+      const int row = row0 + (int)threadIdx.x, t = token_of(p, row), h = hkv * p.group + row - t * p.group;
+      s_row[0][threadIdx.x] = (int64_t)b * p.q_sb + (int64_t)h * p.q_sh + (int64_t)t * p.q_st;
+      s_row[1][threadIdx.x] = (int64_t)b * p.o_sb + (int64_t)h * p.o_sh + (int64_t)t * p.o_st;
+    }
+    __syncwarp();
+    uint4 w[32 / kAtOnce];
+#pragma unroll
+    for (int y = 0; y < 32 / kAtOnce; ++y) {
+      const int r = warp * 32 + y * kAtOnce + lane / kLanes;
+      w[y] = make_uint4(0, 0, 0, 0);
+      if (r < rows) w[y] = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.q) + s_row[0][r] + i * 8);
+    }
+#pragma unroll
+    for (int y = 0; y < 32 / kAtOnce; ++y) {
+      const int r = warp * 32 + y * kAtOnce + lane / kLanes;
+      *reinterpret_cast<uint4*>(smem + r / kTileRows * Shape::kQBytes + i / 8 * Shape::kQHalf + r % kTileRows * 128 +
+                                ((i % 8) ^ (r & 7)) * 16) = w[y];
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  tc_before();
+  __syncthreads();
+  tc_after();
+  const uint32_t tmem = s_tmem;
+
+  if (warp == 9) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    settle(min(kTileStages, n_loads) - 3);
+    for (int i = kTileStages; i < n_loads; ++i) {
+      mbar_wait(empty + 8 * (i % kTileStages), (i / kTileStages - 1) & 1, dead);
+      load(i);
+      settle(i - 2);
+    }
+    settle(n_loads - 1);
+  } else if (warp == 8) {
+    // ---- matrix instructions: the whole warp goes through this, so that addresses stay in uniform registers; one lane issues ----
+    constexpr uint32_t kIdS = tile_idesc<T, kTileKeys, false>(), kIdO = tile_idesc<T, D, true>();
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    const bool leader = elect_one();
+    int last[2] = {-1, -1};                                  // the last tile of each row tile
+    for (int x = 0; x < 2; ++x)
+      for (int tile = n_tiles - 1; tile >= 0 && last[x] < 0; --tile)
+        if (needs(x, range.x + tile)) last[x] = tile;
+    uint32_t begun = 0, phases = 0, fixes = 0;               // bits: row tiles that have a sum; phases of p_full, of `fixed`
+    const uint64_t q_desc = tile_desc(base, 16), k_desc = tile_desc(kv, 16), v_desc = tile_desc(kv, Shape::kHalf);
+    auto wait_full = [&](int i) { mbar_wait(full + 8 * (i % kTileStages), (i / kTileStages) & 1, dead); };
+    auto scores = [&](int x, int stage) {
+      const uint64_t qd = q_desc + x * (Shape::kQBytes >> 4), kd = k_desc + stage * (Shape::kTileBytes >> 4);
+      const uint32_t to = tmem + x * 128;
+      if (leader) {
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s)
+          mma_ss(to, qd + (s / 4 * (Shape::kQHalf >> 4) + s % 4 * 2), kd + (s / 4 * (Shape::kHalf >> 4) + s % 4 * 2), kIdS, s > 0);
+        tc_commit(s_full + 8 * x);
+      }
+      __syncwarp();
+    };
+    if (n_tiles > 0) {
+      wait_full(0);
+      tc_after();
+      for (int x = 0; x < 2; ++x)
+        if (needs(x, range.x)) scores(x, 0);
+      if (leader) tc_commit(empty);
+      __syncwarp();
+    }
+    for (int tile = 0; tile < n_tiles; ++tile) {
+      const int i = 2 * tile + 1, stage = i % kTileStages, k_stage = (i + 1) % kTileStages;
+      const bool more = tile + 1 < n_tiles;
+      wait_full(i);
+      if (unseen(range.x + tile)) {
+        mbar_wait(fixed + 8 * stage, fixes >> stage & 1, dead);
+        fixes ^= 1u << stage;
+      }
+      if (more) wait_full(i + 1);
+      tc_after();
+      const uint64_t vd = v_desc + stage * (Shape::kTileBytes >> 4);
+      for (int x = 0; x < 2; ++x) {
+        if (needs(x, range.x + tile)) {
+          const uint32_t to = tmem + 256 + x * 128, weights = tmem + x * 128;
+          const bool add = begun >> x & 1;
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {             // the weights come in two halves
+            mbar_wait(p_full + 16 * x + 8 * half, phases >> x & 1, dead);
+            tc_after();
+            if (leader) {
+#pragma unroll
+              for (int s = 4 * half; s < 4 * half + 4; ++s) mma_ts(to, weights + s * 8, vd + s * (2048 >> 4), kIdO, add || s > 0);
+            }
+            __syncwarp();
+          }
+          phases ^= 1u << x;
+          begun |= 1u << x;
+          if (leader && tile == last[x]) tc_commit(o_full + 8 * x);
+          __syncwarp();
+        }
+        if (more && needs(x, range.x + tile + 1)) scores(x, k_stage);   // over weights that the contraction just issued takes
+      }
+      if (leader) {
+        tc_commit(empty + 8 * stage);
+        if (more) tc_commit(empty + 8 * k_stage);
+      }
+      __syncwarp();
+    }
   } else if (warp < 8) {
     // ---- softmax: a thread per row ----
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-    const int x = warp / 4, r = threadIdx.x % kTileRows, row = row0 + x * kTileRows + r;
-    const bool there = x * kTileRows + r < rows;
-    const int t = row / p.group, h = hkv * p.group + row % p.group, pos = there ? first + t : -1;
-    const uint32_t s_at = tmem + x * 128 + ((uint32_t)(warp % 4 * 32) << 16), o_at = s_at + 256;
+    const int x = warp / 4, row = row0 + (int)threadIdx.x;
+    const bool there = (int)threadIdx.x < rows;
+    const int t = token_of(p, row), h = hkv * p.group + row - t * p.group, pos = there ? first + t : -1;
+    const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16, s_at = tmem + x * 128 + lanes, o_at = s_at + 256;
     const int all_lo = p.window == 0 ? 0 : tile_hi[x] - p.window + 1;  // every row of the tile sees [all_lo, tile_lo]
     const int window_lo = p.window == 0 ? 0 : pos - p.window + 1;
     const int32_t* table = kPaged ? p.page_table + (int64_t)b * p.page_table_stride : nullptr;
     float m = neg_inf(), l = 0.f;
-    bool begun = false;
-    uint32_t phase = 0;
+    int n = 0;                                               // tiles so far
     for (int it = range.x; it < range.y; ++it) {
       if (!needs(x, it)) continue;
       const int j0 = seen.position(it);
@@ -368,13 +409,12 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
       if constexpr (kPaged) {
         const int j = j0 + lane * 4;
         bool used = false;
-        for (int y = j; y < j + 4; ++y) used |= y <= hi && (p.window == 0 || y > lo - p.window || y < p.sinks);
+        for (int y = j; y < j + 4; ++y) used |= y <= hi && (y >= from || y < p.sinks);
         const bool gone = used && row_of<true>(p, table, j) < 0;
         have = __ballot_sync(~0u, !gone);
         if (gone) flags |= SSA_DEV_BAD_INDEX;
       }
-      mbar_wait(s_full + 8 * x, phase, dead);
-      phase ^= 1;
+      mbar_wait(s_full + 8 * x, n & 1, dead);
       tc_after();
       uint32_t s[4][32];
 #pragma unroll
@@ -388,9 +428,11 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
           const int j = j0 + c * 32;
           uint32_t seen_bits = bits_below(pos + 1 - j) & (~bits_below(window_lo - j) | bits_below(p.sinks - j));
           if constexpr (kPaged) {
+            if (have != ~0u) {
 #pragma unroll
-            for (int y = 0; y < 8; ++y)
-              if (!(have >> (c * 8 + y) & 1)) seen_bits &= ~(15u << (4 * y));
+              for (int y = 0; y < 8; ++y)
+                if (!(have >> (c * 8 + y) & 1)) seen_bits &= ~(15u << (4 * y));
+            }
           }
 #pragma unroll
           for (int i = 0; i < 32; ++i)
@@ -401,14 +443,14 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
 #pragma unroll
       for (int c = 0; c < 128; c += 2)
         top[c / 2 % 4] = max3(top[c / 2 % 4], __uint_as_float(s[c / 32][c % 32]), __uint_as_float(s[c / 32][c % 32 + 1]));
-      const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale_log2;
+      const float now = fmaxf(max3(top[0], top[1], top[2]), top[3]) * p.scale_log2;
       const bool higher = now > m + kLazy;                   // (m = -inf: anything)
       if (__any_sync(~0u, higher)) {
         const float to = higher ? now : m;
         const float a = m == to ? 1.f : fast_exp2(m - to);
         m = to;
         l *= a;
-        if (begun) {                                         // S is there, so the contraction before it has ended
+        if (n > 0) {                                         // S is there, so the contraction before it has ended
 #pragma unroll 1
           for (int c = 0; c < D / 32; ++c) {
             uint32_t o[32];
@@ -420,40 +462,40 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
           }
         }
       }
-      begun = true;
       const float off1 = (m == neg_inf() ? 0.f : -m) + kShift;
       const float2 off = make_float2(off1, off1), by = make_float2(p.scale_log2, p.scale_log2);
       float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
+      for (int half = 0; half < 2; ++half) {
         uint32_t w[32];
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-          const int e = c * 64 + 2 * i;
-          float2 x = fma2(make_float2(__uint_as_float(s[e / 32][e % 32]), __uint_as_float(s[e / 32][e % 32 + 1])), by, off);
-          x.x = fast_exp2(x.x);
-          x.y = fast_exp2(x.y);
-          sum[i & 1] = add2(sum[i & 1], x);
-          w[i] = pack2<T>(x.x, x.y);
+          const int e = half * 64 + 2 * i;
+          float2 y = fma2(make_float2(__uint_as_float(s[e / 32][e % 32]), __uint_as_float(s[e / 32][e % 32 + 1])), by, off);
+          y = make_float2(fast_exp2(y.x), fast_exp2(y.y));
+          sum[i & 1] = add2(sum[i & 1], y);
+          w[i] = pack2<T>(y.x, y.y);
         }
-        tc_st32(s_at + c * 32, w);
+        tc_st32(s_at + half * 32, w);
+        tc_wait_st();
+        tc_before();
+        mbar_arrive(p_full + 16 * x + 8 * half);             // its contraction starts meanwhile
       }
       l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-      tc_wait_st();
-      tc_before();
-      mbar_arrive(p_full + 8 * x);
+      ++n;
     }
-    mbar_wait(o_full + 8 * x, 0, dead);
+    if (n > 0) mbar_wait(o_full + 8 * x, 0, dead);
     tc_after();
 
     // ---- the row: out, or a split's part of it ----
     const int64_t at = ((int64_t)b * p.H + h) * p.n_q + t, slot = at * p.n_splits + split;
     const bool finished = n_splits == 1;
-    float scale = finished ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-    bool odd = !(fabsf(l) <= 3.402823466e38f);
-    T* out16 = reinterpret_cast<T*>(p.out) + (int64_t)b * p.o_sb + (int64_t)h * p.o_sh + (int64_t)t * p.o_st;
-    float* out32 = !finished ? p.ws_acc + slot * D
-                             : reinterpret_cast<float*>(p.out) + (int64_t)b * p.o_sb + (int64_t)h * p.o_sh + (int64_t)t * p.o_st;
+    const float scale = finished ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+    float2 test = make_float2(l * 0.f, 0.f);
+    float* out32 = finished ? reinterpret_cast<float*>(p.out) + s_row[1][threadIdx.x] : p.ws_acc + slot * D;
+    const bool staged = finished && !p.out_f32;              // 16-bit rows go through the queries' place, to be stored whole
+    const int rw = warp % 4 * 32 + lane;
+    uint8_t* stage = smem + x * Shape::kQBytes;
 #pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {
       uint32_t o[32];
@@ -461,19 +503,38 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
       tc_wait_ld();
       float f[32];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        f[i] = l == 0.f ? 0.f : __uint_as_float(o[i]) * scale;
-        odd |= !(fabsf(f[i]) <= 3.402823466e38f);
+      for (int i = 0; i < 32; i += 2) {                      // (0 times an infinity or a NaN is NaN)
+        const float2 y = fma2(make_float2(__uint_as_float(o[i]), __uint_as_float(o[i + 1])), make_float2(scale, scale), make_float2(0.f, 0.f));
+        test = fma2(y, make_float2(0.f, 0.f), test);
+        f[i] = l == 0.f ? 0.f : y.x;
+        f[i + 1] = l == 0.f ? 0.f : y.y;
       }
-      if (!there) continue;
-      if (finished && !p.out_f32) {
+      if (staged) {
 #pragma unroll
-        for (int i = 0; i < 32; i += 8)
-          *reinterpret_cast<uint4*>(out16 + c * 32 + i) = make_uint4(pack2<T>(f[i], f[i + 1]), pack2<T>(f[i + 2], f[i + 3]),
-                                                                     pack2<T>(f[i + 4], f[i + 5]), pack2<T>(f[i + 6], f[i + 7]));
-      } else {
+        for (int i = 0; i < 32; i += 8) {
+          const int at16 = c * 4 + i / 8;
+          *reinterpret_cast<uint4*>(stage + at16 / 8 * Shape::kQHalf + rw * 128 + ((at16 % 8) ^ (rw & 7)) * 16) =
+              make_uint4(pack2<T>(f[i], f[i + 1]), pack2<T>(f[i + 2], f[i + 3]), pack2<T>(f[i + 4], f[i + 5]), pack2<T>(f[i + 6], f[i + 7]));
+        }
+      } else if (there) {
 #pragma unroll
         for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(out32 + c * 32 + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+      }
+    }
+    if (staged) {
+      __syncwarp();
+      constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
+      const int i = lane % kLanes;
+      uint4 w[32 / kAtOnce];
+#pragma unroll
+      for (int y = 0; y < 32 / kAtOnce; ++y) {
+        const int yr = warp % 4 * 32 + y * kAtOnce + lane / kLanes;
+        w[y] = *reinterpret_cast<const uint4*>(stage + i / 8 * Shape::kQHalf + yr * 128 + ((i % 8) ^ (yr & 7)) * 16);
+      }
+#pragma unroll
+      for (int y = 0; y < 32 / kAtOnce; ++y) {
+        const int yr = x * kTileRows + warp % 4 * 32 + y * kAtOnce + lane / kLanes;
+        if (yr < rows) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.out) + s_row[1][yr] + i * 8) = w[y];
       }
     }
     if (there) {
@@ -483,7 +544,8 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
         p.ws_ml[slot] = make_float2(m - kShift, l);
       }
     }
-    unsigned again = __ballot_sync(~0u, there && odd);
+    unsigned again = __ballot_sync(~0u, there && l != 0.f && !(test.x + test.y == 0.f));
+    __syncwarp();
     while (again) {                                          // rows that met an infinity or a NaN, or what they must not see
       const int i = __ffs(again) - 1;
       again &= again - 1;
