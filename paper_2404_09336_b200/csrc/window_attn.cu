@@ -15,9 +15,9 @@
 
 namespace ssa {
 
-constexpr int kRows = 16;              // query rows of a block: (token, head of the group) pairs
-constexpr int kKeys = 16;              // positions of a warp's tile
-constexpr int kWarps = 4;              // of a block; they take the block's tiles in turn
+constexpr int kRows = 16;              // query rows of a warp: (token, head of the group) pairs
+constexpr int kKeys = 16;              // positions of a tile
+constexpr int kWarps = 4;              // of a block
 constexpr int kSplitTiles = 16;        // fewest tiles worth a split of their own
 
 // The weights enter the second contraction as a 16-bit value plus the 16-bit rest, so that the sums keep 16 bits (bf16) or 22
@@ -26,26 +26,32 @@ template <typename T> struct Weight { using Type = __half; static constexpr floa
 template <> struct Weight<__nv_bfloat16> { using Type = __nv_bfloat16; static constexpr float kShift = 0.f; };
 
 // How a lane's pieces of a cache row are cut.  The order of the dimensions within a contraction is free as long as both sides
-// agree, so lanes take whole 16-byte pieces.
+// agree, so lanes take whole 16-byte pieces (8 bytes of V's 64-byte rows).
 template <typename T, int D>
 struct RowPieces {
-  static constexpr int kK = kIsFp8<T> ? 16 : 8;                        // elements of a piece of K, 4 lanes per row
-  static constexpr int kNK = D / (4 * kK);
-  static constexpr int kV = kIsFp8<T> && D == 128 ? 16 : 8;            // elements of a piece of V, 8 lanes per row
-  static constexpr int kNV = D / (8 * kV);
-  static constexpr int kVWords = kV * (kIsFp8<T> ? 1 : 2) / 4;
+  static constexpr int kBytes = kIsFp8<T> ? 1 : 2, kRow = D * kBytes, kChunks = kRow / 16;
+  static constexpr int kK = 16 / kBytes, kNK = D / (4 * kK);           // elements of a piece of K, 4 lanes per row
+  static constexpr int kV = D == 64 ? 8 : 16 / kBytes, kNV = D / (8 * kV);   // of V, 8 lanes per row
+  static constexpr int kVWords = kV * kBytes / 4;
+  static constexpr int kTile = 2 * kKeys * kRow;                       // bytes of K and V of a tile
+  static constexpr int kRingTiles = kTile >= 8192 ? 3 : 6;             // per warp: 24 KB, less for rows of 64 bytes
+  static constexpr int kSmem = kWarps * kRingTiles * kTile;
 };
 
-template <int kWords>
-__device__ __forceinline__ void load_words(uint32_t (&w)[kWords], const void* p) {
-  if constexpr (kWords == 4) {
-    const uint4 x = ld_stream_16B(p);
-    w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
-  } else {
-    static_assert(kWords == 2, "");
-    asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
-  }
+// Where 16-byte piece `chunk` of row `key` lies in a tile: reads of K (lanes 4g+c: rows g, pieces c) and of V (rows 2c, pieces g)
+// by eight lanes at a time then hit eight different bank groups.
+template <int kChunks>
+__device__ __forceinline__ int chunk_at(int key, int chunk) {
+  const int x = ((key >> 1 & 3) << 1) ^ ((key & 1) << 2);
+  return key * kChunks + (chunk ^ (x & (kChunks - 1)));
 }
+
+__device__ __forceinline__ void copy_16B(uint32_t to, const void* from, bool there) {     // zeros where it is not
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
 // Two e4m3 values -> two bf16 or two fp16 values (exact).
 __device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t pair) {
@@ -67,47 +73,85 @@ template <> __device__ __forceinline__ bool pair_not_finite<__half>(uint32_t w) 
   return (w & 0x7c00u) == 0x7c00u || (w & 0x7c000000u) == 0x7c000000u;
 }
 
-// grid (splits x row tiles, H_kv, B).  Fragments come straight from global memory: with the lane layout below, a load
-// instruction takes whole 32-byte sectors, and no value passes through shared memory before the warps' results are joined.
+// grid (splits x row blocks, H_kv, B).  A team of kTeam warps, sixteen query rows each, shares the tiles that it copies into a
+// ring of its own (16 bytes a lane, asynchronously; no block barrier inside the loop); the block's teams take tiles in turn.
+// Matrix fragments come out of the ring in whole 16-byte pieces:
 //   S[16 rows, 8 keys] += Q . K^T   lane 4g+c holds key g's pieces c, c+4, ... ; step s of the contraction takes four of
 //                                   their elements from every lane, and Q's registers follow the same order
 //   O[16 rows, 8 dims] += P . V     lane 4g+c holds, of keys 2c, 2c+1, 2c+8, 2c+9, the pieces g, g+8, ... ; dimension e of
 //                                   all lanes' pieces is one tile of eight
-template <typename T, int D, bool kPaged, bool kMass>
+template <typename T, int D, bool kPaged, bool kMass, int kTeam>
 __global__ void __launch_bounds__(kWarps * 32, 2)
 window_rows_kernel(const WindowParams p) {
   using TQ = typename Storage<T>::Query;
   using TP = typename Weight<T>::Type;
   using RP = RowPieces<T, D>;
   constexpr float kShift = Weight<T>::kShift;
-  constexpr int kSteps = D / 16, kBytes = kIsFp8<T> ? 1 : 2, kTiles = RP::kNV * RP::kV;
-  __shared__ float s_acc[kWarps][kRows][D + 4];
+  constexpr int kSteps = D / 16, kTiles = RP::kNV * RP::kV, kTeams = kWarps / kTeam, kRing = RP::kRingTiles * kTeam;
+  extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float2 s_ml[kWarps][kRows];
+  __shared__ uint32_t s_have[kTeams][kRing];                 // which rows of a tile have a page
 
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, c = lane % 4;
-  const int split = blockIdx.x % p.n_splits, row0 = blockIdx.x / p.n_splits * kRows;
-  const int hkv = blockIdx.y, b = blockIdx.z;
+  const int team = warp / kTeam, member = warp % kTeam;
+  const int block = p.n_splits == 1 ? blockIdx.x : blockIdx.x / p.n_splits, split = blockIdx.x - block * p.n_splits;
+  const int hkv = blockIdx.y, b = blockIdx.z, row0 = block * kTeam * kRows;
   grid_dependency_wait();
   grid_launch_dependents();
   uint32_t flags = 0;
   int ctx, n_new;
   window_sizes(p, b, ctx, n_new, flags);
   if (flags && p.status && split == 0 && row0 == 0 && hkv == 0 && threadIdx.x == 0) atomicOr(p.status, flags);
-  const int rows = min(kRows, n_new * p.group - row0);       // rows of tokens that exist
+  const int rows = min(kTeam * kRows, n_new * p.group - row0);         // rows of tokens that exist
   if (rows <= 0) return;
-  const int first = ctx - n_new;
-  const Seen seen(p, kKeys, first, row0 / p.group, (row0 + rows - 1) / p.group);
+  const int first = ctx - n_new, t_lo = token_of(p, row0), t_hi = token_of(p, row0 + rows - 1);
+  const Seen seen(p, kKeys, first, t_lo, t_hi);
   const int n_splits = splits_used(p, seen.tiles);
   if (split >= n_splits) return;
   const int2 range = split_tiles(seen.tiles, split, n_splits);
+  const int lo = first + t_lo, hi = first + t_hi;
+
+  const int32_t* table = kPaged ? p.page_table + (int64_t)b * p.page_table_stride : nullptr;
+  const char* kb = reinterpret_cast<const char*>(p.k) + ((kPaged ? 0 : (int64_t)b * p.k_sb) + (int64_t)hkv * p.k_sh) * RP::kBytes;
+  const char* vb = reinterpret_cast<const char*>(p.v) + ((kPaged ? 0 : (int64_t)b * p.v_sb) + (int64_t)hkv * p.v_sh) * RP::kBytes;
+  uint8_t* const ring = smem + team * (kRing * RP::kTile);
+  const int n_tiles = (range.y - range.x - team + kTeams - 1) / kTeams;     // of this team
+  auto load = [&](int n) {
+    if (n < n_tiles) {
+      const int stage = n % kRing, j = seen.position(range.x + team + n * kTeams) + lane % kKeys;
+      // what no row sees is not read: it may hold anything, or have no page
+      const bool any = j <= hi && (p.window == 0 || j > lo - p.window || j < p.sinks);
+      const int row = any ? (int)row_of<kPaged>(p, table, j) : -1;
+      if (kPaged && any && row < 0) flags |= SSA_DEV_BAD_INDEX;
+      const unsigned have = __ballot_sync(~0u, row >= 0);
+      if (lane == 0 && member == 0) s_have[team][stage] = have;
+      const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring + stage * RP::kTile);
+      constexpr int kAll = kKeys * RP::kChunks, kLanes = 32 * kTeam;
+#pragma unroll
+      for (int i = 0; i < (kAll + kLanes - 1) / kLanes; ++i) {
+        const int x = i * kLanes + member * 32 + lane;
+        const int key = x / RP::kChunks % kKeys, chunk = x % RP::kChunks;
+        const int64_t from = __shfl_sync(~0u, row, key);
+        if (kAll % kLanes == 0 || x < kAll) {
+          const uint32_t at = to + chunk_at<RP::kChunks>(key, chunk) * 16;
+          copy_16B(at, kb + (from < 0 ? 0 : from * p.k_st) * RP::kBytes + chunk * 16, from >= 0);
+          copy_16B(at + kKeys * RP::kRow, vb + (from < 0 ? 0 : from * p.v_st) * RP::kBytes + chunk * 16, from >= 0);
+        }
+      }
+    }
+    copies_commit();
+  };
+#pragma unroll 1
+  for (int n = 0; n < kRing - 1; ++n) load(n);
 
   // my two rows of every tile: positions (a row that does not exist sees nothing) and the queries' registers
+  const int wrow0 = row0 + member * kRows, wrows = min(kRows, rows - member * kRows);
   int pos[2];
   uint32_t qa[kSteps][4];
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
-    const int row = row0 + g + 8 * r, t = row / p.group, h = hkv * p.group + row % p.group;
-    const bool there = g + 8 * r < rows;
+    const int row = wrow0 + g + 8 * r, t = token_of(p, row), h = hkv * p.group + row - t * p.group;
+    const bool there = g + 8 * r < wrows;
     pos[r] = there ? first + t : -1;
     const TQ* q = reinterpret_cast<const TQ*>(p.q) + (int64_t)b * p.q_sb + (int64_t)h * p.q_sh + (int64_t)t * p.q_st;
 #pragma unroll
@@ -120,57 +164,13 @@ window_rows_kernel(const WindowParams p) {
         qa[u * (RP::kK / 4) + i][r + 2] = x.y;
       }
   }
-  // every row of the tile sees all of [all_lo, lo]; the sinks as well
-  const int lo = first + row0 / p.group, hi = first + (row0 + rows - 1) / p.group;
-  const int all_lo = p.window == 0 ? 0 : hi - p.window + 1;
-
-  const int32_t* table = kPaged ? p.page_table + (int64_t)b * p.page_table_stride : nullptr;
-  const char* kb = reinterpret_cast<const char*>(p.k) + ((kPaged ? 0 : (int64_t)b * p.k_sb) + (int64_t)hkv * p.k_sh) * kBytes;
-  const char* vb = reinterpret_cast<const char*>(p.v) + ((kPaged ? 0 : (int64_t)b * p.v_sb) + (int64_t)hkv * p.v_sh) * kBytes;
-
-  float acc[kTiles][4], m[2], l[2];
-  uint32_t kw[2][RP::kNK][4], vw[4][RP::kNV][RP::kVWords];
-  int64_t k_row[2], v_row[4];                                // rows of the tile that is loaded next; -1: not read
-  auto find = [&](int tile) {
-    const int j0 = seen.position(tile);
-    // what no row sees is not read: it may hold anything, or have no page
-    auto any = [&](int j) { return j <= hi && (p.window == 0 || j > lo - p.window || j < p.sinks); };
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int j = j0 + g + 8 * x;
-      k_row[x] = any(j) ? row_of<kPaged>(p, table, j) : -1;
-      if (kPaged && any(j) && k_row[x] < 0) flags |= SSA_DEV_BAD_INDEX;
-    }
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const int j = j0 + 2 * c + (x & 1) + 4 * (x & 2);
-      v_row[x] = any(j) ? row_of<kPaged>(p, table, j) : -1;
-    }
-  };
-  auto load_k = [&]() {
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int u = 0; u < RP::kNK; ++u) {
-        if (k_row[x] >= 0) load_words(kw[x][u], kb + (k_row[x] * p.k_st + (u * 4 + c) * RP::kK) * kBytes);
-        else kw[x][u][0] = kw[x][u][1] = kw[x][u][2] = kw[x][u][3] = 0;
-      }
-  };
-  auto load_v = [&]() {
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-      for (int u = 0; u < RP::kNV; ++u) {
-        if (v_row[x] >= 0) load_words(vw[x][u], vb + (v_row[x] * p.v_st + (u * 8 + g) * RP::kV) * kBytes);
-        else
-#pragma unroll
-          for (int i = 0; i < RP::kVWords; ++i) vw[x][u][i] = 0;
-      }
-  };
+  // every row of the warp sees all of [all_lo, all_hi]; the sinks as well
+  const int all_hi = first + token_of(p, wrow0), all_lo = p.window == 0 ? 0 : first + token_of(p, wrow0 + max(wrows, 1) - 1) - p.window + 1;
 
   // An infinite or NaN element of V must not reach rows that do not see it (0 * inf), and has to stay infinite for those that do
-  // (its product with a weight's two parts may be inf - inf).  Sums that come out finite met none; else the warp goes through
+  // (its product with a weight's two parts may be inf - inf).  Sums that come out finite met none; else the block goes through
   // its tiles once more and takes such elements out of the contraction, to add them to the rows that see them.
+  float acc[kTiles][4], m[2], l[2];
   bool careful = false;
 again:
 #pragma unroll
@@ -179,10 +179,16 @@ again:
     for (int e = 0; e < 4; ++e) acc[i][e] = 0.f;
   m[0] = m[1] = neg_inf();
   l[0] = l[1] = 0.f;
-  int tile = range.x + warp;
-  if (tile < range.y) { find(tile); load_k(); load_v(); }
-  for (; tile < range.y; tile += kWarps) {
-    const int j0 = seen.position(tile);
+#pragma unroll 1
+  for (int n = 0; n < n_tiles; ++n) {
+    copies_wait<kRing - 2>();
+    if constexpr (kTeam == 1) __syncwarp();                  // the tile is there, and every warp of the team has left the last one
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "n"(kTeam * 32) : "memory");
+    const int j0 = seen.position(range.x + team + n * kTeams), stage = n % kRing;
+    const uint8_t* const kt = ring + stage * RP::kTile;
+    const uint8_t* const vt = kt + kKeys * RP::kRow;
+    load(n + kRing - 1);
+    if (kTeam > 1 && wrows <= 0) continue;
     float s[2][4];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
@@ -190,53 +196,39 @@ again:
       for (int e = 0; e < 4; ++e) s[x][e] = 0.f;
 #pragma unroll
       for (int u = 0; u < RP::kNK; ++u) {
+        const uint4 w4 = *reinterpret_cast<const uint4*>(kt + chunk_at<RP::kChunks>(g + 8 * x, u * 4 + c) * 16);
+        const uint32_t kw[4] = {w4.x, w4.y, w4.z, w4.w};
         if constexpr (kIsFp8<T>) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             mma_16816<TQ>(s[x], qa[u * 4 + i][0], qa[u * 4 + i][1], qa[u * 4 + i][2], qa[u * 4 + i][3],
-                          e4m3x2_to_bf162(kw[x][u][i] & 0xffffu), e4m3x2_to_bf162(kw[x][u][i] >> 16), s[x]);
+                          e4m3x2_to_bf162(kw[i] & 0xffffu), e4m3x2_to_bf162(kw[i] >> 16), s[x]);
         } else {
 #pragma unroll
           for (int i = 0; i < 2; ++i)
-            mma_16816<TQ>(s[x], qa[u * 2 + i][0], qa[u * 2 + i][1], qa[u * 2 + i][2], qa[u * 2 + i][3], kw[x][u][2 * i],
-                          kw[x][u][2 * i + 1], s[x]);
+            mma_16816<TQ>(s[x], qa[u * 2 + i][0], qa[u * 2 + i][1], qa[u * 2 + i][2], qa[u * 2 + i][3], kw[2 * i], kw[2 * i + 1], s[x]);
         }
       }
     }
-    bool all_there = true;
-    bool skipped[2][2] = {{false, false}, {false, false}};   // pages that do not exist: the keys of my scores
-    if constexpr (kPaged) {
-      const unsigned have0 = __ballot_sync(~0u, k_row[0] >= 0), have1 = __ballot_sync(~0u, k_row[1] >= 0);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        skipped[0][e] = !((have0 >> ((2 * c + e) * 4)) & 1);
-        skipped[1][e] = !((have1 >> ((2 * c + e) * 4)) & 1);
-      }
-      all_there = (have0 & have1) == ~0u;
-    }
-    const int next = tile + kWarps;
-    int64_t v_now[4];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) v_now[x] = v_row[x];
-    if (next < range.y) { find(next); load_k(); }
+    const unsigned have = kPaged ? s_have[team][stage] : 0xffffu;
 
     // scores in log2 units; what a row does not see is -inf
-    const bool whole = all_there && j0 + kKeys - 1 <= lo && (j0 >= all_lo || j0 + kKeys <= p.sinks);
+    const bool whole = (have & 0xffffu) == 0xffffu && j0 + kKeys - 1 <= all_hi && (j0 >= all_lo || j0 + kKeys <= p.sinks);
     float top[2] = {m[0], m[1]};
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int r = e / 2;
+        const int r = e / 2, key = 8 * x + 2 * c + (e & 1);
         s[x][e] *= p.scale_log2;
-        if (!whole && (skipped[x][e & 1] || !sees(p, pos[r], j0 + 8 * x + 2 * c + (e & 1)))) s[x][e] = neg_inf();
+        if (!whole && (!(have >> key & 1) || !sees(p, pos[r], j0 + key))) s[x][e] = neg_inf();
         top[r] = fmaxf(top[r], s[x][e]);
       }
     if constexpr (kMass) {
 #pragma unroll
       for (int r = 0; r < 2; ++r)
-        if (g + 8 * r < rows) {
-          const int row = row0 + g + 8 * r, t = row / p.group, h = hkv * p.group + row % p.group;
+        if (g + 8 * r < wrows) {
+          const int row = wrow0 + g + 8 * r, t = token_of(p, row), h = hkv * p.group + row - t * p.group;
           float* to = p.ws_s + (((int64_t)b * p.H + h) * p.n_q + t) * p.s_pitch + j0 + 2 * c;
 #pragma unroll
           for (int x = 0; x < 2; ++x) *reinterpret_cast<float2*>(to + 8 * x) = make_float2(s[x][2 * r], s[x][2 * r + 1]);
@@ -272,84 +264,93 @@ again:
         pl[2 * x + r] = pack2<TP>(w0 - back.x, w1 - back.y);
       }
     bool odd = false;
-    if (careful) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
+    for (int u = 0; u < RP::kNV; ++u) {
+      uint32_t vw[4][RP::kVWords];
 #pragma unroll
-        for (int u = 0; u < RP::kNV; ++u)
+      for (int x = 0; x < 4; ++x) {
+        const int key = 2 * c + (x & 1) + 4 * (x & 2);
+        if constexpr (RP::kVWords == 4) {
+          const uint4 w = *reinterpret_cast<const uint4*>(vt + chunk_at<RP::kChunks>(key, u * 8 + g) * 16);
+          vw[x][0] = w.x; vw[x][1] = w.y; vw[x][2] = w.z; vw[x][3] = w.w;
+        } else {
+          const uint2 w = *reinterpret_cast<const uint2*>(vt + chunk_at<RP::kChunks>(key, g / 2) * 16 + g % 2 * 8);
+          vw[x][0] = w.x; vw[x][1] = w.y;
+        }
+      }
+      if (careful) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
 #pragma unroll
           for (int i = 0; i < RP::kVWords; ++i) {
             if constexpr (kIsFp8<T>) {
 #pragma unroll
               for (int y = 0; y < 32; y += 8) {
-                if (((vw[x][u][i] >> y) & 0x7fu) == 0x7fu) { odd = true; vw[x][u][i] &= ~(0xffu << y); }
+                if (((vw[x][i] >> y) & 0x7fu) == 0x7fu) { odd = true; vw[x][i] &= ~(0xffu << y); }
               }
-            } else if (pair_not_finite<TQ>(vw[x][u][i])) {
+            } else if (pair_not_finite<TQ>(vw[x][i])) {
               odd = true;
-              if (pair_not_finite<TQ>(vw[x][u][i] & 0xffffu)) vw[x][u][i] &= 0xffff0000u;
-              if (pair_not_finite<TQ>(vw[x][u][i] & 0xffff0000u)) vw[x][u][i] &= 0xffffu;
+              if (pair_not_finite<TQ>(vw[x][i] & 0xffffu)) vw[x][i] &= 0xffff0000u;
+              if (pair_not_finite<TQ>(vw[x][i] & 0xffff0000u)) vw[x][i] &= 0xffffu;
             }
           }
-    }
-#pragma unroll
-    for (int u = 0; u < RP::kNV; ++u)
+      }
 #pragma unroll
       for (int e = 0; e < RP::kV; ++e) {
         uint32_t b0, b1;
         if constexpr (kIsFp8<T>) {
           // byte e of the four keys' pieces, two keys to a word
-          const uint32_t a = __byte_perm(vw[0][u][e / 4], vw[1][u][e / 4], (e % 4) | ((e % 4 + 4) << 4));
-          const uint32_t z = __byte_perm(vw[2][u][e / 4], vw[3][u][e / 4], (e % 4) | ((e % 4 + 4) << 4));
+          const uint32_t a = __byte_perm(vw[0][e / 4], vw[1][e / 4], (e % 4) | ((e % 4 + 4) << 4));
+          const uint32_t z = __byte_perm(vw[2][e / 4], vw[3][e / 4], (e % 4) | ((e % 4 + 4) << 4));
           b0 = e4m3x2_to_half2(a & 0xffffu);
           b1 = e4m3x2_to_half2(z & 0xffffu);
         } else {
           constexpr uint32_t kLow = 0x5410, kHigh = 0x7632;
-          b0 = __byte_perm(vw[0][u][e / 2], vw[1][u][e / 2], e & 1 ? kHigh : kLow);
-          b1 = __byte_perm(vw[2][u][e / 2], vw[3][u][e / 2], e & 1 ? kHigh : kLow);
+          b0 = __byte_perm(vw[0][e / 2], vw[1][e / 2], e & 1 ? kHigh : kLow);
+          b1 = __byte_perm(vw[2][e / 2], vw[3][e / 2], e & 1 ? kHigh : kLow);
         }
         float (&o)[4] = acc[u * RP::kV + e];
         mma_16816<TP>(o, ph[0], ph[1], ph[2], ph[3], b0, b1, o);
         mma_16816<TP>(o, pl[0], pl[1], pl[2], pl[3], b0, b1, o);
       }
+    }
     if (careful && __any_sync(~0u, odd)) {                   // add what was taken out, element by element
-      for (int y = 0; y < kKeys; ++y) {
-        const int from = (y % 8) / 2, which = (y % 2) + 2 * (y / 8);   // the lane that holds this key's row, and which of its four
-        const int64_t mine = which == 0 ? v_now[0] : which == 1 ? v_now[1] : which == 2 ? v_now[2] : v_now[3];
-        const int64_t row = __shfl_sync(~0u, mine, from);
-        if (row < 0) continue;
+#pragma unroll 1
+      for (int key = 0; key < kKeys; ++key)
 #pragma unroll
         for (int u = 0; u < RP::kNV; ++u)
 #pragma unroll
-          for (int e = 0; e < RP::kV; ++e)
+          for (int z = 0; z < 2; ++z)
 #pragma unroll
-            for (int z = 0; z < 2; ++z) {
-              const int d = (u * 8 + 2 * c + z) * RP::kV + e;
+            for (int e = 0; e < RP::kV; ++e) {
+              const int at = ((u * 8 + 2 * c + z) * RP::kV + e) * RP::kBytes;
+              const uint8_t* v = vt + chunk_at<RP::kChunks>(key, at / 16) * 16 + at % 16;
               float x;
-              if constexpr (kIsFp8<T>) x = e4m3x2_to_float2(reinterpret_cast<const uint8_t*>(vb)[row * p.v_st + d]).x;
-              else x = to_float(reinterpret_cast<const TQ*>(vb)[row * p.v_st + d]);
+              if constexpr (kIsFp8<T>) x = e4m3x2_to_float2(*v).x;
+              else x = to_float(*reinterpret_cast<const TQ*>(v));
               if (!isfinite(x)) {
 #pragma unroll
                 for (int r = 0; r < 2; ++r)
-                  if (sees(p, pos[r], j0 + y)) acc[u * RP::kV + e][2 * r + z] += x;
+                  if (sees(p, pos[r], j0 + key)) acc[u * RP::kV + e][2 * r + z] += x;
               }
             }
-      }
     }
-    if (next < range.y) load_v();
   }
-  if (!careful) {
-    bool finite = true;
+  copies_wait<0>();
+  bool finite = true;
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i)
+  for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) finite &= fabsf(acc[i][e]) <= 3.402823466e38f;
-    if (__any_sync(~0u, !finite)) {
-      careful = true;
-      goto again;
-    }
+    for (int e = 0; e < 4; ++e) finite &= fabsf(acc[i][e]) <= 3.402823466e38f;
+  if (__syncthreads_or(!finite) && !careful) {               // (the barrier: the rings' place is free from here on)
+    careful = true;
+#pragma unroll 1
+    for (int n = 0; n < kRing - 1; ++n) load(n);
+    goto again;
   }
 
-  // the warps' results, joined by the block
+  // the teams' results, joined by the block
+  float (*s_acc)[kRows][D + 4] = reinterpret_cast<float (*)[kRows][D + 4]>(smem);
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     l[r] += __shfl_xor_sync(~0u, l[r], 1);
@@ -365,20 +366,22 @@ again:
   if (kPaged && p.status && (flags & SSA_DEV_BAD_INDEX)) atomicOr(p.status, SSA_DEV_BAD_INDEX);
   __syncthreads();
   for (int i = warp; i < rows; i += kWarps) {
-    float M = neg_inf(), L = 0.f, w[kWarps];
+    const int of = i / kRows, y = i % kRows;                 // member of every team, its row
+    float M = neg_inf(), L = 0.f, w[kTeams];
 #pragma unroll
-    for (int x = 0; x < kWarps; ++x) M = fmaxf(M, s_ml[x][i].x);
+    for (int x = 0; x < kTeams; ++x) M = fmaxf(M, s_ml[x * kTeam + of][y].x);
 #pragma unroll
-    for (int x = 0; x < kWarps; ++x) {
-      w[x] = s_ml[x][i].y == 0.f ? 0.f : fast_exp2(s_ml[x][i].x - M);
-      L += s_ml[x][i].y * w[x];
+    for (int x = 0; x < kTeams; ++x) {
+      const float2 ml = s_ml[x * kTeam + of][y];
+      w[x] = ml.y == 0.f ? 0.f : fast_exp2(ml.x - M);
+      L += ml.y * w[x];
     }
-    const int row = row0 + i, t = row / p.group, h = hkv * p.group + row % p.group;
+    const int row = row0 + i, t = token_of(p, row), h = hkv * p.group + row - t * p.group;
     const int64_t at = ((int64_t)b * p.H + h) * p.n_q + t, slot = at * p.n_splits + split;
     for (int d = lane; d < D; d += 32) {
       float A = 0.f;
 #pragma unroll
-      for (int x = 0; x < kWarps; ++x) A += s_acc[x][i][d] * w[x];
+      for (int x = 0; x < kTeams; ++x) A += s_acc[x * kTeam + of][y][d] * w[x];
       if (n_splits == 1) store_window_value<TQ>(p, b, h, t, d, L == 0.f ? 0.f : A / L);
       else p.ws_acc[slot * D + d] = A;
     }
@@ -447,7 +450,7 @@ window_mass_kernel(const WindowParams p, const int mass_blocks) {
   for (int i = threadIdx.x / 32; i < n_rows; i += kMassThreads / 32) {       // normalisers, a warp each
     const int h = i / p.n_q, t = i % p.n_q, lane = threadIdx.x % 32;
     if (t >= n_new) continue;
-    const int row0 = (t * p.group + h % p.group) / kRows * kRows, rows = min(kRows, n_new * p.group - row0);
+    const int row0 = (t * p.group + h % p.group) / p.block_rows * p.block_rows, rows = min(p.block_rows, n_new * p.group - row0);
     const Seen seen(p, kKeys, first, row0 / p.group, (row0 + rows - 1) / p.group);
     const int n = splits_used(p, seen.tiles);
     const float2* ml = p.ws_ml + (((int64_t)b * p.H + h) * p.n_q + t) * p.n_splits;
@@ -477,7 +480,7 @@ window_mass_kernel(const WindowParams p, const int mass_blocks) {
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
-struct WindowPlan { bool tiles; int n_splits, s_pitch; size_t ml_bytes, acc_bytes, s_bytes, total_bytes; };
+struct WindowPlan { bool tiles; int block_rows, n_splits, s_pitch; size_t ml_bytes, acc_bytes, s_bytes, total_bytes; };
 
 int32_t check_paging(const ssa_paging* pg, int32_t max_ctx) {
   if (!pg->page_table) return SSA_ERR_NULL;
@@ -506,12 +509,14 @@ static bool tiles_pay(const ssa_attn_desc* d, const ssa_window* w, bool mass) {
 
 static bool plan_window(const ssa_attn_desc* d, const ssa_window* w, bool mass, bool tiles, WindowPlan* pl) {
   pl->tiles = tiles;
-  const int rows = tiles ? kBlockRows : kRows, keys = tiles ? kTileKeys : kKeys, fewest = tiles ? kTileSplit : kSplitTiles;
-  const long long group = d->H / d->H_kv, row_tiles = (group * w->n_q + rows - 1) / rows;
+  const long long per_head = (long long)(d->H / d->H_kv) * w->n_q;
+  const int rows = tiles ? kBlockRows : per_head <= kRows ? kRows : per_head <= 2 * kRows ? 2 * kRows : 4 * kRows, keys = tiles ? kTileKeys : kKeys, fewest = tiles ? kTileSplit : kSplitTiles;
+  const long long group = d->H / d->H_kv, row_tiles = (per_head + rows - 1) / rows;
   const long long blocks = row_tiles * d->H_kv * d->B, tokens = (rows - 1) / group + 2;
   const long long most = w->window == 0 ? d->max_ctx : std::min<long long>(d->max_ctx, (long long)w->window + w->sinks + tokens);
   const long long n_tiles = (most + keys - 1) / keys + 2;
   const long long wanted = tiles ? sm_count() / blocks : (4ll * sm_count() + blocks - 1) / blocks;
+  pl->block_rows = rows;
   pl->n_splits = (int)std::max(1ll, std::min({wanted, n_tiles / fewest, 256ll}));
   const size_t slots = (size_t)d->B * d->H * w->n_q * pl->n_splits;
   pl->ml_bytes = up256(slots * sizeof(float2));
@@ -541,22 +546,29 @@ static cudaError_t launch_tiles(const WindowParams& p, const CUtensorMap& k_map,
   return launch_pdl_smem(kernel, grid, dim3(kTileThreads), kSmem, st, p, k_map, v_map, box_rows);
 }
 
+template <typename T, int D, bool kPaged, bool kMass>
+static cudaError_t launch_rows(const WindowParams& p, cudaStream_t st) {
+  const dim3 grid((unsigned)((p.group * p.n_q + p.block_rows - 1) / p.block_rows * p.n_splits), (unsigned)p.H_kv, (unsigned)p.B);
+  auto kernel = p.block_rows == kRows       ? window_rows_kernel<T, D, kPaged, kMass, 1>
+                : p.block_rows == 2 * kRows ? window_rows_kernel<T, D, kPaged, kMass, 2>
+                                            : window_rows_kernel<T, D, kPaged, kMass, 4>;
+  constexpr int kSmem = std::max(RowPieces<T, D>::kSmem, kWarps * kRows * (D + 4) * 4);
+  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  return err != cudaSuccess ? err : launch_pdl_smem(kernel, grid, dim3(kWarps * 32), kSmem, st, p);
+}
+
 template <typename T, int D>
 static int32_t launch_window(const WindowParams& p, bool mass, const CUtensorMap* maps, int box_rows, cudaStream_t st) {
   using TQ = typename Storage<T>::Query;
-  const dim3 grid((unsigned)((p.group * p.n_q + kRows - 1) / kRows * p.n_splits), (unsigned)p.H_kv, (unsigned)p.B);
   cudaEvent_t begin, end;
   take_kernel_events(&begin, &end);
   if (begin) cudaEventRecord(begin, st);
   cudaError_t err = cudaErrorInvalidValue;
   if (maps) {
     if constexpr (!kIsFp8<T>) err = launch_tiles<T, D>(p, maps[0], maps[1], box_rows, st);
-  } else if (p.page_table) {
-    err = mass ? launch_pdl(window_rows_kernel<T, D, true, true>, grid, dim3(kWarps * 32), st, p)
-               : launch_pdl(window_rows_kernel<T, D, true, false>, grid, dim3(kWarps * 32), st, p);
   } else {
-    err = mass ? launch_pdl(window_rows_kernel<T, D, false, true>, grid, dim3(kWarps * 32), st, p)
-               : launch_pdl(window_rows_kernel<T, D, false, false>, grid, dim3(kWarps * 32), st, p);
+    err = p.page_table ? (mass ? launch_rows<T, D, true, true>(p, st) : launch_rows<T, D, true, false>(p, st))
+                       : (mass ? launch_rows<T, D, false, true>(p, st) : launch_rows<T, D, false, false>(p, st));
   }
   if (err != cudaSuccess) return SSA_ERR_CUDA;
   if (end) cudaEventRecord(end, st);
@@ -596,7 +608,7 @@ static int32_t run_window(const ssa_attn_desc* d, const ssa_window* w, const voi
                               d->v_stride_b, box_rows);
   if (!tiles && !plan_window(d, w, mass, false, &pl)) return SSA_ERR_SHAPE;
   WindowParams p;
-  p.block_rows = tiles ? kBlockRows : kRows;
+  p.block_rows = pl.block_rows;
   p.tile_keys = tiles ? kTileKeys : kKeys;
   p.split_tiles = tiles ? kTileSplit : kSplitTiles;
   p.q = q; p.k = k; p.v = v; p.out = out; p.lse = lse;
