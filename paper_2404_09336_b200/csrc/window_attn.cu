@@ -6,44 +6,62 @@
 //   mass_out[j] = decay mass_in[j] + sum over heads and tokens of exp(s_j - lse)
 //
 // window_rows_kernel serves few query rows per K/V head (decode steps, drafted tokens): all of a K/V head's query heads and
-// tokens are rows of one warp-level m16n8k16 tile, so a cached row is read once for sixteen of them.  HBM bounds it.
+// tokens are rows of warp-level m16n8k16 tiles, so a cached row is read once for up to 32 of them.  HBM bounds it.
 // window_tile_kernel (window_tile.cuh) serves many: prompt chunks.  The tensor cores bound it.
 #include <algorithm>
+#include <type_traits>
 
 #include "mma.cuh"
 #include "window_tile.cuh"
 
 namespace ssa {
 
-constexpr int kRows = 16;              // query rows of a warp: (token, head of the group) pairs
+constexpr int kRows = 8;               // query rows of a warp: (token, head of the group) pairs
 constexpr int kKeys = 16;              // positions of a tile
 constexpr int kWarps = 4;              // of a block
 constexpr int kSplitTiles = 16;        // fewest tiles worth a split of their own
+#ifndef SSA_RING_BYTES
+#define SSA_RING_BYTES 16384
+#endif
 
 // The weights enter the second contraction as a 16-bit value plus the 16-bit rest, so that the sums keep 16 bits (bf16) or 22
 // (fp16) of each.  fp16 has little range below 1: its weights are scaled by 2^13, which the sum divides out again.
 template <typename T> struct Weight { using Type = __half; static constexpr float kShift = 13.f; };
 template <> struct Weight<__nv_bfloat16> { using Type = __nv_bfloat16; static constexpr float kShift = 0.f; };
 
-// How a lane's pieces of a cache row are cut.  The order of the dimensions within a contraction is free as long as both sides
-// agree, so lanes take whole 16-byte pieces (8 bytes of V's 64-byte rows).
+// How the kernel cuts cache rows.  16-bit rows come out of shared memory by ldmatrix.  8-bit rows have to be converted on the
+// way; the order of the dimensions within a contraction is free as long as both sides agree, so lanes take whole 16-byte pieces
+// of them (8 bytes of V's 64-byte rows).
 template <typename T, int D>
-struct RowPieces {
+struct RowShape {
   static constexpr int kBytes = kIsFp8<T> ? 1 : 2, kRow = D * kBytes, kChunks = kRow / 16;
-  static constexpr int kK = 16 / kBytes, kNK = D / (4 * kK);           // elements of a piece of K, 4 lanes per row
-  static constexpr int kV = D == 64 ? 8 : 16 / kBytes, kNV = D / (8 * kV);   // of V, 8 lanes per row
-  static constexpr int kVWords = kV * kBytes / 4;
+  static constexpr int kNK = D / 64, kV = D / 8;                       // 8-bit: pieces of K per lane; elements of V's piece
   static constexpr int kTile = 2 * kKeys * kRow;                       // bytes of K and V of a tile
-  static constexpr int kRingTiles = kTile >= 8192 ? 3 : 6;             // per warp: 24 KB, less for rows of 64 bytes
-  static constexpr int kSmem = kWarps * kRingTiles * kTile;
+  static constexpr int kRingTiles = SSA_RING_BYTES / kTile < 6 ? SSA_RING_BYTES / kTile : 6;   // of a warp
+  static constexpr int kSmem = kWarps * kRingTiles * kTile, kJoin = kWarps * kRows * (D + 4) * 4;
 };
 
-// Where 16-byte piece `chunk` of row `key` lies in a tile: reads of K (lanes 4g+c: rows g, pieces c) and of V (rows 2c, pieces g)
-// by eight lanes at a time then hit eight different bank groups.
-template <int kChunks>
-__device__ __forceinline__ int chunk_at(int key, int chunk) {
-  const int x = ((key >> 1 & 3) << 1) ^ ((key & 1) << 2);
-  return key * kChunks + (chunk ^ (x & (kChunks - 1)));
+// Where 16-byte piece `chunk` of row `key` lies in a tile.  16-bit rows: the eight rows of an ldmatrix hit eight different bank
+// groups.  8-bit rows: so do reads of K (lanes 4g+c: rows g, pieces c) and of V (rows 2c, pieces g) by eight lanes at a time.
+template <typename T, int kChunks>
+__device__ __forceinline__ int turned(int key, int chunk) {
+  const int x = kIsFp8<T> ? ((key >> 1 & 3) << 1) ^ ((key & 1) << 2) : key & 7;
+  return chunk ^ (x & (kChunks - 1));
+}
+template <typename T, int kChunks>
+__device__ __forceinline__ int chunk_at(int key, int chunk) { return key * kChunks + turned<T, kChunks>(key, chunk); }
+
+template <bool kTrans>
+__device__ __forceinline__ void ldmatrix(uint32_t (&w)[4], uint32_t at) {
+  if constexpr (kTrans)
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
+  else
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t w) {
+  uint32_t t;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(t) : "r"(w));
+  return t;
 }
 
 __device__ __forceinline__ void copy_16B(uint32_t to, const void* from, bool there) {     // zeros where it is not
@@ -53,15 +71,34 @@ __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_
 template <int kLeft>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
-// Two e4m3 values -> two bf16 or two fp16 values (exact).
+// Two e4m3 values -> two fp16 values (exact).
 __device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t pair) {
   uint32_t h2;
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"((unsigned short)pair));
   return h2;
 }
-__device__ __forceinline__ uint32_t e4m3x2_to_bf162(uint32_t pair) {
-  const float2 f = e4m3x2_to_float2(pair);
-  return pack2<__nv_bfloat16>(f.x, f.y);
+
+// A row of bf16 queries over an 8-bit cache as fp16 values times a power of two that brings its largest to 2^14: what the others
+// lose is below 2^-39 of that.  w: the row's part of this lane, the rest in the three neighbouring lanes.  Returns the power's
+// inverse.
+template <int N>
+__device__ __forceinline__ float rows_to_half(uint32_t (&w)[N]) {
+  uint32_t most = 0;                                         // bits of the largest finite magnitude
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t a = w[i] & 0x7fffu, z = w[i] >> 16 & 0x7fffu;
+    most = max(most, max(a < 0x7f80u ? a : 0u, z < 0x7f80u ? z : 0u));
+  }
+  most = max(most, __shfl_xor_sync(~0u, most, 1));
+  most = max(most, __shfl_xor_sync(~0u, most, 2));
+  const int up = min(141 - (int)(most >> 7), 126);           // 2^up: the exponent 127 + 14 - that of the largest
+  const float by = __int_as_float((127 + up) << 23), back = __int_as_float((127 - up) << 23);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float2 f = unpack2<__nv_bfloat16>(w[i]);
+    w[i] = pack2<__half>(f.x * by, f.y * by);
+  }
+  return back;
 }
 
 // Whether one of two 16-bit values is infinite or NaN.
@@ -73,24 +110,24 @@ template <> __device__ __forceinline__ bool pair_not_finite<__half>(uint32_t w) 
   return (w & 0x7c00u) == 0x7c00u || (w & 0x7c000000u) == 0x7c000000u;
 }
 
-// grid (splits x row blocks, H_kv, B).  A team of kTeam warps, sixteen query rows each, shares the tiles that it copies into a
-// ring of its own (16 bytes a lane, asynchronously; no block barrier inside the loop); the block's teams take tiles in turn.
-// Matrix fragments come out of the ring in whole 16-byte pieces:
-//   S[16 rows, 8 keys] += Q . K^T   lane 4g+c holds key g's pieces c, c+4, ... ; step s of the contraction takes four of
-//                                   their elements from every lane, and Q's registers follow the same order
-//   O[16 rows, 8 dims] += P . V     lane 4g+c holds, of keys 2c, 2c+1, 2c+8, 2c+9, the pieces g, g+8, ... ; dimension e of
-//                                   all lanes' pieces is one tile of eight
+// grid (splits x row blocks, H_kv, B).  A team of kTeam warps, eight query rows each, shares the tiles that it copies into a ring
+// of its own (16 bytes a lane, asynchronously; no block barrier inside the loop); the block's teams take tiles in turn.  Cached
+// rows and dimensions are the long side of the matrix instructions, m16n8k16, query rows the short one:
+//   S^T[16 keys, 8 rows] += K . Q^T   and   O^T[16 dims, 8 rows] += V^T . P^T   (P transposed by movmatrix)
+// Lane 4g+c holds, of S^T, keys g and g + 8 of rows 2c and 2c + 1.  Bound by HBM where lists are long; by the instructions of a
+// tile (some 230) and a block's start and end where they are short.
 template <typename T, int D, bool kPaged, bool kMass, int kTeam>
-__global__ void __launch_bounds__(kWarps * 32, 2)
+__global__ void __launch_bounds__(kWarps * 32, 3)
 window_rows_kernel(const WindowParams p) {
   using TQ = typename Storage<T>::Query;
-  using TP = typename Weight<T>::Type;
-  using RP = RowPieces<T, D>;
+  using TP = typename Weight<T>::Type;                       // of the second contraction; of the first: TS
+  using TS = std::conditional_t<kIsFp8<T>, __half, TQ>;
+  using RS = RowShape<T, D>;
   constexpr float kShift = Weight<T>::kShift;
-  constexpr int kSteps = D / 16, kTiles = RP::kNV * RP::kV, kTeams = kWarps / kTeam, kRing = RP::kRingTiles * kTeam;
+  constexpr int kTeams = kWarps / kTeam, kRing = RS::kRingTiles * kTeam, kChunks = RS::kChunks;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float2 s_ml[kWarps][kRows];
-  __shared__ uint32_t s_have[kTeams][kRing];                 // which rows of a tile have a page
+  __shared__ uint32_t s_have[kTeams][kRing];                 // which rows of a tile there are: seen, and on a page that exists
 
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, c = lane % 4;
   const int team = warp / kTeam, member = warp % kTeam;
@@ -109,68 +146,109 @@ window_rows_kernel(const WindowParams p) {
   const int n_splits = splits_used(p, seen.tiles);
   if (split >= n_splits) return;
   const int2 range = split_tiles(seen.tiles, split, n_splits);
-  const int lo = first + t_lo, hi = first + t_hi;
+  const int lo = first + t_lo, hi = first + t_hi, from = p.window == 0 ? 0 : max(0, lo - p.window + 1);
 
   const int32_t* table = kPaged ? p.page_table + (int64_t)b * p.page_table_stride : nullptr;
-  const char* kb = reinterpret_cast<const char*>(p.k) + ((kPaged ? 0 : (int64_t)b * p.k_sb) + (int64_t)hkv * p.k_sh) * RP::kBytes;
-  const char* vb = reinterpret_cast<const char*>(p.v) + ((kPaged ? 0 : (int64_t)b * p.v_sb) + (int64_t)hkv * p.v_sh) * RP::kBytes;
-  uint8_t* const ring = smem + team * (kRing * RP::kTile);
+  uint8_t* const ring = smem + team * (kRing * RS::kTile);
+  const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
   const int n_tiles = (range.y - range.x - team + kTeams - 1) / kTeams;     // of this team
+  // a lane copies piece my_chunk of rows my_key, my_key + kPass, ... of K and of V
+  constexpr int kAll = kKeys * kChunks, kLanes = 32 * kTeam, kPass = kLanes / kChunks, kPasses = kAll < kLanes ? 1 : kAll / kLanes;
+  const int my = member * 32 + lane, my_key = my / kChunks, my_chunk = my % kChunks;
+  const bool copies = kAll >= kLanes || my < kAll;
+  const char* const kb = reinterpret_cast<const char*>(p.k) + my_chunk * 16 +
+                         ((kPaged ? 0 : (int64_t)b * p.k_sb) + (int64_t)hkv * p.k_sh) * RS::kBytes;
+  const char* const vb = reinterpret_cast<const char*>(p.v) + my_chunk * 16 +
+                         ((kPaged ? 0 : (int64_t)b * p.v_sb) + (int64_t)hkv * p.v_sh) * RS::kBytes;
+  const int64_t k_step = (int64_t)p.k_st * RS::kBytes, v_step = (int64_t)p.v_st * RS::kBytes;
   auto load = [&](int n) {
     if (n < n_tiles) {
-      const int stage = n % kRing, j = seen.position(range.x + team + n * kTeams) + lane % kKeys;
-      // what no row sees is not read: it may hold anything, or have no page
-      const bool any = j <= hi && (p.window == 0 || j > lo - p.window || j < p.sinks);
-      const int row = any ? (int)row_of<kPaged>(p, table, j) : -1;
-      if (kPaged && any && row < 0) flags |= SSA_DEV_BAD_INDEX;
-      const unsigned have = __ballot_sync(~0u, row >= 0);
-      if (lane == 0 && member == 0) s_have[team][stage] = have;
-      const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring + stage * RP::kTile);
-      constexpr int kAll = kKeys * RP::kChunks, kLanes = 32 * kTeam;
+      const int stage = n % kRing, j0 = seen.position(range.x + team + n * kTeams);
+      const uint32_t to = ring_at + stage * RS::kTile;
+      // tiles that are seen as a whole and lie on one page have rows in a row
+      int64_t at = -1;
+      if (j0 + kKeys - 1 <= hi && (j0 >= from || j0 + kKeys <= p.sinks) && (!kPaged || p.page_shift >= 4)) at = row_of<kPaged>(p, table, j0);
+      unsigned have = 0xffffu;
+      if (at >= 0) {
+        if (copies) {
+          const char *k = kb + (at + my_key) * k_step, *v = vb + (at + my_key) * v_step;
 #pragma unroll
-      for (int i = 0; i < (kAll + kLanes - 1) / kLanes; ++i) {
-        const int x = i * kLanes + member * 32 + lane;
-        const int key = x / RP::kChunks % kKeys, chunk = x % RP::kChunks;
-        const int64_t from = __shfl_sync(~0u, row, key);
-        if (kAll % kLanes == 0 || x < kAll) {
-          const uint32_t at = to + chunk_at<RP::kChunks>(key, chunk) * 16;
-          copy_16B(at, kb + (from < 0 ? 0 : from * p.k_st) * RP::kBytes + chunk * 16, from >= 0);
-          copy_16B(at + kKeys * RP::kRow, vb + (from < 0 ? 0 : from * p.v_st) * RP::kBytes + chunk * 16, from >= 0);
+          for (int i = 0; i < kPasses; ++i) {
+            const int key = i * kPass;
+            const uint32_t x = to + (my_key + key) * kChunks * 16 +
+                               (turned<T, kChunks>(my_key, my_chunk) ^ turned<T, kChunks>(key, 0)) * 16;
+            copy_16B(x, k, true);
+            copy_16B(x + kKeys * RS::kRow, v, true);
+            k += kPass * k_step;
+            v += kPass * v_step;
+          }
+        }
+      } else {
+        // what no row sees is not read: it may hold anything, or have no page
+        const int j = j0 + lane % kKeys;
+        const bool any = j <= hi && (j >= from || j < p.sinks);
+        const int row = any ? (int)row_of<kPaged>(p, table, j) : -1;
+        if (kPaged && any && row < 0) flags |= SSA_DEV_BAD_INDEX;
+        have = __ballot_sync(~0u, row >= 0);
+#pragma unroll 1
+        for (int i = 0; i < kPasses; ++i) {
+          const int key = (my_key + i * kPass) % kKeys;
+          const int64_t r = __shfl_sync(~0u, row, key);
+          if (copies) {
+            const uint32_t x = to + chunk_at<T, kChunks>(key, my_chunk) * 16;
+            copy_16B(x, kb + (r < 0 ? 0 : r * k_step), r >= 0);
+            copy_16B(x + kKeys * RS::kRow, vb + (r < 0 ? 0 : r * v_step), r >= 0);
+          }
         }
       }
+      if (lane == 0 && member == 0) s_have[team][stage] = have;
     }
     copies_commit();
   };
 #pragma unroll 1
   for (int n = 0; n < kRing - 1; ++n) load(n);
 
-  // my two rows of every tile: positions (a row that does not exist sees nothing) and the queries' registers
+  // the queries: row g of the warp's, as the short side of the first contraction; lanes' scores are of rows 2c, 2c + 1
   const int wrow0 = row0 + member * kRows, wrows = min(kRows, rows - member * kRows);
-  int pos[2];
-  uint32_t qa[kSteps][4];
-#pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    const int row = wrow0 + g + 8 * r, t = token_of(p, row), h = hkv * p.group + row - t * p.group;
-    const bool there = g + 8 * r < wrows;
-    pos[r] = there ? first + t : -1;
+  constexpr int kSteps = D / 16;
+  uint32_t qb[2 * kSteps];
+  float unit[2] = {p.scale_log2, p.scale_log2};
+  {
+    const int row = wrow0 + g, t = token_of(p, row), h = hkv * p.group + row - t * p.group;
     const TQ* q = reinterpret_cast<const TQ*>(p.q) + (int64_t)b * p.q_sb + (int64_t)h * p.q_sh + (int64_t)t * p.q_st;
 #pragma unroll
-    for (int u = 0; u < RP::kNK; ++u)
-#pragma unroll
-      for (int i = 0; i < RP::kK / 4; ++i) {
+    for (int i = 0; i < kSteps; ++i) {
+      if constexpr (kIsFp8<T>) {                             // step 4 u + i takes elements 4 i ... of the lane's piece 4 u + c
         uint2 x = make_uint2(0, 0);
-        if (there) x = *reinterpret_cast<const uint2*>(q + (u * 4 + c) * RP::kK + 4 * i);
-        qa[u * (RP::kK / 4) + i][r] = x.x;
-        qa[u * (RP::kK / 4) + i][r + 2] = x.y;
+        if (g < wrows) x = *reinterpret_cast<const uint2*>(q + (i / 4 * 4 + c) * 16 + i % 4 * 4);
+        qb[2 * i] = x.x;
+        qb[2 * i + 1] = x.y;
+      } else {
+        qb[2 * i] = g < wrows ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * c) : 0;
+        qb[2 * i + 1] = g < wrows ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * c + 8) : 0;
       }
+    }
+    if constexpr (kIsFp8<T>) {
+      const float back = rows_to_half(qb);
+#pragma unroll
+      for (int r = 0; r < 2; ++r) unit[r] = p.scale_log2 * __shfl_sync(~0u, back, (2 * c + r) * 4);
+    }
   }
+  int pos[2];                                                // (a row that does not exist sees nothing)
+#pragma unroll
+  for (int r = 0; r < 2; ++r) pos[r] = 2 * c + r < wrows ? first + token_of(p, wrow0 + 2 * c + r) : -1;
   // every row of the warp sees all of [all_lo, all_hi]; the sinks as well
-  const int all_hi = first + token_of(p, wrow0), all_lo = p.window == 0 ? 0 : first + token_of(p, wrow0 + max(wrows, 1) - 1) - p.window + 1;
+  const int all_hi = first + token_of(p, wrow0);
+  const int all_lo = p.window == 0 ? 0 : first + token_of(p, wrow0 + max(wrows, 1) - 1) - p.window + 1;
+  // ldmatrix addresses: lane i of matrix y = i / 8 gives row i % 8 of it.  K: keys 8 (y % 2) ..., pieces 2 s + y / 2;
+  // V: keys 8 (y / 2) ..., pieces 2 i + y % 2
+  const int k_key = lane % 16, v_key = lane % 8 + lane / 16 * 8;
 
   // An infinite or NaN element of V must not reach rows that do not see it (0 * inf), and has to stay infinite for those that do
   // (its product with a weight's two parts may be inf - inf).  Sums that come out finite met none; else the block goes through
   // its tiles once more and takes such elements out of the contraction, to add them to the rows that see them.
-  float acc[kTiles][4], m[2], l[2];
+  constexpr int kTiles = D / 16;
+  float acc[kTiles][4], m[2], l[2];                          // dimensions (16-bit: 16 i + g, + 8; 8-bit: g kV + 2 i, + 1), rows
   bool careful = false;
 again:
 #pragma unroll
@@ -185,155 +263,141 @@ again:
     if constexpr (kTeam == 1) __syncwarp();                  // the tile is there, and every warp of the team has left the last one
     else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "n"(kTeam * 32) : "memory");
     const int j0 = seen.position(range.x + team + n * kTeams), stage = n % kRing;
-    const uint8_t* const kt = ring + stage * RP::kTile;
-    const uint8_t* const vt = kt + kKeys * RP::kRow;
     load(n + kRing - 1);
     if (kTeam > 1 && wrows <= 0) continue;
-    float s[2][4];
+    const uint32_t k_at = ring_at + stage * RS::kTile, v_at = k_at + kKeys * RS::kRow;
+    const uint8_t* const kt = ring + stage * RS::kTile;
+    const uint8_t* const vt = kt + kKeys * RS::kRow;
+    const unsigned have = s_have[team][stage];
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (kIsFp8<T>) {
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
+      for (int u = 0; u < RS::kNK; ++u) {
+        const uint4 a4 = *reinterpret_cast<const uint4*>(kt + chunk_at<T, kChunks>(g, u * 4 + c) * 16);
+        const uint4 z4 = *reinterpret_cast<const uint4*>(kt + chunk_at<T, kChunks>(g + 8, u * 4 + c) * 16);
+        const uint32_t a[4] = {a4.x, a4.y, a4.z, a4.w}, z[4] = {z4.x, z4.y, z4.z, z4.w};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[x][e] = 0.f;
+        for (int i = 0; i < 4; ++i)
+          mma_16816<TS>(s, e4m3x2_to_half2(a[i] & 0xffffu), e4m3x2_to_half2(z[i] & 0xffffu), e4m3x2_to_half2(a[i] >> 16),
+                        e4m3x2_to_half2(z[i] >> 16), qb[2 * (u * 4 + i)], qb[2 * (u * 4 + i) + 1], s);
+      }
+    } else {
 #pragma unroll
-      for (int u = 0; u < RP::kNK; ++u) {
-        const uint4 w4 = *reinterpret_cast<const uint4*>(kt + chunk_at<RP::kChunks>(g + 8 * x, u * 4 + c) * 16);
-        const uint32_t kw[4] = {w4.x, w4.y, w4.z, w4.w};
-        if constexpr (kIsFp8<T>) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            mma_16816<TQ>(s[x], qa[u * 4 + i][0], qa[u * 4 + i][1], qa[u * 4 + i][2], qa[u * 4 + i][3],
-                          e4m3x2_to_bf162(kw[i] & 0xffffu), e4m3x2_to_bf162(kw[i] >> 16), s[x]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-            mma_16816<TQ>(s[x], qa[u * 2 + i][0], qa[u * 2 + i][1], qa[u * 2 + i][2], qa[u * 2 + i][3], kw[2 * i], kw[2 * i + 1], s[x]);
-        }
+      for (int i = 0; i < kSteps; ++i) {
+        uint32_t a[4];
+        ldmatrix<false>(a, k_at + chunk_at<T, kChunks>(k_key, 2 * i + lane / 16) * 16);
+        mma_16816<TS>(s, a[0], a[1], a[2], a[3], qb[2 * i], qb[2 * i + 1], s);
       }
     }
-    const unsigned have = kPaged ? s_have[team][stage] : 0xffffu;
 
     // scores in log2 units; what a row does not see is -inf
     const bool whole = (have & 0xffffu) == 0xffffu && j0 + kKeys - 1 <= all_hi && (j0 >= all_lo || j0 + kKeys <= p.sinks);
     float top[2] = {m[0], m[1]};
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = e / 2, key = 8 * x + 2 * c + (e & 1);
-        s[x][e] *= p.scale_log2;
-        if (!whole && (!(have >> key & 1) || !sees(p, pos[r], j0 + key))) s[x][e] = neg_inf();
-        top[r] = fmaxf(top[r], s[x][e]);
-      }
+    for (int e = 0; e < 4; ++e) {
+      const int r = e % 2, key = g + e / 2 * 8;
+      s[e] *= unit[r];
+      if (!whole && (!(have >> key & 1) || !sees(p, pos[r], j0 + key))) s[e] = neg_inf();
+      top[r] = fmaxf(top[r], s[e]);
+    }
     if constexpr (kMass) {
 #pragma unroll
       for (int r = 0; r < 2; ++r)
-        if (g + 8 * r < wrows) {
-          const int row = wrow0 + g + 8 * r, t = token_of(p, row), h = hkv * p.group + row - t * p.group;
-          float* to = p.ws_s + (((int64_t)b * p.H + h) * p.n_q + t) * p.s_pitch + j0 + 2 * c;
-#pragma unroll
-          for (int x = 0; x < 2; ++x) *reinterpret_cast<float2*>(to + 8 * x) = make_float2(s[x][2 * r], s[x][2 * r + 1]);
+        if (2 * c + r < wrows) {
+          const int row = wrow0 + 2 * c + r, t = token_of(p, row), h = hkv * p.group + row - t * p.group;
+          float* to = p.ws_s + (((int64_t)b * p.H + h) * p.n_q + t) * p.s_pitch + j0 + g;
+          to[0] = s[r];
+          to[8] = s[r + 2];
         }
     }
-    float shift[2], alpha[2];
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 1));
-      top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 2));
-      shift[r] = (top[r] == neg_inf() ? 0.f : top[r]) - kShift;
-      alpha[r] = fast_exp2(m[r] - kShift - shift[r]);        // (m = -inf: 0)
+    for (int o = 4; o < 32; o *= 2) {
+      top[0] = fmaxf(top[0], __shfl_xor_sync(~0u, top[0], o));
+      top[1] = fmaxf(top[1], __shfl_xor_sync(~0u, top[1], o));
     }
+    float shift[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) shift[r] = (top[r] == neg_inf() ? 0.f : top[r]) - kShift;
     if (__any_sync(~0u, top[0] != m[0] || top[1] != m[1])) {
 #pragma unroll
-      for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][e] *= alpha[e / 2];
-      l[0] *= alpha[0];
-      l[1] *= alpha[1];
-      m[0] = top[0];
-      m[1] = top[1];
-    }
-    uint32_t ph[4], pl[4];                                   // the weights as the A operand, and what their rounding left
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
       for (int r = 0; r < 2; ++r) {
-        const float w0 = fast_exp2(s[x][2 * r] - shift[r]), w1 = fast_exp2(s[x][2 * r + 1] - shift[r]);
-        l[r] += w0 + w1;
-        ph[2 * x + r] = pack2<TP>(w0, w1);
-        const float2 back = unpack2<TP>(ph[2 * x + r]);
-        pl[2 * x + r] = pack2<TP>(w0 - back.x, w1 - back.y);
-      }
-    bool odd = false;
+        const float alpha = fast_exp2(m[r] - kShift - shift[r]);       // (m = -inf: 0)
 #pragma unroll
-    for (int u = 0; u < RP::kNV; ++u) {
-      uint32_t vw[4][RP::kVWords];
+        for (int i = 0; i < kTiles; ++i) { acc[i][r] *= alpha; acc[i][r + 2] *= alpha; }
+        l[r] *= alpha;
+        m[r] = top[r];
+      }
+    }
+    uint32_t ph[2], pl[2];                                   // the weights, keys 0-7 and 8-15, and what their rounding left
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const float w0 = fast_exp2(s[2 * x] - shift[0]), w1 = fast_exp2(s[2 * x + 1] - shift[1]);
+      l[0] += w0;
+      l[1] += w1;
+      const uint32_t w = pack2<TP>(w0, w1);
+      const float2 back = unpack2<TP>(w);
+      ph[x] = transposed(w);
+      pl[x] = transposed(pack2<TP>(w0 - back.x, w1 - back.y));
+    }
+    bool odd = false;
+    uint32_t vw[4][kIsFp8<T> ? RS::kV / 4 : 1];              // 8-bit rows: the pieces of keys 2c, 2c + 1, 2c + 8, 2c + 9
+    if constexpr (kIsFp8<T>) {
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         const int key = 2 * c + (x & 1) + 4 * (x & 2);
-        if constexpr (RP::kVWords == 4) {
-          const uint4 w = *reinterpret_cast<const uint4*>(vt + chunk_at<RP::kChunks>(key, u * 8 + g) * 16);
+        if constexpr (D == 128) {
+          const uint4 w = *reinterpret_cast<const uint4*>(vt + chunk_at<T, kChunks>(key, g) * 16);
           vw[x][0] = w.x; vw[x][1] = w.y; vw[x][2] = w.z; vw[x][3] = w.w;
         } else {
-          const uint2 w = *reinterpret_cast<const uint2*>(vt + chunk_at<RP::kChunks>(key, g / 2) * 16 + g % 2 * 8);
+          const uint2 w = *reinterpret_cast<const uint2*>(vt + chunk_at<T, kChunks>(key, g / 2) * 16 + g % 2 * 8);
           vw[x][0] = w.x; vw[x][1] = w.y;
         }
       }
+    }
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+      uint32_t a[4];
+      if constexpr (kIsFp8<T>) {
+        // bytes 2 i, 2 i + 1 of two keys' pieces: two keys' values of one dimension, then of the next
+        const uint32_t x = __byte_perm(vw[0][i / 2], vw[1][i / 2], i % 2 ? 0x7362 : 0x5140);
+        const uint32_t z = __byte_perm(vw[2][i / 2], vw[3][i / 2], i % 2 ? 0x7362 : 0x5140);
+        a[0] = e4m3x2_to_half2(x & 0xffffu);
+        a[1] = e4m3x2_to_half2(x >> 16);
+        a[2] = e4m3x2_to_half2(z & 0xffffu);
+        a[3] = e4m3x2_to_half2(z >> 16);
+      } else {
+        ldmatrix<true>(a, v_at + chunk_at<T, kChunks>(v_key, 2 * i + lane / 8 % 2) * 16);
+      }
       if (careful) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-          for (int i = 0; i < RP::kVWords; ++i) {
-            if constexpr (kIsFp8<T>) {
-#pragma unroll
-              for (int y = 0; y < 32; y += 8) {
-                if (((vw[x][i] >> y) & 0x7fu) == 0x7fu) { odd = true; vw[x][i] &= ~(0xffu << y); }
-              }
-            } else if (pair_not_finite<TQ>(vw[x][i])) {
-              odd = true;
-              if (pair_not_finite<TQ>(vw[x][i] & 0xffffu)) vw[x][i] &= 0xffff0000u;
-              if (pair_not_finite<TQ>(vw[x][i] & 0xffff0000u)) vw[x][i] &= 0xffffu;
-            }
+        for (int y = 0; y < 4; ++y)
+          if (pair_not_finite<TP>(a[y])) {
+            odd = true;
+            if (pair_not_finite<TP>(a[y] & 0xffffu)) a[y] &= 0xffff0000u;
+            if (pair_not_finite<TP>(a[y] & 0xffff0000u)) a[y] &= 0xffffu;
           }
       }
-#pragma unroll
-      for (int e = 0; e < RP::kV; ++e) {
-        uint32_t b0, b1;
-        if constexpr (kIsFp8<T>) {
-          // byte e of the four keys' pieces, two keys to a word
-          const uint32_t a = __byte_perm(vw[0][e / 4], vw[1][e / 4], (e % 4) | ((e % 4 + 4) << 4));
-          const uint32_t z = __byte_perm(vw[2][e / 4], vw[3][e / 4], (e % 4) | ((e % 4 + 4) << 4));
-          b0 = e4m3x2_to_half2(a & 0xffffu);
-          b1 = e4m3x2_to_half2(z & 0xffffu);
-        } else {
-          constexpr uint32_t kLow = 0x5410, kHigh = 0x7632;
-          b0 = __byte_perm(vw[0][e / 2], vw[1][e / 2], e & 1 ? kHigh : kLow);
-          b1 = __byte_perm(vw[2][e / 2], vw[3][e / 2], e & 1 ? kHigh : kLow);
-        }
-        float (&o)[4] = acc[u * RP::kV + e];
-        mma_16816<TP>(o, ph[0], ph[1], ph[2], ph[3], b0, b1, o);
-        mma_16816<TP>(o, pl[0], pl[1], pl[2], pl[3], b0, b1, o);
-      }
+      mma_16816<TP>(acc[i], a[0], a[1], a[2], a[3], ph[0], ph[1], acc[i]);
+      mma_16816<TP>(acc[i], a[0], a[1], a[2], a[3], pl[0], pl[1], acc[i]);
     }
     if (careful && __any_sync(~0u, odd)) {                   // add what was taken out, element by element
 #pragma unroll 1
       for (int key = 0; key < kKeys; ++key)
 #pragma unroll
-        for (int u = 0; u < RP::kNV; ++u)
+        for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-          for (int z = 0; z < 2; ++z)
+          for (int y = 0; y < 2; ++y) {
+            const int at = (kIsFp8<T> ? g * RS::kV + 2 * i + y : 16 * i + g + 8 * y) * RS::kBytes;
+            const uint8_t* v = vt + chunk_at<T, kChunks>(key, at / 16) * 16 + at % 16;
+            float x;
+            if constexpr (kIsFp8<T>) x = e4m3x2_to_float2(*v).x;
+            else x = to_float(*reinterpret_cast<const TQ*>(v));
+            if (!isfinite(x)) {
 #pragma unroll
-            for (int e = 0; e < RP::kV; ++e) {
-              const int at = ((u * 8 + 2 * c + z) * RP::kV + e) * RP::kBytes;
-              const uint8_t* v = vt + chunk_at<RP::kChunks>(key, at / 16) * 16 + at % 16;
-              float x;
-              if constexpr (kIsFp8<T>) x = e4m3x2_to_float2(*v).x;
-              else x = to_float(*reinterpret_cast<const TQ*>(v));
-              if (!isfinite(x)) {
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-                  if (sees(p, pos[r], j0 + key)) acc[u * RP::kV + e][2 * r + z] += x;
-              }
+              for (int r = 0; r < 2; ++r)
+                if (sees(p, pos[r], j0 + key)) acc[i][2 * y + r] += x;
             }
+          }
     }
   }
   copies_wait<0>();
@@ -353,15 +417,13 @@ again:
   float (*s_acc)[kRows][D + 4] = reinterpret_cast<float (*)[kRows][D + 4]>(smem);
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
-    l[r] += __shfl_xor_sync(~0u, l[r], 1);
-    l[r] += __shfl_xor_sync(~0u, l[r], 2);
-    if (c == 0) s_ml[warp][g + 8 * r] = make_float2(m[r] - kShift, l[r]);   // what acc and l are relative to
 #pragma unroll
-    for (int u = 0; u < RP::kNV; ++u)
+    for (int o = 4; o < 32; o *= 2) l[r] += __shfl_xor_sync(~0u, l[r], o);
+    if (g == 0) s_ml[warp][2 * c + r] = make_float2(m[r] - kShift, l[r]);   // what acc and l are relative to
 #pragma unroll
-      for (int z = 0; z < 2; ++z)
+    for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-        for (int e = 0; e < RP::kV; ++e) s_acc[warp][g + 8 * r][(u * 8 + 2 * c + z) * RP::kV + e] = acc[u * RP::kV + e][2 * r + z];
+      for (int y = 0; y < 2; ++y) s_acc[warp][2 * c + r][kIsFp8<T> ? g * RS::kV + 2 * i + y : 16 * i + g + 8 * y] = acc[i][2 * y + r];
   }
   if (kPaged && p.status && (flags & SSA_DEV_BAD_INDEX)) atomicOr(p.status, SSA_DEV_BAD_INDEX);
   __syncthreads();
@@ -501,9 +563,9 @@ static int32_t check_window(const ssa_attn_desc* d, const ssa_window* w, bool ma
 
 static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-// More than two row tiles of the kernel for few rows (which would read the cache once for each) go to the tiles of 256.
+// More rows than a block of the kernel for few serves (its next one would read the cache again) go to the tiles of 256.
 static bool tiles_pay(const ssa_attn_desc* d, const ssa_window* w, bool mass) {
-  return !mass && d->kv_dtype != SSA_FP8_E4M3 && (long long)(d->H / d->H_kv) * w->n_q > 2 * kRows &&
+  return !mass && d->kv_dtype != SSA_FP8_E4M3 && (long long)(d->H / d->H_kv) * w->n_q > 4 * kRows &&
          (!w->paging || w->paging->page_size >= 8);          // (a box of a copy is eight rows at least)
 }
 
@@ -552,7 +614,7 @@ static cudaError_t launch_rows(const WindowParams& p, cudaStream_t st) {
   auto kernel = p.block_rows == kRows       ? window_rows_kernel<T, D, kPaged, kMass, 1>
                 : p.block_rows == 2 * kRows ? window_rows_kernel<T, D, kPaged, kMass, 2>
                                             : window_rows_kernel<T, D, kPaged, kMass, 4>;
-  constexpr int kSmem = std::max(RowPieces<T, D>::kSmem, kWarps * kRows * (D + 4) * 4);
+  constexpr int kSmem = std::max(RowShape<T, D>::kSmem, RowShape<T, D>::kJoin);
   const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   return err != cudaSuccess ? err : launch_pdl_smem(kernel, grid, dim3(kWarps * 32), kSmem, st, p);
 }
