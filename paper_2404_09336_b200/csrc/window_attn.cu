@@ -16,7 +16,7 @@
 
 namespace ssa {
 
-constexpr int kRows = 8;               // query rows of a warp: (token, head of the group) pairs
+constexpr int kGroup = 8;              // query rows of a matrix tile: (token, head of the group) pairs
 constexpr int kKeys = 16;              // positions of a tile
 constexpr int kWarps = 4;              // of a block
 constexpr int kSplitTiles = 16;        // fewest tiles worth a split of their own
@@ -38,7 +38,7 @@ struct RowShape {
   static constexpr int kNK = D / 64, kV = D / 8;                       // 8-bit: pieces of K per lane; elements of V's piece
   static constexpr int kTile = 2 * kKeys * kRow;                       // bytes of K and V of a tile
   static constexpr int kRingTiles = SSA_RING_BYTES / kTile < 6 ? SSA_RING_BYTES / kTile : 6;   // of a warp
-  static constexpr int kSmem = kWarps * kRingTiles * kTile, kJoin = kWarps * kRows * (D + 4) * 4;
+  static constexpr int kSmem = kWarps * kRingTiles * kTile;
 };
 
 // Where 16-byte piece `chunk` of row `key` lies in a tile.  16-bit rows: the eight rows of an ldmatrix hit eight different bank
@@ -110,13 +110,13 @@ template <> __device__ __forceinline__ bool pair_not_finite<__half>(uint32_t w) 
   return (w & 0x7c00u) == 0x7c00u || (w & 0x7c000000u) == 0x7c000000u;
 }
 
-// grid (splits x row blocks, H_kv, B).  A team of kTeam warps, eight query rows each, shares the tiles that it copies into a ring
-// of its own (16 bytes a lane, asynchronously; no block barrier inside the loop); the block's teams take tiles in turn.  Cached
+// grid (splits x row blocks, H_kv, B).  A team of kTeam warps, kGroups times eight query rows each, shares the tiles that it copies
+// into a ring of its own (16 bytes a lane, asynchronously; no block barrier inside the loop); the block's teams take tiles in turn.  Cached
 // rows and dimensions are the long side of the matrix instructions, m16n8k16, query rows the short one:
 //   S^T[16 keys, 8 rows] += K . Q^T   and   O^T[16 dims, 8 rows] += V^T . P^T   (P transposed by movmatrix)
-// Lane 4g+c holds, of S^T, keys g and g + 8 of rows 2c and 2c + 1.  Bound by HBM where lists are long; by the instructions of a
+// Lane 4g+c holds, of S^T, keys g and g + 8 of rows 2c and 2c + 1 of each group of eight.  Bound by HBM where lists are long; by the instructions of a
 // tile (some 230) and a block's start and end where they are short.
-template <typename T, int D, bool kPaged, bool kMass, int kTeam>
+template <typename T, int D, bool kPaged, bool kMass, int kTeam, int kGroups>
 __global__ void __launch_bounds__(kWarps * 32, 3)
 window_rows_kernel(const WindowParams p) {
   using TQ = typename Storage<T>::Query;
@@ -124,6 +124,7 @@ window_rows_kernel(const WindowParams p) {
   using TS = std::conditional_t<kIsFp8<T>, __half, TQ>;
   using RS = RowShape<T, D>;
   constexpr float kShift = Weight<T>::kShift;
+  constexpr int kRows = kGroups * kGroup;                    // of a warp
   constexpr int kTeams = kWarps / kTeam, kRing = RS::kRingTiles * kTeam, kChunks = RS::kChunks;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float2 s_ml[kWarps][kRows];
@@ -208,35 +209,38 @@ window_rows_kernel(const WindowParams p) {
 #pragma unroll 1
   for (int n = 0; n < kRing - 1; ++n) load(n);
 
-  // the queries: row g of the warp's, as the short side of the first contraction; lanes' scores are of rows 2c, 2c + 1
+  // the queries: row g of each group, as the short side of the first contraction; a lane's scores are of rows 2c, 2c + 1
   const int wrow0 = row0 + member * kRows, wrows = min(kRows, rows - member * kRows);
   constexpr int kSteps = D / 16;
-  uint32_t qb[2 * kSteps];
-  float unit[2] = {p.scale_log2, p.scale_log2};
-  {
-    const int row = wrow0 + g, t = token_of(p, row), h = hkv * p.group + row - t * p.group;
+  uint32_t qb[kGroups][2 * kSteps];
+  float unit[kGroups][2];
+  int pos[kGroups][2];                                       // (a row that does not exist sees nothing)
+#pragma unroll
+  for (int y = 0; y < kGroups; ++y) {
+    const int row = wrow0 + y * kGroup + g, t = token_of(p, row), h = hkv * p.group + row - t * p.group;
+    const bool there = y * kGroup + g < wrows;
     const TQ* q = reinterpret_cast<const TQ*>(p.q) + (int64_t)b * p.q_sb + (int64_t)h * p.q_sh + (int64_t)t * p.q_st;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
       if constexpr (kIsFp8<T>) {                             // step 4 u + i takes elements 4 i ... of the lane's piece 4 u + c
         uint2 x = make_uint2(0, 0);
-        if (g < wrows) x = *reinterpret_cast<const uint2*>(q + (i / 4 * 4 + c) * 16 + i % 4 * 4);
-        qb[2 * i] = x.x;
-        qb[2 * i + 1] = x.y;
+        if (there) x = *reinterpret_cast<const uint2*>(q + (i / 4 * 4 + c) * 16 + i % 4 * 4);
+        qb[y][2 * i] = x.x;
+        qb[y][2 * i + 1] = x.y;
       } else {
-        qb[2 * i] = g < wrows ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * c) : 0;
-        qb[2 * i + 1] = g < wrows ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * c + 8) : 0;
+        qb[y][2 * i] = there ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * c) : 0;
+        qb[y][2 * i + 1] = there ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * c + 8) : 0;
       }
     }
-    if constexpr (kIsFp8<T>) {
-      const float back = rows_to_half(qb);
+    float back = 1.f;
+    if constexpr (kIsFp8<T>) back = rows_to_half(qb[y]);
 #pragma unroll
-      for (int r = 0; r < 2; ++r) unit[r] = p.scale_log2 * __shfl_sync(~0u, back, (2 * c + r) * 4);
+    for (int r = 0; r < 2; ++r) {
+      unit[y][r] = kIsFp8<T> ? p.scale_log2 * __shfl_sync(~0u, back, (2 * c + r) * 4) : p.scale_log2;
+      const int mine = y * kGroup + 2 * c + r;
+      pos[y][r] = mine < wrows ? first + token_of(p, wrow0 + mine) : -1;
     }
   }
-  int pos[2];                                                // (a row that does not exist sees nothing)
-#pragma unroll
-  for (int r = 0; r < 2; ++r) pos[r] = 2 * c + r < wrows ? first + token_of(p, wrow0 + 2 * c + r) : -1;
   // every row of the warp sees all of [all_lo, all_hi]; the sinks as well
   const int all_hi = first + token_of(p, wrow0);
   const int all_lo = p.window == 0 ? 0 : first + token_of(p, wrow0 + max(wrows, 1) - 1) - p.window + 1;
@@ -248,15 +252,18 @@ window_rows_kernel(const WindowParams p) {
   // (its product with a weight's two parts may be inf - inf).  Sums that come out finite met none; else the block goes through
   // its tiles once more and takes such elements out of the contraction, to add them to the rows that see them.
   constexpr int kTiles = D / 16;
-  float acc[kTiles][4], m[2], l[2];                          // dimensions (16-bit: 16 i + g, + 8; 8-bit: g kV + 2 i, + 1), rows
+  float acc[kGroups][kTiles][4], m[kGroups][2], l[kGroups][2];   // dimensions (16-bit: 16 i + g, + 8; 8-bit: g kV + 2 i, + 1), rows
   bool careful = false;
 again:
 #pragma unroll
-  for (int i = 0; i < kTiles; ++i)
+  for (int y = 0; y < kGroups; ++y) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[i][e] = 0.f;
-  m[0] = m[1] = neg_inf();
-  l[0] = l[1] = 0.f;
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[y][i][e] = 0.f;
+    m[y][0] = m[y][1] = neg_inf();
+    l[y][0] = l[y][1] = 0.f;
+  }
 #pragma unroll 1
   for (int n = 0; n < n_tiles; ++n) {
     copies_wait<kRing - 2>();
@@ -269,7 +276,11 @@ again:
     const uint8_t* const kt = ring + stage * RS::kTile;
     const uint8_t* const vt = kt + kKeys * RS::kRow;
     const unsigned have = s_have[team][stage];
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    float s[kGroups][4], s2[kGroups][4];                     // (two chains of half the steps each)
+#pragma unroll
+    for (int y = 0; y < kGroups; ++y)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[y][e] = s2[y][e] = 0.f;
     if constexpr (kIsFp8<T>) {
 #pragma unroll
       for (int u = 0; u < RS::kNK; ++u) {
@@ -277,67 +288,83 @@ again:
         const uint4 z4 = *reinterpret_cast<const uint4*>(kt + chunk_at<T, kChunks>(g + 8, u * 4 + c) * 16);
         const uint32_t a[4] = {a4.x, a4.y, a4.z, a4.w}, z[4] = {z4.x, z4.y, z4.z, z4.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          mma_16816<TS>(s, e4m3x2_to_half2(a[i] & 0xffffu), e4m3x2_to_half2(z[i] & 0xffffu), e4m3x2_to_half2(a[i] >> 16),
-                        e4m3x2_to_half2(z[i] >> 16), qb[2 * (u * 4 + i)], qb[2 * (u * 4 + i) + 1], s);
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t a0 = e4m3x2_to_half2(a[i] & 0xffffu), a1 = e4m3x2_to_half2(z[i] & 0xffffu), a2 = e4m3x2_to_half2(a[i] >> 16),
+                         a3 = e4m3x2_to_half2(z[i] >> 16);
+#pragma unroll
+          for (int y = 0; y < kGroups; ++y)
+            mma_16816<TS>(i % 2 ? s2[y] : s[y], a0, a1, a2, a3, qb[y][2 * (u * 4 + i)], qb[y][2 * (u * 4 + i) + 1], i % 2 ? s2[y] : s[y]);
+        }
       }
     } else {
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
         uint32_t a[4];
         ldmatrix<false>(a, k_at + chunk_at<T, kChunks>(k_key, 2 * i + lane / 16) * 16);
-        mma_16816<TS>(s, a[0], a[1], a[2], a[3], qb[2 * i], qb[2 * i + 1], s);
+#pragma unroll
+        for (int y = 0; y < kGroups; ++y)
+          mma_16816<TS>(i % 2 ? s2[y] : s[y], a[0], a[1], a[2], a[3], qb[y][2 * i], qb[y][2 * i + 1], i % 2 ? s2[y] : s[y]);
       }
     }
 
     // scores in log2 units; what a row does not see is -inf
     const bool whole = (have & 0xffffu) == 0xffffu && j0 + kKeys - 1 <= all_hi && (j0 >= all_lo || j0 + kKeys <= p.sinks);
-    float top[2] = {m[0], m[1]};
+    float top[kGroups][2];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int r = e % 2, key = g + e / 2 * 8;
-      s[e] *= unit[r];
-      if (!whole && (!(have >> key & 1) || !sees(p, pos[r], j0 + key))) s[e] = neg_inf();
-      top[r] = fmaxf(top[r], s[e]);
-    }
-    if constexpr (kMass) {
+    for (int y = 0; y < kGroups; ++y) {
+      top[y][0] = m[y][0];
+      top[y][1] = m[y][1];
 #pragma unroll
-      for (int r = 0; r < 2; ++r)
-        if (2 * c + r < wrows) {
-          const int row = wrow0 + 2 * c + r, t = token_of(p, row), h = hkv * p.group + row - t * p.group;
-          float* to = p.ws_s + (((int64_t)b * p.H + h) * p.n_q + t) * p.s_pitch + j0 + g;
-          to[0] = s[r];
-          to[8] = s[r + 2];
-        }
-    }
+      for (int e = 0; e < 4; ++e) {
+        const int r = e % 2, key = g + e / 2 * 8;
+        s[y][e] = (s[y][e] + s2[y][e]) * unit[y][r];
+        if (!whole && (!(have >> key & 1) || !sees(p, pos[y][r], j0 + key))) s[y][e] = neg_inf();
+        top[y][r] = fmaxf(top[y][r], s[y][e]);
+      }
+      if constexpr (kMass) {
 #pragma unroll
-    for (int o = 4; o < 32; o *= 2) {
-      top[0] = fmaxf(top[0], __shfl_xor_sync(~0u, top[0], o));
-      top[1] = fmaxf(top[1], __shfl_xor_sync(~0u, top[1], o));
-    }
-    float shift[2];
-#pragma unroll
-    for (int r = 0; r < 2; ++r) shift[r] = (top[r] == neg_inf() ? 0.f : top[r]) - kShift;
-    if (__any_sync(~0u, top[0] != m[0] || top[1] != m[1])) {
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const float alpha = fast_exp2(m[r] - kShift - shift[r]);       // (m = -inf: 0)
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) { acc[i][r] *= alpha; acc[i][r + 2] *= alpha; }
-        l[r] *= alpha;
-        m[r] = top[r];
+        for (int r = 0; r < 2; ++r)
+          if (y * kGroup + 2 * c + r < wrows) {
+            const int row = wrow0 + y * kGroup + 2 * c + r, t = token_of(p, row), h = hkv * p.group + row - t * p.group;
+            float* to = p.ws_s + (((int64_t)b * p.H + h) * p.n_q + t) * p.s_pitch + j0 + g;
+            to[0] = s[y][r];
+            to[8] = s[y][r + 2];
+          }
       }
     }
-    uint32_t ph[2], pl[2];                                   // the weights, keys 0-7 and 8-15, and what their rounding left
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const float w0 = fast_exp2(s[2 * x] - shift[0]), w1 = fast_exp2(s[2 * x + 1] - shift[1]);
-      l[0] += w0;
-      l[1] += w1;
-      const uint32_t w = pack2<TP>(w0, w1);
-      const float2 back = unpack2<TP>(w);
-      ph[x] = transposed(w);
-      pl[x] = transposed(pack2<TP>(w0 - back.x, w1 - back.y));
+    for (int o = 4; o < 32; o *= 2)
+#pragma unroll
+      for (int y = 0; y < kGroups; ++y) {
+        top[y][0] = fmaxf(top[y][0], __shfl_xor_sync(~0u, top[y][0], o));
+        top[y][1] = fmaxf(top[y][1], __shfl_xor_sync(~0u, top[y][1], o));
+      }
+    uint32_t ph[kGroups][2], pl[kGroups][2];                 // the weights, keys 0-7 and 8-15, and what their rounding left
+#pragma unroll
+    for (int y = 0; y < kGroups; ++y) {
+      float shift[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) shift[r] = (top[y][r] == neg_inf() ? 0.f : top[y][r]) - kShift;
+      if (__any_sync(~0u, top[y][0] != m[y][0] || top[y][1] != m[y][1])) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float alpha = fast_exp2(m[y][r] - kShift - shift[r]);  // (m = -inf: 0)
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i) { acc[y][i][r] *= alpha; acc[y][i][r + 2] *= alpha; }
+          l[y][r] *= alpha;
+          m[y][r] = top[y][r];
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const float w0 = fast_exp2(s[y][2 * x] - shift[0]), w1 = fast_exp2(s[y][2 * x + 1] - shift[1]);
+        l[y][0] += w0;
+        l[y][1] += w1;
+        const uint32_t w = pack2<TP>(w0, w1);
+        const float2 back = unpack2<TP>(w);
+        ph[y][x] = transposed(w);
+        pl[y][x] = transposed(pack2<TP>(w0 - back.x, w1 - back.y));
+      }
     }
     bool odd = false;
     uint32_t vw[4][kIsFp8<T> ? RS::kV / 4 : 1];              // 8-bit rows: the pieces of keys 2c, 2c + 1, 2c + 8, 2c + 9
@@ -377,8 +404,10 @@ again:
             if (pair_not_finite<TP>(a[y] & 0xffff0000u)) a[y] &= 0xffffu;
           }
       }
-      mma_16816<TP>(acc[i], a[0], a[1], a[2], a[3], ph[0], ph[1], acc[i]);
-      mma_16816<TP>(acc[i], a[0], a[1], a[2], a[3], pl[0], pl[1], acc[i]);
+#pragma unroll
+      for (int y = 0; y < kGroups; ++y) mma_16816<TP>(acc[y][i], a[0], a[1], a[2], a[3], ph[y][0], ph[y][1], acc[y][i]);
+#pragma unroll
+      for (int y = 0; y < kGroups; ++y) mma_16816<TP>(acc[y][i], a[0], a[1], a[2], a[3], pl[y][0], pl[y][1], acc[y][i]);
     }
     if (careful && __any_sync(~0u, odd)) {                   // add what was taken out, element by element
 #pragma unroll 1
@@ -386,26 +415,31 @@ again:
 #pragma unroll
         for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const int at = (kIsFp8<T> ? g * RS::kV + 2 * i + y : 16 * i + g + 8 * y) * RS::kBytes;
+          for (int z = 0; z < 2; ++z) {
+            const int at = (kIsFp8<T> ? g * RS::kV + 2 * i + z : 16 * i + g + 8 * z) * RS::kBytes;
             const uint8_t* v = vt + chunk_at<T, kChunks>(key, at / 16) * 16 + at % 16;
             float x;
             if constexpr (kIsFp8<T>) x = e4m3x2_to_float2(*v).x;
             else x = to_float(*reinterpret_cast<const TQ*>(v));
             if (!isfinite(x)) {
 #pragma unroll
-              for (int r = 0; r < 2; ++r)
-                if (sees(p, pos[r], j0 + key)) acc[i][2 * y + r] += x;
+              for (int y = 0; y < kGroups; ++y)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+                  if (sees(p, pos[y][r], j0 + key)) acc[y][i][2 * z + r] += x;
             }
           }
     }
   }
   copies_wait<0>();
-  bool finite = true;
+  float test = 0.f;                                          // (0 times an infinity or a NaN is NaN)
 #pragma unroll
-  for (int i = 0; i < kTiles; ++i)
+  for (int y = 0; y < kGroups; ++y)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) finite &= fabsf(acc[i][e]) <= 3.402823466e38f;
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) test = fmaf(acc[y][i][e], 0.f, test);
+  const bool finite = test == 0.f;
   if (__syncthreads_or(!finite) && !careful) {               // (the barrier: the rings' place is free from here on)
     careful = true;
 #pragma unroll 1
@@ -416,15 +450,18 @@ again:
   // the teams' results, joined by the block
   float (*s_acc)[kRows][D + 4] = reinterpret_cast<float (*)[kRows][D + 4]>(smem);
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
+  for (int y = 0; y < kGroups; ++y)
 #pragma unroll
-    for (int o = 4; o < 32; o *= 2) l[r] += __shfl_xor_sync(~0u, l[r], o);
-    if (g == 0) s_ml[warp][2 * c + r] = make_float2(m[r] - kShift, l[r]);   // what acc and l are relative to
+    for (int r = 0; r < 2; ++r) {
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i)
+      for (int o = 4; o < 32; o *= 2) l[y][r] += __shfl_xor_sync(~0u, l[y][r], o);
+      const int mine = y * kGroup + 2 * c + r;
+      if (g == 0) s_ml[warp][mine] = make_float2(m[y][r] - kShift, l[y][r]);   // what acc and l are relative to
 #pragma unroll
-      for (int y = 0; y < 2; ++y) s_acc[warp][2 * c + r][kIsFp8<T> ? g * RS::kV + 2 * i + y : 16 * i + g + 8 * y] = acc[i][2 * y + r];
-  }
+      for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int z = 0; z < 2; ++z) s_acc[warp][mine][kIsFp8<T> ? g * RS::kV + 2 * i + z : 16 * i + g + 8 * z] = acc[y][i][2 * z + r];
+    }
   if (kPaged && p.status && (flags & SSA_DEV_BAD_INDEX)) atomicOr(p.status, SSA_DEV_BAD_INDEX);
   __syncthreads();
   for (int i = warp; i < rows; i += kWarps) {
@@ -454,89 +491,149 @@ again:
   }
 }
 
-// Joins the splits of query row (b, h, t): a thread per dimension.  Rows with one split are finished already.
+// Splits that query row (h, t) of a request was served by.
+__device__ __forceinline__ int row_splits(const WindowParams& p, int h, int t, int ctx, int n_new) {
+  const int row0 = (t * p.group + h % p.group) / p.block_rows * p.block_rows, rows = min(p.block_rows, n_new * p.group - row0);
+  return splits_used(p, Seen(p, p.tile_keys, ctx - n_new, token_of(p, row0), token_of(p, row0 + rows - 1)).tiles);
+}
+
+// Joins the splits of query row `row` (of H n_q) of a request: a warp, whose lanes have D / 32 dimensions each.  The first few
+// splits are asked for before it is known how many there are: they have their place, and what nothing was written to is not
+// used.  Rows with one split are finished already.
 template <typename TQ, int D>
-__device__ void join_row(const WindowParams& p, int b, int h, int t) {
+__device__ __forceinline__ void join_rows(const WindowParams& p, int b, int row) {
+  constexpr int kN = D / 32, kAhead = 4;
+  if (row >= p.H * p.n_q) return;
+  const int lane = threadIdx.x % 32, h = p.n_q == 1 ? row : row / p.n_q, t = row - h * p.n_q;
+  const int64_t at = (int64_t)b * p.H * p.n_q + row, slot = at * p.n_splits;
+  float2 ml[kAhead];
+  float a[kAhead][kN];
+  auto ask = [&](int i, int x) {
+    if (i >= p.n_splits) return;
+    ml[x] = p.ws_ml[slot + i];
+    const float* from = p.ws_acc + (slot + i) * D + lane * kN;
+    if constexpr (kN == 4) {
+      const float4 f = *reinterpret_cast<const float4*>(from);
+      a[x][0] = f.x; a[x][1] = f.y; a[x][2] = f.z; a[x][3] = f.w;
+    } else {
+      const float2 f = *reinterpret_cast<const float2*>(from);
+      a[x][0] = f.x; a[x][1] = f.y;
+    }
+  };
+#pragma unroll
+  for (int x = 0; x < kAhead; ++x) ask(x, x);
   uint32_t flags = 0;
   int ctx, n_new;
   window_sizes(p, b, ctx, n_new, flags);
   if (t >= n_new) return;
-  const int row0 = (t * p.group + h % p.group) / p.block_rows * p.block_rows, rows = min(p.block_rows, n_new * p.group - row0);
-  const Seen seen(p, p.tile_keys, ctx - n_new, row0 / p.group, (row0 + rows - 1) / p.group);
-  const int n = splits_used(p, seen.tiles), d = threadIdx.x;
-  if (n == 1 || d >= D) return;
-  const int64_t at = ((int64_t)b * p.H + h) * p.n_q + t, slot = at * p.n_splits;
-  float M = neg_inf(), L = 0.f, A = 0.f;
-  for (int i = 0; i < n; ++i) M = fmaxf(M, p.ws_ml[slot + i].x);
-#pragma unroll 8
-  for (int i = 0; i < n; ++i) {
-    const float2 ml = p.ws_ml[slot + i];
-    const float w = ml.y == 0.f ? 0.f : fast_exp2(ml.x - M);
-    L = fmaf(ml.y, w, L);
-    A = fmaf(p.ws_acc[(slot + i) * D + d], w, A);
+  const int n = row_splits(p, h, t, ctx, n_new);
+  if (n == 1) return;
+  float M = neg_inf(), L = 0.f, A[kN];
+#pragma unroll
+  for (int y = 0; y < kN; ++y) A[y] = 0.f;
+  for (int i0 = 0; i0 < n; i0 += kAhead) {
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      if (i0 + x < n && ml[x].y != 0.f) {                    // (a split without a weight adds nothing)
+        const float top = fmaxf(M, ml[x].x), base = top == neg_inf() ? 0.f : top, w = fast_exp2(ml[x].x - base), old = fast_exp2(M - base);
+        L = fmaf(L, old, ml[x].y * w);
+#pragma unroll
+        for (int y = 0; y < kN; ++y) A[y] = fmaf(A[y], old, a[x][y] * w);
+        M = top;
+      }
+      ask(i0 + kAhead + x, x);
+    }
   }
-  store_window_value<TQ>(p, b, h, t, d, L == 0.f ? 0.f : A / L);
-  if (d == 0 && p.lse) p.lse[at] = L == 0.f ? neg_inf() : (M + log2f(L)) * kLn2;
+#pragma unroll
+  for (int y = 0; y < kN; ++y) store_window_value<TQ>(p, b, h, t, lane * kN + y, L == 0.f ? 0.f : A[y] / L);
+  if (lane == 0 && p.lse) p.lse[at] = L == 0.f ? neg_inf() : (M + log2f(L)) * kLn2;
 }
 
+constexpr int kJoinWarps = 4;
+
 template <typename TQ, int D>
-__global__ void __launch_bounds__(D)
+__global__ void __launch_bounds__(kJoinWarps * 32)
 window_join_kernel(const WindowParams p) {
   grid_dependency_wait();
   grid_launch_dependents();
-  join_row<TQ, D>(p, blockIdx.y, blockIdx.x / p.n_q, blockIdx.x % p.n_q);
+  join_rows<TQ, D>(p, blockIdx.y, blockIdx.x * kJoinWarps + threadIdx.x / 32);
 }
 
 constexpr int kMassThreads = 256;
+constexpr int kMassKeys = 128;         // positions of a block: four to a lane, every warp of the block has them all
+constexpr int kMassWarps = kMassThreads / 32;
+constexpr int kMassAhead = 4;          // query rows that a warp has in flight
 
-// Blocks x < mass_blocks of a request: one position per thread, its weights summed over tokens, then heads, in that order.
-// The others join the splits of one query row each.
+// Blocks x < mass_blocks of a request: the weights of kMassKeys positions.  Warp w sums the query rows w, w + 8, ..., the block
+// then the warps, always in that order.  The scores are asked for before the rows' normalisers are made from their splits.  The
+// other blocks join the splits of query rows.
 template <typename TQ, int D>
 __global__ void __launch_bounds__(kMassThreads)
 window_mass_kernel(const WindowParams p, const int mass_blocks) {
   __shared__ float s_lse[SSA_MASS_MAX_ROWS];
-  const int b = blockIdx.y;
+  __shared__ float s_sum[kMassWarps][kMassKeys];
+  const int b = blockIdx.y, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   grid_dependency_wait();
   grid_launch_dependents();
   if ((int)blockIdx.x >= mass_blocks) {
-    const int row = blockIdx.x - mass_blocks;
-    join_row<TQ, D>(p, b, row / p.n_q, row % p.n_q);
+    join_rows<TQ, D>(p, b, (blockIdx.x - mass_blocks) * kMassWarps + warp);
     return;
   }
   uint32_t flags = 0;
   int ctx, n_new;
   window_sizes(p, b, ctx, n_new, flags);
-  const int j0 = blockIdx.x * kMassThreads;
-  if (j0 >= ctx) return;
+  const int j = blockIdx.x * kMassKeys + lane * 4;
+  if ((int)blockIdx.x * kMassKeys >= ctx) return;
   const int n_rows = p.H * p.n_q, first = ctx - n_new;
-  for (int i = threadIdx.x / 32; i < n_rows; i += kMassThreads / 32) {       // normalisers, a warp each
-    const int h = i / p.n_q, t = i % p.n_q, lane = threadIdx.x % 32;
-    if (t >= n_new) continue;
-    const int row0 = (t * p.group + h % p.group) / p.block_rows * p.block_rows, rows = min(p.block_rows, n_new * p.group - row0);
-    const Seen seen(p, kKeys, first, row0 / p.group, (row0 + rows - 1) / p.group);
-    const int n = splits_used(p, seen.tiles);
-    const float2* ml = p.ws_ml + (((int64_t)b * p.H + h) * p.n_q + t) * p.n_splits;
-    float M = neg_inf(), L = 0.f;
-    for (int x = lane; x < n; x += 32) M = fmaxf(M, ml[x].x);
-    for (int o = 16; o; o /= 2) M = fmaxf(M, __shfl_xor_sync(~0u, M, o));
-    for (int x = lane; x < n; x += 32) L += ml[x].y == 0.f ? 0.f : ml[x].y * fast_exp2(ml[x].x - M);
-    for (int o = 16; o; o /= 2) L += __shfl_xor_sync(~0u, L, o);
-    if (lane == 0) s_lse[i] = L == 0.f ? __int_as_float(0x7f800000) : M + log2f(L);   // +inf: nothing seen, weights of zero
+  const float* scores = p.ws_s + (int64_t)b * n_rows * p.s_pitch + j;
+  // (a row of scores is a multiple of sixteen long: four of them are there, or none; what a token does not see is not used)
+  auto ask = [&](int i) {
+    return i < n_rows && j < p.s_pitch ? *reinterpret_cast<const float4*>(scores + (int64_t)i * p.s_pitch) : make_float4(0.f, 0.f, 0.f, 0.f);
+  };
+  float4 s[kMassAhead];
+#pragma unroll
+  for (int x = 0; x < kMassAhead; ++x) s[x] = ask(warp + x * kMassWarps);
+  for (int i = threadIdx.x; i < n_rows; i += kMassThreads) {
+    const int h = p.n_q == 1 ? i : i / p.n_q, t = i - h * p.n_q;
+    float lse = __int_as_float(0x7f800000);                  // +inf: nothing seen, weights of zero
+    if (t < n_new) {
+      const int n = row_splits(p, h, t, ctx, n_new);
+      const float2* ml = p.ws_ml + ((int64_t)b * n_rows + i) * p.n_splits;
+      float M = neg_inf(), L = 0.f;
+#pragma unroll 4
+      for (int x = 0; x < n; ++x) M = fmaxf(M, ml[x].x);
+#pragma unroll 4
+      for (int x = 0; x < n; ++x) L += ml[x].y == 0.f ? 0.f : ml[x].y * fast_exp2(ml[x].x - M);
+      if (L != 0.f) lse = M + log2f(L);
+    }
+    s_lse[i] = lse;
   }
   __syncthreads();
-  const int j = j0 + threadIdx.x;
-  if (j >= ctx) return;
-  float sum = 0.f;
-  for (int t = 0; t < n_new; ++t) {
-    if (!sees(p, first + t, j)) continue;
-    const float* s = p.ws_s + ((int64_t)b * p.H * p.n_q + t) * p.s_pitch + j;
-    float part = 0.f;
-#pragma unroll 8
-    for (int h = 0; h < p.H; ++h) part += fast_exp2(s[(int64_t)h * p.n_q * p.s_pitch] - s_lse[h * p.n_q + t]);
-    sum += part;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = warp; i0 < n_rows; i0 += kMassAhead * kMassWarps) {
+#pragma unroll
+    for (int x = 0; x < kMassAhead; ++x) {
+      const int i = i0 + x * kMassWarps;
+      if (i < n_rows) {
+        const int t = p.n_q == 1 ? 0 : i % p.n_q, pos = t < n_new ? first + t : -1;
+        const float lse = s_lse[i];
+        const float v[4] = {s[x].x, s[x].y, s[x].z, s[x].w};
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          if (sees(p, pos, j + y)) sum[y] += fast_exp2(v[y] - lse);
+      }
+      s[x] = ask(i + kMassAhead * kMassWarps);
+    }
   }
-  if (p.mass_in && j < first) sum = fmaf(p.decay, p.mass_in[(int64_t)b * p.mass_stride + j], sum);
-  p.mass_out[(int64_t)b * p.mass_stride + j] = sum;
+  *reinterpret_cast<float4*>(&s_sum[warp][lane * 4]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+  __syncthreads();
+  const int key = blockIdx.x * kMassKeys + threadIdx.x;
+  if (threadIdx.x >= kMassKeys || key >= ctx) return;
+  float total = 0.f;
+#pragma unroll
+  for (int x = 0; x < kMassWarps; ++x) total += s_sum[x][threadIdx.x];
+  if (p.mass_in && key < first) total = fmaf(p.decay, p.mass_in[(int64_t)b * p.mass_stride + key], total);
+  p.mass_out[(int64_t)b * p.mass_stride + key] = total;
 }
 
 // ---------------------------------------------------------------------------
@@ -565,21 +662,40 @@ static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 // More rows than a block of the kernel for few serves (its next one would read the cache again) go to the tiles of 256.
 static bool tiles_pay(const ssa_attn_desc* d, const ssa_window* w, bool mass) {
-  return !mass && d->kv_dtype != SSA_FP8_E4M3 && (long long)(d->H / d->H_kv) * w->n_q > 4 * kRows &&
+  return !mass && d->kv_dtype != SSA_FP8_E4M3 && (long long)(d->H / d->H_kv) * w->n_q > 4 * kGroup &&
          (!w->paging || w->paging->page_size >= 8);          // (a box of a copy is eight rows at least)
 }
 
 static bool plan_window(const ssa_attn_desc* d, const ssa_window* w, bool mass, bool tiles, WindowPlan* pl) {
   pl->tiles = tiles;
   const long long per_head = (long long)(d->H / d->H_kv) * w->n_q;
-  const int rows = tiles ? kBlockRows : per_head <= kRows ? kRows : per_head <= 2 * kRows ? 2 * kRows : 4 * kRows, keys = tiles ? kTileKeys : kKeys, fewest = tiles ? kTileSplit : kSplitTiles;
+  int rows = kBlockRows;
+  if (!tiles)
+    for (rows = kGroup; rows < per_head && rows < 8 * kGroup; rows *= 2) {}
+  const int keys = tiles ? kTileKeys : kKeys, fewest = tiles ? kTileSplit : kSplitTiles;
   const long long group = d->H / d->H_kv, row_tiles = (per_head + rows - 1) / rows;
   const long long blocks = row_tiles * d->H_kv * d->B, tokens = (rows - 1) / group + 2;
   const long long most = w->window == 0 ? d->max_ctx : std::min<long long>(d->max_ctx, (long long)w->window + w->sinks + tokens);
   const long long n_tiles = (most + keys - 1) / keys + 2;
-  const long long wanted = tiles ? sm_count() / blocks : (4ll * sm_count() + blocks - 1) / blocks;
+  // Splits of the kernel for few rows, by what they cost in units of one tile's time: the work of all blocks, each with a start
+  // and an end, over the places there are (three blocks to an SM), but no less than one block's; half a block's until the last
+  // is done (lengths differ: three quarters of the longest are taken for the mean); joining.
+  long long splits = 1;
+  const long long most_splits = std::min(n_tiles / fewest, 64ll);
+  if (tiles) {
+    splits = sm_count() / blocks;
+  } else {
+    const int teams = kWarps / std::max(1, rows / (2 * kGroup));
+    const double steps = (double)n_tiles / teams, places = 3.0 * sm_count(), ends = 5;
+    double least = 0;
+    for (long long n = 1; n <= most_splits; ++n) {
+      const double one = steps / n + ends, all = blocks * n * (0.75 * steps / n + ends) / places;
+      const double cost = std::max(one, all) + 0.5 * one + (n > 1 ? 6 : 0);
+      if (n == 1 || cost < least) { least = cost; splits = n; }
+    }
+  }
+  pl->n_splits = (int)std::max(1ll, std::min(splits, most_splits));
   pl->block_rows = rows;
-  pl->n_splits = (int)std::max(1ll, std::min({wanted, n_tiles / fewest, 256ll}));
   const size_t slots = (size_t)d->B * d->H * w->n_q * pl->n_splits;
   pl->ml_bytes = up256(slots * sizeof(float2));
   pl->acc_bytes = pl->n_splits > 1 ? up256(slots * d->D * sizeof(float)) : 0;
@@ -611,12 +727,14 @@ static cudaError_t launch_tiles(const WindowParams& p, const CUtensorMap& k_map,
 template <typename T, int D, bool kPaged, bool kMass>
 static cudaError_t launch_rows(const WindowParams& p, cudaStream_t st) {
   const dim3 grid((unsigned)((p.group * p.n_q + p.block_rows - 1) / p.block_rows * p.n_splits), (unsigned)p.H_kv, (unsigned)p.B);
-  auto kernel = p.block_rows == kRows       ? window_rows_kernel<T, D, kPaged, kMass, 1>
-                : p.block_rows == 2 * kRows ? window_rows_kernel<T, D, kPaged, kMass, 2>
-                                            : window_rows_kernel<T, D, kPaged, kMass, 4>;
-  constexpr int kSmem = std::max(RowShape<T, D>::kSmem, RowShape<T, D>::kJoin);
-  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-  return err != cudaSuccess ? err : launch_pdl_smem(kernel, grid, dim3(kWarps * 32), kSmem, st, p);
+  auto kernel = p.block_rows == kGroup       ? window_rows_kernel<T, D, kPaged, kMass, 1, 1>
+                : p.block_rows == 2 * kGroup ? window_rows_kernel<T, D, kPaged, kMass, 1, 2>
+                : p.block_rows == 4 * kGroup ? window_rows_kernel<T, D, kPaged, kMass, 2, 2>
+                                             : window_rows_kernel<T, D, kPaged, kMass, 4, 2>;
+  const int join_bytes = kWarps * std::min(p.block_rows, 2 * kGroup) * (D + 4) * 4;
+  const int smem = std::max(RowShape<T, D>::kSmem, join_bytes);
+  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  return err != cudaSuccess ? err : launch_pdl_smem(kernel, grid, dim3(kWarps * 32), smem, st, p);
 }
 
 template <typename T, int D>
@@ -636,11 +754,11 @@ static int32_t launch_window(const WindowParams& p, bool mass, const CUtensorMap
   if (end) cudaEventRecord(end, st);
   note_launches(1);
   if (mass) {
-    const int mass_blocks = (p.max_ctx + kMassThreads - 1) / kMassThreads;
-    err = launch_pdl(window_mass_kernel<TQ, D>, dim3((unsigned)(mass_blocks + (p.n_splits > 1 ? p.H * p.n_q : 0)), (unsigned)p.B),
-                     dim3(kMassThreads), st, p, mass_blocks);
+    const int mass_blocks = (p.max_ctx + kMassKeys - 1) / kMassKeys, joins = p.n_splits > 1 ? (p.H * p.n_q + kMassWarps - 1) / kMassWarps : 0;
+    err = launch_pdl(window_mass_kernel<TQ, D>, dim3((unsigned)(mass_blocks + joins), (unsigned)p.B), dim3(kMassThreads), st, p, mass_blocks);
   } else if (p.n_splits > 1) {
-    err = launch_pdl(window_join_kernel<TQ, D>, dim3((unsigned)(p.H * p.n_q), (unsigned)p.B), dim3(D), st, p);
+    err = launch_pdl(window_join_kernel<TQ, D>, dim3((unsigned)((p.H * p.n_q + kJoinWarps - 1) / kJoinWarps), (unsigned)p.B),
+                     dim3(kJoinWarps * 32), st, p);
   } else {
     return SSA_OK;
   }
