@@ -17,12 +17,9 @@
 namespace ssa {
 
 constexpr int kGroup = 8;              // query rows of a matrix tile: (token, head of the group) pairs
-constexpr int kKeys = 16;              // positions of a tile
 constexpr int kWarps = 4;              // of a block
-constexpr int kSplitTiles = 16;        // fewest tiles worth a split of their own
-#ifndef SSA_RING_BYTES
-#define SSA_RING_BYTES 16384
-#endif
+constexpr int kSplitKeys = 256;        // fewest positions worth a split of their own
+constexpr int kMostGroups = 4;         // of kGroup rows, of a warp
 
 // The weights enter the second contraction as a 16-bit value plus the 16-bit rest, so that the sums keep 16 bits (bf16) or 22
 // (fp16) of each.  fp16 has little range below 1: its weights are scaled by 2^13, which the sum divides out again.
@@ -32,12 +29,15 @@ template <> struct Weight<__nv_bfloat16> { using Type = __nv_bfloat16; static co
 // How the kernel cuts cache rows.  16-bit rows come out of shared memory by ldmatrix.  8-bit rows have to be converted on the
 // way; the order of the dimensions within a contraction is free as long as both sides agree, so lanes take whole 16-byte pieces
 // of them (8 bytes of V's 64-byte rows).
-template <typename T, int D>
+template <typename T, int D, int kGroups = 1>
 struct RowShape {
   static constexpr int kBytes = kIsFp8<T> ? 1 : 2, kRow = D * kBytes, kChunks = kRow / 16;
   static constexpr int kNK = D / 64, kV = D / 8;                       // 8-bit: pieces of K per lane; elements of V's piece
-  static constexpr int kTile = 2 * kKeys * kRow;                       // bytes of K and V of a tile
-  static constexpr int kRingTiles = SSA_RING_BYTES / kTile < 6 ? SSA_RING_BYTES / kTile : 6;   // of a warp
+  static constexpr int kHalves = kRow == 256 ? 1 : 2;                  // tiles of 16 positions, or of 32 where rows are short
+  static constexpr int kKeys = 16 * kHalves, kTile = 2 * kKeys * kRow; // bytes: of K and V of a tile
+  // blocks that fit an SM by their registers, and tiles of a warp's ring: 64 KB a block, or 96
+  static constexpr int kBlocks = kGroups <= 2 ? 3 : 2, kRingBytes = kBlocks == 3 ? 16384 : 24576;
+  static constexpr int kRingTiles = kRingBytes / kTile < 4 ? kRingBytes / kTile : 4;
   static constexpr int kSmem = kWarps * kRingTiles * kTile;
 };
 
@@ -117,12 +117,13 @@ template <> __device__ __forceinline__ bool pair_not_finite<__half>(uint32_t w) 
 // Lane 4g+c holds, of S^T, keys g and g + 8 of rows 2c and 2c + 1 of each group of eight.  Bound by HBM where lists are long; by the instructions of a
 // tile (some 230) and a block's start and end where they are short.
 template <typename T, int D, bool kPaged, bool kMass, int kTeam, int kGroups>
-__global__ void __launch_bounds__(kWarps * 32, 3)
+__global__ void __launch_bounds__(kWarps * 32, (RowShape<T, D, kGroups>::kBlocks))
 window_rows_kernel(const WindowParams p) {
   using TQ = typename Storage<T>::Query;
   using TP = typename Weight<T>::Type;                       // of the second contraction; of the first: TS
   using TS = std::conditional_t<kIsFp8<T>, __half, TQ>;
-  using RS = RowShape<T, D>;
+  using RS = RowShape<T, D, kGroups>;
+  constexpr int kKeys = RS::kKeys, kHalves = RS::kHalves;
   constexpr float kShift = Weight<T>::kShift;
   constexpr int kRows = kGroups * kGroup;                    // of a warp
   constexpr int kTeams = kWarps / kTeam, kRing = RS::kRingTiles * kTeam, kChunks = RS::kChunks;
@@ -168,8 +169,8 @@ window_rows_kernel(const WindowParams p) {
       const uint32_t to = ring_at + stage * RS::kTile;
       // tiles that are seen as a whole and lie on one page have rows in a row
       int64_t at = -1;
-      if (j0 + kKeys - 1 <= hi && (j0 >= from || j0 + kKeys <= p.sinks) && (!kPaged || p.page_shift >= 4)) at = row_of<kPaged>(p, table, j0);
-      unsigned have = 0xffffu;
+      if (j0 + kKeys - 1 <= hi && (j0 >= from || j0 + kKeys <= p.sinks) && (!kPaged || kKeys >> p.page_shift <= 1)) at = row_of<kPaged>(p, table, j0);
+      unsigned have = ~0u;
       if (at >= 0) {
         if (copies) {
           const char *k = kb + (at + my_key) * k_step, *v = vb + (at + my_key) * v_step;
@@ -246,7 +247,7 @@ window_rows_kernel(const WindowParams p) {
   const int all_lo = p.window == 0 ? 0 : first + token_of(p, wrow0 + max(wrows, 1) - 1) - p.window + 1;
   // ldmatrix addresses: lane i of matrix y = i / 8 gives row i % 8 of it.  K: keys 8 (y % 2) ..., pieces 2 s + y / 2;
   // V: keys 8 (y / 2) ..., pieces 2 i + y % 2
-  const int k_key = lane % 16, v_key = lane % 8 + lane / 16 * 8;
+  const int k_key = lane % 16, v_key = lane % 8 + lane / 16 * 8;       // (of each sixteen positions)
 
   // An infinite or NaN element of V must not reach rows that do not see it (0 * inf), and has to stay infinite for those that do
   // (its product with a weight's two parts may be inf - inf).  Sums that come out finite met none; else the block goes through
@@ -276,50 +277,65 @@ again:
     const uint8_t* const kt = ring + stage * RS::kTile;
     const uint8_t* const vt = kt + kKeys * RS::kRow;
     const unsigned have = s_have[team][stage];
-    float s[kGroups][4], s2[kGroups][4];                     // (two chains of half the steps each)
+    float s[kHalves][kGroups][4];
 #pragma unroll
-    for (int y = 0; y < kGroups; ++y)
+    for (int x = 0; x < kHalves; ++x) {
+      float s2[kGroups][4];                                  // (two chains of half the steps each)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[y][e] = s2[y][e] = 0.f;
-    if constexpr (kIsFp8<T>) {
+      for (int y = 0; y < kGroups; ++y)
 #pragma unroll
-      for (int u = 0; u < RS::kNK; ++u) {
-        const uint4 a4 = *reinterpret_cast<const uint4*>(kt + chunk_at<T, kChunks>(g, u * 4 + c) * 16);
-        const uint4 z4 = *reinterpret_cast<const uint4*>(kt + chunk_at<T, kChunks>(g + 8, u * 4 + c) * 16);
-        const uint32_t a[4] = {a4.x, a4.y, a4.z, a4.w}, z[4] = {z4.x, z4.y, z4.z, z4.w};
+        for (int e = 0; e < 4; ++e) s[x][y][e] = s2[y][e] = 0.f;
+      if constexpr (kIsFp8<T>) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t a0 = e4m3x2_to_half2(a[i] & 0xffffu), a1 = e4m3x2_to_half2(z[i] & 0xffffu), a2 = e4m3x2_to_half2(a[i] >> 16),
-                         a3 = e4m3x2_to_half2(z[i] >> 16);
+        for (int u = 0; u < RS::kNK; ++u) {
+          const uint4 a4 = *reinterpret_cast<const uint4*>(kt + chunk_at<T, kChunks>(16 * x + g, u * 4 + c) * 16);
+          const uint4 z4 = *reinterpret_cast<const uint4*>(kt + chunk_at<T, kChunks>(16 * x + g + 8, u * 4 + c) * 16);
+          const uint32_t a[4] = {a4.x, a4.y, a4.z, a4.w}, z[4] = {z4.x, z4.y, z4.z, z4.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t a0 = e4m3x2_to_half2(a[i] & 0xffffu), a1 = e4m3x2_to_half2(z[i] & 0xffffu), a2 = e4m3x2_to_half2(a[i] >> 16),
+                           a3 = e4m3x2_to_half2(z[i] >> 16);
+#pragma unroll
+            for (int y = 0; y < kGroups; ++y)
+              mma_16816<TS>(i % 2 ? s2[y] : s[x][y], a0, a1, a2, a3, qb[y][2 * (u * 4 + i)], qb[y][2 * (u * 4 + i) + 1], i % 2 ? s2[y] : s[x][y]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+          uint32_t a[4];
+          ldmatrix<false>(a, k_at + chunk_at<T, kChunks>(16 * x + k_key, 2 * i + lane / 16) * 16);
 #pragma unroll
           for (int y = 0; y < kGroups; ++y)
-            mma_16816<TS>(i % 2 ? s2[y] : s[y], a0, a1, a2, a3, qb[y][2 * (u * 4 + i)], qb[y][2 * (u * 4 + i) + 1], i % 2 ? s2[y] : s[y]);
+            mma_16816<TS>(i % 2 ? s2[y] : s[x][y], a[0], a[1], a[2], a[3], qb[y][2 * i], qb[y][2 * i + 1], i % 2 ? s2[y] : s[x][y]);
         }
       }
-    } else {
 #pragma unroll
-      for (int i = 0; i < kSteps; ++i) {
-        uint32_t a[4];
-        ldmatrix<false>(a, k_at + chunk_at<T, kChunks>(k_key, 2 * i + lane / 16) * 16);
+      for (int y = 0; y < kGroups; ++y)
 #pragma unroll
-        for (int y = 0; y < kGroups; ++y)
-          mma_16816<TS>(i % 2 ? s2[y] : s[y], a[0], a[1], a[2], a[3], qb[y][2 * i], qb[y][2 * i + 1], i % 2 ? s2[y] : s[y]);
-      }
+        for (int e = 0; e < 4; ++e) s[x][y][e] = (s[x][y][e] + s2[y][e]) * unit[y][e % 2];
     }
 
     // scores in log2 units; what a row does not see is -inf
-    const bool whole = (have & 0xffffu) == 0xffffu && j0 + kKeys - 1 <= all_hi && (j0 >= all_lo || j0 + kKeys <= p.sinks);
+    if (!(have == ~0u && j0 + kKeys - 1 <= all_hi && (j0 >= all_lo || j0 + kKeys <= p.sinks))) {
+#pragma unroll
+      for (int x = 0; x < kHalves; ++x)
+#pragma unroll
+        for (int y = 0; y < kGroups; ++y)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int key = 16 * x + g + e / 2 * 8;
+            if (!(have >> key & 1) || !sees(p, pos[y][e % 2], j0 + key)) s[x][y][e] = neg_inf();
+          }
+    }
     float top[kGroups][2];
 #pragma unroll
     for (int y = 0; y < kGroups; ++y) {
-      top[y][0] = m[y][0];
-      top[y][1] = m[y][1];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = e % 2, key = g + e / 2 * 8;
-        s[y][e] = (s[y][e] + s2[y][e]) * unit[y][r];
-        if (!whole && (!(have >> key & 1) || !sees(p, pos[y][r], j0 + key))) s[y][e] = neg_inf();
-        top[y][r] = fmaxf(top[y][r], s[y][e]);
+      for (int r = 0; r < 2; ++r) {
+        top[y][r] = m[y][r];
+#pragma unroll
+        for (int x = 0; x < kHalves; ++x) top[y][r] = fmaxf(top[y][r], fmaxf(s[x][y][r], s[x][y][r + 2]));
       }
       if constexpr (kMass) {
 #pragma unroll
@@ -327,8 +343,11 @@ again:
           if (y * kGroup + 2 * c + r < wrows) {
             const int row = wrow0 + y * kGroup + 2 * c + r, t = token_of(p, row), h = hkv * p.group + row - t * p.group;
             float* to = p.ws_s + (((int64_t)b * p.H + h) * p.n_q + t) * p.s_pitch + j0 + g;
-            to[0] = s[y][r];
-            to[8] = s[y][r + 2];
+#pragma unroll
+            for (int x = 0; x < kHalves; ++x) {
+              to[16 * x] = s[x][y][r];
+              to[16 * x + 8] = s[x][y][r + 2];
+            }
           }
       }
     }
@@ -339,7 +358,7 @@ again:
         top[y][0] = fmaxf(top[y][0], __shfl_xor_sync(~0u, top[y][0], o));
         top[y][1] = fmaxf(top[y][1], __shfl_xor_sync(~0u, top[y][1], o));
       }
-    uint32_t ph[kGroups][2], pl[kGroups][2];                 // the weights, keys 0-7 and 8-15, and what their rounding left
+    uint32_t ph[kHalves][kGroups][2], pl[kHalves][kGroups][2];         // the weights, keys 0-7 and 8-15, and what their rounding left
 #pragma unroll
     for (int y = 0; y < kGroups; ++y) {
       float shift[2];
@@ -356,58 +375,63 @@ again:
         }
       }
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const float w0 = fast_exp2(s[y][2 * x] - shift[0]), w1 = fast_exp2(s[y][2 * x + 1] - shift[1]);
-        l[y][0] += w0;
-        l[y][1] += w1;
-        const uint32_t w = pack2<TP>(w0, w1);
-        const float2 back = unpack2<TP>(w);
-        ph[y][x] = transposed(w);
-        pl[y][x] = transposed(pack2<TP>(w0 - back.x, w1 - back.y));
-      }
+      for (int x = 0; x < kHalves; ++x)
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const float w0 = fast_exp2(s[x][y][2 * z] - shift[0]), w1 = fast_exp2(s[x][y][2 * z + 1] - shift[1]);
+          l[y][0] += w0;
+          l[y][1] += w1;
+          const uint32_t w = pack2<TP>(w0, w1);
+          const float2 back = unpack2<TP>(w);
+          ph[x][y][z] = transposed(w);
+          pl[x][y][z] = transposed(pack2<TP>(w0 - back.x, w1 - back.y));
+        }
     }
     bool odd = false;
-    uint32_t vw[4][kIsFp8<T> ? RS::kV / 4 : 1];              // 8-bit rows: the pieces of keys 2c, 2c + 1, 2c + 8, 2c + 9
-    if constexpr (kIsFp8<T>) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int key = 2 * c + (x & 1) + 4 * (x & 2);
-        if constexpr (D == 128) {
-          const uint4 w = *reinterpret_cast<const uint4*>(vt + chunk_at<T, kChunks>(key, g) * 16);
-          vw[x][0] = w.x; vw[x][1] = w.y; vw[x][2] = w.z; vw[x][3] = w.w;
-        } else {
-          const uint2 w = *reinterpret_cast<const uint2*>(vt + chunk_at<T, kChunks>(key, g / 2) * 16 + g % 2 * 8);
-          vw[x][0] = w.x; vw[x][1] = w.y;
+    for (int x = 0; x < kHalves; ++x) {
+      uint32_t vw[4][kIsFp8<T> ? RS::kV / 4 : 1];            // 8-bit rows: the pieces of keys 2c, 2c + 1, 2c + 8, 2c + 9
+      if constexpr (kIsFp8<T>) {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const int key = 16 * x + 2 * c + (y & 1) + 4 * (y & 2);
+          if constexpr (D == 128) {
+            const uint4 w = *reinterpret_cast<const uint4*>(vt + chunk_at<T, kChunks>(key, g) * 16);
+            vw[y][0] = w.x; vw[y][1] = w.y; vw[y][2] = w.z; vw[y][3] = w.w;
+          } else {
+            const uint2 w = *reinterpret_cast<const uint2*>(vt + chunk_at<T, kChunks>(key, g / 2) * 16 + g % 2 * 8);
+            vw[y][0] = w.x; vw[y][1] = w.y;
+          }
         }
       }
-    }
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-      uint32_t a[4];
-      if constexpr (kIsFp8<T>) {
-        // bytes 2 i, 2 i + 1 of two keys' pieces: two keys' values of one dimension, then of the next
-        const uint32_t x = __byte_perm(vw[0][i / 2], vw[1][i / 2], i % 2 ? 0x7362 : 0x5140);
-        const uint32_t z = __byte_perm(vw[2][i / 2], vw[3][i / 2], i % 2 ? 0x7362 : 0x5140);
-        a[0] = e4m3x2_to_half2(x & 0xffffu);
-        a[1] = e4m3x2_to_half2(x >> 16);
-        a[2] = e4m3x2_to_half2(z & 0xffffu);
-        a[3] = e4m3x2_to_half2(z >> 16);
-      } else {
-        ldmatrix<true>(a, v_at + chunk_at<T, kChunks>(v_key, 2 * i + lane / 8 % 2) * 16);
+      for (int i = 0; i < kTiles; ++i) {
+        uint32_t a[4];
+        if constexpr (kIsFp8<T>) {
+          // bytes 2 i, 2 i + 1 of two keys' pieces: two keys' values of one dimension, then of the next
+          const uint32_t lo2 = __byte_perm(vw[0][i / 2], vw[1][i / 2], i % 2 ? 0x7362 : 0x5140);
+          const uint32_t hi2 = __byte_perm(vw[2][i / 2], vw[3][i / 2], i % 2 ? 0x7362 : 0x5140);
+          a[0] = e4m3x2_to_half2(lo2 & 0xffffu);
+          a[1] = e4m3x2_to_half2(lo2 >> 16);
+          a[2] = e4m3x2_to_half2(hi2 & 0xffffu);
+          a[3] = e4m3x2_to_half2(hi2 >> 16);
+        } else {
+          ldmatrix<true>(a, v_at + chunk_at<T, kChunks>(16 * x + v_key, 2 * i + lane / 8 % 2) * 16);
+        }
+        if (careful) {
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            if (pair_not_finite<TP>(a[y])) {
+              odd = true;
+              if (pair_not_finite<TP>(a[y] & 0xffffu)) a[y] &= 0xffff0000u;
+              if (pair_not_finite<TP>(a[y] & 0xffff0000u)) a[y] &= 0xffffu;
+            }
+        }
+#pragma unroll
+        for (int y = 0; y < kGroups; ++y) mma_16816<TP>(acc[y][i], a[0], a[1], a[2], a[3], ph[x][y][0], ph[x][y][1], acc[y][i]);
+#pragma unroll
+        for (int y = 0; y < kGroups; ++y) mma_16816<TP>(acc[y][i], a[0], a[1], a[2], a[3], pl[x][y][0], pl[x][y][1], acc[y][i]);
       }
-      if (careful) {
-#pragma unroll
-        for (int y = 0; y < 4; ++y)
-          if (pair_not_finite<TP>(a[y])) {
-            odd = true;
-            if (pair_not_finite<TP>(a[y] & 0xffffu)) a[y] &= 0xffff0000u;
-            if (pair_not_finite<TP>(a[y] & 0xffff0000u)) a[y] &= 0xffffu;
-          }
-      }
-#pragma unroll
-      for (int y = 0; y < kGroups; ++y) mma_16816<TP>(acc[y][i], a[0], a[1], a[2], a[3], ph[y][0], ph[y][1], acc[y][i]);
-#pragma unroll
-      for (int y = 0; y < kGroups; ++y) mma_16816<TP>(acc[y][i], a[0], a[1], a[2], a[3], pl[y][0], pl[y][1], acc[y][i]);
     }
     if (careful && __any_sync(~0u, odd)) {                   // add what was taken out, element by element
 #pragma unroll 1
@@ -418,15 +442,15 @@ again:
           for (int z = 0; z < 2; ++z) {
             const int at = (kIsFp8<T> ? g * RS::kV + 2 * i + z : 16 * i + g + 8 * z) * RS::kBytes;
             const uint8_t* v = vt + chunk_at<T, kChunks>(key, at / 16) * 16 + at % 16;
-            float x;
-            if constexpr (kIsFp8<T>) x = e4m3x2_to_float2(*v).x;
-            else x = to_float(*reinterpret_cast<const TQ*>(v));
-            if (!isfinite(x)) {
+            float f;
+            if constexpr (kIsFp8<T>) f = e4m3x2_to_float2(*v).x;
+            else f = to_float(*reinterpret_cast<const TQ*>(v));
+            if (!isfinite(f)) {
 #pragma unroll
               for (int y = 0; y < kGroups; ++y)
 #pragma unroll
                 for (int r = 0; r < 2; ++r)
-                  if (sees(p, pos[y][r], j0 + key)) acc[y][i][2 * z + r] += x;
+                  if (sees(p, pos[y][r], j0 + key)) acc[y][i][2 * z + r] += f;
             }
           }
     }
@@ -586,7 +610,7 @@ window_mass_kernel(const WindowParams p, const int mass_blocks) {
   if ((int)blockIdx.x * kMassKeys >= ctx) return;
   const int n_rows = p.H * p.n_q, first = ctx - n_new;
   const float* scores = p.ws_s + (int64_t)b * n_rows * p.s_pitch + j;
-  // (a row of scores is a multiple of sixteen long: four of them are there, or none; what a token does not see is not used)
+  // (a row of scores is a multiple of 32 long: four of them are there, or none; what a token does not see is not used)
   auto ask = [&](int i) {
     return i < n_rows && j < p.s_pitch ? *reinterpret_cast<const float4*>(scores + (int64_t)i * p.s_pitch) : make_float4(0.f, 0.f, 0.f, 0.f);
   };
@@ -639,7 +663,7 @@ window_mass_kernel(const WindowParams p, const int mass_blocks) {
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
-struct WindowPlan { bool tiles; int block_rows, n_splits, s_pitch; size_t ml_bytes, acc_bytes, s_bytes, total_bytes; };
+struct WindowPlan { bool tiles; int block_rows, keys, fewest, n_splits, s_pitch; size_t ml_bytes, acc_bytes, s_bytes, total_bytes; };
 
 int32_t check_paging(const ssa_paging* pg, int32_t max_ctx) {
   if (!pg->page_table) return SSA_ERR_NULL;
@@ -669,24 +693,26 @@ static bool tiles_pay(const ssa_attn_desc* d, const ssa_window* w, bool mass) {
 static bool plan_window(const ssa_attn_desc* d, const ssa_window* w, bool mass, bool tiles, WindowPlan* pl) {
   pl->tiles = tiles;
   const long long per_head = (long long)(d->H / d->H_kv) * w->n_q;
-  int rows = kBlockRows;
-  if (!tiles)
-    for (rows = kGroup; rows < per_head && rows < 8 * kGroup; rows *= 2) {}
-  const int keys = tiles ? kTileKeys : kKeys, fewest = tiles ? kTileSplit : kSplitTiles;
+  const int keys = tiles ? kTileKeys : d->D * (d->kv_dtype == SSA_FP8_E4M3 ? 1 : 2) == 256 ? 16 : 32, fewest = tiles ? kTileSplit : kSplitKeys / keys;
+  // rows of a block: a warp's groups of eight, or four groups of two warps each
+  const int groups = (int)std::min<long long>((per_head + kGroup - 1) / kGroup, 8);
+  const int rows = tiles ? kBlockRows : kGroup * (groups <= kMostGroups ? groups : 8);
   const long long group = d->H / d->H_kv, row_tiles = (per_head + rows - 1) / rows;
   const long long blocks = row_tiles * d->H_kv * d->B, tokens = (rows - 1) / group + 2;
   const long long most = w->window == 0 ? d->max_ctx : std::min<long long>(d->max_ctx, (long long)w->window + w->sinks + tokens);
   const long long n_tiles = (most + keys - 1) / keys + 2;
+  pl->keys = keys;
+  pl->fewest = fewest;
   // Splits of the kernel for few rows, by what they cost in units of one tile's time: the work of all blocks, each with a start
-  // and an end, over the places there are (three blocks to an SM), but no less than one block's; half a block's until the last
+  // and an end, over the places there are (two or three blocks to an SM), but no less than one block's; half a block's until the last
   // is done (lengths differ: three quarters of the longest are taken for the mean); joining.
   long long splits = 1;
   const long long most_splits = std::min(n_tiles / fewest, 64ll);
   if (tiles) {
     splits = sm_count() / blocks;
   } else {
-    const int teams = kWarps / std::max(1, rows / (2 * kGroup));
-    const double steps = (double)n_tiles / teams, places = 3.0 * sm_count(), ends = 5;
+    const int teams = rows <= kMostGroups * kGroup ? kWarps : kWarps / 2;
+    const double steps = (double)n_tiles / teams, places = (rows <= 2 * kGroup ? 3.0 : 2.0) * sm_count(), ends = 5;
     double least = 0;
     for (long long n = 1; n <= most_splits; ++n) {
       const double one = steps / n + ends, all = blocks * n * (0.75 * steps / n + ends) / places;
@@ -699,7 +725,7 @@ static bool plan_window(const ssa_attn_desc* d, const ssa_window* w, bool mass, 
   const size_t slots = (size_t)d->B * d->H * w->n_q * pl->n_splits;
   pl->ml_bytes = up256(slots * sizeof(float2));
   pl->acc_bytes = pl->n_splits > 1 ? up256(slots * d->D * sizeof(float)) : 0;
-  pl->s_pitch = mass ? (d->max_ctx + kKeys - 1) / kKeys * kKeys : 0;
+  pl->s_pitch = mass ? (int)(((long long)d->max_ctx + 31) / 32 * 32) : 0;
   pl->s_bytes = up256((size_t)d->B * d->H * w->n_q * pl->s_pitch * sizeof(float));
   pl->total_bytes = pl->ml_bytes + pl->acc_bytes + pl->s_bytes;
   return row_tiles * pl->n_splits <= 0x7fffffffll;
@@ -727,14 +753,18 @@ static cudaError_t launch_tiles(const WindowParams& p, const CUtensorMap& k_map,
 template <typename T, int D, bool kPaged, bool kMass>
 static cudaError_t launch_rows(const WindowParams& p, cudaStream_t st) {
   const dim3 grid((unsigned)((p.group * p.n_q + p.block_rows - 1) / p.block_rows * p.n_splits), (unsigned)p.H_kv, (unsigned)p.B);
-  auto kernel = p.block_rows == kGroup       ? window_rows_kernel<T, D, kPaged, kMass, 1, 1>
-                : p.block_rows == 2 * kGroup ? window_rows_kernel<T, D, kPaged, kMass, 1, 2>
-                : p.block_rows == 4 * kGroup ? window_rows_kernel<T, D, kPaged, kMass, 2, 2>
-                                             : window_rows_kernel<T, D, kPaged, kMass, 4, 2>;
-  const int join_bytes = kWarps * std::min(p.block_rows, 2 * kGroup) * (D + 4) * 4;
-  const int smem = std::max(RowShape<T, D>::kSmem, join_bytes);
-  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  return err != cudaSuccess ? err : launch_pdl_smem(kernel, grid, dim3(kWarps * 32), smem, st, p);
+  auto launch = [&](auto kernel, int bytes, int warp_rows) {
+    const int smem = std::max(bytes, kWarps * warp_rows * (D + 4) * (int)sizeof(float));     // (the join's place)
+    const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    return err != cudaSuccess ? err : launch_pdl_smem(kernel, grid, dim3(kWarps * 32), smem, st, p);
+  };
+  switch (p.block_rows / kGroup) {
+    case 1: return launch(window_rows_kernel<T, D, kPaged, kMass, 1, 1>, RowShape<T, D, 1>::kSmem, kGroup);
+    case 2: return launch(window_rows_kernel<T, D, kPaged, kMass, 1, 2>, RowShape<T, D, 2>::kSmem, 2 * kGroup);
+    case 3: return launch(window_rows_kernel<T, D, kPaged, kMass, 1, 3>, RowShape<T, D, 3>::kSmem, 3 * kGroup);
+    case 4: return launch(window_rows_kernel<T, D, kPaged, kMass, 1, 4>, RowShape<T, D, 4>::kSmem, 4 * kGroup);
+    default: return launch(window_rows_kernel<T, D, kPaged, kMass, 2, 4>, RowShape<T, D, 4>::kSmem, 4 * kGroup);
+  }
 }
 
 template <typename T, int D>
@@ -789,8 +819,8 @@ static int32_t run_window(const ssa_attn_desc* d, const ssa_window* w, const voi
   if (!tiles && !plan_window(d, w, mass, false, &pl)) return SSA_ERR_SHAPE;
   WindowParams p;
   p.block_rows = pl.block_rows;
-  p.tile_keys = tiles ? kTileKeys : kKeys;
-  p.split_tiles = tiles ? kTileSplit : kSplitTiles;
+  p.tile_keys = pl.keys;
+  p.split_tiles = pl.fewest;
   p.q = q; p.k = k; p.v = v; p.out = out; p.lse = lse;
   p.ctx_lens = ctx_lens; p.q_lens = w->q_lens; p.page_table = pg ? pg->page_table : nullptr;
   char* at = static_cast<char*>(ws);
