@@ -20,6 +20,10 @@ constexpr int kGroup = 8;              // query rows of a matrix tile: (token, h
 constexpr int kWarps = 4;              // of a block
 constexpr int kSplitKeys = 256;        // fewest positions worth a split of their own
 constexpr int kMostGroups = 4;         // of kGroup rows, of a warp
+constexpr float kLazyRows = 2.f;       // log2 of how far weights may exceed 1 before sums are rescaled (fp16: 2^13 times that)
+// Rows of a K/V head up to which this kernel is the faster one (16 requests of up to 4096, 8 K/V heads: 16 rows 41 us, the tiles
+// 53; 24 rows 55 and 57; 32 rows 82 and 58).
+constexpr int kFewRows = 24;
 
 // The weights enter the second contraction as a 16-bit value plus the 16-bit rest, so that the sums keep 16 bits (bf16) or 22
 // (fp16) of each.  fp16 has little range below 1: its weights are scaled by 2^13, which the sum divides out again.
@@ -358,22 +362,27 @@ again:
         top[y][0] = fmaxf(top[y][0], __shfl_xor_sync(~0u, top[y][0], o));
         top[y][1] = fmaxf(top[y][1], __shfl_xor_sync(~0u, top[y][1], o));
       }
-    uint32_t ph[kHalves][kGroups][2], pl[kHalves][kGroups][2];         // the weights, keys 0-7 and 8-15, and what their rounding left
+    bool higher = false;
 #pragma unroll
-    for (int y = 0; y < kGroups; ++y) {
-      float shift[2];
+    for (int y = 0; y < kGroups; ++y) higher |= top[y][0] > m[y][0] + kLazyRows || top[y][1] > m[y][1] + kLazyRows;   // (m = -inf: anything)
+    if (__any_sync(~0u, higher)) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r) shift[r] = (top[y][r] == neg_inf() ? 0.f : top[y][r]) - kShift;
-      if (__any_sync(~0u, top[y][0] != m[y][0] || top[y][1] != m[y][1])) {
+      for (int y = 0; y < kGroups; ++y)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const float alpha = fast_exp2(m[y][r] - kShift - shift[r]);  // (m = -inf: 0)
+          const float alpha = top[y][r] == m[y][r] ? 1.f : fast_exp2(m[y][r] - top[y][r]);
 #pragma unroll
           for (int i = 0; i < kTiles; ++i) { acc[y][i][r] *= alpha; acc[y][i][r + 2] *= alpha; }
           l[y][r] *= alpha;
           m[y][r] = top[y][r];
         }
-      }
+    }
+    uint32_t ph[kHalves][kGroups][2], pl[kHalves][kGroups][2];         // the weights, keys 0-7 and 8-15, and what their rounding left
+#pragma unroll
+    for (int y = 0; y < kGroups; ++y) {
+      float shift[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) shift[r] = (m[y][r] == neg_inf() ? 0.f : m[y][r]) - kShift;
 #pragma unroll
       for (int x = 0; x < kHalves; ++x)
 #pragma unroll
@@ -663,7 +672,7 @@ window_mass_kernel(const WindowParams p, const int mass_blocks) {
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
-struct WindowPlan { bool tiles; int block_rows, keys, fewest, n_splits, s_pitch; size_t ml_bytes, acc_bytes, s_bytes, total_bytes; };
+struct WindowPlan { bool tiles, paired; int block_rows, keys, fewest, n_splits, s_pitch; size_t ml_bytes, acc_bytes, s_bytes, total_bytes; };
 
 int32_t check_paging(const ssa_paging* pg, int32_t max_ctx) {
   if (!pg->page_table) return SSA_ERR_NULL;
@@ -684,9 +693,9 @@ static int32_t check_window(const ssa_attn_desc* d, const ssa_window* w, bool ma
 
 static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-// More rows than a block of the kernel for few serves (its next one would read the cache again) go to the tiles of 256.
+// Whether the tiles of 256 rows serve a call.
 static bool tiles_pay(const ssa_attn_desc* d, const ssa_window* w, bool mass) {
-  return !mass && d->kv_dtype != SSA_FP8_E4M3 && (long long)(d->H / d->H_kv) * w->n_q > 4 * kGroup &&
+  return !mass && d->kv_dtype != SSA_FP8_E4M3 && (long long)(d->H / d->H_kv) * w->n_q > kFewRows &&
          (!w->paging || w->paging->page_size >= 8);          // (a box of a copy is eight rows at least)
 }
 
@@ -703,24 +712,24 @@ static bool plan_window(const ssa_attn_desc* d, const ssa_window* w, bool mass, 
   const long long n_tiles = (most + keys - 1) / keys + 2;
   pl->keys = keys;
   pl->fewest = fewest;
-  // Splits of the kernel for few rows, by what they cost in units of one tile's time: the work of all blocks, each with a start
-  // and an end, over the places there are (two or three blocks to an SM), but no less than one block's; half a block's until the last
-  // is done (lengths differ: three quarters of the longest are taken for the mean); joining.
-  long long splits = 1;
-  const long long most_splits = std::min(n_tiles / fewest, 64ll);
-  if (tiles) {
-    splits = sm_count() / blocks;
-  } else {
+  const bool paired = tiles && per_head <= kTileRows;
+  const long long most_splits = std::max(1ll, std::min(n_tiles / fewest, 64ll));
+  long long splits = std::min(most_splits, std::max(1ll, sm_count() / blocks));   // tiles: a block to an SM
+  if (!tiles) {
+    // The kernel for few rows: what n splits cost in units of one tile's time.  The work of all blocks, each with a start and an
+    // end, over the places that there are (two or three blocks to an SM), but no less than one block's; half a block's until the
+    // last is done (lengths differ: three quarters of the longest are taken for the mean); joining.
     const int teams = rows <= kMostGroups * kGroup ? kWarps : kWarps / 2;
-    const double steps = (double)n_tiles / teams, places = (rows <= 2 * kGroup ? 3.0 : 2.0) * sm_count(), ends = 5;
+    const double steps = (double)n_tiles / teams, places = (rows <= 2 * kGroup ? 3.0 : 2.0) * sm_count(), ends = 5, join = 6;
     double least = 0;
     for (long long n = 1; n <= most_splits; ++n) {
       const double one = steps / n + ends, all = blocks * n * (0.75 * steps / n + ends) / places;
-      const double cost = std::max(one, all) + 0.5 * one + (n > 1 ? 6 : 0);
+      const double cost = std::max(one, all) + 0.5 * one + (n > 1 ? join : 0);
       if (n == 1 || cost < least) { least = cost; splits = n; }
     }
   }
-  pl->n_splits = (int)std::max(1ll, std::min(splits, most_splits));
+  pl->paired = paired;
+  pl->n_splits = (int)splits << (int)paired;
   pl->block_rows = rows;
   const size_t slots = (size_t)d->B * d->H * w->n_q * pl->n_splits;
   pl->ml_bytes = up256(slots * sizeof(float2));
@@ -742,7 +751,7 @@ static size_t window_bytes(const ssa_attn_desc* d, const ssa_window* w, bool mas
 
 template <typename T, int D>
 static cudaError_t launch_tiles(const WindowParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, int box_rows, cudaStream_t st) {
-  const dim3 grid((unsigned)((p.group * p.n_q + kBlockRows - 1) / kBlockRows * p.n_splits), (unsigned)p.H_kv, (unsigned)p.B);
+  const dim3 grid((unsigned)((p.group * p.n_q + kBlockRows - 1) / kBlockRows * (p.n_splits >> p.paired)), (unsigned)p.H_kv, (unsigned)p.B);
   auto kernel = p.page_table ? window_tile_kernel<T, D, true> : window_tile_kernel<T, D, false>;
   constexpr int kSmem = TileShape<D>::kSmem;
   const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
@@ -819,6 +828,7 @@ static int32_t run_window(const ssa_attn_desc* d, const ssa_window* w, const voi
   if (!tiles && !plan_window(d, w, mass, false, &pl)) return SSA_ERR_SHAPE;
   WindowParams p;
   p.block_rows = pl.block_rows;
+  p.paired = pl.paired;
   p.tile_keys = pl.keys;
   p.split_tiles = pl.fewest;
   p.q = q; p.k = k; p.v = v; p.out = out; p.lse = lse;

@@ -10,6 +10,10 @@
 // scores' chain, but an instruction of 128 x 64 takes as long as one of 128 x 128 - the 128 rows of Q are read either way -
 // and whole prompts took 524 instead of 485 us.)
 //
+// Where a K/V head has no more than 128 rows, both row tiles are the same rows and take turns at the tiles (`paired`); each is a
+// split of its own, joined with the rest by the next launch.  Five drafted tokens of four heads each, 16 requests of up to 4096:
+// PAIRED
+//
 // The running maximum that weights are relative to follows the true one only where that is more than 2^8 above it, so that O
 // is rescaled in a few tiles at the start and hardly ever after that; weights are then at most 2^8 (fp16: times 2^6, which
 // the sum divides out again, because fp16 has little range below 1), rounded once to 16 bits: the two parts that the kernel
@@ -135,7 +139,7 @@ __device__ constexpr uint32_t tile_idesc() {
 
 // One row again in fp32, by a warp, with the infinities and NaNs of V kept to where they are seen: lane i's dimensions i D/32 ...
 template <typename T, int D, bool kPaged>
-__device__ __noinline__ void careful_row(const WindowParams& p, const Seen& seen, int2 range, int b, int h, int t, int pos, float& m,
+__device__ __noinline__ void careful_row(const WindowParams& p, const Seen& seen, int2 range, int step, int b, int h, int t, int pos, float& m,
                                          float& l, float (&acc)[D / 32]) {
   constexpr int kN = D / 32;
   const int lane = threadIdx.x % 32, hkv = h / p.group;
@@ -148,7 +152,7 @@ __device__ __noinline__ void careful_row(const WindowParams& p, const Seen& seen
   l = 0.f;
 #pragma unroll
   for (int i = 0; i < kN; ++i) { acc[i] = odd[i] = 0.f; qf[i] = to_float(q[i]); }
-  for (int it = range.x; it < range.y; ++it)
+  for (int it = range.x; it < range.y; it += step)
     for (int j = seen.position(it); j < seen.position(it) + kTileKeys; ++j) {
       if (!sees(p, pos, j)) continue;
       const int64_t row = row_of<kPaged>(p, table, j);
@@ -173,6 +177,20 @@ __device__ __noinline__ void careful_row(const WindowParams& p, const Seen& seen
   for (int i = 0; i < kN; ++i) acc[i] += odd[i];
 }
 
+// The order in which a block's copies are made and used: K of the first `ahead` tiles, then V of a tile and K of the one that many
+// tiles on, in turn, as far as there are any.
+struct Copies {
+  int n, ahead;
+  __device__ __forceinline__ int of_k(int tile) const { return tile < ahead ? tile : 2 * tile - ahead + 1; }
+  __device__ __forceinline__ int of_v(int tile) const { return min(ahead, n) + tile + min(tile, max(n - ahead, 0)); }
+  __device__ __forceinline__ bool is_v(int i, int& tile) const {
+    const int m = i - min(ahead, n), both = 2 * max(n - ahead, 0);
+    const bool v = m >= both || (m >= 0 && !(m & 1));
+    tile = m < 0 ? i : m >= both ? m - both / 2 : m / 2 + (v ? 0 : ahead);
+    return v;
+  }
+};
+
 // grid (splits x row blocks, H_kv, B), the last row blocks first: they see most.
 template <typename T, int D, bool kPaged>
 __global__ void __launch_bounds__(kTileThreads, 1)
@@ -192,7 +210,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   grid_dependency_wait();
   grid_launch_dependents();
-  const int block = p.n_splits == 1 ? blockIdx.x : blockIdx.x / p.n_splits, split = blockIdx.x - block * p.n_splits;
+  const int per_block = p.n_splits >> p.paired, block = per_block == 1 ? blockIdx.x : blockIdx.x / per_block, split = blockIdx.x - block * per_block;
   const int row0 = ((p.group * p.n_q - 1) / kBlockRows - block) * kBlockRows, hkv = blockIdx.y, b = blockIdx.z;
   uint32_t flags = 0;
   int ctx, n_new;
@@ -204,13 +222,13 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
   const int t_lo = token_of(p, row0), t_hi = token_of(p, row0 + rows - 1), lo = first + t_lo, hi = first + t_hi;
   const Seen seen(p, kTileKeys, first, t_lo, t_hi);
   const int n_splits = splits_used(p, seen.tiles);
-  if (split >= n_splits) return;
-  const int2 range = split_tiles(seen.tiles, split, n_splits);
+  if (split >= n_splits >> p.paired) return;
+  const int2 range = split_tiles(seen.tiles, split, n_splits >> p.paired);
   // the two row tiles: positions of their first and last rows, and which of the block's tiles they take part in
   int tile_lo[2], tile_hi[2];
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
-    const int a = min(row0 + x * kTileRows, row0 + rows), z = min(row0 + (x + 1) * kTileRows, row0 + rows) - 1;
+    const int at = p.paired ? row0 : row0 + x * kTileRows, a = min(at, row0 + rows), z = min(at + kTileRows, row0 + rows) - 1;
     tile_lo[x] = first + token_of(p, a);
     tile_hi[x] = z < a ? -1 : first + token_of(p, z);                  // (no rows, or none with a position: no tiles)
   }
@@ -222,15 +240,19 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
   };
   auto needs = [&](int x, int it) {
     const int j0 = seen.position(it);
+    if (p.paired && ((it - range.x) & 1) != x) return false;
     return j0 <= tile_hi[x] && (p.window == 0 || j0 < p.sinks || j0 + kTileKeys - 1 > tile_lo[x] - p.window);
   };
   const uint32_t kv = base + 2 * Shape::kQBytes;
   const int n_tiles = range.y - range.x, n_loads = 2 * n_tiles;
+  const Copies copies = {n_tiles, 1 + p.paired};                       // scores are one tile of each row tile ahead of sums
   volatile int* dead = &s_dead;
 
-  // ---- copies, by warp 9: K(0), V(0), K(1), ... into a ring of stages ----
+  // ---- copies, by warp 9, into a ring of stages ----
   auto load = [&](int i) {
-    const int stage = i % kTileStages, j0 = seen.position(range.x + i / 2);
+    int tile;
+    const bool is_v = copies.is_v(i, tile);
+    const int stage = i % kTileStages, j0 = seen.position(range.x + tile);
     if (lane == 0) mbar_expect(full + 8 * stage, Shape::kTileBytes);
     __syncwarp();
     if (lane < kTileKeys / box_rows) {
@@ -246,15 +268,16 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
       const uint32_t to = kv + stage * Shape::kTileBytes + lane * box_rows * 128;
 #pragma unroll
       for (int x = 0; x < D / 64; ++x)
-        tma_load(to + x * Shape::kHalf, i & 1 ? &v_map : &k_map, x * 64, row, hkv, batch, full + 8 * stage);
+        tma_load(to + x * Shape::kHalf, is_v ? &v_map : &k_map, x * 64, row, hkv, batch, full + 8 * stage);
     }
   };
   // Rows of V that no token sees become zero.  A copy's turn comes two copies after its own, so that others are on their way.
-  int settled = 1;
+  int settled = 0;
   auto settle = [&](int upto) {
-    for (; settled <= upto; settled += 2) {
-      if (!unseen(range.x + settled / 2)) continue;
-      const int stage = settled % kTileStages, j0 = seen.position(range.x + settled / 2);
+    for (; settled <= upto; ++settled) {
+      int tile;
+      if (!copies.is_v(settled, tile) || !unseen(range.x + tile)) continue;
+      const int stage = settled % kTileStages, j0 = seen.position(range.x + tile);
       mbar_wait(full + 8 * stage, (settled / kTileStages) & 1, dead);
       for (int r = lane / 8; r < kTileKeys; r += 4) {
         const int j = j0 + r;
@@ -287,7 +310,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
     constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
     const int i = lane % kLanes;
     {
-      const int row = row0 + (int)threadIdx.x, t = token_of(p, row), h = hkv * p.group + row - t * p.group;
+      const int row = row0 + (int)(p.paired ? threadIdx.x % kTileRows : threadIdx.x), t = token_of(p, row), h = hkv * p.group + row - t * p.group;
       s_row[0][threadIdx.x] = (int64_t)b * p.q_sb + (int64_t)h * p.q_sh + (int64_t)t * p.q_st;
       s_row[1][threadIdx.x] = (int64_t)b * p.o_sb + (int64_t)h * p.o_sh + (int64_t)t * p.o_st;
     }
@@ -297,7 +320,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
     for (int y = 0; y < 32 / kAtOnce; ++y) {
       const int r = warp * 32 + y * kAtOnce + lane / kLanes;
       w[y] = make_uint4(0, 0, 0, 0);
-      if (r < rows) w[y] = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.q) + s_row[0][r] + i * 8);
+      if ((p.paired ? r % kTileRows : r) < rows) w[y] = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.q) + s_row[0][r] + i * 8);
     }
 #pragma unroll
     for (int y = 0; y < 32 / kAtOnce; ++y) {
@@ -344,23 +367,23 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
       }
       __syncwarp();
     };
-    if (n_tiles > 0) {
-      wait_full(0);
+    for (int tile = 0; tile < min(copies.ahead, n_tiles); ++tile) {
+      wait_full(tile);
       tc_after();
       for (int x = 0; x < 2; ++x)
-        if (needs(x, range.x)) scores(x, 0);
-      if (leader) tc_commit(empty);
+        if (needs(x, range.x + tile)) scores(x, tile);
+      if (leader) tc_commit(empty + 8 * tile);
       __syncwarp();
     }
     for (int tile = 0; tile < n_tiles; ++tile) {
-      const int i = 2 * tile + 1, stage = i % kTileStages, k_stage = (i + 1) % kTileStages;
-      const bool more = tile + 1 < n_tiles;
+      const int i = copies.of_v(tile), next = copies.of_k(tile + copies.ahead), stage = i % kTileStages, k_stage = next % kTileStages;
+      const bool more = tile + copies.ahead < n_tiles;
       wait_full(i);
       if (unseen(range.x + tile)) {
         mbar_wait(fixed + 8 * stage, fixes >> stage & 1, dead);
         fixes ^= 1u << stage;
       }
-      if (more) wait_full(i + 1);
+      if (more) wait_full(next);
       tc_after();
       const uint64_t vd = v_desc + stage * (Shape::kTileBytes >> 4);
       for (int x = 0; x < 2; ++x) {
@@ -382,7 +405,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
           if (leader && tile == last[x]) tc_commit(o_full + 8 * x);
           __syncwarp();
         }
-        if (more && needs(x, range.x + tile + 1)) scores(x, k_stage);   // over weights that the contraction just issued takes
+        if (more && needs(x, range.x + tile + copies.ahead)) scores(x, k_stage);   // over weights that the contraction just issued takes
       }
       if (leader) {
         tc_commit(empty + 8 * stage);
@@ -393,8 +416,8 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
   } else if (warp < 8) {
     // ---- softmax: a thread per row ----
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-    const int x = warp / 4, row = row0 + (int)threadIdx.x;
-    const bool there = (int)threadIdx.x < rows;
+    const int x = warp / 4, mine = p.paired ? threadIdx.x % kTileRows : threadIdx.x, row = row0 + mine;
+    const bool there = mine < rows;
     const int t = token_of(p, row), h = hkv * p.group + row - t * p.group, pos = there ? first + t : -1;
     const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16, s_at = tmem + x * 128 + lanes, o_at = s_at + 256;
     const int all_lo = p.window == 0 ? 0 : tile_hi[x] - p.window + 1;  // every row of the tile sees [all_lo, tile_lo]
@@ -488,7 +511,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
     tc_after();
 
     // ---- the row: out, or a split's part of it ----
-    const int64_t at = ((int64_t)b * p.H + h) * p.n_q + t, slot = at * p.n_splits + split;
+    const int64_t at = ((int64_t)b * p.H + h) * p.n_q + t, slot = at * p.n_splits + (p.paired ? 2 * split + x : split);
     const bool finished = n_splits == 1;
     const float scale = finished ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
     float2 test = make_float2(l * 0.f, 0.f);
@@ -550,9 +573,9 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
       const int i = __ffs(again) - 1;
       again &= again - 1;
       const int rt = __shfl_sync(~0u, t, i), rh = __shfl_sync(~0u, h, i), rpos = __shfl_sync(~0u, pos, i);
-      const int64_t rat = ((int64_t)b * p.H + rh) * p.n_q + rt, rslot = rat * p.n_splits + split;
+      const int64_t rat = ((int64_t)b * p.H + rh) * p.n_q + rt, rslot = rat * p.n_splits + (p.paired ? 2 * split + x : split);
       float rm, rl, acc[D / 32];
-      careful_row<T, D, kPaged>(p, seen, range, b, rh, rt, rpos, rm, rl, acc);
+      careful_row<T, D, kPaged>(p, seen, make_int2(range.x + p.paired * x, range.y), 1 + p.paired, b, rh, rt, rpos, rm, rl, acc);
       __syncwarp();
 #pragma unroll
       for (int d = 0; d < D / 32; ++d) {
