@@ -56,22 +56,31 @@ __device__ __forceinline__ uint32_t load_from(const void* mine, uint32_t rank) {
   return v;
 }
 
-// grid (blocks of a request, requests): kItems keys a thread, in registers; several blocks of a request are a cluster and add
-// their histograms up over distributed shared memory.  kLong: more than a cluster's threads hold, keys are read anew each time.
+// grid (blocks of a request, requests): kItems neighbouring positions a thread, their keys in registers; several blocks of a
+// request are a cluster and add their histograms up over distributed shared memory.  kLong: more than a cluster's threads hold,
+// keys are read anew each time.  Positions that are not ranked have key 0, the lowest, and are left out of the histograms; so are
+// NaNs, and the lowest bin counts as one that never runs out.
 template <int kItems, bool kLong>
 __global__ void __launch_bounds__(kKeepThreads)
 mass_keep_kernel(const KeepParams p) {
-  __shared__ uint32_t s_bins[kBins];
-  __shared__ uint32_t s_count[kLong ? 1 : kItems * 32];    // (item, warp): larger keys, and equal ones from bit 16 on
-  __shared__ uint32_t s_sum[kKeepWarps], s_total, s_digit, s_left;
+  __shared__ uint32_t s_bins[3][kBins];                    // of a digit each
+  __shared__ uint32_t s_all[kBins];                        // clusters: all blocks' of the digit at hand
+  __shared__ uint32_t s_sum[2][kKeepWarps], s_total[2];
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid % 32, warp = tid / 32, blocks = gridDim.x;
   const int rank = blocks == 1 ? 0 : (int)cluster_rank();
+  for (int i = tid; i < 3 * kBins; i += kKeepThreads) s_bins[0][i] = 0;
   grid_dependency_wait();
   grid_launch_dependents();
+  const float* mass = p.mass + (int64_t)b * p.mass_stride;
+  const int j0 = (rank * kKeepThreads + tid) * kItems;
+  float mine[kItems];                                      // (asked for before it is known how long the context is)
+  if constexpr (!kLong) {
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) mine[i] = j0 + i < p.max_ctx ? mass[j0 + i] : 0.f;
+  }
   int n = p.ctx_lens[b];
   if (n > p.max_ctx && tid == 0 && rank == 0 && p.status) atomicOr(p.status, SSA_DEV_BAD_COUNT);
   n = max(0, min(n, p.max_ctx));
-  const float* mass = p.mass + (int64_t)b * p.mass_stride;
   int32_t* index = p.index + (int64_t)b * p.index_stride;
   if (tid == 0 && rank == 0) p.counts[b] = min(n, p.budget);
   if (n <= p.budget) {
@@ -80,136 +89,140 @@ mass_keep_kernel(const KeepParams p) {
   }
   const int from = p.sinks, to = n - p.recent;             // those between are ranked
   int want = p.budget - p.sinks - p.recent;                // >= 0, and < to - from
-  const int j0 = rank * kItems * kKeepThreads + tid;       // items lie kKeepThreads apart
-  uint32_t mine[kLong ? 1 : kItems];
+  auto ranked = [&](int j) { return j >= from && j < to; };
+  uint32_t keys[kItems];
   if constexpr (!kLong) {
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      const int j = j0 + i * kKeepThreads;
-      mine[i] = j >= from && j < to ? order_key(mass[j]) : 0;
-    }
+    for (int i = 0; i < kItems; ++i) keys[i] = ranked(j0 + i) ? order_key(mine[i]) : 0;
   }
-  auto ranked = [&](int j) { return j >= from && j < to; };
   auto sync = [&]() {
     if (blocks > 1) cluster_sync();
     else __syncthreads();
   };
   uint32_t key = 0, known = 0;                             // digits found so far, and their mask
-  if (want > 0) {
+  const bool none = want == 0;                             // the budget has no room for ranked positions
+  __syncthreads();
+  if (!none) {
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
       const uint32_t digits = pass == 2 ? 1023u : 2047u;
-      for (int i = tid; i < kBins; i += kKeepThreads) s_bins[i] = 0;
-      __syncthreads();
+      uint32_t* const bins = s_bins[pass];
       // Sums are often all alike (nothing looked at yet): a warp whose first keys share the digit adds once for all that do.
-      const uint32_t first = kLong ? 0 : mine[0] >> shift & digits;
-      const bool alike = kLong || __all_sync(~0u, first == __shfl_sync(~0u, first, 0));
-      auto add = [&](bool on, uint32_t k) {
+      const uint32_t sample = kLong ? 0 : keys[0] >> shift & digits;
+      const bool alike = kLong || __all_sync(~0u, sample == __shfl_sync(~0u, sample, 0));
+      auto add = [&](uint32_t k) {
+        const bool on = k != 0 && (k & known) == key;
         const uint32_t digit = k >> shift & digits;
         if (!alike) {
-          if (on) atomicAdd(&s_bins[digit], 1u);
+          if (on) atomicAdd(&bins[digit], 1u);
           return;
         }
         const unsigned votes = __ballot_sync(~0u, on);
         if (votes == 0) return;
         const uint32_t one = __shfl_sync(~0u, digit, __ffs(votes) - 1);
         if (__ballot_sync(~0u, on && digit == one) == votes) {
-          if (lane == 0) atomicAdd(&s_bins[one], (uint32_t)__popc(votes));
+          if (lane == 0) atomicAdd(&bins[one], (uint32_t)__popc(votes));
         } else if (on) {
-          atomicAdd(&s_bins[digit], 1u);
+          atomicAdd(&bins[digit], 1u);
         }
       };
       if constexpr (kLong) {
-        for (int j = from + tid; j - lane < to; j += kKeepThreads) {
-          const uint32_t k = ranked(j) ? order_key(mass[j]) : 0;
-          add(ranked(j) && (k & known) == key, k);
-        }
+        for (int j = from + tid; j - lane < to; j += kKeepThreads) add(ranked(j) ? order_key(mass[j]) : 0);
       } else {
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) add(ranked(j0 + i * kKeepThreads) && (mine[i] & known) == key, mine[i]);
+        for (int i = 0; i < kItems; ++i) add(keys[i]);
       }
       sync();
-      // the digit at which the count from the top reaches `want`: a thread has two bins
-      uint32_t count[2];
+      // A warp sums 64 bins, from the top; then every warp finds the 64 in which the count reaches `want`, and the bin.
+      const uint32_t* all = bins;
+      uint32_t two = 0;
+      if (blocks == 1) {
+        two = bins[kBins - 1 - 2 * tid] + bins[kBins - 2 - 2 * tid];
+      } else {
+        uint32_t part[2] = {0, 0};
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint32_t* bin = &s_bins[kBins - 1 - (2 * tid + i)];
-        count[i] = blocks == 1 ? *bin : 0;
-        for (int r = 0; blocks > 1 && r < blocks; ++r) count[i] += load_from(bin, r);
+        for (int r = 0; r < 8; ++r)
+          if (r < blocks) {
+            part[0] += load_from(&bins[kBins - 1 - 2 * tid], r);
+            part[1] += load_from(&bins[kBins - 2 - 2 * tid], r);
+          }
+        s_all[kBins - 1 - 2 * tid] = part[0];
+        s_all[kBins - 2 - 2 * tid] = part[1];
+        two = part[0] + part[1];
+        all = s_all;
       }
-      const int upto = warp_inclusive((int)(count[0] + count[1]), lane);
-      if (lane == 31) s_sum[warp] = (uint32_t)upto;
+      const uint32_t sum = __reduce_add_sync(~0u, two);
+      if (lane == 0) s_sum[pass & 1][warp] = sum;
       __syncthreads();
-      const int sums = warp_inclusive((int)s_sum[lane], lane);
-      int above = (warp ? __shfl_sync(~0u, sums, warp - 1) : 0) + upto - (int)(count[0] + count[1]);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (above < want && above + (int)count[i] >= want) { s_digit = kBins - 1 - (2 * tid + i); s_left = want - above; }
-        above += (int)count[i];
-      }
-      sync();                                              // (every block has read every histogram)
-      key |= s_digit << shift;
+      const int upto = warp_inclusive((int)s_sum[pass & 1][lane], lane);
+      const unsigned reached = __ballot_sync(~0u, upto >= want) | 1u << 31;  // (the last bin never runs out)
+      const int at = __ffs(reached) - 1;
+      const int above = at ? __shfl_sync(~0u, upto, at - 1) : 0;
+      const int first = kBins - 1 - at * 64;               // bins first, first - 1, ... : a lane has two
+      const int c0 = (int)all[first - 2 * lane], c1 = (int)all[first - 2 * lane - 1];
+      const int here = above + warp_inclusive(c0 + c1, lane), before = here - c0 - c1;
+      const unsigned hit = __ballot_sync(~0u, here >= want) | 1u << 31;
+      const int who = __ffs(hit) - 1;
+      const bool second = before + c0 < want;
+      const int digit = __shfl_sync(~0u, first - 2 * lane - (second ? 1 : 0), who);
+      want -= __shfl_sync(~0u, second ? before + c0 : before, who);
+      key |= (uint32_t)digit << shift;
       known |= digits << shift;
-      want = (int)s_left;
-      __syncthreads();
+      if (blocks > 1) __syncthreads();                     // (s_all is read until here)
+      if (key == 0) break;                                 // the rest are NaNs
     }
   }
   // `want` of the keys equal to `key` stay
-  const bool none = want == 0;                             // the budget has no room for ranked positions
+  auto larger = [&](int j, uint32_t k) { return j < n && (!ranked(j) || (!none && k > key)); };
+  auto equals = [&](int j, uint32_t k) { return ranked(j) && !none && k == key; };
   if constexpr (kLong) {
     int kept = 0, equal = 0;                               // before this step's positions
     for (int at = 0; at < n; at += kKeepThreads) {
       const int j = at + tid;
       const uint32_t k = ranked(j) ? order_key(mass[j]) : 0;
-      const bool same = ranked(j) && !none && k == key, stays = j < n && (!ranked(j) || (!none && k > key));
-      const unsigned larger = __ballot_sync(~0u, stays), equals = __ballot_sync(~0u, same), below = (1u << lane) - 1;
-      if (lane == 0) s_sum[warp] = (uint32_t)__popc(larger) | (uint32_t)__popc(equals) << 16;
+      const unsigned more = __ballot_sync(~0u, larger(j, k)), same = __ballot_sync(~0u, equals(j, k)), below = (1u << lane) - 1;
+      if (lane == 0) s_sum[0][warp] = (uint32_t)__popc(more) | (uint32_t)__popc(same) << 16;
       __syncthreads();
-      const uint32_t upto = (uint32_t)warp_inclusive((int)s_sum[lane], lane), before = warp ? __shfl_sync(~0u, upto, warp - 1) : 0;
+      const uint32_t upto = (uint32_t)warp_inclusive((int)s_sum[0][lane], lane), before = warp ? __shfl_sync(~0u, upto, warp - 1) : 0;
       const uint32_t all = __shfl_sync(~0u, upto, 31);
-      const int larger_before = kept + (int)(before & 0xffffu) + __popc(larger & below);
-      const int equal_before = equal + (int)(before >> 16) + __popc(equals & below);
-      if (stays || (same && equal_before < want)) index[larger_before + min(equal_before, want)] = j;
+      const int more_before = kept + (int)(before & 0xffffu) + __popc(more & below);
+      const int same_before = equal + (int)(before >> 16) + __popc(same & below);
+      if (larger(j, k) || (equals(j, k) && same_before < want)) index[more_before + min(same_before, want)] = j;
       kept += (int)(all & 0xffffu);
       equal += (int)(all >> 16);
       __syncthreads();
     }
   } else {
-    const unsigned below = (1u << lane) - 1;
-    unsigned larger[kItems], equals[kItems];
+    uint32_t count = 0;                                    // larger keys, equal ones from bit 16 on (a block has 2^14 positions at most)
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      const int j = j0 + i * kKeepThreads;
-      equals[i] = __ballot_sync(~0u, ranked(j) && !none && mine[i] == key);
-      larger[i] = __ballot_sync(~0u, j < n && (!ranked(j) || (!none && mine[i] > key)));
-      if (lane == 0) s_count[i * 32 + warp] = (uint32_t)__popc(larger[i]) | (uint32_t)__popc(equals[i]) << 16;
-    }
-    __syncthreads();
-    const uint32_t count = tid < kItems * 32 ? s_count[tid] : 0;     // (no half carries: a block has 2^14 positions at most)
+    for (int i = 0; i < kItems; ++i) count += larger(j0 + i, keys[i]) ? 1u : equals(j0 + i, keys[i]) ? 1u << 16 : 0u;
     const uint32_t upto = (uint32_t)warp_inclusive((int)count, lane);
-    if (lane == 31) s_sum[warp] = upto;
     __syncthreads();
-    const uint32_t sums = (uint32_t)warp_inclusive((int)s_sum[lane], lane);
-    const uint32_t ahead = warp ? __shfl_sync(~0u, sums, warp - 1) : 0;
-    if (tid < kItems * 32) s_count[tid] = ahead + upto - count;
-    if (tid == kKeepThreads - 1) s_total = sums;
-    sync();
-    int kept = 0, equal = 0;                               // in the blocks before this one
-    for (int r = 0; r < rank; ++r) {
-      const uint32_t total = load_from(&s_total, r);
-      kept += (int)(total & 0xffffu);
-      equal += (int)(total >> 16);
+    if (lane == 31) s_sum[0][warp] = upto;
+    __syncthreads();
+    const uint32_t sums = (uint32_t)warp_inclusive((int)s_sum[0][lane], lane);
+    const uint32_t before = (warp ? __shfl_sync(~0u, sums, warp - 1) : 0) + upto - count;
+    int at = (int)(before & 0xffffu), same = (int)(before >> 16);
+    if (blocks > 1) {                                      // and in the blocks before this one
+      if (tid == kKeepThreads - 1) s_total[0] = sums;
+      cluster_sync();
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
+        if (r < rank) {
+          const uint32_t total = load_from(&s_total[0], r);
+          at += (int)(total & 0xffffu);
+          same += (int)(total >> 16);
+        }
+      cluster_sync();                                      // (totals are read by the others until here)
     }
+    at += min(same, want);
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
-      const uint32_t before = s_count[i * 32 + warp];
-      const int larger_before = kept + (int)(before & 0xffffu) + __popc(larger[i] & below);
-      const int equal_before = equal + (int)(before >> 16) + __popc(equals[i] & below);
-      if ((larger[i] >> lane & 1) || ((equals[i] >> lane & 1) && equal_before < want))
-        index[larger_before + min(equal_before, want)] = j0 + i * kKeepThreads;
+      const bool more = larger(j0 + i, keys[i]), equal = equals(j0 + i, keys[i]);
+      if (more || (equal && same < want)) index[at++] = j0 + i;
+      same += equal;
     }
-    if (blocks > 1) cluster_sync();                        // (totals are read by the others until here)
   }
 }
 
