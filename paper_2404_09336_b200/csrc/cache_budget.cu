@@ -11,8 +11,6 @@ namespace ssa {
 // the lowest position.  Sums are compared as 32-bit keys of the same order (order_key); the key of the want-th largest is found
 // in three digits from the top, each by a histogram of the keys that match the digits found.  Then every larger key stays and
 // the first few equal ones, numbered by a prefix sum over (item, warp) counts.  Latency bounds it: a request is a few dozen KB.
-constexpr int kKeepThreads = 1024;
-constexpr int kKeepWarps = kKeepThreads / 32;
 constexpr int kBins = 2048;
 
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -49,6 +47,11 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // A word of another block's shared memory.
+__device__ __forceinline__ void store_to(const void* mine, uint32_t rank, uint32_t v) {
+  uint32_t at = (uint32_t)__cvta_generic_to_shared(mine);
+  asm volatile("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(at) : "r"(rank));
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
+}
 __device__ __forceinline__ uint32_t load_from(const void* mine, uint32_t rank) {
   uint32_t at = (uint32_t)__cvta_generic_to_shared(mine), v;
   asm volatile("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(at) : "r"(rank));
@@ -56,27 +59,45 @@ __device__ __forceinline__ uint32_t load_from(const void* mine, uint32_t rank) {
   return v;
 }
 
-// grid (blocks of a request, requests): kItems neighbouring positions a thread, their keys in registers; several blocks of a
-// request are a cluster and add their histograms up over distributed shared memory.  kLong: more than a cluster's threads hold,
-// keys are read anew each time.  Positions that are not ranked have key 0, the lowest, and are left out of the histograms; so are
-// NaNs, and the lowest bin counts as one that never runs out.
-template <int kItems, bool kLong>
-__global__ void __launch_bounds__(kKeepThreads)
+// grid (blocks of a request, requests): kItems keys a thread, in registers: four neighbouring positions of each of the parts that a
+// block has.  Several blocks of a request are a cluster; each adds up its share of all blocks' bins over distributed shared memory
+// and hands the sums out.  kLong: more than a cluster's threads hold, keys are read anew each time.  Positions that are not
+// ranked have key 0, the lowest, and are left out of the histograms; so are NaNs, and the lowest bin counts as one that never
+// runs out.  What stays is put in order in shared memory and written from there.
+template <int kThreads, int kItems, bool kLong>
+__global__ void __launch_bounds__(kThreads)
 mass_keep_kernel(const KeepParams p) {
-  __shared__ uint32_t s_bins[3][kBins];                    // of a digit each
+  constexpr int kWarps = kThreads / 32, kOwn = kBins / kThreads, kParts = kItems / 4, kPart = 4 * kThreads;
+  __shared__ uint32_t s_bins[3][kBins];                    // of a digit each; afterwards the positions that stay
   __shared__ uint32_t s_all[kBins];                        // clusters: all blocks' of the digit at hand
-  __shared__ uint32_t s_sum[2][kKeepWarps], s_total[2];
+  __shared__ uint32_t s_sum[kParts < 2 ? 2 : kParts][kWarps], s_total;
+  static_assert(kLong || kItems * kThreads * 2 <= (int)sizeof(s_bins) + (int)sizeof(s_all), "");
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid % 32, warp = tid / 32, blocks = gridDim.x;
   const int rank = blocks == 1 ? 0 : (int)cluster_rank();
-  for (int i = tid; i < 3 * kBins; i += kKeepThreads) s_bins[0][i] = 0;
+  for (int i = tid; i < 3 * kBins; i += kThreads) s_bins[0][i] = 0;
   grid_dependency_wait();
   grid_launch_dependents();
   const float* mass = p.mass + (int64_t)b * p.mass_stride;
-  const int j0 = (rank * kKeepThreads + tid) * kItems;
-  float mine[kItems];                                      // (asked for before it is known how long the context is)
+  const int block0 = rank * kItems * kThreads, j0 = block0 + tid * 4;
+  auto place = [&](int i) { return j0 + i / 4 * kPart + i % 4; };
+  uint32_t keys[kItems];                               // (asked for before it is known how long the context is)
   if constexpr (!kLong) {
+    const bool wide = ((reinterpret_cast<uintptr_t>(mass) | (uintptr_t)p.max_ctx * 4) & 15) == 0;
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) mine[i] = j0 + i < p.max_ctx ? mass[j0 + i] : 0.f;
+    for (int i = 0; i < kItems; i += 4) {
+      const int j = place(i);
+      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (wide) {
+        if (j < p.max_ctx) f = *reinterpret_cast<const float4*>(mass + j);
+      } else {
+        if (j < p.max_ctx) f.x = mass[j];
+        if (j + 1 < p.max_ctx) f.y = mass[j + 1];
+        if (j + 2 < p.max_ctx) f.z = mass[j + 2];
+        if (j + 3 < p.max_ctx) f.w = mass[j + 3];
+      }
+      keys[i] = __float_as_uint(f.x); keys[i + 1] = __float_as_uint(f.y);
+      keys[i + 2] = __float_as_uint(f.z); keys[i + 3] = __float_as_uint(f.w);
+    }
   }
   int n = p.ctx_lens[b];
   if (n > p.max_ctx && tid == 0 && rank == 0 && p.status) atomicOr(p.status, SSA_DEV_BAD_COUNT);
@@ -84,24 +105,20 @@ mass_keep_kernel(const KeepParams p) {
   int32_t* index = p.index + (int64_t)b * p.index_stride;
   if (tid == 0 && rank == 0) p.counts[b] = min(n, p.budget);
   if (n <= p.budget) {
-    for (int j = rank * kKeepThreads + tid; j < n; j += blocks * kKeepThreads) index[j] = j;
+    for (int j = rank * kThreads + tid; j < n; j += blocks * kThreads) index[j] = j;
     return;
   }
   const int from = p.sinks, to = n - p.recent;             // those between are ranked
   int want = p.budget - p.sinks - p.recent;                // >= 0, and < to - from
   auto ranked = [&](int j) { return j >= from && j < to; };
-  uint32_t keys[kItems];
   if constexpr (!kLong) {
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) keys[i] = ranked(j0 + i) ? order_key(mine[i]) : 0;
+    for (int i = 0; i < kItems; ++i) keys[i] = ranked(place(i)) ? order_key(__uint_as_float(keys[i])) : 0;
   }
-  auto sync = [&]() {
-    if (blocks > 1) cluster_sync();
-    else __syncthreads();
-  };
   uint32_t key = 0, known = 0;                             // digits found so far, and their mask
   const bool none = want == 0;                             // the budget has no room for ranked positions
-  __syncthreads();
+  if (blocks > 1) cluster_sync();                          // (every block has begun: its shared memory is there)
+  else __syncthreads();
   if (!none) {
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
@@ -128,48 +145,58 @@ mass_keep_kernel(const KeepParams p) {
         }
       };
       if constexpr (kLong) {
-        for (int j = from + tid; j - lane < to; j += kKeepThreads) add(ranked(j) ? order_key(mass[j]) : 0);
+        for (int j = from + tid; j - lane < to; j += kThreads) add(ranked(j) ? order_key(mass[j]) : 0);
       } else {
 #pragma unroll
         for (int i = 0; i < kItems; ++i) add(keys[i]);
       }
-      sync();
-      // A warp sums 64 bins, from the top; then every warp finds the 64 in which the count reaches `want`, and the bin.
       const uint32_t* all = bins;
-      uint32_t two = 0;
       if (blocks == 1) {
-        two = bins[kBins - 1 - 2 * tid] + bins[kBins - 2 - 2 * tid];
+        __syncthreads();
       } else {
-        uint32_t part[2] = {0, 0};
+        cluster_sync();
+        const int share = kBins / blocks;
+        for (int i = tid; i < share; i += kThreads) {
+          uint32_t sum = 0;
 #pragma unroll
-        for (int r = 0; r < 8; ++r)
-          if (r < blocks) {
-            part[0] += load_from(&bins[kBins - 1 - 2 * tid], r);
-            part[1] += load_from(&bins[kBins - 2 - 2 * tid], r);
-          }
-        s_all[kBins - 1 - 2 * tid] = part[0];
-        s_all[kBins - 2 - 2 * tid] = part[1];
-        two = part[0] + part[1];
+          for (int r = 0; r < 8; ++r)
+            if (r < blocks) sum += load_from(&bins[rank * share + i], r);
+          for (int r = 0; r < blocks; ++r) store_to(&s_all[rank * share + i], r, sum);
+        }
+        cluster_sync();
         all = s_all;
       }
-      const uint32_t sum = __reduce_add_sync(~0u, two);
+      // A warp sums its share of the bins, from the top; then every warp finds the share in which the count reaches `want`, and
+      // the bin.
+      uint32_t mine = 0;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) mine += all[kBins - 1 - (i * 32 + warp * 32 * kOwn + lane)];
+      const uint32_t sum = __reduce_add_sync(~0u, mine);
       if (lane == 0) s_sum[pass & 1][warp] = sum;
       __syncthreads();
-      const int upto = warp_inclusive((int)s_sum[pass & 1][lane], lane);
-      const unsigned reached = __ballot_sync(~0u, upto >= want) | 1u << 31;  // (the last bin never runs out)
+      const int upto = warp_inclusive(lane < kWarps ? (int)s_sum[pass & 1][lane] : 0, lane);
+      const unsigned reached = __ballot_sync(~0u, upto >= want) | 1u << (kWarps - 1);   // (the last bin never runs out)
       const int at = __ffs(reached) - 1;
-      const int above = at ? __shfl_sync(~0u, upto, at - 1) : 0;
-      const int first = kBins - 1 - at * 64;               // bins first, first - 1, ... : a lane has two
-      const int c0 = (int)all[first - 2 * lane], c1 = (int)all[first - 2 * lane - 1];
-      const int here = above + warp_inclusive(c0 + c1, lane), before = here - c0 - c1;
-      const unsigned hit = __ballot_sync(~0u, here >= want) | 1u << 31;
-      const int who = __ffs(hit) - 1;
-      const bool second = before + c0 < want;
-      const int digit = __shfl_sync(~0u, first - 2 * lane - (second ? 1 : 0), who);
-      want -= __shfl_sync(~0u, second ? before + c0 : before, who);
+      int above = at ? __shfl_sync(~0u, upto, at - 1) : 0;
+      const int first = kBins - 1 - at * 32 * kOwn - lane * kOwn;      // bins first, first - 1, ... are this lane's
+      int here = 0;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) here += (int)all[first - i];
+      const int end = above + warp_inclusive(here, lane);
+      const int who = __ffs(__ballot_sync(~0u, end >= want) | 1u << 31) - 1;
+      above = end - here;
+      int digit = first, left = want - above;              // (of the lane in question: the last of its bins never runs out either)
+      bool found = false;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) {
+        if (!found) { digit = first - i; left = want - above; }
+        above += (int)all[first - i];
+        found |= above >= want;
+      }
+      digit = __shfl_sync(~0u, digit, who);
+      want = __shfl_sync(~0u, left, who);
       key |= (uint32_t)digit << shift;
       known |= digits << shift;
-      if (blocks > 1) __syncthreads();                     // (s_all is read until here)
       if (key == 0) break;                                 // the rest are NaNs
     }
   }
@@ -178,51 +205,73 @@ mass_keep_kernel(const KeepParams p) {
   auto equals = [&](int j, uint32_t k) { return ranked(j) && !none && k == key; };
   if constexpr (kLong) {
     int kept = 0, equal = 0;                               // before this step's positions
-    for (int at = 0; at < n; at += kKeepThreads) {
+    __syncthreads();
+    for (int at = 0; at < n; at += kThreads) {
       const int j = at + tid;
       const uint32_t k = ranked(j) ? order_key(mass[j]) : 0;
       const unsigned more = __ballot_sync(~0u, larger(j, k)), same = __ballot_sync(~0u, equals(j, k)), below = (1u << lane) - 1;
       if (lane == 0) s_sum[0][warp] = (uint32_t)__popc(more) | (uint32_t)__popc(same) << 16;
       __syncthreads();
       const uint32_t upto = (uint32_t)warp_inclusive((int)s_sum[0][lane], lane), before = warp ? __shfl_sync(~0u, upto, warp - 1) : 0;
-      const uint32_t all = __shfl_sync(~0u, upto, 31);
+      const uint32_t sums = __shfl_sync(~0u, upto, 31);
       const int more_before = kept + (int)(before & 0xffffu) + __popc(more & below);
       const int same_before = equal + (int)(before >> 16) + __popc(same & below);
       if (larger(j, k) || (equals(j, k) && same_before < want)) index[more_before + min(same_before, want)] = j;
-      kept += (int)(all & 0xffffu);
-      equal += (int)(all >> 16);
+      kept += (int)(sums & 0xffffu);
+      equal += (int)(sums >> 16);
       __syncthreads();
     }
   } else {
-    uint32_t count = 0;                                    // larger keys, equal ones from bit 16 on (a block has 2^14 positions at most)
+    // larger keys, and equal ones from bit 16 on (a block has 2^14 positions at most), counted in order: part, thread, neighbour
+    uint32_t more = 0, same = 0;                           // bits of this thread's items
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) count += larger(j0 + i, keys[i]) ? 1u : equals(j0 + i, keys[i]) ? 1u << 16 : 0u;
-    const uint32_t upto = (uint32_t)warp_inclusive((int)count, lane);
+    for (int i = 0; i < kItems; ++i) {
+      more |= (uint32_t)larger(place(i), keys[i]) << i;
+      same |= (uint32_t)equals(place(i), keys[i]) << i;
+    }
+    uint32_t before[kParts];
+    __syncthreads();                                       // (the last digit's sums and bins have been read)
+#pragma unroll
+    for (int q = 0; q < kParts; ++q) {
+      const uint32_t count = (uint32_t)__popc(more >> 4 * q & 15u) | (uint32_t)__popc(same >> 4 * q & 15u) << 16;
+      const uint32_t upto = (uint32_t)warp_inclusive((int)count, lane);
+      before[q] = upto - count;
+      if (lane == 31) s_sum[q][warp] = upto;
+    }
     __syncthreads();
-    if (lane == 31) s_sum[0][warp] = upto;
-    __syncthreads();
-    const uint32_t sums = (uint32_t)warp_inclusive((int)s_sum[0][lane], lane);
-    const uint32_t before = (warp ? __shfl_sync(~0u, sums, warp - 1) : 0) + upto - count;
-    int at = (int)(before & 0xffffu), same = (int)(before >> 16);
-    if (blocks > 1) {                                      // and in the blocks before this one
-      if (tid == kKeepThreads - 1) s_total[0] = sums;
+    uint32_t total = 0;
+#pragma unroll
+    for (int q = 0; q < kParts; ++q) {
+      const uint32_t upto = (uint32_t)warp_inclusive(lane < kWarps ? (int)s_sum[q][lane] : 0, lane);
+      before[q] += total + (warp ? __shfl_sync(~0u, upto, warp - 1) : 0);
+      total += __shfl_sync(~0u, upto, kWarps - 1);
+    }
+    int kept = 0, equal = 0;                               // in the blocks before this one
+    if (blocks > 1) {
+      if (tid == 0) s_total = total;
       cluster_sync();
 #pragma unroll
       for (int r = 0; r < 8; ++r)
         if (r < rank) {
-          const uint32_t total = load_from(&s_total[0], r);
-          at += (int)(total & 0xffffu);
-          same += (int)(total >> 16);
+          const uint32_t theirs = load_from(&s_total, r);
+          kept += (int)(theirs & 0xffffu);
+          equal += (int)(theirs >> 16);
         }
       cluster_sync();                                      // (totals are read by the others until here)
     }
-    at += min(same, want);
+    const int room = max(0, want - equal);                 // equal keys of this block that stay
+    uint16_t* const list = reinterpret_cast<uint16_t*>(&s_bins[0][0]);       // positions within the block
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
-      const bool more = larger(j0 + i, keys[i]), equal = equals(j0 + i, keys[i]);
-      if (more || (equal && same < want)) index[at++] = j0 + i;
-      same += equal;
+      uint32_t& at = before[i / 4];                          // counts so far
+      const int equals_before = (int)(at >> 16);
+      const bool is_more = more >> i & 1, is_same = same >> i & 1;
+      if (is_more || (is_same && equals_before < room)) list[(int)(at & 0xffffu) + min(equals_before, room)] = (uint16_t)(place(i) - block0);
+      at += is_more ? 1u : is_same ? 1u << 16 : 0u;
     }
+    __syncthreads();
+    const int stay = (int)(total & 0xffffu) + min((int)(total >> 16), room), first = kept + min(equal, want);
+    for (int i = tid; i < stay; i += kThreads) index[first + i] = block0 + list[i];
   }
 }
 
@@ -244,16 +293,16 @@ static cudaError_t launch_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 bloc
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+// Few positions take few threads, whose barriers are short (512 positions: 256 threads of 4 items 4.6 us, of 16 items 7.5); a block
+// has up to 1024 x 16, a cluster eight times that.
 static cudaError_t launch_keep(const KeepParams& p, int B, cudaStream_t st) {
-  const dim3 block(kKeepThreads);
-  constexpr int kFew = 4, kMany = 16, kMost = 8;           // items of a thread; blocks of a cluster that every GPU takes
-  if (p.max_ctx <= kFew * kKeepThreads) return launch_pdl(mass_keep_kernel<kFew, false>, dim3(1, (unsigned)B), block, st, p);
-  int blocks = 1;
-  while (blocks < kMost && blocks * kMany * kKeepThreads < p.max_ctx) blocks *= 2;
-  if (blocks == 1) return launch_pdl(mass_keep_kernel<kMany, false>, dim3(1, (unsigned)B), block, st, p);
-  if (blocks * kMany * kKeepThreads >= p.max_ctx)
-    return launch_cluster(mass_keep_kernel<kMany, false>, dim3((unsigned)blocks, (unsigned)B), block, st, p);
-  return launch_pdl(mass_keep_kernel<1, true>, dim3(1, (unsigned)B), block, st, p);
+  constexpr int kBlock = 1024 * 16, kMost = 8;             // blocks of a cluster that every GPU takes
+  if (p.max_ctx <= 256 * 4) return launch_pdl(mass_keep_kernel<256, 4, false>, dim3(1, (unsigned)B), dim3(256), st, p);
+  if (p.max_ctx <= 1024 * 4) return launch_pdl(mass_keep_kernel<1024, 4, false>, dim3(1, (unsigned)B), dim3(1024), st, p);
+  if (p.max_ctx <= kBlock) return launch_pdl(mass_keep_kernel<1024, 16, false>, dim3(1, (unsigned)B), dim3(1024), st, p);
+  if (p.max_ctx > kMost * kBlock) return launch_pdl(mass_keep_kernel<1024, 16, true>, dim3(1, (unsigned)B), dim3(1024), st, p);
+  const unsigned blocks = p.max_ctx <= 2 * kBlock ? 2 : p.max_ctx <= 4 * kBlock ? 4 : 8;
+  return launch_cluster(mass_keep_kernel<1024, 16, false>, dim3(blocks, (unsigned)B), dim3(1024), st, p);
 }
 
 // ---- moving their rows ----------------------------------------------------------------------------------------------

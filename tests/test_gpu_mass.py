@@ -51,7 +51,7 @@ def test_mass_in_place_repeats_to_the_bit_and_ignores_what_new_positions_hold():
 
 
 @pytest.mark.parametrize("T,budget,sinks,recent", [(1, 1, 0, 0), (40, 7, 2, 3), (700, 128, 4, 32), (1500, 1499, 0, 0), (5000, 700, 64, 100),
-                                                   (5000, 100, 60, 40), (5000, 1, 0, 0), (40000, 9000, 3, 1)])
+                                                   (5000, 100, 60, 40), (5000, 1, 0, 0), (16384, 3000, 0, 7), (40000, 9000, 3, 1), (140001, 20000, 5, 100)])
 def test_keep(T, budget, sinks, recent):
     rng = np.random.default_rng(T + budget)
     kinds = [rng.standard_normal(T), np.round(rng.standard_normal(T)), np.zeros(T), rng.permutation(T) * 1e-42, np.where(rng.random(T) < .5, 0., -0.),
