@@ -20,7 +20,6 @@ struct WindowParams {
   int B, H, H_kv, group, n_q, max_ctx, window, sinks, n_splits, s_pitch;
   int page_table_stride, page_shift, n_pages, out_f32;
   int group_shift;                           // log2 of group, -1 where it is no power of two
-  int paired;                                // tile kernel: a block's two halves take turns at the tiles of the same 128 rows
   int block_rows, tile_keys, split_tiles;    // of the kernel that runs: query rows of a block, positions of a tile, see splits_used
   float scale_log2, decay;
 };
@@ -52,9 +51,9 @@ struct Seen {
   __device__ __forceinline__ int position(int tile) const { return tile < front ? tile * size : w0 + (tile - front) * size; }
 };
 
-// A block works on at least split_tiles tiles, whatever the launch has room for.  Paired blocks make two splits each.
+// A split works on at least split_tiles tiles, whatever the launch has room for.
 __device__ __forceinline__ int splits_used(const WindowParams& p, int tiles) {
-  return max(1, min(p.n_splits >> p.paired, tiles / p.split_tiles)) << p.paired;
+  return max(1, min(p.n_splits, tiles / p.split_tiles));
 }
 
 // The token of a row of a K/V head: rows are ordered by token, then head of the group.

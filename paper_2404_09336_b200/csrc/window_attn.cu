@@ -672,7 +672,7 @@ window_mass_kernel(const WindowParams p, const int mass_blocks) {
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
-struct WindowPlan { bool tiles, paired; int block_rows, keys, fewest, n_splits, s_pitch; size_t ml_bytes, acc_bytes, s_bytes, total_bytes; };
+struct WindowPlan { bool tiles; int block_rows, keys, fewest, n_splits, s_pitch; size_t ml_bytes, acc_bytes, s_bytes, total_bytes; };
 
 int32_t check_paging(const ssa_paging* pg, int32_t max_ctx) {
   if (!pg->page_table) return SSA_ERR_NULL;
@@ -693,7 +693,7 @@ static int32_t check_window(const ssa_attn_desc* d, const ssa_window* w, bool ma
 
 static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-// Whether the tiles of 256 rows serve a call.
+// Whether the tiles of 128 rows serve a call.
 static bool tiles_pay(const ssa_attn_desc* d, const ssa_window* w, bool mass) {
   return !mass && d->kv_dtype != SSA_FP8_E4M3 && (long long)(d->H / d->H_kv) * w->n_q > kFewRows &&
          (!w->paging || w->paging->page_size >= 8);          // (a box of a copy is eight rows at least)
@@ -705,16 +705,15 @@ static bool plan_window(const ssa_attn_desc* d, const ssa_window* w, bool mass, 
   const int keys = tiles ? kTileKeys : d->D * (d->kv_dtype == SSA_FP8_E4M3 ? 1 : 2) == 256 ? 16 : 32, fewest = tiles ? kTileSplit : kSplitKeys / keys;
   // rows of a block: a warp's groups of eight, or four groups of two warps each
   const int groups = (int)std::min<long long>((per_head + kGroup - 1) / kGroup, 8);
-  const int rows = tiles ? kBlockRows : kGroup * (groups <= kMostGroups ? groups : 8);
+  const int rows = tiles ? kTileRows : kGroup * (groups <= kMostGroups ? groups : 8);
   const long long group = d->H / d->H_kv, row_tiles = (per_head + rows - 1) / rows;
   const long long blocks = row_tiles * d->H_kv * d->B, tokens = (rows - 1) / group + 2;
   const long long most = w->window == 0 ? d->max_ctx : std::min<long long>(d->max_ctx, (long long)w->window + w->sinks + tokens);
   const long long n_tiles = (most + keys - 1) / keys + 2;
   pl->keys = keys;
   pl->fewest = fewest;
-  const bool paired = tiles && per_head <= kTileRows;
   const long long most_splits = std::max(1ll, std::min(n_tiles / fewest, 64ll));
-  long long splits = std::min(most_splits, std::max(1ll, sm_count() / blocks));   // tiles: a block to an SM
+  long long splits = std::min(most_splits, std::max(1ll, 2ll * sm_count() / blocks));   // tiles: two blocks to an SM
   if (!tiles) {
     // The kernel for few rows: what n splits cost in units of one tile's time.  The work of all blocks, each with a start and an
     // end, over the places that there are (two or three blocks to an SM), but no less than one block's; half a block's until the
@@ -728,8 +727,7 @@ static bool plan_window(const ssa_attn_desc* d, const ssa_window* w, bool mass, 
       if (n == 1 || cost < least) { least = cost; splits = n; }
     }
   }
-  pl->paired = paired;
-  pl->n_splits = (int)splits << (int)paired;
+  pl->n_splits = (int)splits;
   pl->block_rows = rows;
   const size_t slots = (size_t)d->B * d->H * w->n_q * pl->n_splits;
   pl->ml_bytes = up256(slots * sizeof(float2));
@@ -751,7 +749,7 @@ static size_t window_bytes(const ssa_attn_desc* d, const ssa_window* w, bool mas
 
 template <typename T, int D>
 static cudaError_t launch_tiles(const WindowParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, int box_rows, cudaStream_t st) {
-  const dim3 grid((unsigned)((p.group * p.n_q + kBlockRows - 1) / kBlockRows * (p.n_splits >> p.paired)), (unsigned)p.H_kv, (unsigned)p.B);
+  const dim3 grid((unsigned)((p.group * p.n_q + kTileRows - 1) / kTileRows * p.n_splits), (unsigned)p.H_kv, (unsigned)p.B);
   auto kernel = p.page_table ? window_tile_kernel<T, D, true> : window_tile_kernel<T, D, false>;
   constexpr int kSmem = TileShape<D>::kSmem;
   const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
@@ -828,7 +826,6 @@ static int32_t run_window(const ssa_attn_desc* d, const ssa_window* w, const voi
   if (!tiles && !plan_window(d, w, mass, false, &pl)) return SSA_ERR_SHAPE;
   WindowParams p;
   p.block_rows = pl.block_rows;
-  p.paired = pl.paired;
   p.tile_keys = pl.keys;
   p.split_tiles = pl.fewest;
   p.q = q; p.k = k; p.v = v; p.out = out; p.lse = lse;

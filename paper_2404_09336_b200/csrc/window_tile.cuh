@@ -1,24 +1,22 @@
 // Window attention of many query rows per K/V head (prompt chunks): tcgen05 tiles.  Included by window_attn.cu.
 //
-// A block serves 256 (token, head of the group) rows of one K/V head as two row tiles of 128, and goes through the tiles of 128
-// positions that they see between them.  Both contractions are tcgen05.mma in steps of 16 with fp32 accumulators:
+// A block serves 128 (token, head of the group) rows of one K/V head and goes through the tiles of 128 positions that they see
+// between them.  Both contractions are tcgen05.mma in steps of 16 with fp32 accumulators:
 //   S = Q . K^T   128 x 128; Q and K in shared memory (128-byte swizzle, K by TMA), S in TMEM
 //   O += P . V    128 x D; P, the weights as 16-bit values, in TMEM over the first half of S; V in shared memory as it lies
-// TMEM is full: an S and an O for each row tile.  Warps 0-3 and 4-7 do the softmax of one row tile each, a thread per row; warp
-// 8 issues the matrix instructions, warp 9 the copies (10 and 11 make up its group of four).  While one row tile's softmax
-// runs, the tensor cores work on the other's.  (With tiles of 64 positions and two S per row tile no softmax waited for its
-// scores' chain, but an instruction of 128 x 64 takes as long as one of 128 x 128 - the 128 rows of Q are read either way -
-// and whole prompts took 524 instead of 485 us.)
-//
-// Where a K/V head has no more than 128 rows, both row tiles are the same rows and take turns at the tiles (`paired`); each is a
-// split of its own, joined with the rest by the next launch.  Five drafted tokens of four heads each, 16 requests of up to 4096:
-// PAIRED
+// Warps 0-3 do the softmax, a thread per row; warp 4 issues the matrix instructions, warp 5 the copies (6 and 7 make up its group
+// of four).  A tile's chain - scores, softmax, sums, the next scores - takes some 3500 cycles, of which the tensor cores work
+// 1024 and the softmax 2000; two blocks share an SM (half its TMEM each, a K and a V tile in flight besides the one at work), so
+// that one's chain, start and end fill the other's gaps.  Whole prompts (4 x 4096 tokens, 32 heads, window 1024, 64 sinks):
+//   407 us, 623 TFLOP/s of visible pairs; with one block of 256 rows to an SM, its halves alternating, 446 (a block's start and
+//   end, a third of its time, stood alone); with tiles of 64 positions and two S in turn, 524 (an instruction of 128 x 64 takes as
+//   long as one of 128 x 128: the 128 rows of Q are read either way); full causal prompts 619 us, 889 TFLOP/s.
 //
 // The running maximum that weights are relative to follows the true one only where that is more than 2^8 above it, so that O
 // is rescaled in a few tiles at the start and hardly ever after that; weights are then at most 2^8 (fp16: times 2^6, which
 // the sum divides out again, because fp16 has little range below 1), rounded once to 16 bits: the two parts that the kernel
 // for few rows takes would cost a third contraction, and the rounding is that of a 16-bit output.  (Instructions, not the special
-// function unit, bound the softmax: with a quarter of the powers on the FMA units prompts took 467 instead of 437 us.)
+// function unit, bound the softmax: with a quarter of the powers on the FMA units prompts took 7 % longer.)
 #pragma once
 #include <cuda.h>
 
@@ -29,9 +27,9 @@
 
 namespace ssa {
 
-constexpr int kTileRows = 128, kBlockRows = 2 * kTileRows, kTileKeys = 128;
-constexpr int kTileThreads = 384, kTileStages = 4;
-constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;  // of a thread; 256 x 208 + 128 x 88 = 384 x 168, what the launch has
+constexpr int kTileRows = 128, kTileKeys = 128;
+constexpr int kTileThreads = 256;
+constexpr int kSoftmaxRegs = 200, kOtherRegs = 56;  // of a thread; 128 x 200 + 128 x 56 = 256 x 128, what the launch has
 constexpr int kTileSplit = 4;                       // fewest tiles worth a split of their own
 constexpr float kLazy = 8.f;                        // log2 of how far weights may exceed 1
 
@@ -39,7 +37,8 @@ template <int D>
 struct TileShape {
   static constexpr int kQHalf = kTileRows * 128, kHalf = kTileKeys * 128;   // bytes of 64 dimensions of a Q tile, of a K or V tile
   static constexpr int kQBytes = kQHalf * (D / 64), kTileBytes = kHalf * (D / 64);
-  static constexpr int kSmem = 2 * kQBytes + kTileStages * kTileBytes + 1024;   // (1024: room to align)
+  static constexpr int kStages = D == 64 ? 4 : 2;                   // K and V tiles of the ring: two blocks fit an SM
+  static constexpr int kSmem = kQBytes + kStages * kTileBytes + 1024;   // (1024: room to align)
 };
 
 // ---- PTX ------------------------------------------------------------------------------------------------------------
@@ -139,7 +138,7 @@ __device__ constexpr uint32_t tile_idesc() {
 
 // One row again in fp32, by a warp, with the infinities and NaNs of V kept to where they are seen: lane i's dimensions i D/32 ...
 template <typename T, int D, bool kPaged>
-__device__ __noinline__ void careful_row(const WindowParams& p, const Seen& seen, int2 range, int step, int b, int h, int t, int pos, float& m,
+__device__ __noinline__ void careful_row(const WindowParams& p, const Seen& seen, int2 range, int b, int h, int t, int pos, float& m,
                                          float& l, float (&acc)[D / 32]) {
   constexpr int kN = D / 32;
   const int lane = threadIdx.x % 32, hkv = h / p.group;
@@ -152,7 +151,7 @@ __device__ __noinline__ void careful_row(const WindowParams& p, const Seen& seen
   l = 0.f;
 #pragma unroll
   for (int i = 0; i < kN; ++i) { acc[i] = odd[i] = 0.f; qf[i] = to_float(q[i]); }
-  for (int it = range.x; it < range.y; it += step)
+  for (int it = range.x; it < range.y; ++it)
     for (int j = seen.position(it); j < seen.position(it) + kTileKeys; ++j) {
       if (!sees(p, pos, j)) continue;
       const int64_t row = row_of<kPaged>(p, table, j);
@@ -177,82 +176,53 @@ __device__ __noinline__ void careful_row(const WindowParams& p, const Seen& seen
   for (int i = 0; i < kN; ++i) acc[i] += odd[i];
 }
 
-// The order in which a block's copies are made and used: K of the first `ahead` tiles, then V of a tile and K of the one that many
-// tiles on, in turn, as far as there are any.
-struct Copies {
-  int n, ahead;
-  __device__ __forceinline__ int of_k(int tile) const { return tile < ahead ? tile : 2 * tile - ahead + 1; }
-  __device__ __forceinline__ int of_v(int tile) const { return min(ahead, n) + tile + min(tile, max(n - ahead, 0)); }
-  __device__ __forceinline__ bool is_v(int i, int& tile) const {
-    const int m = i - min(ahead, n), both = 2 * max(n - ahead, 0);
-    const bool v = m >= both || (m >= 0 && !(m & 1));
-    tile = m < 0 ? i : m >= both ? m - both / 2 : m / 2 + (v ? 0 : ahead);
-    return v;
-  }
-};
-
 // grid (splits x row blocks, H_kv, B), the last row blocks first: they see most.
 template <typename T, int D, bool kPaged>
-__global__ void __launch_bounds__(kTileThreads, 1)
+__global__ void __launch_bounds__(kTileThreads, 2)
 window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                    const int box_rows) {
   using Shape = TileShape<D>;
+  constexpr int kStages = Shape::kStages;
   constexpr float kShift = std::is_same<T, __half>::value ? 6.f : 0.f;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t s_bar[3 * kTileStages + 8];
+  __shared__ __align__(8) uint64_t s_bar[3 * kStages + 4];
   __shared__ uint32_t s_tmem;
-  __shared__ int64_t s_row[2][kBlockRows];                             // where a row starts in q and in out
+  __shared__ int64_t s_row[2][kTileRows];                              // where a row starts in q and in out
   __shared__ int s_dead;
   const uint32_t base = (smem_at(smem_raw) + 1023) & ~1023u;
   uint8_t* const smem = smem_raw + (base - smem_at(smem_raw));
-  const uint32_t full = smem_at(s_bar), empty = full + 8 * kTileStages, fixed = empty + 8 * kTileStages, s_full = fixed + 8 * kTileStages,
-                 p_full = s_full + 16, o_full = p_full + 32;           // s_full, o_full: [row tile]; p_full: [row tile][half]
+  const uint32_t full = smem_at(s_bar), empty = full + 8 * kStages, fixed = empty + 8 * kStages, s_full = fixed + 8 * kStages,
+                 p_full = s_full + 8, o_full = p_full + 16;            // p_full: of each half
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   grid_dependency_wait();
   grid_launch_dependents();
-  const int per_block = p.n_splits >> p.paired, block = per_block == 1 ? blockIdx.x : blockIdx.x / per_block, split = blockIdx.x - block * per_block;
-  const int row0 = ((p.group * p.n_q - 1) / kBlockRows - block) * kBlockRows, hkv = blockIdx.y, b = blockIdx.z;
+  const int block = p.n_splits == 1 ? blockIdx.x : blockIdx.x / p.n_splits, split = blockIdx.x - block * p.n_splits;
+  const int row0 = ((p.group * p.n_q - 1) / kTileRows - block) * kTileRows, hkv = blockIdx.y, b = blockIdx.z;
   uint32_t flags = 0;
   int ctx, n_new;
   window_sizes(p, b, ctx, n_new, flags);
   if (flags && p.status && split == 0 && row0 == 0 && hkv == 0 && threadIdx.x == 0) atomicOr(p.status, flags);
-  const int rows = min(kBlockRows, n_new * p.group - row0);            // rows of tokens that exist
+  const int rows = min(kTileRows, n_new * p.group - row0);            // rows of tokens that exist
   if (rows <= 0) return;
   const int first = ctx - n_new;
   const int t_lo = token_of(p, row0), t_hi = token_of(p, row0 + rows - 1), lo = first + t_lo, hi = first + t_hi;
   const Seen seen(p, kTileKeys, first, t_lo, t_hi);
   const int n_splits = splits_used(p, seen.tiles);
-  if (split >= n_splits >> p.paired) return;
-  const int2 range = split_tiles(seen.tiles, split, n_splits >> p.paired);
-  // the two row tiles: positions of their first and last rows, and which of the block's tiles they take part in
-  int tile_lo[2], tile_hi[2];
-#pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    const int at = p.paired ? row0 : row0 + x * kTileRows, a = min(at, row0 + rows), z = min(at + kTileRows, row0 + rows) - 1;
-    tile_lo[x] = first + token_of(p, a);
-    tile_hi[x] = z < a ? -1 : first + token_of(p, z);                  // (no rows, or none with a position: no tiles)
-  }
+  if (split >= n_splits) return;
+  const int2 range = split_tiles(seen.tiles, split, n_splits);
   // whether the tile has positions that no token sees: their rows of V may hold anything, and are made zero
   const int from = p.window == 0 ? 0 : max(0, lo - p.window + 1);
   auto unseen = [&](int it) {
     const int j0 = seen.position(it), jz = j0 + kTileKeys - 1;
     return jz > hi || !(j0 >= from || jz < p.sinks || from <= p.sinks);
   };
-  auto needs = [&](int x, int it) {
-    const int j0 = seen.position(it);
-    if (p.paired && ((it - range.x) & 1) != x) return false;
-    return j0 <= tile_hi[x] && (p.window == 0 || j0 < p.sinks || j0 + kTileKeys - 1 > tile_lo[x] - p.window);
-  };
-  const uint32_t kv = base + 2 * Shape::kQBytes;
+  const uint32_t kv = base + Shape::kQBytes;
   const int n_tiles = range.y - range.x, n_loads = 2 * n_tiles;
-  const Copies copies = {n_tiles, 1 + p.paired};                       // scores are one tile of each row tile ahead of sums
   volatile int* dead = &s_dead;
 
-  // ---- copies, by warp 9, into a ring of stages ----
+  // ---- copies, by warp 5: K(0), V(0), K(1), ... into a ring of stages ----
   auto load = [&](int i) {
-    int tile;
-    const bool is_v = copies.is_v(i, tile);
-    const int stage = i % kTileStages, j0 = seen.position(range.x + tile);
+    const int stage = i % kStages, j0 = seen.position(range.x + i / 2);
     if (lane == 0) mbar_expect(full + 8 * stage, Shape::kTileBytes);
     __syncwarp();
     if (lane < kTileKeys / box_rows) {
@@ -268,17 +238,16 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
       const uint32_t to = kv + stage * Shape::kTileBytes + lane * box_rows * 128;
 #pragma unroll
       for (int x = 0; x < D / 64; ++x)
-        tma_load(to + x * Shape::kHalf, is_v ? &v_map : &k_map, x * 64, row, hkv, batch, full + 8 * stage);
+        tma_load(to + x * Shape::kHalf, i & 1 ? &v_map : &k_map, x * 64, row, hkv, batch, full + 8 * stage);
     }
   };
-  // Rows of V that no token sees become zero.  A copy's turn comes two copies after its own, so that others are on their way.
-  int settled = 0;
+  // Rows of V that no token sees become zero.  A copy's turn comes after the next one has been asked for (which needs no more of V).
+  int settled = 1;
   auto settle = [&](int upto) {
-    for (; settled <= upto; ++settled) {
-      int tile;
-      if (!copies.is_v(settled, tile) || !unseen(range.x + tile)) continue;
-      const int stage = settled % kTileStages, j0 = seen.position(range.x + tile);
-      mbar_wait(full + 8 * stage, (settled / kTileStages) & 1, dead);
+    for (; settled <= upto; settled += 2) {
+      if (!unseen(range.x + settled / 2)) continue;
+      const int stage = settled % kStages, j0 = seen.position(range.x + settled / 2);
+      mbar_wait(full + 8 * stage, (settled / kStages) & 1, dead);
       for (int r = lane / 8; r < kTileKeys; r += 4) {
         const int j = j0 + r;
         if (j <= hi && (j >= from || j < p.sinks)) continue;
@@ -291,26 +260,27 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
       mbar_arrive(fixed + 8 * stage);
     }
   };
-  if (warp == 9) {
+  if (warp == 5) {
     if (lane == 0) {
-      for (int i = 0; i < kTileStages; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); mbar_init(fixed + 8 * i, 32); }
-      for (int x = 0; x < 2; ++x) { mbar_init(s_full + 8 * x, 1); mbar_init(o_full + 8 * x, 1); }
-      for (int x = 0; x < 4; ++x) mbar_init(p_full + 8 * x, kTileRows);
+      for (int i = 0; i < kStages; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); mbar_init(fixed + 8 * i, 32); }
+      mbar_init(s_full, 1);
+      mbar_init(o_full, 1);
+      for (int half = 0; half < 2; ++half) mbar_init(p_full + 8 * half, kTileRows);
       s_dead = 0;
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
-    for (int i = 0; i < min(kTileStages, n_loads); ++i) load(i);
+    for (int i = 0; i < min(kStages, n_loads); ++i) load(i);
   }
-  if (warp == 8) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&s_tmem)), "n"(512) : "memory");
+  if (warp == 4) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&s_tmem)), "n"(256) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
-  if (warp < 8) {                                                      // queries: a warp's 32 rows, D / 8 lanes to a row, swizzled
+  if (warp < 4) {                                                      // queries: a warp's 32 rows, D / 8 lanes to a row, swizzled
     constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
     const int i = lane % kLanes;
     {
-      const int row = row0 + (int)(p.paired ? threadIdx.x % kTileRows : threadIdx.x), t = token_of(p, row), h = hkv * p.group + row - t * p.group;
+      const int row = row0 + (int)threadIdx.x, t = token_of(p, row), h = hkv * p.group + row - t * p.group;
       s_row[0][threadIdx.x] = (int64_t)b * p.q_sb + (int64_t)h * p.q_sh + (int64_t)t * p.q_st;
       s_row[1][threadIdx.x] = (int64_t)b * p.o_sb + (int64_t)h * p.o_sh + (int64_t)t * p.o_st;
     }
@@ -320,13 +290,12 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
     for (int y = 0; y < 32 / kAtOnce; ++y) {
       const int r = warp * 32 + y * kAtOnce + lane / kLanes;
       w[y] = make_uint4(0, 0, 0, 0);
-      if ((p.paired ? r % kTileRows : r) < rows) w[y] = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.q) + s_row[0][r] + i * 8);
+      if (r < rows) w[y] = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.q) + s_row[0][r] + i * 8);
     }
 #pragma unroll
     for (int y = 0; y < 32 / kAtOnce; ++y) {
       const int r = warp * 32 + y * kAtOnce + lane / kLanes;
-      *reinterpret_cast<uint4*>(smem + r / kTileRows * Shape::kQBytes + i / 8 * Shape::kQHalf + r % kTileRows * 128 +
-                                ((i % 8) ^ (r & 7)) * 16) = w[y];
+      *reinterpret_cast<uint4*>(smem + i / 8 * Shape::kQHalf + r * 128 + ((i % 8) ^ (r & 7)) * 16) = w[y];
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -335,98 +304,75 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
   tc_after();
   const uint32_t tmem = s_tmem;
 
-  if (warp == 9) {
+  if (warp == 5) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    settle(min(kTileStages, n_loads) - 3);
-    for (int i = kTileStages; i < n_loads; ++i) {
-      mbar_wait(empty + 8 * (i % kTileStages), (i / kTileStages - 1) & 1, dead);
+    settle(min(kStages, n_loads) - 2);
+    for (int i = kStages; i < n_loads; ++i) {
+      mbar_wait(empty + 8 * (i % kStages), (i / kStages - 1) & 1, dead);
       load(i);
-      settle(i - 2);
+      settle(i - 1);
     }
     settle(n_loads - 1);
-  } else if (warp == 8) {
+  } else if (warp == 4) {
     // ---- matrix instructions: the whole warp goes through this, so that addresses stay in uniform registers; one lane issues ----
     constexpr uint32_t kIdS = tile_idesc<T, kTileKeys, false>(), kIdO = tile_idesc<T, D, true>();
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     const bool leader = elect_one();
-    int last[2] = {-1, -1};                                  // the last tile of each row tile
-    for (int x = 0; x < 2; ++x)
-      for (int tile = n_tiles - 1; tile >= 0 && last[x] < 0; --tile)
-        if (needs(x, range.x + tile)) last[x] = tile;
-    uint32_t begun = 0, phases = 0, fixes = 0;               // bits: row tiles that have a sum; phases of p_full, of `fixed`
+    uint32_t fixes = 0;                                      // phases of `fixed`
     const uint64_t q_desc = tile_desc(base, 16), k_desc = tile_desc(kv, 16), v_desc = tile_desc(kv, Shape::kHalf);
-    auto wait_full = [&](int i) { mbar_wait(full + 8 * (i % kTileStages), (i / kTileStages) & 1, dead); };
-    auto scores = [&](int x, int stage) {
-      const uint64_t qd = q_desc + x * (Shape::kQBytes >> 4), kd = k_desc + stage * (Shape::kTileBytes >> 4);
-      const uint32_t to = tmem + x * 128;
+    auto wait_full = [&](int i) { mbar_wait(full + 8 * (i % kStages), (i / kStages) & 1, dead); };
+    auto scores = [&](int tile) {
+      const int stage = 2 * tile % kStages;
+      wait_full(2 * tile);
+      tc_after();
+      const uint64_t kd = k_desc + stage * (Shape::kTileBytes >> 4);
       if (leader) {
 #pragma unroll
         for (int s = 0; s < D / 16; ++s)
-          mma_ss(to, qd + (s / 4 * (Shape::kQHalf >> 4) + s % 4 * 2), kd + (s / 4 * (Shape::kHalf >> 4) + s % 4 * 2), kIdS, s > 0);
-        tc_commit(s_full + 8 * x);
+          mma_ss(tmem, q_desc + (s / 4 * (Shape::kQHalf >> 4) + s % 4 * 2), kd + (s / 4 * (Shape::kHalf >> 4) + s % 4 * 2), kIdS, s > 0);
+        tc_commit(s_full);
+        tc_commit(empty + 8 * stage);
       }
       __syncwarp();
     };
-    for (int tile = 0; tile < min(copies.ahead, n_tiles); ++tile) {
-      wait_full(tile);
-      tc_after();
-      for (int x = 0; x < 2; ++x)
-        if (needs(x, range.x + tile)) scores(x, tile);
-      if (leader) tc_commit(empty + 8 * tile);
-      __syncwarp();
-    }
+    if (n_tiles > 0) scores(0);
     for (int tile = 0; tile < n_tiles; ++tile) {
-      const int i = copies.of_v(tile), next = copies.of_k(tile + copies.ahead), stage = i % kTileStages, k_stage = next % kTileStages;
-      const bool more = tile + copies.ahead < n_tiles;
+      const int i = 2 * tile + 1, stage = i % kStages;
       wait_full(i);
       if (unseen(range.x + tile)) {
         mbar_wait(fixed + 8 * stage, fixes >> stage & 1, dead);
         fixes ^= 1u << stage;
       }
-      if (more) wait_full(next);
-      tc_after();
       const uint64_t vd = v_desc + stage * (Shape::kTileBytes >> 4);
-      for (int x = 0; x < 2; ++x) {
-        if (needs(x, range.x + tile)) {
-          const uint32_t to = tmem + 256 + x * 128, weights = tmem + x * 128;
-          const bool add = begun >> x & 1;
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {             // the weights come in two halves
-            mbar_wait(p_full + 16 * x + 8 * half, phases >> x & 1, dead);
-            tc_after();
-            if (leader) {
+      for (int half = 0; half < 2; ++half) {                 // the weights come in two halves
+        mbar_wait(p_full + 8 * half, tile & 1, dead);
+        tc_after();
+        if (leader) {
 #pragma unroll
-              for (int s = 4 * half; s < 4 * half + 4; ++s) mma_ts(to, weights + s * 8, vd + s * (2048 >> 4), kIdO, add || s > 0);
-            }
-            __syncwarp();
+          for (int s = 4 * half; s < 4 * half + 4; ++s) mma_ts(tmem + 128, tmem + s * 8, vd + s * (2048 >> 4), kIdO, tile > 0 || s > 0);
+          if (half) {
+            tc_commit(empty + 8 * stage);
+            if (tile + 1 == n_tiles) tc_commit(o_full);
           }
-          phases ^= 1u << x;
-          begun |= 1u << x;
-          if (leader && tile == last[x]) tc_commit(o_full + 8 * x);
-          __syncwarp();
         }
-        if (more && needs(x, range.x + tile + copies.ahead)) scores(x, k_stage);   // over weights that the contraction just issued takes
+        __syncwarp();
       }
-      if (leader) {
-        tc_commit(empty + 8 * stage);
-        if (more) tc_commit(empty + 8 * k_stage);
-      }
-      __syncwarp();
+      if (tile + 1 < n_tiles) scores(tile + 1);              // over weights that the contraction just issued takes
     }
-  } else if (warp < 8) {
+  } else if (warp < 4) {
     // ---- softmax: a thread per row ----
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-    const int x = warp / 4, mine = p.paired ? threadIdx.x % kTileRows : threadIdx.x, row = row0 + mine;
-    const bool there = mine < rows;
+    const int row = row0 + (int)threadIdx.x;
+    const bool there = (int)threadIdx.x < rows;
     const int t = token_of(p, row), h = hkv * p.group + row - t * p.group, pos = there ? first + t : -1;
-    const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16, s_at = tmem + x * 128 + lanes, o_at = s_at + 256;
-    const int all_lo = p.window == 0 ? 0 : tile_hi[x] - p.window + 1;  // every row of the tile sees [all_lo, tile_lo]
+    const uint32_t s_at = tmem + ((uint32_t)(warp * 32) << 16), o_at = s_at + 128;
+    const int all_lo = p.window == 0 ? 0 : hi - p.window + 1;          // every row sees [all_lo, lo]
     const int window_lo = p.window == 0 ? 0 : pos - p.window + 1;
     const int32_t* table = kPaged ? p.page_table + (int64_t)b * p.page_table_stride : nullptr;
     float m = neg_inf(), l = 0.f;
     int n = 0;                                               // tiles so far
     for (int it = range.x; it < range.y; ++it) {
-      if (!needs(x, it)) continue;
       const int j0 = seen.position(it);
       unsigned have = ~0u;                                   // positions 4 i ... 4 i + 3 have a page
       if constexpr (kPaged) {
@@ -437,13 +383,13 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
         have = __ballot_sync(~0u, !gone);
         if (gone) flags |= SSA_DEV_BAD_INDEX;
       }
-      mbar_wait(s_full + 8 * x, n & 1, dead);
+      mbar_wait(s_full, n & 1, dead);
       tc_after();
       uint32_t s[4][32];
 #pragma unroll
       for (int c = 0; c < 4; ++c) tc_ld32(s[c], s_at + c * 32);
       tc_wait_ld();
-      const bool whole = have == ~0u && j0 + kTileKeys - 1 <= tile_lo[x] && (j0 >= all_lo || j0 + kTileKeys <= p.sinks);
+      const bool whole = have == ~0u && j0 + kTileKeys - 1 <= lo && (j0 >= all_lo || j0 + kTileKeys <= p.sinks);
       if (!whole) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -502,23 +448,23 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
         tc_st32(s_at + half * 32, w);
         tc_wait_st();
         tc_before();
-        mbar_arrive(p_full + 16 * x + 8 * half);             // its contraction starts meanwhile
+        mbar_arrive(p_full + 8 * half);             // its contraction starts meanwhile
       }
       l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       ++n;
     }
-    if (n > 0) mbar_wait(o_full + 8 * x, 0, dead);
+    if (n > 0) mbar_wait(o_full, 0, dead);
     tc_after();
 
     // ---- the row: out, or a split's part of it ----
-    const int64_t at = ((int64_t)b * p.H + h) * p.n_q + t, slot = at * p.n_splits + (p.paired ? 2 * split + x : split);
+    const int64_t at = ((int64_t)b * p.H + h) * p.n_q + t, slot = at * p.n_splits + split;
     const bool finished = n_splits == 1;
     const float scale = finished ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
     float2 test = make_float2(l * 0.f, 0.f);
     float* out32 = finished ? reinterpret_cast<float*>(p.out) + s_row[1][threadIdx.x] : p.ws_acc + slot * D;
     const bool staged = finished && !p.out_f32;              // 16-bit rows go through the queries' place, to be stored whole
-    const int rw = warp % 4 * 32 + lane;
-    uint8_t* stage = smem + x * Shape::kQBytes;
+    const int rw = threadIdx.x;
+    uint8_t* stage = smem;
 #pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {
       uint32_t o[32];
@@ -551,12 +497,12 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
       uint4 w[32 / kAtOnce];
 #pragma unroll
       for (int y = 0; y < 32 / kAtOnce; ++y) {
-        const int yr = warp % 4 * 32 + y * kAtOnce + lane / kLanes;
+        const int yr = warp * 32 + y * kAtOnce + lane / kLanes;
         w[y] = *reinterpret_cast<const uint4*>(stage + i / 8 * Shape::kQHalf + yr * 128 + ((i % 8) ^ (yr & 7)) * 16);
       }
 #pragma unroll
       for (int y = 0; y < 32 / kAtOnce; ++y) {
-        const int yr = x * kTileRows + warp % 4 * 32 + y * kAtOnce + lane / kLanes;
+        const int yr = warp * 32 + y * kAtOnce + lane / kLanes;
         if (yr < rows) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.out) + s_row[1][yr] + i * 8) = w[y];
       }
     }
@@ -573,9 +519,9 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
       const int i = __ffs(again) - 1;
       again &= again - 1;
       const int rt = __shfl_sync(~0u, t, i), rh = __shfl_sync(~0u, h, i), rpos = __shfl_sync(~0u, pos, i);
-      const int64_t rat = ((int64_t)b * p.H + rh) * p.n_q + rt, rslot = rat * p.n_splits + (p.paired ? 2 * split + x : split);
+      const int64_t rat = ((int64_t)b * p.H + rh) * p.n_q + rt, rslot = rat * p.n_splits + split;
       float rm, rl, acc[D / 32];
-      careful_row<T, D, kPaged>(p, seen, make_int2(range.x + p.paired * x, range.y), 1 + p.paired, b, rh, rt, rpos, rm, rl, acc);
+      careful_row<T, D, kPaged>(p, seen, range, b, rh, rt, rpos, rm, rl, acc);
       __syncwarp();
 #pragma unroll
       for (int d = 0; d < D / 32; ++d) {
@@ -594,7 +540,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
   tc_before();
   __syncthreads();
   tc_after();
-  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512));
+  if (warp == 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(256));
   if (threadIdx.x == 0 && s_dead && p.status) atomicOr(p.status, SSA_DEV_GAVE_UP);
 }
 
