@@ -463,7 +463,7 @@ int32_t ssa_decode_attn_blockmask(const ssa_attn_desc* desc, const void* q, cons
  *   desc     host; max_ctx rows of cache per request.  All its types: F16,
  *            BF16, FP8_E4M3; H_kv dividing H
  *   window   host; n_q >= 1 query rows are laid out per head and request,
- *            H*n_q <= 2^24
+ *            H*n_q <= 2^24; desc->max_ctx <= 2^30
  *   q_lens   dev int32 [B], 0 <= q_lens[b] <= n_q, or NULL: n_q tokens each.
  *            Larger values and ctx_lens[b] > max_ctx are clamped
  *            (SSA_DEV_BAD_COUNT)
@@ -472,9 +472,14 @@ int32_t ssa_decode_attn_blockmask(const ssa_attn_desc* desc, const void* q, cons
  *            [0, n_pages) are skipped (SSA_DEV_BAD_INDEX) where a token sees
  *            them, and table entries of positions that none sees are not used
  *   workspace  dev, 16-byte aligned, >= ssa_attn_window_workspace_bytes(desc,
- *            window) (0: invalid arguments); needs no initialisation
- * Few rows per K/V head (tokens x grouped heads) split a long context over the
- * GPU and join the parts in a second launch.
+ *            window) (0: invalid arguments); needs no initialisation.  Calls
+ *            that may run at the same time (other streams, graphs) need one each
+ * Up to 24 rows per K/V head (tokens x grouped heads) keep their softmax weights
+ * to 16 bits (bf16) or 22; more rows over a 16-bit cache, and with pages of eight
+ * rows at least, go to tensor-core tiles that round each weight to the cache's
+ * type once (a relative 2^-8 of bf16, 2^-11 of fp16: as much as an output of
+ * that type is rounded; scores, maxima, sums and lse are fp32).  A long context
+ * of few rows is split over the GPU and joined in a second launch.
  * Errors: SSA_ERR_NULL, SSA_ERR_SHAPE, SSA_ERR_DTYPE, SSA_ERR_ALIGN,
  * SSA_ERR_WORKSPACE, SSA_ERR_UNSUPPORTED, SSA_ERR_CUDA.
  */
@@ -523,7 +528,7 @@ int32_t ssa_attn_mass(const ssa_attn_desc* desc, const ssa_window* window, const
  * largest mass, of equal ones the lowest positions (-0 equals 0; NaN ranks
  * below everything).  index[b*index_stride ..] ascends as ssa_spans_to_index
  * writes it, counts[b] = min(n, budget); entries past it are left untouched.
- *   mass       dev float, rows of max_ctx entries mass_stride apart
+ *   mass       dev float, rows of max_ctx (<= 2^30) entries mass_stride apart
  *   ctx_lens   dev int32 [B]; above max_ctx: clamped (SSA_DEV_BAD_COUNT)
  *   index      dev int32 [B * index_stride]; counts dev int32 [B] (written)
  * Errors: SSA_ERR_NULL, SSA_ERR_SHAPE (B, max_ctx, index_stride, mass_stride <
@@ -550,7 +555,9 @@ int32_t ssa_mass_to_index(const float* mass, int64_t mass_stride, const int32_t*
  * pages that hold such rows only; other pages must belong to one request.
  * A row whose page, or whose new row's page, does not exist is not moved
  * (SSA_DEV_BAD_INDEX).
- *   desc   host; the fields of q and out are checked but not used
+ *   desc   host; the fields of q and out are checked but not used.  K and V in
+ *          the same place, and strides of zero between rows, heads or requests,
+ *          are refused (SSA_ERR_UNSUPPORTED); max_ctx <= 2^30
  * Errors: SSA_ERR_NULL, SSA_ERR_SHAPE, SSA_ERR_DTYPE, SSA_ERR_ALIGN,
  * SSA_ERR_CAPACITY, SSA_ERR_UNSUPPORTED, SSA_ERR_CUDA.
  */

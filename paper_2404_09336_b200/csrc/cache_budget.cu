@@ -413,7 +413,7 @@ int32_t ssa_mass_to_index(const float* mass, int64_t mass_stride, const int32_t*
                           int32_t budget, int32_t sinks, int32_t recent, int32_t* index, int32_t index_stride,
                           int32_t* counts, uint32_t* dev_status, void* stream) {
   if (!mass || !ctx_lens || !index || !counts) return SSA_ERR_NULL;
-  if (B <= 0 || B > 65535 || max_ctx <= 0 || index_stride <= 0 || mass_stride < max_ctx) return SSA_ERR_SHAPE;
+  if (B <= 0 || B > 65535 || max_ctx <= 0 || max_ctx > ssa::kMostContext || index_stride <= 0 || mass_stride < max_ctx) return SSA_ERR_SHAPE;
   if (budget <= 0 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget || budget > index_stride) return SSA_ERR_CAPACITY;
   const ssa::KeepParams p = {mass, ctx_lens, index, counts, dev_status, mass_stride, max_ctx, budget, sinks, recent, index_stride};
   if (ssa::launch_keep(p, B, (cudaStream_t)stream) != cudaSuccess) return SSA_ERR_CUDA;
@@ -428,7 +428,12 @@ int32_t ssa_cache_compact(const ssa_attn_desc* desc, const ssa_paging* paging, v
   int32_t rc = ssa::check_desc(desc);
   if (rc == SSA_OK && paging) rc = ssa::check_paging(paging, desc->max_ctx);
   if (rc != SSA_OK) return rc;
-  if (mass && mass_stride < desc->max_ctx) return SSA_ERR_SHAPE;
+  if (desc->max_ctx > ssa::kMostContext || (mass && mass_stride < desc->max_ctx)) return SSA_ERR_SHAPE;
+  // rows that several heads or requests share, or that K and V do, would be moved more than once
+  if (k_cache == v_cache || desc->k_stride_t == 0 || desc->v_stride_t == 0 ||
+      (desc->H_kv > 1 && (desc->k_stride_h == 0 || desc->v_stride_h == 0)) ||
+      (desc->B > 1 && !paging && (desc->k_stride_b == 0 || desc->v_stride_b == 0)))
+    return SSA_ERR_UNSUPPORTED;
   if (index_stride <= 0 || max_selected <= 0 || max_selected > index_stride) return SSA_ERR_CAPACITY;
   if (!ssa::aligned16(k_cache) || !ssa::aligned16(v_cache)) return SSA_ERR_ALIGN;
   const int E = desc->kv_dtype == SSA_FP8_E4M3 ? 1 : 2;

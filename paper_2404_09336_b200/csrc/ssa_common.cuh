@@ -17,6 +17,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 void note_launches(int n);
 void take_kernel_events(cudaEvent_t* begin, cudaEvent_t* end);
 int32_t check_desc(const ssa_attn_desc* d);   // status of a descriptor (defined in decode_attn.cu)
+constexpr int32_t kMostContext = 1 << 30;   // positions of the calls around a budget: sums with a tile's size stay below 2^31
 int32_t check_paging(const ssa_paging* pg, int32_t max_ctx);   // status of a paged cache (defined in window_attn.cu)
 int sm_count();   // multiprocessors of the current device (cached; no synchronisation)
 // Bytes from p to the end of the allocation it lies in, as far as that is device memory mapped as a whole; else 0.  Reading

@@ -685,7 +685,7 @@ int32_t check_paging(const ssa_paging* pg, int32_t max_ctx) {
 static int32_t check_window(const ssa_attn_desc* d, const ssa_window* w, bool mass) {
   const int32_t rc = check_desc(d);
   if (rc != SSA_OK) return rc;
-  if (w->n_q <= 0 || w->window < 0 || w->sinks < 0 || w->q_stride_t < 0 || w->o_stride_t < 0) return SSA_ERR_SHAPE;
+  if (d->max_ctx > kMostContext || w->n_q <= 0 || w->window < 0 || w->sinks < 0 || w->q_stride_t < 0 || w->o_stride_t < 0) return SSA_ERR_SHAPE;
   if (w->q_stride_t % 8 != 0 || w->o_stride_t % 8 != 0) return SSA_ERR_ALIGN;
   if ((long long)d->H * w->n_q > (mass ? (long long)SSA_MASS_MAX_ROWS : 1ll << 24)) return SSA_ERR_SHAPE;
   return w->paging ? check_paging(w->paging, d->max_ctx) : SSA_OK;

@@ -420,6 +420,8 @@ def decode_attn_dense_paged(desc, q, k_pool, v_pool, paging, ctx_lens, out, lse=
 def make_window(q, out, window: int = 0, sinks: int = 0, q_lens=None, paging: Paging | None = None) -> Window:
     """ssa_window for q[B,H,n_q,D], out[B,H,n_q,D] (any strides; the descriptor is made from q[:, :, 0], out[:, :, 0]).  q_lens
     (int32 [B], device) must stay alive."""
+    if q_lens is not None and q_lens.dtype != torch.int32:
+        raise ValueError("q_lens must be int32")
     w = Window()
     w.n_q, w.window, w.sinks = int(q.shape[2]), int(window), int(sinks)
     w.q_stride_t, w.o_stride_t = int(q.stride(2)), int(out.stride(2))
@@ -427,6 +429,12 @@ def make_window(q, out, window: int = 0, sinks: int = 0, q_lens=None, paging: Pa
     if paging is not None:
         w.paging = C.pointer(paging)
     return w
+
+
+def _check_mass(mass, width):
+    """mass[B, width or more], fp32, entries side by side."""
+    if mass.dtype != torch.float32 or mass.stride(-1) != 1 or mass.shape[-1] < width:
+        raise ValueError(f"sums are rows of {width} fp32 values")
 
 
 def attn_window_workspace_bytes(desc: AttnDesc, window: Window) -> int:
@@ -448,8 +456,11 @@ def attn_mass(desc, window, q, k_cache, v_cache, ctx_lens, out, lse, mass_in, ma
               dev_status=None, stream=None, check=True):
     """ssa_attn_mass: attn_window, and mass_out[B, max_ctx] = decay * mass_in + the weight of every position (mass_in: a tensor
     of mass_out's strides, mass_out itself, or None)."""
-    if mass_in is not None and _row_stride(mass_in) != _row_stride(mass_out):
-        raise ValueError("mass_in and mass_out must have the same row stride")
+    _check_mass(mass_out, desc.max_ctx)
+    if mass_in is not None and mass_in is not mass_out:
+        _check_mass(mass_in, desc.max_ctx)
+        if _row_stride(mass_in) != _row_stride(mass_out):
+            raise ValueError("mass_in and mass_out must have the same row stride")
     rc = _call.attn_mass(desc, window, q, k_cache, v_cache, ctx_lens, out, lse, mass_in, mass_out, decay, workspace,
                          dev_status, _stream(stream))
     return _check("ssa_attn_mass", rc, check)
@@ -457,6 +468,7 @@ def attn_mass(desc, window, q, k_cache, v_cache, ctx_lens, out, lse, mass_in, ma
 
 def mass_to_index(mass, ctx_lens, budget, sinks, recent, index, counts, dev_status=None, stream=None, check=True):
     """ssa_mass_to_index: the positions of mass[B, max_ctx] that the budget keeps -> index[B, index_stride], counts[B]."""
+    _check_mass(mass, 1)
     rc = _call.mass_to_index(mass, ctx_lens, mass.shape[1], budget, sinks, recent, index, counts, dev_status, _stream(stream))
     return _check("ssa_mass_to_index", rc, check)
 
@@ -464,6 +476,8 @@ def mass_to_index(mass, ctx_lens, budget, sinks, recent, index, counts, dev_stat
 def cache_compact(desc, k_cache, v_cache, ctx_lens, index, counts, max_selected, mass=None, paging=None, dev_status=None,
                   stream=None, check=True):
     """ssa_cache_compact: listed rows of K and V (and entries of mass[B, max_ctx]) to the front, in place."""
+    if mass is not None:
+        _check_mass(mass, desc.max_ctx)
     rc = _call.cache_compact(desc, paging, k_cache, v_cache, ctx_lens, index, counts, max_selected, mass, dev_status,
                              _stream(stream))
     return _check("ssa_cache_compact", rc, check)

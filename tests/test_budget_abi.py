@@ -56,7 +56,8 @@ def test_attention_refuses_bad_arguments_before_launching():
             assert call(d, w) == err, field
             assert ssa.attn_window_workspace_bytes(d, w) == 0 and ssa.attn_mass_workspace_bytes(d, w) == 0
         for field, val, err in [("D", 96, ssa.ERR_UNSUPPORTED), ("H_kv", 3, ssa.ERR_UNSUPPORTED), ("kv_dtype", ssa.F32, ssa.ERR_DTYPE),
-                                ("out_dtype", ssa.F16, ssa.ERR_DTYPE), ("k_stride_t", 132, ssa.ERR_ALIGN), ("B", 0, ssa.ERR_SHAPE)]:
+                                ("out_dtype", ssa.F16, ssa.ERR_DTYPE), ("k_stride_t", 132, ssa.ERR_ALIGN), ("B", 0, ssa.ERR_SHAPE),
+                                ("max_ctx", (1 << 30) + 1, ssa.ERR_SHAPE)]:
             d, w = good()
             setattr(d, field, val)
             assert call(d, w) == err, field
@@ -84,7 +85,8 @@ def test_selection_refuses_bad_arguments():
     before = ssa.launch_count()
     for k in ("mass", "ctx", "index", "counts"):
         assert call(**{k: NUL}) == ssa.ERR_NULL
-    for k in (dict(B=0), dict(B=65536), dict(max_ctx=0), dict(index_stride=0), dict(mass_stride=511)):
+    for k in (dict(B=0), dict(B=65536), dict(max_ctx=0), dict(index_stride=0), dict(mass_stride=511),
+              dict(max_ctx=(1 << 30) + 1, mass_stride=1 << 31)):
         assert call(**k) == ssa.ERR_SHAPE
     for k in (dict(budget=0), dict(budget=65), dict(sinks=-1), dict(recent=-1), dict(sinks=33), dict(sinks=2**31 - 1, recent=2**31 - 1)):
         assert call(**k) == ssa.ERR_CAPACITY
@@ -96,7 +98,7 @@ def test_compaction_refuses_bad_arguments():
     before = ssa.launch_count()
 
     def call(d=None, pg=None, **k):
-        a = {**dict(k=P, v=P, ctx=P, index=P, index_stride=64, counts=P, max_selected=64, mass=P, mass_stride=512), **k}
+        a = {**dict(k=P, v=C.c_void_p(0x2000), ctx=P, index=P, index_stride=64, counts=P, max_selected=64, mass=P, mass_stride=512), **k}
         return f(C.byref(d or good()[0]), pg, *a.values(), NUL, NUL)
 
     assert f(None, None, P, P, P, P, 64, P, 64, P, 512, NUL, NUL) == ssa.ERR_NULL
@@ -105,9 +107,13 @@ def test_compaction_refuses_bad_arguments():
     assert call(mass_stride=511) == ssa.ERR_SHAPE
     assert call(max_selected=65) == call(max_selected=0) == call(index_stride=0) == ssa.ERR_CAPACITY
     assert call(k=C.c_void_p(0x1008)) == call(v=C.c_void_p(0x1001)) == ssa.ERR_ALIGN
+    assert call(v=P) == ssa.ERR_UNSUPPORTED                  # K and V in one place
+    for field, val, err in (("D", 32, ssa.ERR_UNSUPPORTED), ("k_stride_t", 0, ssa.ERR_UNSUPPORTED), ("v_stride_h", 0, ssa.ERR_UNSUPPORTED),
+                            ("k_stride_b", 0, ssa.ERR_UNSUPPORTED), ("max_ctx", (1 << 30) + 1, ssa.ERR_SHAPE)):
+        d, w = good()
+        setattr(d, field, val)
+        assert call(d) == err, field
     d, w = good()
-    d.D = 32
-    assert call(d) == ssa.ERR_UNSUPPORTED
     assert call(pg=paged(w, size=3).paging) == ssa.ERR_SHAPE and call(pg=paged(w, table=0).paging) == ssa.ERR_NULL
     assert ssa.launch_count() == before
 
@@ -115,17 +121,28 @@ def test_compaction_refuses_bad_arguments():
 def test_errors_raise_through_the_binding():
     d, w = good()
     i = torch.zeros(2, 64, dtype=torch.int32)
-    for f, args in ((ssa.attn_window, (d, w, None, None, None, None, None)), (ssa.attn_mass, (d, w, None, None, None, None, None, None, None, i)),
+    sums = torch.zeros(2, 512)
+    for f, args in ((ssa.attn_window, (d, w, None, None, None, None, None)), (ssa.attn_mass, (d, w, None, None, None, None, None, None, None, sums)),
                     (ssa.mass_to_index, (torch.zeros(2, 9), i[:, 0], 65, 0, 0, i, i[:, 0])), (ssa.cache_compact, (d, None, None, None, i, None, 5))):
         with pytest.raises(ssa.SsaError, match=f.__name__):
             f(*args, stream=0)
         assert f(*args, stream=0, check=False) != ssa.OK
     with pytest.raises(ValueError, match="row stride"):
-        ssa.attn_mass(d, w, None, None, None, None, None, None, i, torch.zeros(2, 65), stream=0)
+        ssa.attn_mass(d, w, None, None, None, None, None, None, sums, torch.zeros(2, 513), stream=0)
+    for bad in (i, sums[:, :511], sums.double(), torch.zeros(512, 2).t()):
+        with pytest.raises(ValueError, match="fp32"):
+            ssa.attn_mass(d, w, None, None, None, None, None, None, None, bad, stream=0)
+        with pytest.raises(ValueError, match="fp32"):
+            ssa.cache_compact(d, None, None, None, i, None, 5, mass=bad, stream=0)
+    with pytest.raises(ValueError, match="fp32"):
+        ssa.mass_to_index(i, i[:, 0], 5, 0, 0, i, i[:, 0], stream=0)
+    q = torch.zeros(2, 8, 4, 128)
+    with pytest.raises(ValueError, match="int32"):
+        ssa.make_window(q, q, q_lens=torch.zeros(2, dtype=torch.int64))
     with pytest.raises(TypeError, match="ssa_window"):
         ssa.attn_window(d, d, None, None, None, None, None, stream=0)
     with pytest.raises(TypeError):
-        ssa.attn_mass(d, w, None, None, None, None, None, None, None, i, "much", stream=0)
+        ssa.attn_mass(d, w, None, None, None, None, None, None, None, sums, "much", stream=0)
 
 
 def test_struct_layout_matches_the_header(tmp_path):

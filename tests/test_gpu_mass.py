@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("dtype,H,H_kv,D,n_q,page", [("bf16", 4, 4, 128, 1, 0), ("f16", 8, 2, 64, 3, 0), ("fp8", 4, 1, 128, 2, 0),
-                                                     ("bf16", 8, 2, 128, 17, 0), ("f16", 32, 8, 128, 1, 16), ("bf16", 4, 2, 128, 5, 2)])
+                                                     ("bf16", 8, 2, 128, 17, 0), ("f16", 32, 8, 128, 1, 16), ("bf16", 4, 2, 128, 5, 2), ("fp8", 8, 2, 64, 6, 0), ("f16", 16, 1, 128, 2, 8)])
 def test_mass(dtype, H, H_kv, D, n_q, page):
     p = Tokens(3, H, H_kv, 700, D, n_q, dtype, page=page)
     old = torch.rand(3, 700, generator=torch.Generator().manual_seed(1)) * 3
@@ -195,3 +195,39 @@ def test_a_run_of_steps_within_a_budget(page):
     dense(desc, one, k, v, *([paging] if page else []), counts, out, None, ws)
     torch.cuda.synchronize()
     assert (out - by_list).abs().max() < 1e-5 and torch.equal(mass[:, :budget], old.gather(1, index.long()))
+
+
+def test_a_captured_step_replayed_on_new_lengths():
+    """Sums, selection and attention through the lists in one graph; lengths, queries and sums are read when it runs."""
+    B, H, H_kv, T, D, budget = 2, 8, 2, 700, 128, 64
+    p = Tokens(B, H, H_kv, T, D, 1, "bf16")
+    k, v = p.stores
+    ctx = torch.tensor([700, 400], dtype=torch.int32, device=DEV)
+    out, lse, mass = torch.zeros(B, H, 1, D, device=DEV), torch.zeros(B, H, 1, device=DEV), torch.zeros(B, T, device=DEV)
+    by_list, index = torch.zeros(B, H, D, device=DEV), torch.zeros(B, budget, dtype=torch.int32, device=DEV)
+    counts = torch.zeros(B, dtype=torch.int32, device=DEV)
+    desc, win = ssa.make_desc(p.q[:, :, 0], k, v, out[:, :, 0]), ssa.make_window(p.q, out)
+    ws = torch.empty(ssa.attn_mass_workspace_bytes(desc, win), dtype=torch.uint8, device=DEV)
+    desc2 = ssa.make_desc(p.q[:, :, 0], k, v, by_list)
+    ws2 = torch.empty(ssa.decode_workspace_bytes(desc2, budget), dtype=torch.uint8, device=DEV)
+
+    def step():
+        ssa.attn_mass(desc, win, p.q, k, v, ctx, out, lse, mass, mass, 0.5, ws)
+        ssa.mass_to_index(mass, ctx, budget, 2, 16, index, counts)
+        ssa.decode_attn_sparse(desc2, p.q[:, :, 0], k, v, ctx, index, counts, budget, by_list, None, ws2)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for lens in ([700, 400], [64, 1], [333, 699]):
+        ctx.copy_(torch.tensor(lens, dtype=torch.int32, device=DEV))
+        p.q.mul_(-0.5)
+        mass.fill_(0.25)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (out, lse, mass, index, counts, by_list)]
+        mass.fill_(0.25)
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (out, lse, mass, index, counts, by_list)))
+        assert counts.tolist() == [min(n, budget) for n in lens]

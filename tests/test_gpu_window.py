@@ -28,9 +28,11 @@ def test_one_token(dtype, D, layout):
 
 
 @pytest.mark.parametrize("dtype,H,H_kv,n_q", [("bf16", 8, 2, 2), ("f16", 4, 4, 5), ("fp8", 8, 2, 3), ("bf16", 6, 2, 16),
-                                              ("f16", 16, 1, 1), ("bf16", 24, 1, 1), ("fp8", 5, 1, 7), ("f16", 32, 1, 3)])
-def test_few_tokens_with_grouped_heads(dtype, H, H_kv, n_q):
-    p = Tokens(3, H, H_kv, 290, 128, n_q, dtype)
+                                              ("f16", 16, 1, 1), ("bf16", 24, 1, 1), ("fp8", 5, 1, 7), ("f16", 32, 1, 3),
+                                              ("fp8", 4, 1, 8), ("fp8", 8, 1, 3), ("fp8", 10, 1, 13)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_few_tokens_with_grouped_heads(dtype, H, H_kv, n_q, D):
+    p = Tokens(3, H, H_kv, 290, D, n_q, dtype)
     ctx, new, many = [290, n_q, 61], [n_q, n_q, max(1, n_q - 1)], H // H_kv * n_q > 32
     for window, sinks in ((0, 0), (1, 0), (7, 2), (64, 30), (200, 0)):
         run(p, ctx, new, window, sinks, many=many)
@@ -190,6 +192,18 @@ def test_paged_chunk_whose_pages_are_gone():
     got = p.call([570], None, 150, 100, table=table)         # from 321: nothing that is gone is seen
     assert got[3] == 0
     check(p, got, [570], None, 150, 100, torch.float32, many=True)
+
+
+@pytest.mark.parametrize("n_q", [1, 60])
+def test_heads_and_requests_that_share_a_cache(n_q):
+    """Strides of zero: one K/V head's rows for two heads, one request's for two."""
+    p = Tokens(2, 4, 2, 200, 128, n_q)
+    for heads, requests in ((True, False), (False, True), (True, True)):
+        q = Tokens.__new__(Tokens)
+        q.__dict__.update(p.__dict__)
+        share = lambda x: (x[:, :1] if heads else x)[:1 if requests else 2].expand(2, 2, -1, -1)
+        q.host, q.stores = [share(x) for x in p.host], [share(x) for x in p.stores]
+        run(q, [200, 133], None, 70, 3, many=n_q > 16)
 
 
 def test_a_chunk_is_its_tokens_one_by_one():
