@@ -6,6 +6,7 @@ Only allocation, host<->device copies and calls of ``ssa.*`` happen here.
 from __future__ import annotations
 
 import concurrent.futures as _cf
+import contextlib
 import os
 
 import numpy as np
@@ -146,6 +147,42 @@ class DecodeStep:
     def attend_dense(self, stream=None):
         return ssa.decode_attn_dense(self.desc, self.q, self.k, self.v, self.ctx_lens, self.out, self.lse,
                                      self.workspace, self.status, stream)
+
+    # ---- a cache kept within a budget ---------------------------------------------------
+    def _window(self, window, sinks, mass):
+        q, out = self.q.unsqueeze(2), self.out.unsqueeze(2)
+        win = ssa.make_window(q, out, window, sinks)
+        need = (ssa.attn_mass_workspace_bytes if mass else ssa.attn_window_workspace_bytes)(self.desc, win)
+        if need > self.workspace.numel():
+            self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+            self._steps = {}
+        return q, out, win
+
+    def attend_window(self, window: int, sinks: int = 0, stream=None):
+        """The step's token over the newest `window` positions and the first `sinks`."""
+        q, out, win = self._window(window, sinks, False)
+        return ssa.attn_window(self.desc, win, q, self.k, self.v, self.ctx_lens, out, self.lse, self.workspace, self.status, stream)
+
+    def attend_mass(self, decay: float = 1.0, window: int = 0, sinks: int = 0, stream=None):
+        """The step's token over its context (or window), every position's weight added to self.mass [B, max_ctx]."""
+        if not hasattr(self, "mass"):
+            self.mass = torch.zeros((self.wl.B, self.wl.max_ctx), dtype=torch.float32, device=self.device)
+        q, out, win = self._window(window, sinks, True)
+        return ssa.attn_mass(self.desc, win, q, self.k, self.v, self.ctx_lens, out, self.lse, self.mass, self.mass, decay,
+                             self.workspace, self.status, stream)
+
+    def select_heaviest(self, budget: int, sinks: int = 0, recent: int = 0, stream=None):
+        """Index lists (self.index, self.counts) of the positions that the budget keeps, by self.mass."""
+        self.max_selected = int(budget)
+        return ssa.mass_to_index(self.mass, self.ctx_lens, budget, sinks, recent, self.index, self.counts, self.status, stream)
+
+    def compact(self, stream=None):
+        """The listed rows of the cache, and their sums, to its front; contexts become the lists' lengths."""
+        rc = ssa.cache_compact(self.desc, self.k, self.v, self.ctx_lens, self.index, self.counts, self.max_selected,
+                               getattr(self, "mass", None), None, self.status, stream)
+        with torch.cuda.stream(torch.cuda.ExternalStream(ssa._stream(stream))) if stream is not None else contextlib.nullcontext():
+            self.ctx_lens.copy_(self.counts)
+        return rc
 
     # ---- the paper's blocked encoding as the metadata format ---------------------------
     def enable_blockmask(self, block_size: int = 256):

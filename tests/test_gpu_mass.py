@@ -231,3 +231,29 @@ def test_a_captured_step_replayed_on_new_lengths():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, (out, lse, mass, index, counts, by_list)))
         assert counts.tolist() == [min(n, budget) for n in lens]
+
+
+def test_the_runner_keeps_a_workload_within_a_budget():
+    """DecodeStep: weights of a step, selection, attention through the lists, then over the compacted cache: the same rows."""
+    from paper_2404_09336_b200 import inputs
+    from paper_2404_09336_b200.runner import DecodeStep
+    ds = DecodeStep(inputs.make_config(2, B=3, H=4), out_dtype=torch.float32, index_stride=128)
+    T = ds.wl.max_ctx
+    ds.attend_window(T)
+    whole = ds.out.clone()
+    ds.attend_mass()
+    assert torch.equal(ds.out, whole)
+    ctx = ds.ctx_lens.tolist()
+    assert all(abs(ds.mass[b].sum().item() - 4) < 1e-4 and (ds.mass[b, n:] == 0).all() for b, n in enumerate(ctx))
+    ds.select_heaviest(128, sinks=4, recent=32)
+    ds.attend_sparse()
+    by_list, counts = ds.out.clone(), ds.counts.tolist()
+    assert counts == [min(n, 128) for n in ctx]
+    ds.compact()
+    assert ds.ctx_lens.tolist() == counts
+    ds.attend_dense()
+    torch.cuda.synchronize()
+    assert (ds.out - by_list).abs().max() < 1e-5 and int(ds.status) == 0
+    ds.attend_window(32, 4)
+    torch.cuda.synchronize()
+    assert int(ds.status) == 0 and ds.out.isfinite().all()
