@@ -173,6 +173,10 @@ class DecodeStep:
 
     def select_heaviest(self, budget: int, sinks: int = 0, recent: int = 0, stream=None):
         """Index lists (self.index, self.counts) of the positions that the budget keeps, by self.mass."""
+        if budget > self.index_stride:
+            self.index_stride = (int(budget) + 31) // 32 * 32
+            self.index = torch.full((self.wl.B, self.index_stride), -7, dtype=torch.int32, device=self.device)
+            self._steps = {}
         self.max_selected = int(budget)
         return ssa.mass_to_index(self.mass, self.ctx_lens, budget, sinks, recent, self.index, self.counts, self.status, stream)
 

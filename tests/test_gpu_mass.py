@@ -237,7 +237,8 @@ def test_the_runner_keeps_a_workload_within_a_budget():
     """DecodeStep: weights of a step, selection, attention through the lists, then over the compacted cache: the same rows."""
     from paper_2404_09336_b200 import inputs
     from paper_2404_09336_b200.runner import DecodeStep
-    ds = DecodeStep(inputs.make_config(2, B=3, H=4), out_dtype=torch.float32, index_stride=128)
+    ds = DecodeStep(inputs.make_config(2, B=3, H=4), out_dtype=torch.float32)
+    budget = ds.index_stride + 40
     T = ds.wl.max_ctx
     ds.attend_window(T)
     whole = ds.out.clone()
@@ -245,10 +246,10 @@ def test_the_runner_keeps_a_workload_within_a_budget():
     assert torch.equal(ds.out, whole)
     ctx = ds.ctx_lens.tolist()
     assert all(abs(ds.mass[b].sum().item() - 4) < 1e-4 and (ds.mass[b, n:] == 0).all() for b, n in enumerate(ctx))
-    ds.select_heaviest(128, sinks=4, recent=32)
+    ds.select_heaviest(budget, sinks=4, recent=32)
     ds.attend_sparse()
     by_list, counts = ds.out.clone(), ds.counts.tolist()
-    assert counts == [min(n, 128) for n in ctx]
+    assert counts == [min(n, budget) for n in ctx]
     ds.compact()
     assert ds.ctx_lens.tolist() == counts
     ds.attend_dense()
