@@ -21,8 +21,8 @@ constexpr int kWarps = 4;              // of a block
 constexpr int kSplitKeys = 256;        // fewest positions worth a split of their own
 constexpr int kMostGroups = 4;         // of kGroup rows, of a warp
 constexpr float kLazyRows = 2.f;       // log2 of how far weights may exceed 1 before sums are rescaled (fp16: 2^13 times that)
-// Rows of a K/V head up to which this kernel is the faster one (16 requests of up to 4096, 8 K/V heads: 16 rows 41 us, the tiles
-// 53; 24 rows 55 and 57; 32 rows 82 and 58).
+// Rows of a K/V head up to which this kernel is the faster one (16 requests of up to 4096, 8 K/V heads: 41 us for 16 rows, 55 for
+// 24, 82 for 32; the tiles 54 to 58 for 32 and more, up to 128).
 constexpr int kFewRows = 24;
 
 // The weights enter the second contraction as a 16-bit value plus the 16-bit rest, so that the sums keep 16 bits (bf16) or 22
