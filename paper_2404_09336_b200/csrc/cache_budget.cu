@@ -68,13 +68,16 @@ template <int kThreads, int kItems, bool kLong>
 __global__ void __launch_bounds__(kThreads)
 mass_keep_kernel(const KeepParams p) {
   constexpr int kWarps = kThreads / 32, kOwn = kBins / kThreads, kParts = kItems / 4, kPart = 4 * kThreads;
-  __shared__ uint32_t s_bins[3][kBins];                    // of a digit each; afterwards the positions that stay
-  __shared__ uint32_t s_all[kBins];                        // clusters: all blocks' of the digit at hand
+  // One array: three digits' bins and, for clusters, all blocks' bins of the digit at hand; afterwards, over all of it, the
+  // positions that stay, of which a block may have as many as it has items.
+  __shared__ uint32_t s_mem[4 * kBins];
+  uint32_t* const s_bins = s_mem;
+  uint32_t* const s_all = s_mem + 3 * kBins;
   __shared__ uint32_t s_sum[kParts < 2 ? 2 : kParts][kWarps], s_total;
-  static_assert(kLong || kItems * kThreads * 2 <= (int)sizeof(s_bins) + (int)sizeof(s_all), "");
+  static_assert(kLong || kItems * kThreads * sizeof(uint16_t) <= sizeof(s_mem), "");
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid % 32, warp = tid / 32, blocks = gridDim.x;
   const int rank = blocks == 1 ? 0 : (int)cluster_rank();
-  for (int i = tid; i < 3 * kBins; i += kThreads) s_bins[0][i] = 0;
+  for (int i = tid; i < 3 * kBins; i += kThreads) s_bins[i] = 0;
   grid_dependency_wait();
   grid_launch_dependents();
   const float* mass = p.mass + (int64_t)b * p.mass_stride;
@@ -124,7 +127,7 @@ mass_keep_kernel(const KeepParams p) {
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
       const uint32_t digits = pass == 2 ? 1023u : 2047u;
-      uint32_t* const bins = s_bins[pass];
+      uint32_t* const bins = s_bins + pass * kBins;
       // Sums are often all alike (nothing looked at yet): a warp whose first keys share the digit adds once for all that do.
       const uint32_t sample = kLong ? 0 : keys[0] >> shift & digits;
       const bool alike = kLong || __all_sync(~0u, sample == __shfl_sync(~0u, sample, 0));
@@ -260,7 +263,7 @@ mass_keep_kernel(const KeepParams p) {
       cluster_sync();                                      // (totals are read by the others until here)
     }
     const int room = max(0, want - equal);                 // equal keys of this block that stay
-    uint16_t* const list = reinterpret_cast<uint16_t*>(&s_bins[0][0]);       // positions within the block
+    uint16_t* const list = reinterpret_cast<uint16_t*>(s_mem);       // positions within the block
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
       uint32_t& at = before[i / 4];                          // counts so far
