@@ -112,6 +112,11 @@ class DecodeStep:
         self.counts.fill_(-7)
         self.status.zero_()
         self.index = torch.full((B, self.index_stride), -7, dtype=torch.int32, device=dev)
+        # what a budget keeps has lists of its own, with room for whole contexts: the span lists' bound and buffers stay theirs
+        self.budget = 0
+        self._budget_lists = (torch.full((B, (T + 31) // 32 * 32), -7, dtype=torch.int32, device=dev),
+                              torch.full((B,), -7, dtype=torch.int32, device=dev))
+        self._span_lists = None                              # (index, counts) while the budget's are in their place
         self.desc = ssa.make_desc(self.q, self.k, self.v, self.out, max_ctx=T)
         self.max_spans = int(max(1, np.diff(wl.span_offsets).max() if wl.B else 1))
         need = max(ssa.decode_workspace_bytes(self.desc, self.max_selected),
@@ -128,17 +133,31 @@ class DecodeStep:
         self.v = vs if self.layout == "bhtd" else vs.permute(0, 2, 1, 3)
 
     # ---- the calls ------------------------------------------------------------------
+    # self.index, self.counts are the lists that were asked for last, from spans or by a budget; max_selected bounds the first,
+    # budget the second.
+    def _lists_of_spans(self):
+        if self._span_lists is not None:
+            (self.index, self.counts), self._span_lists = self._span_lists, None
+
     def build_index(self, stream=None):
+        self._lists_of_spans()
         return ssa.spans_to_index(self.span_offsets, self.spans, self.ctx_lens, self.index, self.counts,
                                   self.status, stream)
 
     def attend_sparse(self, stream=None):
+        if self._span_lists is not None:
+            bound = self.budget
+            workspace = self._room(ssa.decode_workspace_bytes(self.desc, bound))
+        else:
+            bound, workspace = self.max_selected, self.workspace
         return ssa.decode_attn_sparse(self.desc, self.q, self.k, self.v, self.ctx_lens, self.index,
-                                      self.counts, self.max_selected, self.out, self.lse, self.workspace,
+                                      self.counts, bound, self.out, self.lse, workspace,
                                       self.status, stream)
 
     def attend_spans(self, stream=None, want_lists=False):
         """Span lists -> attention output in one call (no index list unless want_lists)."""
+        if want_lists:
+            self._lists_of_spans()
         return ssa.decode_attn_spans(self.desc, self.q, self.k, self.v, self.ctx_lens, self.span_offsets, self.spans,
                                      self.max_spans, self.max_selected, self.out, self.lse,
                                      self.index if want_lists else None, self.counts if want_lists else None,
@@ -149,13 +168,16 @@ class DecodeStep:
                                      self.workspace, self.status, stream)
 
     # ---- a cache kept within a budget ---------------------------------------------------
-    def _window(self, window, sinks, mass):
-        q, out = self.q.unsqueeze(2), self.out.unsqueeze(2)
-        win = ssa.make_window(q, out, window, sinks)
-        need = (ssa.attn_mass_workspace_bytes if mass else ssa.attn_window_workspace_bytes)(self.desc, win)
+    def _room(self, need):
         if need > self.workspace.numel():
             self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
             self._steps = {}
+        return self.workspace
+
+    def _window(self, window, sinks, mass):
+        q, out = self.q.unsqueeze(2), self.out.unsqueeze(2)
+        win = ssa.make_window(q, out, window, sinks)
+        self._room((ssa.attn_mass_workspace_bytes if mass else ssa.attn_window_workspace_bytes)(self.desc, win))
         return q, out, win
 
     def attend_window(self, window: int, sinks: int = 0, stream=None):
@@ -172,17 +194,21 @@ class DecodeStep:
                              self.workspace, self.status, stream)
 
     def select_heaviest(self, budget: int, sinks: int = 0, recent: int = 0, stream=None):
-        """Index lists (self.index, self.counts) of the positions that the budget keeps, by self.mass."""
-        if budget > self.index_stride:
-            self.index_stride = (int(budget) + 31) // 32 * 32
-            self.index = torch.full((self.wl.B, self.index_stride), -7, dtype=torch.int32, device=self.device)
-            self._steps = {}
-        self.max_selected = int(budget)
-        return ssa.mass_to_index(self.mass, self.ctx_lens, budget, sinks, recent, self.index, self.counts, self.status, stream)
+        """Index lists (self.index, self.counts, until the next ones from spans) of the positions that the budget keeps, by
+        self.mass."""
+        if budget > self._budget_lists[0].shape[1] and sinks >= 0 and recent >= 0 and sinks + recent <= budget:
+            budget, sinks, recent = self.wl.max_ctx, 0, 0    # (room for every position: all stay)
+        rc = ssa.mass_to_index(self.mass, self.ctx_lens, budget, sinks, recent, *self._budget_lists, self.status, stream)
+        if self._span_lists is None:
+            self._span_lists = self.index, self.counts
+        self.index, self.counts = self._budget_lists
+        self.budget = int(budget)
+        return rc
 
     def compact(self, stream=None):
         """The listed rows of the cache, and their sums, to its front; contexts become the lists' lengths."""
-        rc = ssa.cache_compact(self.desc, self.k, self.v, self.ctx_lens, self.index, self.counts, self.max_selected,
+        rc = ssa.cache_compact(self.desc, self.k, self.v, self.ctx_lens, self.index, self.counts,
+                               self.max_selected if self._span_lists is None else self.budget,
                                getattr(self, "mass", None), None, self.status, stream)
         with torch.cuda.stream(torch.cuda.ExternalStream(ssa._stream(stream))) if stream is not None else contextlib.nullcontext():
             self.ctx_lens.copy_(self.counts)
@@ -230,6 +256,7 @@ class DecodeStep:
         """One decode step of the method through ssa_decode_step with everything resident on the
         device: index lists, counts and the attention output are written.  kernels: "auto" (the
         library picks one kernel or index + attention launches), "one" or "two"."""
+        self._lists_of_spans()
         key = ("resident", self.k.data_ptr(), self.max_selected, self.max_spans, kernels)
         st = self._steps.get(key)
         if st is None:
@@ -262,6 +289,7 @@ class DecodeStep:
         (SSA_STEP_COPY_BY_KERNEL).  Same bytes, same result, less latency."""
         if not hasattr(self, "h_in"):
             raise RuntimeError("call make_host_buffers() before step_from_host()")
+        self._lists_of_spans()
         key = ("host", self.k.data_ptr(), self.max_selected, self.max_spans, bool(direct))
         st = self._steps.get(key)
         if st is None:

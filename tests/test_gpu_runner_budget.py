@@ -1,0 +1,42 @@
+"""DecodeStep: calls over span lists before, between and behind the calls around a budget."""
+import pytest
+import torch
+
+from paper_2404_09336_b200 import inputs
+from paper_2404_09336_b200.runner import DecodeStep
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("budget", [3, 64, 460, 512])
+def test_steps_over_spans_are_as_without_a_budget(budget):
+    ds = DecodeStep(inputs.make_config(1), out_dtype=torch.float32)
+    calls = (ds.step, ds.step_two_calls, ds.attend_spans, lambda: ds.attend_spans(want_lists=True))
+    want = []
+    for call in calls:
+        call()
+        want.append((ds.out.clone(), ds.lse.clone(), ds.counts.clone(), ds.index.clone()))
+    for call, (out, lse, counts, index) in zip(calls, want):
+        ds.attend_mass()
+        ds.select_heaviest(budget)
+        ds.attend_sparse()
+        ds.out.fill_(9)
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(ds.out, out) and torch.equal(ds.lse, lse) and int(ds.status) == 0
+        if call is not calls[2]:
+            assert torch.equal(ds.counts, counts) and torch.equal(ds.index, index)
+
+
+def test_budgets_of_any_size_are_attended_to():
+    ds = DecodeStep(inputs.make_config(2, B=3, H=4), out_dtype=torch.float32)
+    ds.attend_mass()
+    ds.attend_dense()
+    whole, ctx = ds.out.clone(), ds.ctx_lens.tolist()
+    for budget in (5, 200, 1000, 1024, 5000):
+        ds.select_heaviest(budget, sinks=2, recent=3)
+        ds.attend_sparse()
+        torch.cuda.synchronize()
+        assert ds.counts.tolist() == [min(n, budget) for n in ctx] and int(ds.status) == 0
+        if budget >= max(ctx):
+            assert (ds.out - whole).abs().max() < 1e-5

@@ -1,0 +1,94 @@
+"""DecodeStep's calls around a budget: what they hand to the library, and what they leave to the calls over span lists (no GPU: the
+library's calls are recorded)."""
+import inspect
+
+import pytest
+import torch
+
+from paper_2404_09336_b200 import inputs, ssa
+from paper_2404_09336_b200.runner import DecodeStep
+
+CALLS = ("spans_to_index", "decode_attn_sparse", "decode_attn_spans", "decode_attn_dense", "attn_window", "attn_mass", "mass_to_index",
+         "cache_compact", "decode_step", "make_step")
+
+
+@pytest.fixture
+def made(monkeypatch):
+    """-> the calls made, as (name, arguments by name)."""
+    calls = []
+
+    def record(name):
+        signature = inspect.signature(getattr(ssa, name))
+
+        def call(*a, **k):
+            bound = signature.bind(*a, **k)
+            bound.apply_defaults()
+            calls.append((name, bound.arguments))
+            return 0
+        return call
+
+    for name in CALLS:
+        monkeypatch.setattr(ssa, name, record(name))
+    return calls
+
+
+def small(**kw):
+    return DecodeStep(inputs.make_config(2, B=3, H=4), device="cpu", **kw)
+
+
+def budgets(ds):
+    return [1, ds.max_selected // 2, ds.max_selected, ds.index_stride + 40, ds.wl.max_ctx, ds.wl.max_ctx + 100]
+
+
+def test_a_budget_does_not_bound_the_span_lists(made):
+    ds = small()
+    spans = ds.max_selected, ds.index, ds.counts, ds.index_stride
+    for budget in budgets(ds):
+        ds.mass = torch.zeros(3, ds.wl.max_ctx)
+        ds.select_heaviest(budget)
+        ds.build_index()
+        ds.attend_sparse()
+        ds.select_heaviest(budget)
+        ds.attend_spans()
+        ds.step()
+        ds.attend_sparse()
+        ds.select_heaviest(budget)
+        ds.attend_spans(want_lists=True)
+        for name, a in made:
+            if name in ("decode_attn_sparse", "decode_attn_spans", "make_step"):
+                assert a["max_selected"] == spans[0], (name, budget)
+                index = a.get("index", a.get("index_out"))
+                assert index is None or (index is spans[1] and a.get("counts", a.get("counts_out")) is spans[2]), (name, budget)
+        assert (ds.max_selected, ds.index, ds.counts, ds.index_stride) == spans
+        made.clear()
+
+
+def test_lists_of_a_budget_are_attended_to_and_compacted_with_its_bound(made):
+    ds = small()
+    ds.mass = torch.zeros(3, ds.wl.max_ctx)
+    ds.build_index()
+    for budget in budgets(ds):
+        ds.select_heaviest(budget, sinks=1, recent=0)
+        ds.attend_spans()                                    # writes no lists
+        ds.attend_sparse()
+        ds.compact()
+        (_, kept), _, (_, sparse), (_, moved) = made[-4:]
+        assert kept["budget"] == min(budget, ds.wl.max_ctx) == sparse["max_selected"] == moved["max_selected"]
+        assert kept["sinks"] == (1 if budget <= ds.wl.max_ctx else 0) and kept["budget"] <= kept["index"].shape[1]
+        assert kept["index"] is sparse["index"] is moved["index"] is ds.index
+        assert kept["counts"] is sparse["counts"] is moved["counts"] is ds.counts
+        assert sparse["workspace"].numel() >= ssa.decode_workspace_bytes(ds.desc, sparse["max_selected"])
+    ds.step()
+    ds.compact()
+    assert made[-1][1]["max_selected"] == ds.max_selected and made[-1][1]["index"] is made[-3][1]["index"]
+
+
+def test_refused_budgets_change_nothing():
+    ds = small()
+    ds.mass = torch.zeros(3, ds.wl.max_ctx)
+    before = ds.index, ds.counts, ds.max_selected
+    for bad in (dict(budget=0), dict(budget=-3), dict(budget=8, sinks=5, recent=4), dict(budget=8, sinks=-1), dict(budget=9999, recent=-1),
+                dict(budget=9999, sinks=9000, recent=1000)):
+        with pytest.raises(ssa.SsaError):
+            ds.select_heaviest(**bad, stream=0)
+        assert (ds.index, ds.counts, ds.max_selected) == before
