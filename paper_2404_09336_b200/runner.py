@@ -125,6 +125,7 @@ class DecodeStep:
         if need == 0:
             raise RuntimeError("ssa_decode_workspace_bytes rejected the descriptor")
         self.workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        self._rooms = []
         self._steps = {}
 
     def select_copy(self, c: int):
@@ -147,7 +148,7 @@ class DecodeStep:
     def attend_sparse(self, stream=None):
         if self._span_lists is not None:
             bound = self.budget
-            workspace = self._room(ssa.decode_workspace_bytes(self.desc, bound))
+            workspace = self._room(ssa.decode_workspace_bytes(self.desc, bound), stream)
         else:
             bound, workspace = self.max_selected, self.workspace
         return ssa.decode_attn_sparse(self.desc, self.q, self.k, self.v, self.ctx_lens, self.index,
@@ -168,30 +169,39 @@ class DecodeStep:
                                      self.workspace, self.status, stream)
 
     # ---- a cache kept within a budget ---------------------------------------------------
-    def _room(self, need):
-        if need > self.workspace.numel():
-            self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
-            self._steps = {}
-        return self.workspace
+    def _on(self, stream):
+        """The caller's stream as torch's current one."""
+        if stream is None:
+            return contextlib.nullcontext()
+        return torch.cuda.stream(torch.cuda.ExternalStream(ssa._stream(stream), device=self.device))
 
-    def _window(self, window, sinks, mass):
+    def _room(self, need, stream):
+        """Workspace of these calls, apart from that of the calls over spans.  One that is too small stays as it is beside the
+        next: graphs captured with it and calls still running on another stream go on using it."""
+        most = self._rooms[-1].numel() if self._rooms else 0
+        if need > most:
+            with self._on(stream):
+                self._rooms.append(torch.empty(max(need, 2 * most), dtype=torch.uint8, device=self.device))
+        return self._rooms[-1]
+
+    def _window(self, window, sinks, mass, stream):
         q, out = self.q.unsqueeze(2), self.out.unsqueeze(2)
         win = ssa.make_window(q, out, window, sinks)
-        self._room((ssa.attn_mass_workspace_bytes if mass else ssa.attn_window_workspace_bytes)(self.desc, win))
-        return q, out, win
+        need = (ssa.attn_mass_workspace_bytes if mass else ssa.attn_window_workspace_bytes)(self.desc, win)
+        return q, out, win, self._room(need, stream)
 
     def attend_window(self, window: int, sinks: int = 0, stream=None):
         """The step's token over the newest `window` positions and the first `sinks`."""
-        q, out, win = self._window(window, sinks, False)
-        return ssa.attn_window(self.desc, win, q, self.k, self.v, self.ctx_lens, out, self.lse, self.workspace, self.status, stream)
+        q, out, win, room = self._window(window, sinks, False, stream)
+        return ssa.attn_window(self.desc, win, q, self.k, self.v, self.ctx_lens, out, self.lse, room, self.status, stream)
 
     def attend_mass(self, decay: float = 1.0, window: int = 0, sinks: int = 0, stream=None):
         """The step's token over its context (or window), every position's weight added to self.mass [B, max_ctx]."""
         if not hasattr(self, "mass"):
             self.mass = torch.zeros((self.wl.B, self.wl.max_ctx), dtype=torch.float32, device=self.device)
-        q, out, win = self._window(window, sinks, True)
+        q, out, win, room = self._window(window, sinks, True, stream)
         return ssa.attn_mass(self.desc, win, q, self.k, self.v, self.ctx_lens, out, self.lse, self.mass, self.mass, decay,
-                             self.workspace, self.status, stream)
+                             room, self.status, stream)
 
     def select_heaviest(self, budget: int, sinks: int = 0, recent: int = 0, stream=None):
         """Index lists (self.index, self.counts, until the next ones from spans) of the positions that the budget keeps, by
@@ -210,7 +220,7 @@ class DecodeStep:
         rc = ssa.cache_compact(self.desc, self.k, self.v, self.ctx_lens, self.index, self.counts,
                                self.max_selected if self._span_lists is None else self.budget,
                                getattr(self, "mass", None), None, self.status, stream)
-        with torch.cuda.stream(torch.cuda.ExternalStream(ssa._stream(stream))) if stream is not None else contextlib.nullcontext():
+        with self._on(stream):
             self.ctx_lens.copy_(self.counts)
         return rc
 

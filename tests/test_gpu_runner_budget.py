@@ -40,3 +40,36 @@ def test_budgets_of_any_size_are_attended_to():
         assert ds.counts.tolist() == [min(n, budget) for n in ctx] and int(ds.status) == 0
         if budget >= max(ctx):
             assert (ds.out - whole).abs().max() < 1e-5
+
+
+def test_captured_steps_keep_their_buffers():
+    """Graphs of a step, of a window and of an attention through a budget's lists, replayed behind calls that need more room."""
+    ds = DecodeStep(inputs.make_config(2, B=2, H=4), out_dtype=torch.float32)
+    ds.attend_mass()
+    mass = ds.mass.clone()
+    ds.select_heaviest(40)
+    calls, graphs, want = (ds.step, lambda: ds.attend_window(9), ds.attend_sparse), [], []
+    for call in (calls[2], calls[1], calls[0]):              # (a step puts its own lists in place)
+        call()
+        want.append(ds.out.clone())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        graphs.append(graph)
+    sizes = {ds.workspace.numel(), *(x.numel() for x in ds._rooms)}
+    with pytest.MonkeyPatch.context() as m:
+        from paper_2404_09336_b200 import ssa
+        need = 3 * max(sizes)
+        m.setattr(ssa, "attn_mass_workspace_bytes", lambda *a: need)
+        ds.attend_mass()
+    ds.select_heaviest(ds.index_stride + 200)
+    poison = [torch.full((n,), 0xff, dtype=torch.uint8, device=ds.device) for n in sizes for _ in range(4)]
+    for graph, out in zip(graphs, want):
+        ds.out.fill_(9)
+        if out is want[0]:
+            ds.mass.copy_(mass)
+            ds.select_heaviest(40)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(ds.out, out)
+    assert all(bool((x == 0xff).all()) for x in poison)      # nothing wrote where others' memory is by now

@@ -92,3 +92,29 @@ def test_refused_budgets_change_nothing():
         with pytest.raises(ssa.SsaError):
             ds.select_heaviest(**bad, stream=0)
         assert (ds.index, ds.counts, ds.max_selected) == before
+
+
+def test_calls_around_a_budget_leave_the_other_calls_their_workspace_and_keep_their_own(made):
+    import gc
+    import weakref
+    ds = small()
+    ds.mass = torch.zeros(3, ds.wl.max_ctx)
+    ds.step()
+    steps, workspace = dict(ds._steps), ds.workspace
+    refs, sizes = [], []
+    for i, need in enumerate((1000, workspace.numel() + 1, 100, 2 * workspace.numel() + 7, 2 * workspace.numel() + 8)):
+        with pytest.MonkeyPatch.context() as m:
+            m.setattr(ssa, "attn_mass_workspace_bytes" if i % 2 else "attn_window_workspace_bytes", lambda *a: need)
+            ds.attend_mass() if i % 2 else ds.attend_window(7)
+        room = made.pop()[1]["workspace"]
+        assert room.numel() >= need and room is not workspace
+        refs.append(weakref.ref(room))
+        sizes.append(room.numel())
+        del room
+    gc.collect()
+    assert ds.workspace is workspace and ds._steps == steps
+    assert all(r() is not None for r in refs)                # a captured graph may still hold their addresses
+    assert sum(sorted(set(sizes))[:-1]) <= max(sizes)
+    ds.select_heaviest(30)
+    ds.attend_sparse()
+    assert made[-1][1]["workspace"] is not workspace
