@@ -112,6 +112,7 @@ class DecodeStep:
         self.counts.fill_(-7)
         self.status.zero_()
         self.index = torch.full((B, self.index_stride), -7, dtype=torch.int32, device=dev)
+        self.mass = torch.zeros((B, T), dtype=torch.float32, device=dev)     # weight of every position so far (attend_mass)
         # what a budget keeps has lists of its own, with room for whole contexts: the span lists' bound and buffers stay theirs
         self.budget = 0
         self._budget_lists = (torch.full((B, (T + 31) // 32 * 32), -7, dtype=torch.int32, device=dev),
@@ -127,6 +128,8 @@ class DecodeStep:
         self.workspace = torch.empty(need, dtype=torch.uint8, device=dev)
         self._rooms = []
         self._steps = {}
+        if dev.type == "cuda":                               # calls may come on any stream: what was filled above is there
+            torch.cuda.current_stream(dev).synchronize()
 
     def select_copy(self, c: int):
         ks, vs = self.k_store[c % len(self.k_store)], self.v_store[c % len(self.v_store)]
@@ -197,8 +200,6 @@ class DecodeStep:
 
     def attend_mass(self, decay: float = 1.0, window: int = 0, sinks: int = 0, stream=None):
         """The step's token over its context (or window), every position's weight added to self.mass [B, max_ctx]."""
-        if not hasattr(self, "mass"):
-            self.mass = torch.zeros((self.wl.B, self.wl.max_ctx), dtype=torch.float32, device=self.device)
         q, out, win, room = self._window(window, sinks, True, stream)
         return ssa.attn_mass(self.desc, win, q, self.k, self.v, self.ctx_lens, out, self.lse, self.mass, self.mass, decay,
                              room, self.status, stream)
@@ -219,7 +220,7 @@ class DecodeStep:
         """The listed rows of the cache, and their sums, to its front; contexts become the lists' lengths."""
         rc = ssa.cache_compact(self.desc, self.k, self.v, self.ctx_lens, self.index, self.counts,
                                self.max_selected if self._span_lists is None else self.budget,
-                               getattr(self, "mass", None), None, self.status, stream)
+                               self.mass, None, self.status, stream)
         with self._on(stream):
             self.ctx_lens.copy_(self.counts)
         return rc

@@ -73,3 +73,34 @@ def test_captured_steps_keep_their_buffers():
         torch.cuda.synchronize()
         assert torch.equal(ds.out, out)
     assert all(bool((x == 0xff).all()) for x in poison)      # nothing wrote where others' memory is by now
+
+
+def test_first_calls_on_a_side_stream_and_in_a_graph():
+    """Sums start from zero once: not behind the call that adds to them, and not with every replay."""
+    wl = inputs.make_config(2, B=2, H=4)
+    want = DecodeStep(wl, out_dtype=torch.float32)
+    for _ in range(3):
+        want.attend_mass()
+    torch.cuda.synchronize()
+    ds, side = DecodeStep(wl, out_dtype=torch.float32), torch.cuda.Stream()
+    busy = torch.randn(8192, 8192, device=ds.device)
+    torch.cuda.synchronize()
+    for _ in range(8):                                       # the current stream is behind the side stream by this
+        busy = busy @ busy * 1e-4
+    for _ in range(3):
+        ds.attend_mass(stream=side)
+    ds.select_heaviest(ds.index_stride + 100, stream=side)
+    ds.attend_sparse(stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(ds.mass, want.mass)
+    want.select_heaviest(ds.index_stride + 100)
+    want.attend_sparse()
+    torch.cuda.synchronize()
+    assert torch.equal(ds.index, want.index) and torch.equal(ds.counts, want.counts) and torch.equal(ds.out, want.out)
+    ds, graph = DecodeStep(wl, out_dtype=torch.float32), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ds.attend_mass()
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(ds.mass, want.mass)

@@ -118,3 +118,23 @@ def test_calls_around_a_budget_leave_the_other_calls_their_workspace_and_keep_th
     ds.select_heaviest(30)
     ds.attend_sparse()
     assert made[-1][1]["workspace"] is not workspace
+
+
+def test_no_call_fills_a_buffer(made, monkeypatch):
+    """A fill would go to torch's current stream and not to the call's, and into a graph that is being captured."""
+    ds = small()
+    assert ds.mass.shape == (3, ds.wl.max_ctx) and not ds.mass.any()
+
+    def never(*a, **k):
+        raise AssertionError("a buffer was filled")
+
+    for name in ("zeros", "full", "ones", "zeros_like", "full_like", "tensor"):
+        monkeypatch.setattr(torch, name, never)
+    ds.select_heaviest(20)                                   # before any sums: nothing was looked at yet
+    ds.attend_mass(0.5)
+    ds.attend_window(30, 2)
+    for budget in (50, ds.index_stride + 1, ds.wl.max_ctx):
+        ds.select_heaviest(budget)
+        ds.attend_sparse()
+    assert all(a["mass"] is ds.mass for name, a in made if name == "mass_to_index")
+    assert all(a["mass_in"] is a["mass_out"] is ds.mass for name, a in made if name == "attn_mass")
