@@ -131,10 +131,12 @@ class DecodeStep:
         if dev.type == "cuda":                               # calls may come on any stream: what was filled above is there
             torch.cuda.current_stream(dev).synchronize()
 
-    def select_copy(self, c: int):
+    def _copy(self, c: int):
         ks, vs = self.k_store[c % len(self.k_store)], self.v_store[c % len(self.v_store)]
-        self.k = ks if self.layout == "bhtd" else ks.permute(0, 2, 1, 3)
-        self.v = vs if self.layout == "bhtd" else vs.permute(0, 2, 1, 3)
+        return (ks, vs) if self.layout == "bhtd" else (ks.permute(0, 2, 1, 3), vs.permute(0, 2, 1, 3))
+
+    def select_copy(self, c: int):
+        self.k, self.v = self._copy(c)
 
     # ---- the calls ------------------------------------------------------------------
     # self.index, self.counts are the lists that were asked for last, from spans or by a budget; max_selected bounds the first,
@@ -217,13 +219,16 @@ class DecodeStep:
         return rc
 
     def compact(self, stream=None):
-        """The listed rows of the cache, and their sums, to its front; contexts become the lists' lengths."""
-        rc = ssa.cache_compact(self.desc, self.k, self.v, self.ctx_lens, self.index, self.counts,
-                               self.max_selected if self._span_lists is None else self.budget,
-                               self.mass, None, self.status, stream)
+        """The listed rows of every copy of the cache, and their sums, to the front; contexts become the lists' lengths.  What names
+        positions (lists, spans, lengths in host buffers) names those from before the move."""
+        bound = self.max_selected if self._span_lists is None else self.budget
+        for c in range(len(self.k_store)):                   # contexts and sums belong to all copies
+            k, v = self._copy(c)
+            ssa.cache_compact(self.desc, k, v, self.ctx_lens, self.index, self.counts, bound, None if c else self.mass, None,
+                              self.status, stream)
         with self._on(stream):
             self.ctx_lens.copy_(self.counts)
-        return rc
+        return ssa.OK
 
     # ---- the paper's blocked encoding as the metadata format ---------------------------
     def enable_blockmask(self, block_size: int = 256):

@@ -104,3 +104,21 @@ def test_first_calls_on_a_side_stream_and_in_a_graph():
         graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(ds.mass, want.mass)
+
+
+@pytest.mark.parametrize("layout", ["bhtd", "bthd"])
+def test_all_copies_of_a_compacted_cache_are_alike(layout):
+    ds = DecodeStep(inputs.make_config(2, B=3, H=4), layout=layout, kv_copies=2, out_dtype=torch.float32)
+    ds.attend_mass()
+    ds.select_heaviest(50, sinks=3, recent=9)
+    mass, index = ds.mass.clone(), ds.index[:, :50].clone()
+    ds.compact()
+    got = []
+    for c in range(2):
+        ds.select_copy(c)
+        ds.attend_dense()
+        got.append(ds.out.clone())
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], got[1]) and int(ds.status) == 0 and ds.ctx_lens.tolist() == ds.counts.tolist()
+    for b, n in enumerate(ds.counts.tolist()):
+        assert torch.equal(ds.mass[b, :n], mass[b, index[b, :n].long()])

@@ -138,3 +138,16 @@ def test_no_call_fills_a_buffer(made, monkeypatch):
         ds.attend_sparse()
     assert all(a["mass"] is ds.mass for name, a in made if name == "mass_to_index")
     assert all(a["mass_in"] is a["mass_out"] is ds.mass for name, a in made if name == "attn_mass")
+
+
+@pytest.mark.parametrize("layout", ["bhtd", "bthd"])
+def test_every_copy_of_the_cache_is_compacted_the_sums_once(made, layout):
+    ds = small(kv_copies=3, layout=layout)
+    ds.counts.fill_(5)
+    ds.select_copy(1)
+    ds.compact()
+    assert [a["k_cache"].data_ptr() for _, a in made] == [x.data_ptr() for x in ds.k_store]
+    assert [a["v_cache"].data_ptr() for _, a in made] == [x.data_ptr() for x in ds.v_store]
+    assert all(a["k_cache"].shape == a["v_cache"].shape == (3, 4, ds.wl.max_ctx, ds.wl.D) for _, a in made)
+    assert [a["mass"] is ds.mass for _, a in made] == [True, False, False] and all(a["mass"] is None for _, a in made[1:])
+    assert ds.ctx_lens.tolist() == [5, 5, 5] and ds.k.data_ptr() == ds.k_store[1].data_ptr()
