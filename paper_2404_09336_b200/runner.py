@@ -227,7 +227,8 @@ class DecodeStep:
             ssa.cache_compact(self.desc, k, v, self.ctx_lens, self.index, self.counts, bound, None if c else self.mass, None,
                               self.status, stream)
         with self._on(stream):
-            self.ctx_lens.copy_(self.counts)
+            # (no longer than what was moved, where a count is above its bound or was never written)
+            self.ctx_lens.copy_(torch.minimum(self.ctx_lens, self.counts.clamp(0, bound)))
         return ssa.OK
 
     # ---- the paper's blocked encoding as the metadata format ---------------------------

@@ -151,3 +151,12 @@ def test_every_copy_of_the_cache_is_compacted_the_sums_once(made, layout):
     assert all(a["k_cache"].shape == a["v_cache"].shape == (3, 4, ds.wl.max_ctx, ds.wl.D) for _, a in made)
     assert [a["mass"] is ds.mass for _, a in made] == [True, False, False] and all(a["mass"] is None for _, a in made[1:])
     assert ds.ctx_lens.tolist() == [5, 5, 5] and ds.k.data_ptr() == ds.k_store[1].data_ptr()
+
+
+def test_contexts_are_no_longer_than_what_was_moved(made):
+    ds = small()
+    bound = ds.max_selected
+    ds.ctx_lens.copy_(torch.tensor([900, 100, 7]))
+    ds.counts.copy_(torch.tensor([bound + 9, -7, 8]))        # clamped by the call: its bound, nothing, its context
+    ds.compact()
+    assert ds.ctx_lens.tolist() == [bound, 0, 7]
