@@ -419,9 +419,12 @@ def decode_attn_dense_paged(desc, q, k_pool, v_pool, paging, ctx_lens, out, lse=
 
 def make_window(q, out, window: int = 0, sinks: int = 0, q_lens=None, paging: Paging | None = None) -> Window:
     """ssa_window for q[B,H,n_q,D], out[B,H,n_q,D] (any strides; the descriptor is made from q[:, :, 0], out[:, :, 0]).  q_lens
-    (int32 [B], device) must stay alive."""
-    if q_lens is not None and q_lens.dtype != torch.int32:
-        raise ValueError("q_lens must be int32")
+    (int32 [B], side by side, on q's device) must stay alive."""
+    if q_lens is not None:
+        if q_lens.dtype != torch.int32:
+            raise ValueError("q_lens must be int32")
+        if q_lens.device != q.device or not q_lens.is_contiguous() or q_lens.numel() < q.shape[0]:
+            raise ValueError("q_lens is one length per request, side by side, on the device of q")
     w = Window()
     w.n_q, w.window, w.sinks = int(q.shape[2]), int(window), int(sinks)
     w.q_stride_t, w.o_stride_t = int(q.stride(2)), int(out.stride(2))
