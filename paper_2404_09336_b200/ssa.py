@@ -434,10 +434,10 @@ def make_window(q, out, window: int = 0, sinks: int = 0, q_lens=None, paging: Pa
     return w
 
 
-def _check_mass(mass, width):
-    """mass[B, width or more], fp32, entries side by side."""
-    if mass.dtype != torch.float32 or mass.stride(-1) != 1 or mass.shape[-1] < width:
-        raise ValueError(f"sums are rows of {width} fp32 values")
+def _check_mass(mass, rows, width):
+    """mass[rows or more, width or more], fp32, entries of a row side by side."""
+    if mass.dim() != 2 or mass.dtype != torch.float32 or mass.stride(1) != 1 or mass.shape[0] < rows or mass.shape[1] < width:
+        raise ValueError(f"sums are {rows} rows of {width} fp32 values")
 
 
 def attn_window_workspace_bytes(desc: AttnDesc, window: Window) -> int:
@@ -459,9 +459,9 @@ def attn_mass(desc, window, q, k_cache, v_cache, ctx_lens, out, lse, mass_in, ma
               dev_status=None, stream=None, check=True):
     """ssa_attn_mass: attn_window, and mass_out[B, max_ctx] = decay * mass_in + the weight of every position (mass_in: a tensor
     of mass_out's strides, mass_out itself, or None)."""
-    _check_mass(mass_out, desc.max_ctx)
+    _check_mass(mass_out, desc.B, desc.max_ctx)
     if mass_in is not None and mass_in is not mass_out:
-        _check_mass(mass_in, desc.max_ctx)
+        _check_mass(mass_in, desc.B, desc.max_ctx)
         if _row_stride(mass_in) != _row_stride(mass_out):
             raise ValueError("mass_in and mass_out must have the same row stride")
     rc = _call.attn_mass(desc, window, q, k_cache, v_cache, ctx_lens, out, lse, mass_in, mass_out, decay, workspace,
@@ -471,7 +471,7 @@ def attn_mass(desc, window, q, k_cache, v_cache, ctx_lens, out, lse, mass_in, ma
 
 def mass_to_index(mass, ctx_lens, budget, sinks, recent, index, counts, dev_status=None, stream=None, check=True):
     """ssa_mass_to_index: the positions of mass[B, max_ctx] that the budget keeps -> index[B, index_stride], counts[B]."""
-    _check_mass(mass, 1)
+    _check_mass(mass, ctx_lens.numel(), 1)
     rc = _call.mass_to_index(mass, ctx_lens, mass.shape[1], budget, sinks, recent, index, counts, dev_status, _stream(stream))
     return _check("ssa_mass_to_index", rc, check)
 
@@ -480,7 +480,7 @@ def cache_compact(desc, k_cache, v_cache, ctx_lens, index, counts, max_selected,
                   stream=None, check=True):
     """ssa_cache_compact: listed rows of K and V (and entries of mass[B, max_ctx]) to the front, in place."""
     if mass is not None:
-        _check_mass(mass, desc.max_ctx)
+        _check_mass(mass, desc.B, desc.max_ctx)
     rc = _call.cache_compact(desc, paging, k_cache, v_cache, ctx_lens, index, counts, max_selected, mass, dev_status,
                              _stream(stream))
     return _check("ssa_cache_compact", rc, check)

@@ -14,3 +14,20 @@ def test_lengths_of_new_tokens_are_one_per_request_side_by_side():
     for good in (lens[1], lens, lens[0, :3].view(3, 1)):
         assert ssa.make_window(q, q, q_lens=good).q_lens == good.data_ptr()
     assert ssa.make_window(q[:1], q[:1], q_lens=lens[2:3, 0]).q_lens == lens[2, 0].data_ptr()
+
+
+def test_sums_have_a_row_for_every_request():
+    d, w = ssa.AttnDesc(), ssa.Window()
+    d.B, d.max_ctx = 3, 40
+    i = torch.zeros(3, 40, dtype=torch.int32)
+    few, enough = torch.zeros(2, 40), torch.zeros(3, 40)
+    calls = {"attn_mass": lambda m: ssa.attn_mass(d, w, None, None, None, None, None, None, None, m, stream=0),
+             "attn_mass in": lambda m: ssa.attn_mass(d, w, None, None, None, None, None, None, m, enough, stream=0),
+             "mass_to_index": lambda m: ssa.mass_to_index(m, i[:, 0], 41, 0, 0, i, i[:, 0], stream=0),
+             "cache_compact": lambda m: ssa.cache_compact(d, None, None, None, i, None, 5, mass=m, stream=0)}
+    for name, call in calls.items():
+        for bad in (few, enough[0], enough[None]):
+            with pytest.raises(ValueError, match="3 rows of"):
+                call(bad)
+        with pytest.raises(ssa.SsaError):                    # (on to the library, which refuses the rest)
+            call(enough)
