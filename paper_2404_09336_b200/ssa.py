@@ -458,11 +458,11 @@ def attn_mass_workspace_bytes(desc: AttnDesc, window: Window) -> int:
 def attn_mass(desc, window, q, k_cache, v_cache, ctx_lens, out, lse, mass_in, mass_out, decay=1.0, workspace=None,
               dev_status=None, stream=None, check=True):
     """ssa_attn_mass: attn_window, and mass_out[B, max_ctx] = decay * mass_in + the weight of every position (mass_in: a tensor
-    of mass_out's strides, mass_out itself, or None)."""
+    of mass_out's row stride, where there are several rows, mass_out itself, or None)."""
     _check_mass(mass_out, desc.B, desc.max_ctx)
     if mass_in is not None and mass_in is not mass_out:
         _check_mass(mass_in, desc.B, desc.max_ctx)
-        if _row_stride(mass_in) != _row_stride(mass_out):
+        if desc.B > 1 and _row_stride(mass_in) != _row_stride(mass_out):
             raise ValueError("mass_in and mass_out must have the same row stride")
     rc = _call.attn_mass(desc, window, q, k_cache, v_cache, ctx_lens, out, lse, mass_in, mass_out, decay, workspace,
                          dev_status, _stream(stream))

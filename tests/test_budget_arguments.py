@@ -31,3 +31,14 @@ def test_sums_have_a_row_for_every_request():
                 call(bad)
         with pytest.raises(ssa.SsaError):                    # (on to the library, which refuses the rest)
             call(enough)
+
+
+def test_one_row_of_sums_has_no_row_stride():
+    d, w = ssa.AttnDesc(), ssa.Window()
+    d.B, d.max_ctx = 1, 40
+    call = lambda a, b: ssa.attn_mass(d, w, None, None, None, None, None, None, a, b, stream=0)
+    with pytest.raises(ssa.SsaError):                        # (on to the library, which refuses the rest)
+        call(torch.zeros(1, 64), torch.zeros(1, 40))
+    d.B = 2
+    with pytest.raises(ValueError, match="row stride"):
+        call(torch.zeros(2, 64), torch.zeros(2, 40))
