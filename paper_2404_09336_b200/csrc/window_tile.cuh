@@ -59,15 +59,21 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
   return ok;
 }
 constexpr long long kPatience = 4000000000;         // cycles
-// Waits end: after some two seconds the block gives up (*dead), and everything in it runs to its end without waiting.
-__device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
+// Waits end: after some two seconds the block gives up (*dead), and everything in it runs to its end without waiting, asking for
+// no more copies.  What is under way then is still waited for (mbar_drain): nothing arrives in memory that is another block's by
+// that time.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {      // false: given up
   for (int i = 0; i < 64; ++i)
-    if (mbar_try(bar, parity)) return;
+    if (mbar_try(bar, parity)) return true;
   const long long since = clock64();
   while (!mbar_try(bar, parity)) {
-    if (*dead) return;
-    if (clock64() - since > kPatience) { *dead = 1; return; }
+    if (*dead) return false;
+    if (clock64() - since > kPatience) { *dead = 1; return false; }
   }
+  return true;
+}
+__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
+  for (const long long since = clock64(); !mbar_try(bar, parity) && clock64() - since <= kPatience;) {}
 }
 __device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap* map, int x, int row, int head, int b, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
@@ -188,7 +194,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
   __shared__ __align__(8) uint64_t s_bar[3 * kStages + 4];
   __shared__ uint32_t s_tmem;
   __shared__ int64_t s_row[2][kTileRows];                              // where a row starts in q and in out
-  __shared__ int s_dead;
+  __shared__ int s_dead, s_asked;                                      // the block has given up; copies asked for
   const uint32_t base = (smem_at(smem_raw) + 1023) & ~1023u;
   uint8_t* const smem = smem_raw + (base - smem_at(smem_raw));
   const uint32_t full = smem_at(s_bar), empty = full + 8 * kStages, fixed = empty + 8 * kStages, s_full = fixed + 8 * kStages,
@@ -267,6 +273,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
       mbar_init(o_full, 1);
       for (int half = 0; half < 2; ++half) mbar_init(p_full + 8 * half, kTileRows);
       s_dead = 0;
+      s_asked = n_loads;
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
@@ -308,7 +315,10 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     settle(min(kStages, n_loads) - 2);
     for (int i = kStages; i < n_loads; ++i) {
-      mbar_wait(empty + 8 * (i % kStages), (i / kStages - 1) & 1, dead);
+      if (!__all_sync(~0u, mbar_wait(empty + 8 * (i % kStages), (i / kStages - 1) & 1, dead))) {
+        s_asked = i;
+        break;
+      }
       load(i);
       settle(i - 1);
     }
@@ -540,8 +550,14 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
   tc_before();
   __syncthreads();
   tc_after();
+  if (s_dead) {                                              // (otherwise all that was asked for has been waited for)
+    for (int i = max(0, s_asked - kStages); i < s_asked; ++i) mbar_drain(full + 8 * (i % kStages), (i / kStages) & 1);
+    if (n_tiles > 0) mbar_drain(o_full, 0);                  // instructions end in order: these have all
+    if (threadIdx.x == 0 && p.status) atomicOr(p.status, SSA_DEV_GAVE_UP);
+    __syncthreads();
+    tc_after();
+  }
   if (warp == 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(256));
-  if (threadIdx.x == 0 && s_dead && p.status) atomicOr(p.status, SSA_DEV_GAVE_UP);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
