@@ -474,12 +474,15 @@ int32_t ssa_decode_attn_blockmask(const ssa_attn_desc* desc, const void* q, cons
  *   workspace  dev, 16-byte aligned, >= ssa_attn_window_workspace_bytes(desc,
  *            window) (0: invalid arguments); needs no initialisation.  Calls
  *            that may run at the same time (other streams, graphs) need one each
- * Up to 24 rows per K/V head (tokens x grouped heads) keep their softmax weights
- * to 16 bits (bf16) or 22; more rows over a 16-bit cache, and with pages of eight
- * rows at least, go to tensor-core tiles that round each weight to the cache's
- * type once (a relative 2^-8 of bf16, 2^-11 of fp16: as much as an output of
- * that type is rounded; scores, maxima, sums and lse are fp32).  A long context
- * of few rows is split over the GPU and joined in a second launch.
+ * Softmax weights enter the second product as two 16-bit parts (16 bits of bf16,
+ * 22 of fp16 and of an 8-bit cache) - except where more than 24 rows per K/V head
+ * (tokens x grouped heads) over a 16-bit cache go to tensor-core tiles and
+ * out_dtype is the cache's type: those round each weight to that type once (a
+ * relative 2^-8 of bf16, 2^-11 of fp16: as much as the output is rounded).  Ask
+ * for fp32 outputs to have both parts there too.  (Pages of fewer than eight
+ * rows, strides of zero and ssa_attn_mass do not go to the tiles.)  Scores,
+ * maxima, sums and lse are fp32.  A long context of few rows is split over the
+ * GPU and joined in a second launch.
  * Errors: SSA_ERR_NULL, SSA_ERR_SHAPE, SSA_ERR_DTYPE, SSA_ERR_ALIGN,
  * SSA_ERR_WORKSPACE, SSA_ERR_UNSUPPORTED, SSA_ERR_CUDA.
  */

@@ -750,7 +750,8 @@ static size_t window_bytes(const ssa_attn_desc* d, const ssa_window* w, bool mas
 template <typename T, int D>
 static cudaError_t launch_tiles(const WindowParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, int box_rows, cudaStream_t st) {
   const dim3 grid((unsigned)((p.group * p.n_q + kTileRows - 1) / kTileRows * p.n_splits), (unsigned)p.H_kv, (unsigned)p.B);
-  auto kernel = p.page_table ? window_tile_kernel<T, D, true> : window_tile_kernel<T, D, false>;
+  auto kernel = p.page_table ? (p.out_f32 ? window_tile_kernel<T, D, true, true> : window_tile_kernel<T, D, true, false>)
+                             : (p.out_f32 ? window_tile_kernel<T, D, false, true> : window_tile_kernel<T, D, false, false>);
   constexpr int kSmem = TileShape<D>::kSmem;
   const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (err != cudaSuccess) return err;

@@ -3,7 +3,7 @@
 // A block serves 128 (token, head of the group) rows of one K/V head and goes through the tiles of 128 positions that they see
 // between them.  Both contractions are tcgen05.mma in steps of 16 with fp32 accumulators:
 //   S = Q . K^T   128 x 128; Q and K in shared memory (128-byte swizzle, K by TMA), S in TMEM
-//   O += P . V    128 x D; P, the weights as 16-bit values, in TMEM over the first half of S; V in shared memory as it lies
+//   O += P . V    128 x D; P, the weights as 16-bit values, in TMEM over the first half of S (both halves: two parts); V in shared memory as it lies
 // Warps 0-3 do the softmax, a thread per row; warp 4 issues the matrix instructions, warp 5 the copies (6 and 7 make up its group
 // of four).  A tile's chain - scores, softmax, sums, the next scores - takes some 3500 cycles, of which the tensor cores work
 // 1024 and the softmax 2000; two blocks share an SM (half its TMEM each, a K and a V tile in flight besides the one at work), so
@@ -14,9 +14,10 @@
 //
 // The running maximum that weights are relative to follows the true one only where that is more than 2^8 above it, so that O
 // is rescaled in a few tiles at the start and hardly ever after that; weights are then at most 2^8 (fp16: times 2^6, which
-// the sum divides out again, because fp16 has little range below 1), rounded once to 16 bits: the two parts that the kernel
-// for few rows takes would cost a third contraction, and the rounding is that of a 16-bit output.  (Instructions, not the special
-// function unit, bound the softmax: with a quarter of the powers on the FMA units prompts took 7 % longer.)
+// the sum divides out again, because fp16 has little range below 1).  For a 16-bit output they are rounded once to 16 bits: as much
+// as that output is rounded.  An fp32 output keeps the rest of each weight as a second 16-bit part, over the other half of S, with
+// a contraction of its own, as in the kernel for few rows.  (Instructions, not the special function unit, bound the softmax: with a
+// quarter of the powers on the FMA units prompts took 7 % longer.)
 #pragma once
 #include <cuda.h>
 
@@ -182,8 +183,8 @@ __device__ __noinline__ void careful_row(const WindowParams& p, const Seen& seen
   for (int i = 0; i < kN; ++i) acc[i] += odd[i];
 }
 
-// grid (splits x row blocks, H_kv, B), the last row blocks first: they see most.
-template <typename T, int D, bool kPaged>
+// grid (splits x row blocks, H_kv, B), the last row blocks first: they see most.  kBoth: weights in two 16-bit parts.
+template <typename T, int D, bool kPaged, bool kBoth>
 __global__ void __launch_bounds__(kTileThreads, 2)
 window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                    const int box_rows) {
@@ -360,7 +361,10 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
         tc_after();
         if (leader) {
 #pragma unroll
-          for (int s = 4 * half; s < 4 * half + 4; ++s) mma_ts(tmem + 128, tmem + s * 8, vd + s * (2048 >> 4), kIdO, tile > 0 || s > 0);
+          for (int s = 4 * half; s < 4 * half + 4; ++s) {
+            mma_ts(tmem + 128, tmem + s * 8, vd + s * (2048 >> 4), kIdO, tile > 0 || s > 0);
+            if constexpr (kBoth) mma_ts(tmem + 128, tmem + 64 + s * 8, vd + s * (2048 >> 4), kIdO, true);
+          }
           if (half) {
             tc_commit(empty + 8 * stage);
             if (tile + 1 == n_tiles) tc_commit(o_full);
@@ -446,7 +450,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
       float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        uint32_t w[32];
+        uint32_t w[32], rest[kBoth ? 32 : 1];
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
           const int e = half * 64 + 2 * i;
@@ -454,8 +458,13 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
           y = make_float2(fast_exp2(y.x), fast_exp2(y.y));
           sum[i & 1] = add2(sum[i & 1], y);
           w[i] = pack2<T>(y.x, y.y);
+          if constexpr (kBoth) {
+            const float2 back = unpack2<T>(w[i]);
+            rest[i] = pack2<T>(y.x - back.x, y.y - back.y);
+          }
         }
         tc_st32(s_at + half * 32, w);
+        if constexpr (kBoth) tc_st32(s_at + 64 + half * 32, rest);
         tc_wait_st();
         tc_before();
         mbar_arrive(p_full + 8 * half);             // its contraction starts meanwhile

@@ -39,3 +39,23 @@ def test_strides_of_zero_are_left_to_the_kernel_for_few_rows(n_q, heads, request
     p.host, p.stores = [share(x) for x in p.host], [share(x) for x in p.stores]
     for window, sinks in ((0, 0), (2, 1), (70, 3)):
         run(p, [300, 233], None, window, sinks)
+
+
+@pytest.mark.parametrize("dtype,H,H_kv,D,n_q,page", [("bf16", 4, 4, 128, 130, 0), ("bf16", 8, 2, 64, 75, 0), ("f16", 4, 1, 64, 300, 0), ("f16", 6, 2, 128, 64, 0),
+                                                     ("bf16", 8, 2, 128, 150, 8), ("f16", 4, 2, 128, 90, 32), ("bf16", 4, 2, 64, 257, 512)])
+def test_fp32_outputs_of_the_tiles_have_weights_of_two_parts(dtype, H, H_kv, D, n_q, page):
+    T = 700
+    p = Tokens(3, H, H_kv, T, D, n_q, dtype, page=page)
+    assert tiles_serve(p)
+    ctx, new = [T, max(n_q, 333), 31], [n_q, n_q - n_q // 3, n_q]
+    for window, sinks in ((0, 0), (3, 1), (50, 7), (128, 130)):
+        got = p.call(ctx, new, window, sinks, torch.float32)
+        check(p, got, ctx, new, window, sinks, torch.float32, many=False)
+
+
+def test_fp32_outputs_of_a_chunk_over_a_split_context():
+    p = Tokens(1, 4, 2, 5000, 128, 40)
+    assert tiles_serve(p)
+    for window, sinks in ((0, 0), (2500, 64)):
+        got = p.call([5000], None, window, sinks, torch.float32)
+        check(p, got, [5000], None, window, sinks, torch.float32, many=False)
