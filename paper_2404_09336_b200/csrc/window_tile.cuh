@@ -7,10 +7,12 @@
 // Warps 0-3 do the softmax, a thread per row; warp 4 issues the matrix instructions, warp 5 the copies (6 and 7 make up its group
 // of four).  A tile's chain - scores, softmax, sums, the next scores - takes some 3500 cycles, of which the tensor cores work
 // 1024 and the softmax 2000; two blocks share an SM (half its TMEM each, a K and a V tile in flight besides the one at work), so
-// that one's chain, start and end fill the other's gaps.  Whole prompts (4 x 4096 tokens, 32 heads, window 1024, 64 sinks):
-//   407 us, 623 TFLOP/s of visible pairs; with one block of 256 rows to an SM, its halves alternating, 446 (a block's start and
-//   end, a third of its time, stood alone); with tiles of 64 positions and two S in turn, 524 (an instruction of 128 x 64 takes as
-//   long as one of 128 x 128: the 128 rows of Q are read either way); full causal prompts 619 us, 889 TFLOP/s.
+// that one's chain, start and end fill the other's gaps.  Whole prompts (4 x 4096 tokens, 32 heads, window 1024, 64 sinks) in runs
+// of many calls, at the clock that the power limit leaves:
+//   452 us, 561 TFLOP/s of visible pairs; full causal prompts 707 us, 778 TFLOP/s; fp32 outputs 609 and 976 us.
+// In 20 calls in a row, where clocks are higher, 407 us; there with one block of 256 rows to an SM, its halves alternating, 446 (a
+// block's start and end, a third of its time, stood alone); with tiles of 64 positions and two S in turn 524, when this form took
+// 485 (an instruction of 128 x 64 takes as long as one of 128 x 128: the 128 rows of Q are read either way).
 //
 // The running maximum that weights are relative to follows the true one only where that is more than 2^8 above it, so that O
 // is rescaled in a few tiles at the start and hardly ever after that; weights are then at most 2^8 (fp16: times 2^6, which
