@@ -66,6 +66,8 @@ constexpr long long kPatience = 4000000000;         // cycles
 // no more copies.  What is under way then is still waited for (mbar_drain): nothing arrives in memory that is another block's by
 // that time.
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {      // false: given up
+  if (mbar_try(bar, parity)) return true;
+  if (*dead) return false;                                   // (a try may last: one for each wait that is left)
   for (int i = 0; i < 64; ++i)
     if (mbar_try(bar, parity)) return true;
   const long long since = clock64();
@@ -534,7 +536,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
         p.ws_ml[slot] = make_float2(m - kShift, l);
       }
     }
-    unsigned again = __ballot_sync(~0u, there && l != 0.f && !(test.x + test.y == 0.f));
+    unsigned again = __ballot_sync(~0u, there && l != 0.f && !(test.x + test.y == 0.f) && !*dead);
     __syncwarp();
     while (again) {                                          // rows that met an infinity or a NaN, or what they must not see
       const int i = __ffs(again) - 1;
