@@ -126,7 +126,7 @@ class DecodeStep:
         if need == 0:
             raise RuntimeError("ssa_decode_workspace_bytes rejected the descriptor")
         self.workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-        self._rooms = []
+        self._rooms, self._outgrown = [], []
         self._steps = {}
         if dev.type == "cuda":                               # calls may come on any stream: what was filled above is there
             torch.cuda.current_stream(dev).synchronize()
@@ -243,6 +243,7 @@ class DecodeStep:
         self.block_counts = torch.zeros((B,), dtype=torch.int32, device=dev)
         need = ssa.decode_blockmask_workspace_bytes(self.desc, block_size, self.block_stride)
         if need > self.workspace.numel():
+            self._outgrown.append(self.workspace)            # graphs captured with it go on using it
             self.workspace = torch.empty(need, dtype=torch.uint8, device=dev)
             self._steps = {}
 

@@ -160,3 +160,15 @@ def test_contexts_are_no_longer_than_what_was_moved(made):
     ds.counts.copy_(torch.tensor([bound + 9, -7, 8]))        # clamped by the call: its bound, nothing, its context
     ds.compact()
     assert ds.ctx_lens.tolist() == [bound, 0, 7]
+
+
+def test_a_workspace_that_block_lists_outgrow_stays_alive(made, monkeypatch):
+    import gc
+    import weakref
+    ds = small()
+    ds.attend_dense()
+    ref = weakref.ref(made.pop()[1]["workspace"])
+    monkeypatch.setattr(ssa, "decode_blockmask_workspace_bytes", lambda *a: ds.workspace.numel() + 1)
+    ds.enable_blockmask()
+    gc.collect()
+    assert ref() is not None and ds.workspace is not ref()   # a captured graph may still hold its address
