@@ -3,7 +3,8 @@
 // A block serves 128 (token, head of the group) rows of one K/V head and goes through the tiles of 128 positions that they see
 // between them.  Both contractions are tcgen05.mma in steps of 16 with fp32 accumulators:
 //   S = Q . K^T   128 x 128; Q and K in shared memory (128-byte swizzle, K by TMA), S in TMEM
-//   O += P . V    128 x D; P, the weights as 16-bit values, in TMEM over the first half of S (both halves: two parts); V in shared memory as it lies
+//   O += P . V    128 x D; P, the weights as 16-bit values, in TMEM over the first half of S (two parts: over both); V in
+//                 shared memory as it lies
 // Warps 0-3 do the softmax, a thread per row; warp 4 issues the matrix instructions, warp 5 the copies (6 and 7 make up its group
 // of four).  A tile's chain - scores, softmax, sums, the next scores - takes some 3500 cycles, of which the tensor cores work
 // 1024 and the softmax 2000; two blocks share an SM (half its TMEM each, a K and a V tile in flight besides the one at work), so
