@@ -70,7 +70,7 @@ enum {
 
 #define SSA_MAX_SPANS_PER_SEQ 2048
 
-typedef enum { SSA_F16 = 0, SSA_BF16 = 1, SSA_F32 = 2, SSA_FP8_E4M3 = 3 } ssa_dtype;
+typedef enum { SSA_F16 = 0, SSA_BF16 = 1, SSA_F32 = 2, SSA_FP8_E4M3 = 3, SSA_FP4_E2M1 = 4 } ssa_dtype;
 
 /*
  * Geometry of q, the KV cache and the output.  Strides are in ELEMENTS; the
@@ -567,6 +567,182 @@ int32_t ssa_mass_to_index(const float* mass, int64_t mass_stride, const int32_t*
 int32_t ssa_cache_compact(const ssa_attn_desc* desc, const ssa_paging* paging, void* k_cache, void* v_cache,
                           const int32_t* ctx_lens, const int32_t* index, int32_t index_stride, const int32_t* counts,
                           int32_t max_selected, float* mass, int64_t mass_stride, uint32_t* dev_status, void* stream);
+
+/*
+ * A cache of 4-bit values, kv_dtype SSA_FP4_E2M1 (outside the paper, whose
+ * cache is 16-bit; the calls below up to ssa_cache_append take it, all others
+ * refuse it with SSA_ERR_DTYPE).  Dimension d of a row of K or V is
+ *     e4m3(scale[d / 16]) * e2m1(code[d])
+ * e2m1: sign, two bits of exponent (bias 1), one of fraction: 0, 0.5, 1, 1.5,
+ * 2, 3, 4, 6 and their negatives.  Codes lie two a byte, the lower dimension in
+ * the low half; scales, one byte for 16 dimensions, in arrays of their own.  The
+ * strides of K and V are in VALUES, multiples of D: a row that starts at value o
+ * has its codes from byte o/2 of k_cache on and its scales from byte o/16 of
+ * k_scales on (V likewise), so that codes [B, H_kv, T, D/2] go with scales
+ * [B, H_kv, T, D/16].  72 bytes hold a row of 128.  Queries and outputs are as
+ * over an 8-bit cache (BF16; outputs also F32), and so is a factor kept with the
+ * whole cache: K's folds into `scale`, V's applies to the output.
+ *
+ * ssa_attn_window_fp4 is ssa_attn_window over such a cache: the same tokens,
+ * windows, sinks, lengths, pages, results, status bits and errors (desc->kv_dtype
+ * other than SSA_FP4_E2M1: SSA_ERR_DTYPE; strides of K and V that are no
+ * multiples of D, k_cache, v_cache, k_scales, v_scales not 16-byte aligned:
+ * SSA_ERR_ALIGN).  Scores, maxima, sums and lse are fp32.  Softmax weights enter
+ * the second product as two fp16 parts (22 bits) - except where more than 24
+ * rows per K/V head (tokens x grouped heads; pages of eight rows and more) go to
+ * tensor-core tiles and out_dtype is BF16: those round each weight to fp16 once
+ * (a relative 2^-11).  A scale that is NaN makes its 16 values NaN.
+ */
+size_t ssa_attn_window_fp4_workspace_bytes(const ssa_attn_desc* desc, const ssa_window* window);
+int32_t ssa_attn_window_fp4(const ssa_attn_desc* desc, const ssa_window* window, const void* q, const void* k_cache,
+                            const void* v_cache, const void* k_scales, const void* v_scales, const int32_t* ctx_lens,
+                            void* out, float* lse, void* workspace, size_t workspace_bytes, uint32_t* dev_status,
+                            void* stream);
+
+/*
+ * Attention of each token over blocks of positions that its own queries select
+ * (outside the paper, whose model names the spans by itself): the context is cut
+ * into blocks of block_size positions, a few numbers are kept of the keys of
+ * each (ssa_block_bounds), a token ranks the blocks by them (ssa_block_select)
+ * and attends to those on its list (ssa_attn_blocks).  Lists are per request,
+ * K/V head and token.  The step's tokens are those of ssa_window: token t of
+ * request b sits at position pos = ctx_lens[b] - q_lens[b] + t, its K/V in the
+ * cache; rows t >= q_lens[b] and tokens of negative position are neither read
+ * nor written, ctx_lens[b] > max_ctx and q_lens[b] > n_q are clamped
+ * (SSA_DEV_BAD_COUNT).  n = ceil(max_ctx / block_size), SSA_MAX_BLOCKS at most,
+ * is the number of blocks that arrays have room for.
+ */
+#define SSA_MAX_BLOCKS 16384
+typedef struct {
+  int32_t n_q;                 /* query rows laid out per head and request; H*n_q <= 2^24   */
+  int32_t block_size;          /* positions of a block: 32, 64, 128 or 256                  */
+  int32_t budget;              /* entries of a list, the most that a token attends to       */
+  int32_t sinks, recent;       /* ssa_block_select: first and newest blocks, always listed  */
+  int64_t q_stride_t, o_stride_t;
+  int64_t bounds_stride_b, bounds_stride_h;   /* elements from request to request, head to head */
+  const int32_t* q_lens;       /* dev [B] or NULL: n_q tokens each                          */
+  const ssa_paging* paging;    /* host or NULL, of the cache                                */
+} ssa_blocks;
+
+/*
+ * The least and the largest value of every dimension over the keys of a block:
+ *   bounds[b*bounds_stride_b + h*bounds_stride_h + j*2*D + d]      min over the
+ *   bounds[b*bounds_stride_b + h*bounds_stride_h + j*2*D + D + d]  max    rows of
+ * K/V head h at positions [j*block_size, (j+1)*block_size) below ctx_lens[b], for
+ * every block j that holds one of the request's newest q_lens[b] positions; other
+ * blocks' entries are left as they are.  q_lens[b] >= ctx_lens[b] makes all of
+ * them anew (n_q = max_ctx and q_lens = NULL: for every request); n_q may be as
+ * large as max_ctx here.  A step that appends its tokens names those; after
+ * ssa_cache_compact all are made anew.  A NaN key makes the dimension's bounds
+ * NaN.  Rows on pages outside [0, n_pages) are left out (SSA_DEV_BAD_INDEX); a
+ * block without any has +inf and -inf.
+ *   desc     host; the fields of q, v and out are checked but not used.  kv_dtype
+ *            any; bounds (dev, written) have the type of the queries
+ *   k_scales dev, 4-bit caches only
+ * Errors: SSA_ERR_NULL, SSA_ERR_SHAPE (n_q <= 0; n above SSA_MAX_BLOCKS; negative
+ * strides), SSA_ERR_UNSUPPORTED (block_size), SSA_ERR_DTYPE, SSA_ERR_ALIGN (the
+ * bounds and their strides: 16 bytes), SSA_ERR_CUDA.
+ */
+int32_t ssa_block_bounds(const ssa_attn_desc* desc, const ssa_blocks* blocks, const void* k_cache, const void* k_scales,
+                         const int32_t* ctx_lens, void* bounds, uint32_t* dev_status, void* stream);
+
+/*
+ * The blocks that each token of the step attends to.  With q_h the token's query
+ * of head h, over the heads of a K/V head and the dimensions,
+ *   score[j] = sum_h sum_d max(q_h[d] * min_j[d], q_h[d] * max_j[d])
+ * which no sum of the heads' products with a key of the block exceeds.  Of the
+ * m = pos / block_size + 1 blocks that the token sees all are listed where m <=
+ * budget; else the first `sinks`, the newest `recent`, and of those between the
+ * budget - sinks - recent with the largest scores, of equal ones the lowest blocks
+ * (NaN ranks below everything).  Row r = (b*H_kv + h)*n_q + t of
+ *   index  dev int32 [B*H_kv*n_q, budget]: ascending; entries past the count are
+ *          left as they are
+ *   counts dev int32 [B*H_kv*n_q]: min(m, budget)
+ *   scores dev float [B*H_kv*n_q, n] or NULL: entries [0, m) of the row
+ * Scores are summed in 64 bits and rounded to 32 once, so that lists do not depend
+ * on the order of summation.  (bounds of a block hold all its keys, those behind
+ * the token's own position among them.)
+ *   desc     host; the fields of k, v and out are checked but not used, but for
+ *            H_kv; q and bounds (dev) have the queries' type for kv_dtype
+ * Errors: SSA_ERR_NULL, SSA_ERR_SHAPE, SSA_ERR_UNSUPPORTED, SSA_ERR_DTYPE,
+ * SSA_ERR_ALIGN, SSA_ERR_CAPACITY (budget <= 0; sinks or recent negative or
+ * together above the budget), SSA_ERR_CUDA.
+ */
+int32_t ssa_block_select(const ssa_attn_desc* desc, const ssa_blocks* blocks, const void* q, const void* bounds,
+                         const int32_t* ctx_lens, int32_t* index, int32_t* counts, float* scores,
+                         uint32_t* dev_status, void* stream);
+
+/*
+ * Attention of each token over the blocks of its list: the Background equations
+ * over the positions j <= pos of blocks index[r*budget .. + counts[r]), r =
+ * (b*H_kv + h)*n_q + t, for the query heads of K/V head h.  Lists need not be
+ * sorted; a block listed twice counts twice; one outside [0, pos / block_size] is
+ * skipped (SSA_DEV_BAD_INDEX); counts[r] > budget is clamped (SSA_DEV_BAD_COUNT).
+ * q, out and lse are laid out, and rows without a position written, as by
+ * ssa_attn_window; infinities and NaN likewise.  kv_dtype any; k_scales and
+ * v_scales (dev) for 4-bit caches only.
+ *   workspace  dev, 16-byte aligned, >= ssa_attn_blocks_workspace_bytes(desc,
+ *              blocks) (0: invalid arguments); one for each of the calls that may
+ *              run at the same time
+ * Softmax weights enter as two 16-bit parts, scores and sums are fp32.
+ * Errors: those of ssa_attn_window, SSA_ERR_CAPACITY (budget <= 0) and
+ * SSA_ERR_UNSUPPORTED (block_size).
+ */
+size_t ssa_attn_blocks_workspace_bytes(const ssa_attn_desc* desc, const ssa_blocks* blocks);
+int32_t ssa_attn_blocks(const ssa_attn_desc* desc, const ssa_blocks* blocks, const void* q, const void* k_cache,
+                        const void* v_cache, const void* k_scales, const void* v_scales, const int32_t* ctx_lens,
+                        const int32_t* index, const int32_t* counts, void* out, float* lse, void* workspace,
+                        size_t workspace_bytes, uint32_t* dev_status, void* stream);
+
+/*
+ * A step's keys and values into the cache, rotated by position on the way, and
+ * its queries rotated (outside the paper, where the caller appends before the
+ * call).  ctx_lens counts the step's tokens already: token t of request b goes to
+ * position pos = ctx_lens[b] - q_lens[b] + t.  Rows t >= q_lens[b] and tokens of
+ * negative position are neither read nor written; ctx_lens[b] > max_ctx and
+ * q_lens[b] > n_q are clamped (SSA_DEV_BAD_COUNT).  With R = rotary_dims and
+ * (c_i, s_i) = cos_sin[p*R + i], cos_sin[p*R + R/2 + i] for p = positions[b*n_q +
+ * t] (NULL: pos), i < R/2, the pairs (x_i, x_{i+R/2}) of a query or key, or
+ * (x_{2i}, x_{2i+1}) where `interleaved`, become
+ *     (x c_i - y s_i,  y c_i + x s_i)
+ * computed in 64 bits and rounded to fp32; the dimensions from R on stay.  Keys
+ * times k_factor and values times v_factor (<= 0 selects 1) are then stored: a
+ * 16-bit cache rounds to nearest; SSA_FP8_E4M3 too, beyond 448 to 448;
+ * SSA_FP4_E2M1 takes for each 16 dimensions the scale e4m3(max |x| / 6), at most
+ * 448, and the codes e2m1(x / scale), rounded to nearest and to even halfway, zero
+ * where the scale is zero.  Queries are rounded to their type.
+ * A token whose p lies outside [0, n_positions) is left out as a whole, one whose
+ * page lies outside [0, n_pages) keeps only its rotated queries
+ * (SSA_DEV_BAD_INDEX).  Positions of one step must not share a row of the cache.
+ *   desc     host; out's fields are checked but not used.  k_new and v_new have the
+ *            type of the queries
+ *   q, q_out dev or both NULL: queries to rotate.  They may be the same rows
+ *   k_new, v_new  dev [b, h, t, :] at the strides below, elements
+ *   cos_sin  dev float [n_positions, R], NULL where R = 0
+ * Errors: SSA_ERR_NULL, SSA_ERR_SHAPE (n_q, R no multiple of 32 in [0, D],
+ * n_positions), SSA_ERR_DTYPE, SSA_ERR_ALIGN (all rows: 16 bytes; cos_sin too),
+ * SSA_ERR_UNSUPPORTED (K and V in one place, strides of zero between the cache's
+ * rows, heads or requests), SSA_ERR_CUDA.
+ */
+typedef struct {
+  int32_t n_q;                 /* rows laid out per head and request; H*n_q <= 2^24 */
+  int32_t rotary_dims;         /* R: a multiple of 32, 0: no rotation               */
+  int32_t interleaved;
+  int32_t n_positions;         /* rows of cos_sin                                   */
+  float k_factor, v_factor;
+  int64_t q_stride_t;          /* (q's other strides are the descriptor's)          */
+  int64_t qo_stride_b, qo_stride_h, qo_stride_t;
+  int64_t kn_stride_b, kn_stride_h, kn_stride_t;
+  int64_t vn_stride_b, vn_stride_h, vn_stride_t;
+  const float* cos_sin;        /* dev                                               */
+  const int32_t* positions;    /* dev [B*n_q] or NULL                               */
+  const int32_t* q_lens;       /* dev [B] or NULL: n_q tokens each                  */
+  const ssa_paging* paging;    /* host or NULL                                      */
+} ssa_append;
+
+int32_t ssa_cache_append(const ssa_attn_desc* desc, const ssa_append* append, const void* k_new, const void* v_new,
+                         const int32_t* ctx_lens, void* k_cache, void* v_cache, const void* q, void* q_out,
+                         void* k_scales, void* v_scales, uint32_t* dev_status, void* stream);
 
 /*
  * One decode step of the method in one call (Sec. "Self-selected attention

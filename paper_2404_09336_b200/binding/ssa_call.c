@@ -18,14 +18,17 @@
   X(spans_to_index) X(decode_attn_sparse) X(decode_attn_spans) X(decode_attn_sparse_multiq) X(decode_attn_dense_multiq) \
   X(spans_to_blockmask) X(decode_attn_blockmask) X(decode_attn_sparse_paged) X(decode_attn_dense_paged)               \
   X(refs_to_index) X(refs_to_spans) X(decode_step) X(decode_attn_sparse_noalloc) X(decode_attn_dense)                 \
-  X(attn_window) X(attn_mass) X(mass_to_index) X(cache_compact)
+  X(attn_window) X(attn_mass) X(mass_to_index) X(cache_compact)                                                     \
+  X(attn_window_fp4) X(block_bounds) X(block_select) X(attn_blocks) X(cache_append)
 
 /* Structures that a caller fills.  Only instances of the class that bind() was given for one are taken (without a class:
  * buffers of its exact size), so that no other structure and no other buffer is read as sizes and strides. */
-enum { kDesc, kStep, kPaging, kWindow, kStructures };
-static const char* const structure_name[kStructures] = {"ssa_attn_desc", "ssa_step", "ssa_paging", "ssa_window"};
+enum { kDesc, kStep, kPaging, kWindow, kBlocks, kAppend, kStructures };
+static const char* const structure_name[kStructures] = {"ssa_attn_desc", "ssa_step", "ssa_paging", "ssa_window", "ssa_blocks",
+                                                        "ssa_append"};
 static const size_t structure_size[kStructures] = {sizeof(ssa_attn_desc), sizeof(ssa_step), sizeof(ssa_paging),
-                                                     sizeof(ssa_window)};
+                                                     sizeof(ssa_window), sizeof(ssa_blocks), sizeof(ssa_append)};
+static const char structure_kind[kStructures + 1] = "DSPQKA";         /* in a format */
 
 typedef struct {
 #define X(name) __typeof__(&ssa_##name) name;
@@ -104,7 +107,7 @@ static int structure(const State* st, int which, PyObject* o, Py_buffer* held) {
   return -1;
 }
 
-/* format: D ssa_attn_desc, S ssa_step, P ssa_paging or None, Q ssa_window, f number as a float, t tensor or None, r tensor or None and its row stride,
+/* format: D ssa_attn_desc, S ssa_step, P ssa_paging or None, Q ssa_window, K ssa_blocks, A ssa_append, f number as a float, t tensor or None, r tensor or None and its row stride,
  * w tensor or None and its bytes, i integer, n tensor and its number of elements. */
 static int parse(const State* st, Args* x, const char* name, const char* format, PyObject* const* a, Py_ssize_t n) {
   int np = 0, nv = 0;
@@ -122,7 +125,9 @@ static int parse(const State* st, Args* x, const char* name, const char* format,
       case 'D':
       case 'S':
       case 'Q':
-        if (structure(st, format[i] == 'D' ? kDesc : format[i] == 'S' ? kStep : format[i] == 'Q' ? kWindow : kPaging, o, &x->held[x->n_held]) < 0) goto bad;
+      case 'K':
+      case 'A':
+        if (structure(st, (int)(strchr(structure_kind, format[i]) - structure_kind), o, &x->held[x->n_held]) < 0) goto bad;
         x->p[np++] = x->held[x->n_held++].buf;
         break;
       case 'f': {
@@ -219,6 +224,15 @@ CALL(mass_to_index, "rniiii" "rtti",
      (p[0], v[0], p[1], I(1), I(2), I(3), I(4), I(5), p[2], I(6), p[3], p[4], STREAM(7)))
 CALL(cache_compact, "DPtttrti" "rti",
      (p[0], p[1], p[2], p[3], p[4], p[5], I(0), p[6], I(1), p[7], v[2], p[8], STREAM(3)))
+
+CALL(attn_window_fp4, "DQttttt" "ttt" "wti",
+     (p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], (size_t)v[0], p[11], STREAM(1)))
+CALL(block_bounds, "DKtt" "ttti", (p[0], p[1], p[2], p[3], p[4], p[5], p[6], STREAM(0)))
+CALL(block_select, "DKtt" "ttttti", (p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], STREAM(0)))
+CALL(attn_blocks, "DKttttt" "ttt" "tt" "wti",
+     (p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], p[11], p[12], (size_t)v[0], p[13], STREAM(1)))
+CALL(cache_append, "DAttt" "tttt" "ttti",
+     (p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], p[11], STREAM(0)))
 
 static ssa_anchor_tables tables(void* const* p) {
   ssa_anchor_tables t;

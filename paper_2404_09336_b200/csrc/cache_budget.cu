@@ -2,7 +2,7 @@
 // (ssa_cache_compact).
 #include <algorithm>
 
-#include "ssa_common.cuh"
+#include "ranking.cuh"
 
 namespace ssa {
 
@@ -13,12 +13,6 @@ namespace ssa {
 // the first few equal ones, numbered by a prefix sum over (item, warp) counts.  Latency bounds it: a request is a few dozen KB.
 constexpr int kBins = 2048;
 
-__device__ __forceinline__ uint32_t order_key(float x) {
-  if (x != x) return 0;                                    // NaN ranks below everything
-  const uint32_t u = __float_as_uint(x == 0.f ? 0.f : x);  // -0 equals 0
-  return (u & 0x80000000u) ? ~u : u | 0x80000000u;         // -inf is 0x007fffff: above NaN
-}
-
 struct KeepParams {
   const float* mass;
   const int32_t* ctx_lens;
@@ -28,36 +22,6 @@ struct KeepParams {
   int64_t mass_stride;
   int max_ctx, budget, sinks, recent, index_stride;
 };
-
-__device__ __forceinline__ int warp_inclusive(int x, int lane) {
-#pragma unroll
-  for (int o = 1; o < 32; o *= 2) {
-    const int y = __shfl_up_sync(~0u, x, o);
-    if (lane >= o) x += y;
-  }
-  return x;
-}
-
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// A word of another block's shared memory.
-__device__ __forceinline__ void store_to(const void* mine, uint32_t rank, uint32_t v) {
-  uint32_t at = (uint32_t)__cvta_generic_to_shared(mine);
-  asm volatile("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(at) : "r"(rank));
-  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
-}
-__device__ __forceinline__ uint32_t load_from(const void* mine, uint32_t rank) {
-  uint32_t at = (uint32_t)__cvta_generic_to_shared(mine), v;
-  asm volatile("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(at) : "r"(rank));
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-  return v;
-}
 
 // grid (blocks of a request, requests): kItems keys a thread, in registers: four neighbouring positions of each of the parts that a
 // block has.  Several blocks of a request are a cluster; each adds up its share of all blocks' bins over distributed shared memory
@@ -278,24 +242,6 @@ mass_keep_kernel(const KeepParams p) {
   }
 }
 
-// A request's blocks as one cluster.
-template <typename... KArgs, typename... Args>
-static cudaError_t launch_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, cudaStream_t stream, Args... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = grid.x;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
-
 // Few positions take few threads, whose barriers are short (512 positions: 256 threads of 4 items 4.6 us, of 16 items 7.5); a block
 // has up to 1024 x 16, a cluster eight times that.
 static cudaError_t launch_keep(const KeepParams& p, int B, cudaStream_t st) {
@@ -305,7 +251,7 @@ static cudaError_t launch_keep(const KeepParams& p, int B, cudaStream_t st) {
   if (p.max_ctx <= kBlock) return launch_pdl(mass_keep_kernel<1024, 16, false>, dim3(1, (unsigned)B), dim3(1024), st, p);
   if (p.max_ctx > kMost * kBlock) return launch_pdl(mass_keep_kernel<1024, 16, true>, dim3(1, (unsigned)B), dim3(1024), st, p);
   const unsigned blocks = p.max_ctx <= 2 * kBlock ? 2 : p.max_ctx <= 4 * kBlock ? 4 : 8;
-  return launch_cluster(mass_keep_kernel<1024, 16, false>, dim3(blocks, (unsigned)B), dim3(1024), st, p);
+  return launch_cluster(mass_keep_kernel<1024, 16, false>, blocks, dim3(blocks, (unsigned)B), dim3(1024), 0, st, p);
 }
 
 // ---- moving their rows ----------------------------------------------------------------------------------------------

@@ -1,0 +1,25 @@
+// Window attention over a cache of 4-bit values (ssa_attn_window_fp4): the kernels of window_rows.cuh for such rows.
+#include "window_rows.cuh"
+
+namespace ssa {
+
+template <int D>
+static int32_t launch(const Fp4Params& p, cudaStream_t st) {
+  cudaEvent_t begin, end;
+  take_kernel_events(&begin, &end);
+  if (begin) cudaEventRecord(begin, st);
+  cudaError_t err = p.page_table ? launch_rows<Fp4E2M1, D, true, false>(p, st) : launch_rows<Fp4E2M1, D, false, false>(p, st);
+  if (err != cudaSuccess) return SSA_ERR_CUDA;
+  if (end) cudaEventRecord(end, st);
+  note_launches(1);
+  if (p.n_splits == 1) return SSA_OK;
+  err = launch_pdl(window_join_kernel<__nv_bfloat16, D, Fp4Params>, dim3((unsigned)((p.H * p.n_q + kJoinWarps - 1) / kJoinWarps), (unsigned)p.B),
+                   dim3(kJoinWarps * 32), st, p);
+  if (err != cudaSuccess) return SSA_ERR_CUDA;
+  note_launches(1);
+  return SSA_OK;
+}
+
+int32_t launch_window_fp4(const Fp4Params& p, int D, cudaStream_t st) { return D == 128 ? launch<128>(p, st) : launch<64>(p, st); }
+
+}  // namespace ssa

@@ -18,7 +18,9 @@ void note_launches(int n);
 void take_kernel_events(cudaEvent_t* begin, cudaEvent_t* end);
 int32_t check_desc(const ssa_attn_desc* d);   // status of a descriptor (defined in decode_attn.cu)
 constexpr int32_t kMostContext = 1 << 30;   // positions of the calls around a budget: sums with a tile's size stay below 2^31
+int32_t check_block_sizes(const ssa_attn_desc* d, const ssa_blocks* k);   // n_q, block size, number of blocks (block_select.cu)
 int32_t check_paging(const ssa_paging* pg, int32_t max_ctx);   // status of a paged cache (defined in window_attn.cu)
+int32_t check_cache(const ssa_attn_desc* d);  // the same, of one that may have a 4-bit cache (defined in block_select.cu)
 int sm_count();   // multiprocessors of the current device (cached; no synchronisation)
 // Bytes from p to the end of the allocation it lies in, as far as that is device memory mapped as a whole; else 0.  Reading
 // these is safe whatever offsets said that they are a list.  `known`: an allocation asked for before, which may hold p too.
@@ -117,12 +119,37 @@ template <typename T> struct Storage { using Query = T; };
 template <> struct Storage<Fp8E4M3> { using Query = __nv_bfloat16; };
 template <typename T> constexpr bool kIsFp8 = false;
 template <> constexpr bool kIsFp8<Fp8E4M3> = true;
+// One stored as 4-bit e2m1 values, two a byte, with an e4m3 scale for 16 of them in an array of its own.
+struct Fp4E2M1 { uint8_t bits; };
+template <> struct Storage<Fp4E2M1> { using Query = __nv_bfloat16; };
+template <typename T> constexpr bool kIsFp4 = false;
+template <> constexpr bool kIsFp4<Fp4E2M1> = true;
+template <typename T> constexpr bool kIsNarrow = kIsFp8<T> || kIsFp4<T>;     // values that are converted to fp16 where they are used
+constexpr int kScaleDims = 16;         // dimensions of a scale
 
 // Two e4m3 values (the low 16 bits of `pair`) -> two floats (exact: every e4m3 value is an fp16 value).
 __device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t pair) {
   uint32_t h2;
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"((unsigned short)pair));
   return __half22float2(*reinterpret_cast<const __half2*>(&h2));
+}
+
+// Four bytes of two e2m1 values each (the lower dimension in the low half) -> four pairs of fp16 values (exact).
+__device__ __forceinline__ void e2m1x8_to_half2(uint32_t w, uint32_t (&h)[4]) {
+  asm("{ .reg .b8 b0, b1, b2, b3; mov.b32 {b0, b1, b2, b3}, %4; cvt.rn.f16x2.e2m1x2 %0, b0; cvt.rn.f16x2.e2m1x2 %1, b1; "
+      "cvt.rn.f16x2.e2m1x2 %2, b2; cvt.rn.f16x2.e2m1x2 %3, b3; }"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+}
+// Two e4m3 values -> two fp16 values (exact).
+__device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t pair) {
+  uint32_t h2;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"((unsigned short)pair));
+  return h2;
+}
+__device__ __forceinline__ uint32_t half2_mul(uint32_t a, uint32_t b) {
+  uint32_t y;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
+  return y;
 }
 
 // Two packed 16-bit storage values -> two floats (exact).

@@ -1,10 +1,12 @@
-// What the kernels of the window attention share: parameters, and which positions a run of query rows sees.
+// What the kernels of the window attention, and of attention over lists of blocks, share: parameters, and which positions a run
+// of query rows sees.
 #pragma once
 #include "ssa_common.cuh"
 
 namespace ssa {
 
 struct WindowParams {
+  static constexpr bool kListed = false;
   const void *q, *k, *v;
   void* out;
   float* lse;
@@ -24,8 +26,19 @@ struct WindowParams {
   float scale_log2, decay;
 };
 
+// A 4-bit cache's scales, those of the row that starts at value o from byte o / 16 on.
+struct Fp4Params : WindowParams { const uint8_t *k_scales, *v_scales; };
+
+// Every token of a K/V head over its own list of blocks: no window, no sinks.
+struct ListParams : Fp4Params {
+  static constexpr bool kListed = true;
+  const int32_t *list, *list_counts;         // [B][H_kv][n_q][budget], [B][H_kv][n_q]
+  int budget, block_shift, parts;            // parts: runs of block_rows query heads that a K/V head's are cut into
+};
+
 // Context length and new tokens of a request, clamped to what the call allows.
-__device__ __forceinline__ void window_sizes(const WindowParams& p, int b, int& ctx, int& n_new, uint32_t& flags) {
+template <typename Params>
+__device__ __forceinline__ void window_sizes(const Params& p, int b, int& ctx, int& n_new, uint32_t& flags) {
   ctx = p.ctx_lens[b];
   n_new = p.q_lens ? p.q_lens[b] : p.n_q;
   if (ctx > p.max_ctx || n_new > p.n_q) flags |= SSA_DEV_BAD_COUNT;
@@ -51,6 +64,40 @@ struct Seen {
   __device__ __forceinline__ int position(int tile) const { return tile < front ? tile * size : w0 + (tile - front) * size; }
 };
 
+// The blocks that token t of a K/V head has on its list, as tiles of 1 << tile_shift positions.
+struct Listed {
+  const int32_t* list;
+  int count, per_shift, tile_shift, tiles, pos;              // pos: the token's own position
+  int first = 0, mine = 0;                                   // entries first ... first + 31 are in the warp's lanes
+  __device__ __forceinline__ Listed(const ListParams& p, int tile_size, int b, int hkv, int t, int pos_, uint32_t& flags) : pos(pos_) {
+    const int64_t r = ((int64_t)b * p.H_kv + hkv) * p.n_q + t;
+    list = p.list + r * p.budget;
+    const int lane = threadIdx.x % 32;
+    mine = lane < p.budget ? list[lane] : -1;                // (asked for before it is known how many there are)
+    count = p.list_counts[r];
+    if (count > p.budget) flags |= SSA_DEV_BAD_COUNT;
+    count = pos < 0 ? 0 : max(0, min(count, p.budget));
+    tile_shift = 31 - __clz(tile_size);
+    per_shift = p.block_shift - tile_shift;
+    tiles = count << per_shift;
+  }
+  // Where a tile starts; behind every position where its block is none that the token sees.  All lanes of a warp ask together.
+  __device__ __forceinline__ int position(int tile, uint32_t& flags) {
+    const int e = tile >> per_shift;
+    if ((unsigned)(e - first) >= 32u) {
+      first = e;
+      mine = e + (int)(threadIdx.x % 32) < count ? list[e + threadIdx.x % 32] : -1;
+    }
+    const int block = __shfl_sync(~0u, mine, e - first);
+    if ((unsigned)block > (unsigned)(pos >> (per_shift + tile_shift))) {
+      flags |= SSA_DEV_BAD_INDEX;
+      return kNowhere;
+    }
+    return (block << (per_shift + tile_shift)) + ((tile & ((1 << per_shift) - 1)) << tile_shift);
+  }
+  static constexpr int kNowhere = 1 << 30;
+};
+
 // A split works on at least split_tiles tiles, whatever the launch has room for.
 __device__ __forceinline__ int splits_used(const WindowParams& p, int tiles) {
   return max(1, min(p.n_splits, tiles / p.split_tiles));
@@ -72,8 +119,8 @@ __device__ __forceinline__ bool sees(const WindowParams& p, int pos, int j) {
 }
 
 // Pool row of logical position j, -1 where its page does not exist.
-template <bool kPaged>
-__device__ __forceinline__ int64_t row_of(const WindowParams& p, const int32_t* table, int j) {
+template <bool kPaged, typename Params>
+__device__ __forceinline__ int64_t row_of(const Params& p, const int32_t* table, int j) {
   if constexpr (!kPaged) return j;
   const int page = table[j >> p.page_shift];
   if ((unsigned)page >= (unsigned)p.n_pages) return -1;

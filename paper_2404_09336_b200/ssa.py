@@ -26,7 +26,8 @@ DEV_BAD_SPAN, DEV_CLIPPED, DEV_OVERFLOW, DEV_BAD_INDEX, DEV_BAD_COUNT, DEV_TOO_M
 DEV_BAD_REF, DEV_GAVE_UP = 64, 128
 MAX_SPANS_PER_SEQ = 2048
 MASS_MAX_ROWS = 1024
-F16, BF16, F32, FP8_E4M3 = 0, 1, 2, 3
+F16, BF16, F32, FP8_E4M3, FP4_E2M1 = 0, 1, 2, 3, 4
+MAX_BLOCKS = 16384
 _DTYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32, torch.float8_e4m3fn: FP8_E4M3}
 
 
@@ -65,6 +66,21 @@ class Window(C.Structure):
     """ssa_window (see include/ssa.h)."""
     _fields_ = [("n_q", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32),
                 ("q_stride_t", C.c_int64), ("o_stride_t", C.c_int64), ("q_lens", C.c_void_p), ("paging", C.POINTER(Paging))]
+
+
+class Blocks(C.Structure):
+    """ssa_blocks (see include/ssa.h)."""
+    _fields_ = [("n_q", C.c_int32), ("block_size", C.c_int32), ("budget", C.c_int32), ("sinks", C.c_int32), ("recent", C.c_int32),
+                ("q_stride_t", C.c_int64), ("o_stride_t", C.c_int64), ("bounds_stride_b", C.c_int64), ("bounds_stride_h", C.c_int64),
+                ("q_lens", C.c_void_p), ("paging", C.POINTER(Paging))]
+
+
+class Append(C.Structure):
+    """ssa_append (see include/ssa.h)."""
+    _fields_ = [("n_q", C.c_int32), ("rotary_dims", C.c_int32), ("interleaved", C.c_int32), ("n_positions", C.c_int32),
+                ("k_factor", C.c_float), ("v_factor", C.c_float), ("q_stride_t", C.c_int64),
+                *((f"{n}_stride_{d}", C.c_int64) for n in ("qo", "kn", "vn") for d in "bht"),
+                ("cos_sin", C.c_void_p), ("positions", C.c_void_p), ("q_lens", C.c_void_p), ("paging", C.POINTER(Paging))]
 
 
 class AnchorTables(C.Structure):
@@ -142,6 +158,21 @@ def _load():
                                       vp, vp, vp]
     lib.ssa_cache_compact.restype = C.c_int32
     lib.ssa_cache_compact.argtypes = [desc, C.POINTER(Paging), vp, vp, vp, vp, C.c_int32, vp, C.c_int32, vp, C.c_int64, vp, vp]
+    blocks = C.POINTER(Blocks)
+    lib.ssa_attn_window_fp4_workspace_bytes.restype = C.c_size_t
+    lib.ssa_attn_window_fp4_workspace_bytes.argtypes = [desc, win]
+    lib.ssa_attn_window_fp4.restype = C.c_int32
+    lib.ssa_attn_window_fp4.argtypes = [desc, win, *[vp] * 9, C.c_size_t, vp, vp]
+    lib.ssa_block_bounds.restype = C.c_int32
+    lib.ssa_block_bounds.argtypes = [desc, blocks, *[vp] * 6]
+    lib.ssa_block_select.restype = C.c_int32
+    lib.ssa_block_select.argtypes = [desc, blocks, *[vp] * 8]
+    lib.ssa_attn_blocks_workspace_bytes.restype = C.c_size_t
+    lib.ssa_attn_blocks_workspace_bytes.argtypes = [desc, blocks]
+    lib.ssa_attn_blocks.restype = C.c_int32
+    lib.ssa_attn_blocks.argtypes = [desc, blocks, *[vp] * 11, C.c_size_t, vp, vp]
+    lib.ssa_cache_append.restype = C.c_int32
+    lib.ssa_cache_append.argtypes = [desc, C.POINTER(Append), *[vp] * 11]
     lib.ssa_set_kernel_events.restype = None
     lib.ssa_set_kernel_events.argtypes = [vp, vp]
     lib.ssa_launch_count.restype = C.c_uint64
@@ -156,7 +187,7 @@ def _load():
 lib = _load()
 LIBRARY_PATH = lib._name
 
-# The calls of a decode step and their arguments, as binding/ssa_call.c reads them: D, S, P, Q structure (P: or None), i integer,
+# The calls of a decode step and their arguments, as binding/ssa_call.c reads them: D, S, P, Q, K, A structure (P: or None), i integer,
 # f number,
 # t tensor or None, r the same and its row stride (R: behind the next tensor), w and its bytes, n and its number of elements.
 _CALLS = {
@@ -178,6 +209,11 @@ _CALLS = {
     "attn_mass": "DQtttttttrfwti",
     "mass_to_index": "rniiiirtti",
     "cache_compact": "DPtttrtirti",
+    "attn_window_fp4": "DQttttttttwti",
+    "block_bounds": "DKttttti",
+    "block_select": "DKttttttti",
+    "attn_blocks": "DKttttttttttwti",
+    "cache_append": "DAtttttttttti",
 }
 
 
@@ -200,7 +236,7 @@ class _CtypesCalls:
                 given.append(int(a))
             elif kind == "f":
                 given.append(float(a))
-            elif kind in "DSPQ":
+            elif kind in "DSPQKA":
                 given.append(None if kind == "P" and a is None else C.byref(a))
             else:
                 given.append(None if a is None else C.c_void_p(a.data_ptr()))
@@ -226,7 +262,8 @@ def _load_calls():
     spec = importlib.util.spec_from_file_location(__package__ + "._ssa_call", path)
     calls = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(calls)
-    calls.bind({"ssa_attn_desc": AttnDesc, "ssa_step": Step, "ssa_paging": Paging, "ssa_window": Window} |
+    calls.bind({"ssa_attn_desc": AttnDesc, "ssa_step": Step, "ssa_paging": Paging, "ssa_window": Window, "ssa_blocks": Blocks,
+                "ssa_append": Append} |
                {"ssa_" + name: C.cast(getattr(lib, "ssa_" + name), C.c_void_p).value for name in _CALLS})
     return calls
 
@@ -417,14 +454,18 @@ def decode_attn_dense_paged(desc, q, k_pool, v_pool, paging, ctx_lens, out, lse=
     return _check("ssa_decode_attn_dense_paged", rc, check)
 
 
-def make_window(q, out, window: int = 0, sinks: int = 0, q_lens=None, paging: Paging | None = None) -> Window:
-    """ssa_window for q[B,H,n_q,D], out[B,H,n_q,D] (any strides; the descriptor is made from q[:, :, 0], out[:, :, 0]).  q_lens
-    (int32 [B], side by side, on q's device) must stay alive."""
+def _check_lens(q_lens, B, device):
     if q_lens is not None:
         if q_lens.dtype != torch.int32:
             raise ValueError("q_lens must be int32")
-        if q_lens.device != q.device or not q_lens.is_contiguous() or q_lens.numel() < q.shape[0]:
+        if q_lens.device != device or not q_lens.is_contiguous() or q_lens.numel() < B:
             raise ValueError("q_lens is one length per request, side by side, on the device of q")
+
+
+def make_window(q, out, window: int = 0, sinks: int = 0, q_lens=None, paging: Paging | None = None) -> Window:
+    """ssa_window for q[B,H,n_q,D], out[B,H,n_q,D] (any strides; the descriptor is made from q[:, :, 0], out[:, :, 0]).  q_lens
+    (int32 [B], side by side, on q's device) must stay alive."""
+    _check_lens(q_lens, q.shape[0], q.device)
     w = Window()
     w.n_q, w.window, w.sinks = int(q.shape[2]), int(window), int(sinks)
     w.q_stride_t, w.o_stride_t = int(q.stride(2)), int(out.stride(2))
@@ -484,6 +525,143 @@ def cache_compact(desc, k_cache, v_cache, ctx_lens, index, counts, max_selected,
     rc = _call.cache_compact(desc, paging, k_cache, v_cache, ctx_lens, index, counts, max_selected, mass, dev_status,
                              _stream(stream))
     return _check("ssa_cache_compact", rc, check)
+
+
+def make_desc_fp4(q, k, v, k_scales, v_scales, out, max_ctx=None, scale: float = 0.0, paged: bool = False) -> AttnDesc:
+    """Descriptor for q[B,H,D], out[B,H,D] over a cache of 4-bit values: codes k, v [B,H_kv,T,D/2] (any strides) and their scales
+    [B,H_kv,T,D/16]; paged: pools [n_pages, page_size, H_kv, D/2] and [n_pages, page_size, H_kv, D/16], max_ctx given."""
+    D = q.shape[2]
+    for x, scales in ((k, k_scales), (v, v_scales)):
+        if x.element_size() != 1 or scales.element_size() != 1 or x.shape[-1] * 2 != D or scales.shape[-1] * 16 != D:
+            raise ValueError("a row of D values is D/2 bytes of codes and D/16 bytes of scales")
+        if scales.shape[:-1] != x.shape[:-1] or any(a != 8 * b for a, b, n in zip(x.stride()[:-1], scales.stride()[:-1], x.shape) if n > 1):
+            raise ValueError("codes and scales must lie alike: every stride of the scales an eighth of the codes'")
+        if scales.stride(-1) != 1:
+            raise ValueError("the head dimension must be contiguous")
+    d = make_desc_paged(q, k, v, out, max_ctx, scale) if paged else make_desc(q, k, v, out, max_ctx, scale)
+    d.kv_dtype = FP4_E2M1
+    for name in ("k_stride_b", "k_stride_t", "k_stride_h", "v_stride_b", "v_stride_t", "v_stride_h"):
+        setattr(d, name, 2 * getattr(d, name))               # values, not bytes
+    return d
+
+
+def attn_window_fp4_workspace_bytes(desc: AttnDesc, window: Window) -> int:
+    return int(lib.ssa_attn_window_fp4_workspace_bytes(C.byref(desc), C.byref(window)))
+
+
+def attn_window_fp4(desc, window, q, k_cache, v_cache, k_scales, v_scales, ctx_lens, out, lse=None, workspace=None, dev_status=None,
+                    stream=None, check=True):
+    """ssa_attn_window_fp4: attn_window over a cache of 4-bit values (make_desc_fp4)."""
+    rc = _call.attn_window_fp4(desc, window, q, k_cache, v_cache, k_scales, v_scales, ctx_lens, out, lse, workspace, dev_status,
+                               _stream(stream))
+    return _check("ssa_attn_window_fp4", rc, check)
+
+
+def make_blocks(n_q: int, block_size: int, budget: int, sinks: int = 0, recent: int = 0, q=None, out=None, bounds=None, q_lens=None,
+                paging: Paging | None = None) -> Blocks:
+    """ssa_blocks for n_q tokens: q[B,H,n_q,D], out[B,H,n_q,D] (any strides) and bounds[B,H_kv,n,2,D] (a head's blocks side by side),
+    as far as the calls to be made take them.  q_lens (int32 [B], side by side) must stay alive."""
+    for x in (q, out):
+        if x is not None and x.shape[2] != n_q:
+            raise ValueError("q and out are [B, H, n_q, D]")
+    for x in (q, bounds):
+        if x is not None:
+            _check_lens(q_lens, x.shape[0], x.device)
+    k = Blocks()
+    k.n_q, k.block_size, k.budget, k.sinks, k.recent = int(n_q), int(block_size), int(budget), int(sinks), int(recent)
+    k.q_stride_t = 0 if q is None else int(q.stride(2))
+    k.o_stride_t = 0 if out is None else int(out.stride(2))
+    if bounds is not None:
+        if bounds.dim() != 5 or bounds.shape[3] != 2 or not bounds[0, 0].is_contiguous():
+            raise ValueError("bounds are [B, H_kv, blocks, 2, D], the last three dimensions contiguous")
+        k.bounds_stride_b, k.bounds_stride_h = int(bounds.stride(0)), int(bounds.stride(1))
+    k.q_lens = None if q_lens is None else q_lens.data_ptr()
+    if paging is not None:
+        k.paging = C.pointer(paging)
+    return k
+
+
+def _check_bounds(desc, blocks, bounds):
+    if bounds.shape[0] < desc.B or bounds.shape[1] < desc.H_kv or bounds.shape[2] * blocks.block_size < desc.max_ctx or bounds.shape[4] != desc.D:
+        raise ValueError(f"bounds have room for {desc.B} requests, {desc.H_kv} heads and the blocks of {desc.max_ctx} positions")
+
+
+def _check_lists(desc, blocks, index, counts):
+    rows = desc.B * desc.H_kv * blocks.n_q
+    if index.dtype != torch.int32 or counts.dtype != torch.int32 or not index.is_contiguous() or not counts.is_contiguous():
+        raise ValueError("lists are contiguous int32 arrays")
+    if index.shape[-1] != blocks.budget or index.numel() < rows * blocks.budget or counts.numel() < rows:
+        raise ValueError(f"lists are {rows} rows of {blocks.budget} blocks, and as many counts")
+
+
+def block_bounds(desc, blocks, k_cache, ctx_lens, bounds, k_scales=None, dev_status=None, stream=None, check=True):
+    """ssa_block_bounds: least and largest values over the keys of the blocks of the newest positions -> bounds[B,H_kv,n,2,D]."""
+    _check_bounds(desc, blocks, bounds)
+    rc = _call.block_bounds(desc, blocks, k_cache, k_scales, ctx_lens, bounds, dev_status, _stream(stream))
+    return _check("ssa_block_bounds", rc, check)
+
+
+def block_select(desc, blocks, q, bounds, ctx_lens, index, counts, scores=None, dev_status=None, stream=None, check=True):
+    """ssa_block_select: the blocks that each token attends to -> index[B,H_kv,n_q,budget], counts[B,H_kv,n_q] (and
+    scores[B,H_kv,n_q,n], fp32)."""
+    _check_bounds(desc, blocks, bounds)
+    _check_lists(desc, blocks, index, counts)
+    if scores is not None:
+        n = -(-desc.max_ctx // max(1, blocks.block_size))
+        if scores.dtype != torch.float32 or not scores.is_contiguous() or scores.shape[-1] != n or scores.numel() < desc.B * desc.H_kv * blocks.n_q * n:
+            raise ValueError(f"scores are rows of {n} fp32 values")
+    rc = _call.block_select(desc, blocks, q, bounds, ctx_lens, index, counts, scores, dev_status, _stream(stream))
+    return _check("ssa_block_select", rc, check)
+
+
+def attn_blocks_workspace_bytes(desc: AttnDesc, blocks: Blocks) -> int:
+    return int(lib.ssa_attn_blocks_workspace_bytes(C.byref(desc), C.byref(blocks)))
+
+
+def attn_blocks(desc, blocks, q, k_cache, v_cache, ctx_lens, index, counts, out, lse=None, k_scales=None, v_scales=None,
+                workspace=None, dev_status=None, stream=None, check=True):
+    """ssa_attn_blocks: every token over the blocks of its list; out (and lse[B,H,n_q]) are written."""
+    _check_lists(desc, blocks, index, counts)
+    rc = _call.attn_blocks(desc, blocks, q, k_cache, v_cache, k_scales, v_scales, ctx_lens, index, counts, out, lse, workspace,
+                           dev_status, _stream(stream))
+    return _check("ssa_attn_blocks", rc, check)
+
+
+def make_append(k_new, v_new, q=None, q_out=None, cos_sin=None, interleaved: bool = False, positions=None, q_lens=None,
+                paging: Paging | None = None, k_factor: float = 1.0, v_factor: float = 1.0) -> Append:
+    """ssa_append for k_new, v_new [B,H_kv,n_q,D], q and q_out [B,H,n_q,D] (any strides), cos_sin[positions, rotary dimensions]
+    (fp32: cosines, then sines) and positions[B,n_q] (int32).  cos_sin, positions and q_lens must stay alive."""
+    B, _, n_q, D = k_new.shape
+    for x in (k_new, v_new, q, q_out):
+        if x is not None and (x.shape[0] != B or x.shape[2] != n_q or x.shape[3] != D or x.stride(3) != 1 or x.dtype != k_new.dtype):
+            raise ValueError("new rows are [B, heads, n_q, D] of one type, the head dimension contiguous")
+    _check_lens(q_lens, B, k_new.device)
+    a = Append()
+    a.n_q, a.interleaved, a.k_factor, a.v_factor = int(n_q), int(bool(interleaved)), float(k_factor), float(v_factor)
+    a.q_stride_t = 0 if q is None else int(q.stride(2))
+    for name, x in (("qo", q_out), ("kn", k_new), ("vn", v_new)):
+        for i, d in enumerate("bht"):
+            setattr(a, f"{name}_stride_{d}", 0 if x is None else int(x.stride(i)))
+    if cos_sin is not None:
+        if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous() or cos_sin.device != k_new.device:
+            raise ValueError("cos_sin is a contiguous fp32 table [positions, rotary dimensions] on the device of k_new")
+        a.n_positions, a.rotary_dims, a.cos_sin = int(cos_sin.shape[0]), int(cos_sin.shape[1]), cos_sin.data_ptr()
+    if positions is not None:
+        if positions.dtype != torch.int32 or not positions.is_contiguous() or positions.numel() < B * n_q or positions.device != k_new.device:
+            raise ValueError("positions are a contiguous int32 array [B, n_q] on the device of k_new")
+        a.positions = positions.data_ptr()
+    a.q_lens = None if q_lens is None else q_lens.data_ptr()
+    if paging is not None:
+        a.paging = C.pointer(paging)
+    return a
+
+
+def cache_append(desc, append, k_new, v_new, ctx_lens, k_cache, v_cache, q=None, q_out=None, k_scales=None, v_scales=None,
+                 dev_status=None, stream=None, check=True):
+    """ssa_cache_append: the step's keys and values into the cache, rotated by position, and its queries rotated into q_out."""
+    rc = _call.cache_append(desc, append, k_new, v_new, ctx_lens, k_cache, v_cache, q, q_out, k_scales, v_scales, dev_status,
+                            _stream(stream))
+    return _check("ssa_cache_append", rc, check)
 
 
 def refs_to_index(line_offsets, lines, anchor_offsets, anchor_line, ref_offsets, refs, prefix_len, line_start,
