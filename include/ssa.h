@@ -588,7 +588,8 @@ int32_t ssa_cache_compact(const ssa_attn_desc* desc, const ssa_paging* paging, v
  * other than SSA_FP4_E2M1: SSA_ERR_DTYPE; strides of K and V that are no
  * multiples of D, k_cache, v_cache, k_scales, v_scales not 16-byte aligned:
  * SSA_ERR_ALIGN).  Scores, maxima, sums and lse are fp32.  Softmax weights enter
- * the second product as two fp16 parts (22 bits) - except where more than 24
+ * the second product as two fp16 parts (22 bits; weights far below the largest
+ * to an absolute 2^-38 of it, from tiles 2^-31) - except where more than 24
  * rows per K/V head (tokens x grouped heads; pages of eight rows and more) go to
  * tensor-core tiles and out_dtype is BF16: those round each weight to fp16 once
  * (a relative 2^-11).  A scale that is NaN makes its 16 values NaN.
@@ -660,8 +661,9 @@ int32_t ssa_block_bounds(const ssa_attn_desc* desc, const ssa_blocks* blocks, co
  *   counts dev int32 [B*H_kv*n_q]: min(m, budget)
  *   scores dev float [B*H_kv*n_q, n] or NULL: entries [0, m) of the row
  * Scores are summed in 64 bits and rounded to 32 once, so that lists do not depend
- * on the order of summation.  (bounds of a block hold all its keys, those behind
- * the token's own position among them.)
+ * on the order of summation; an infinite bound against queries all of the other
+ * sign makes a NaN.  (Bounds of a block hold all its keys, those behind the
+ * token's own position among them.)
  *   desc     host; the fields of k, v and out are checked but not used, but for
  *            H_kv; q and bounds (dev) have the queries' type for kv_dtype
  * Errors: SSA_ERR_NULL, SSA_ERR_SHAPE, SSA_ERR_UNSUPPORTED, SSA_ERR_DTYPE,
@@ -684,7 +686,8 @@ int32_t ssa_block_select(const ssa_attn_desc* desc, const ssa_blocks* blocks, co
  *   workspace  dev, 16-byte aligned, >= ssa_attn_blocks_workspace_bytes(desc,
  *              blocks) (0: invalid arguments); one for each of the calls that may
  *              run at the same time
- * Softmax weights enter as two 16-bit parts, scores and sums are fp32.
+ * Softmax weights enter as two 16-bit parts (fp16 ones far below the largest to an
+ * absolute 2^-38 of it), scores and sums are fp32.
  * Errors: those of ssa_attn_window, SSA_ERR_CAPACITY (budget <= 0) and
  * SSA_ERR_UNSUPPORTED (block_size).
  */

@@ -229,7 +229,87 @@ class DecodeStep:
         with self._on(stream):
             # (no longer than what was moved, where a count is above its bound or was never written)
             self.ctx_lens.copy_(torch.minimum(self.ctx_lens, self.counts.clamp(0, bound)))
+        if hasattr(self, "bounds"):
+            self.refresh_bounds(stream=stream)
+        if hasattr(self, "fp4"):
+            self._fill_fp4(stream)
         return ssa.OK
+
+    # ---- filling the cache ----------------------------------------------------------------
+    def append(self, k_new, v_new, q=None, cos_sin=None, interleaved=False, positions=None, stream=None):
+        """A new token of every request: contexts are one longer, its key k_new[B,H,D], rotated by position (cos_sin, positions as for
+        make_append), and its value v_new are in every copy of the cache (the 4-bit one too), its query q, rotated, in self.q; the
+        bounds of its block are made anew.  What bounds lists on the host (max_selected, spans) stays."""
+        with self._on(stream):
+            self.ctx_lens.add_(1)
+        new = ssa.make_append(k_new.unsqueeze(2), v_new.unsqueeze(2), None if q is None else q.unsqueeze(2),
+                              None if q is None else self.q.unsqueeze(2), cos_sin, interleaved, positions)
+        caches = [(*self._copy(c), None, None) for c in range(len(self.k_store))]
+        if hasattr(self, "fp4"):
+            caches.append(self.fp4)
+        desc = self.desc if q is None else ssa.make_desc(q, self.k, self.v, self.out, max_ctx=self.wl.max_ctx)
+        for i, (k, v, k_scales, v_scales) in enumerate(caches):
+            if i == 1:                                       # (queries are rotated once)
+                q, new = None, ssa.make_append(k_new.unsqueeze(2), v_new.unsqueeze(2), None, None, cos_sin, interleaved, positions)
+            ssa.cache_append(desc if k_scales is None else self.desc_fp4, new, k_new, v_new, self.ctx_lens, k, v, q,
+                             None if q is None else self.q, k_scales, v_scales, self.status, stream)
+        if hasattr(self, "bounds"):
+            self.refresh_bounds(1, stream)
+        return ssa.OK
+
+    # ---- blocks that the queries select ------------------------------------------------------
+    def enable_blocks(self, block_size: int = 64, budget: int = 32, sinks: int = 1, recent: int = 1, stream=None):
+        """Bounds of every block of the cache, and room for the lists of attention over the `budget` blocks that score best."""
+        B, H, D, T, dev = self.wl.B, self.wl.H, self.wl.D, self.wl.max_ctx, self.device
+        with self._on(stream):
+            self.bounds = torch.zeros(B, H, -(-T // block_size), 2, D, dtype=self.q.dtype, device=dev)
+            self.block_lists = (torch.full((B, H, 1, budget), -7, dtype=torch.int32, device=dev),
+                                torch.zeros((B, H, 1), dtype=torch.int32, device=dev))
+        self.blocks = ssa.make_blocks(1, block_size, budget, sinks, recent, self.q.unsqueeze(2), self.out.unsqueeze(2), self.bounds)
+        return self.refresh_bounds(stream=stream)
+
+    def refresh_bounds(self, newest=None, stream=None):
+        """Bounds of the blocks of the newest positions (None: of all)."""
+        which = ssa.make_blocks(newest or self.wl.max_ctx, self.blocks.block_size, self.blocks.budget, bounds=self.bounds)
+        return ssa.block_bounds(self.desc, which, self.k, self.ctx_lens, self.bounds, None, self.status, stream)
+
+    def select_blocks(self, stream=None):
+        """self.block_lists: for every K/V head the blocks that the step's queries rank first."""
+        return ssa.block_select(self.desc, self.blocks, self.q, self.bounds, self.ctx_lens, *self.block_lists, None, self.status, stream)
+
+    def attend_blocks(self, stream=None):
+        """The step's token over the blocks on its lists."""
+        room = self._room(ssa.attn_blocks_workspace_bytes(self.desc, self.blocks), stream)
+        return ssa.attn_blocks(self.desc, self.blocks, self.q, self.k, self.v, self.ctx_lens, *self.block_lists, self.out, self.lse,
+                               None, None, room, self.status, stream)
+
+    # ---- the cache in 4 bits -------------------------------------------------------------------
+    def enable_fp4(self, stream=None):
+        """A copy of the cache in 4-bit values (codes and scales of K and of V)."""
+        B, H, D, T, dev = self.wl.B, self.wl.H, self.wl.D, self.wl.max_ctx, self.device
+        if self.q.dtype != torch.bfloat16:
+            raise ValueError("queries over a 4-bit cache are bf16")
+        with self._on(stream):
+            k, v = (torch.zeros(B, H, T, D // 2, dtype=torch.uint8, device=dev) for _ in range(2))
+            k_scales, v_scales = (torch.zeros(B, H, T, D // 16, dtype=torch.uint8, device=dev) for _ in range(2))
+            self._filled = torch.full_like(self.ctx_lens, T) # contexts whose newest T positions are all there are
+        self.fp4 = k, v, k_scales, v_scales
+        self.desc_fp4 = ssa.make_desc_fp4(self.q, k, v, k_scales, v_scales, self.out, T)
+        return self._fill_fp4(stream)
+
+    def _fill_fp4(self, stream):
+        k, v, k_scales, v_scales = self.fp4
+        return ssa.cache_append(self.desc_fp4, ssa.make_append(self.k, self.v), self.k, self.v, self._filled, k, v, None, None,
+                                k_scales, v_scales, self.status, stream)
+
+    def attend_fp4(self, window: int = 0, sinks: int = 0, stream=None):
+        """The step's token over its context (or window), read from the 4-bit cache."""
+        q, out = self.q.unsqueeze(2), self.out.unsqueeze(2)
+        win = ssa.make_window(q, out, window, sinks)
+        room = self._room(ssa.attn_window_fp4_workspace_bytes(self.desc_fp4, win), stream)
+        k, v, k_scales, v_scales = self.fp4
+        return ssa.attn_window_fp4(self.desc_fp4, win, q, k, v, k_scales, v_scales, self.ctx_lens, out, self.lse, room, self.status,
+                                   stream)
 
     # ---- the paper's blocked encoding as the metadata format ---------------------------
     def enable_blockmask(self, block_size: int = 256):
