@@ -123,8 +123,7 @@ block_bounds_kernel(const BoundsParams p) {
 
 // ---- selection ----------------------------------------------------------------------------------------------------------
 constexpr int kSelectThreads = 256, kSelectWarps = kSelectThreads / 32;
-constexpr int kScoreLanes = 8;         // of a block of positions
-constexpr int kScored = kSelectThreads / kScoreLanes;        // blocks of positions that a thread block scores at a time
+constexpr int kDeep = 8;               // 16-byte pieces that a lane asks for at a time, of as many blocks of positions
 
 struct SelectParams {
   const void *q, *bounds;
@@ -136,22 +135,58 @@ struct SelectParams {
   int H_kv, group, n_q, max_ctx, block_shift, n_blocks, budget, sinks, recent;
 };
 
+// Sums of v[i] over the kLanes lanes of a block's bounds, eight blocks together: each exchange halves what a lane has left.  The lane
+// ends up with the sum of block `which`, or (the last lanes' bits) one that another has too.
+template <int kLanes>
+__device__ __forceinline__ double sums_of(double (&v)[kDeep], int lane, int& which) {
+  which = 0;
+  int o = kLanes / 2;
+#pragma unroll
+  for (int left = kDeep / 2; left >= 1; left /= 2, o /= 2) {
+    const bool high = lane & o;
+    which = 2 * which + high;
+#pragma unroll
+    for (int i = 0; i < left; ++i) {
+      const double mine = high ? v[i + left] : v[i], theirs = high ? v[i] : v[i + left];
+      v[i] = mine + __shfl_xor_sync(~0u, theirs, o);
+    }
+  }
+#pragma unroll
+  for (; o >= 1; o /= 2) v[0] += __shfl_xor_sync(~0u, v[0], o);
+  return v[0];
+}
+
 // grid (ranks x tokens, H_kv, B).  Thread blocks share a token's blocks of positions out; the first of them gets all scores, over
-// distributed shared memory where they are a cluster, and ranks them: the key of the last one that stays is found in four digits
-// from the top, each by a histogram of the keys that match the digits found, and what stays is numbered by a prefix sum.
-// Products of 16-bit values are summed in fp64: HBM bounds the scores (the bounds' bytes) all the same, and lists depend on no order.
+// distributed shared memory where they are a cluster, and ranks them: the key of the last one that stays is found in digits of eight
+// bits from the top, each by a histogram of the keys that match the digits found, and what stays is numbered by a prefix sum.
+// Products of 16-bit values are summed in fp64, so that lists depend on no order; HBM bounds the scores (the bounds' bytes) all the
+// same, as long as eight pieces a lane are under way while the eight before them are converted and summed.
 template <typename TQ, int D>
-__global__ void __launch_bounds__(kSelectThreads)
+__global__ void __launch_bounds__(kSelectThreads, 2)
 block_select_kernel(const SelectParams p, const int ranks) {
-  constexpr int kPieces = 2 * D / 8 / kScoreLanes;           // 16-byte pieces of a block's bounds per lane
+  constexpr int kLanes = 2 * D / 8, kSide = 32 / kLanes;     // lanes of a block's bounds; blocks side by side in a warp
+  constexpr int kStep = kSelectWarps * kSide * kDeep;        // blocks that a thread block scores at a time
   extern __shared__ uint32_t s_key[];                        // [n_blocks], of the first thread block
   __shared__ double s_weight[2 * D];
-  __shared__ uint32_t s_bins[256], s_sum[kSelectWarps];
-  __shared__ int2 s_found;
+  __shared__ uint32_t s_bins[4][256], s_sum[kSelectWarps];
+  __shared__ uint2 s_range[kSelectWarps];
   const int t = (int)blockIdx.x / ranks, rank = (int)blockIdx.x - t * ranks, hkv = blockIdx.y, b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
   grid_dependency_wait();
   grid_launch_dependents();
+  // the first pieces are asked for before it is known how many blocks the token sees: there is room for n_blocks
+  const uint4* bounds = reinterpret_cast<const uint4*>(static_cast<const TQ*>(p.bounds) + (int64_t)b * p.bounds_sb + (int64_t)hkv * p.bounds_sh) +
+                        lane % kLanes;
+  auto place = [&](int j0, int i) { return j0 + (warp * kDeep + i) * kSide + lane / kLanes; };
+  uint4 w[2][kDeep];
+  auto ask = [&](int j0, int upto, uint4 (&x)[kDeep]) {
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) {
+      const int j = place(j0, i);
+      x[i] = j < upto ? ld_stream_16B(bounds + (int64_t)j * kLanes) : make_uint4(0, 0, 0, 0);
+    }
+  };
+  ask(rank * kStep, p.n_blocks, w[0]);
   uint32_t flags = 0;
   int ctx, n_new;
   window_sizes(p, b, ctx, n_new, flags);
@@ -170,6 +205,7 @@ block_select_kernel(const SelectParams p, const int ranks) {
   if (tid < D) {
     const TQ* q = static_cast<const TQ*>(p.q) + (int64_t)b * p.q_sb + (int64_t)hkv * p.group * p.q_sh + (int64_t)t * p.q_st + tid;
     double below = 0, above = 0;
+#pragma unroll 4
     for (int h = 0; h < p.group; ++h) {
       const double x = (double)to_float(q[h * p.q_sh]);
       below += fmin(x, 0.0);
@@ -179,35 +215,37 @@ block_select_kernel(const SelectParams p, const int ranks) {
     s_weight[tid] = below;
     s_weight[D + tid] = above;
   }
+  for (int i = tid; i < 4 * 256; i += kSelectThreads) s_bins[i / 256][i % 256] = 0;
   __syncthreads();
-  const int part = lane % kScoreLanes;
-  double weight[kPieces][8];
+  double weight[8];
 #pragma unroll
-  for (int i = 0; i < kPieces; ++i)
+  for (int e = 0; e < 8; ++e) weight[e] = s_weight[lane % kLanes * 8 + e];
+  auto score = [&](int j0, const uint4 (&x)[kDeep]) {
+    double sum[kDeep];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) weight[i][e] = s_weight[(i * kScoreLanes + part) * 8 + e];
-  const uint4* bounds = reinterpret_cast<const uint4*>(static_cast<const TQ*>(p.bounds) + (int64_t)b * p.bounds_sb + (int64_t)hkv * p.bounds_sh);
-#pragma unroll 2
-  for (int j0 = rank * kScored; j0 < m; j0 += ranks * kScored) {
-    const int j = j0 + tid / kScoreLanes;
-    double sum = 0;
-    if (j < m) {
+    for (int i = 0; i < kDeep; ++i) {
+      float f[8];
+      unpack8<TQ>(x[i], f);
+      double a = (double)f[0] * weight[0], z = (double)f[1] * weight[1];
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        float f[8];
-        unpack8<TQ>(ld_stream_16B(bounds + (int64_t)j * (2 * D / 8) + i * kScoreLanes + part), f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fma((double)f[e], weight[i][e], sum);
-      }
+      for (int e = 2; e < 8; e += 2) { a = fma((double)f[e], weight[e], a); z = fma((double)f[e + 1], weight[e + 1], z); }
+      sum[i] = a + z;
     }
-#pragma unroll
-    for (int o = 1; o < kScoreLanes; o *= 2) sum += __shfl_xor_sync(~0u, sum, o);
-    if (j < m && part == 0) {
-      const float score = (float)sum;
-      if (p.scores) p.scores[r * p.n_blocks + j] = score;
-      if (rank == 0) s_key[j] = order_key(score);
-      else store_to(&s_key[j], 0, order_key(score));
+    int which;
+    const float total = (float)sums_of<kLanes>(sum, lane, which);
+    const int j = place(j0, which);
+    if (j < m && lane % (kLanes / kDeep) == 0) {
+      if (p.scores) p.scores[r * p.n_blocks + j] = total;
+      if (rank == 0) s_key[j] = order_key(total);
+      else store_to(&s_key[j], 0, order_key(total));
     }
+  };
+#pragma unroll 1
+  for (int j0 = rank * kStep; j0 < m; j0 += 2 * ranks * kStep) {
+    ask(j0 + ranks * kStep, m, w[1]);
+    score(j0, w[0]);
+    ask(j0 + 2 * ranks * kStep, m, w[0]);
+    if (j0 + ranks * kStep < m) score(j0 + ranks * kStep, w[1]);
   }
   if (ranks > 1) cluster_sync();
   else __syncthreads();
@@ -216,45 +254,54 @@ block_select_kernel(const SelectParams p, const int ranks) {
   const int from = p.sinks, to = m - p.recent;               // those between are ranked
   int want = p.budget - p.sinks - p.recent;                  // >= 0, and < to - from
   const bool none = want == 0;
-  uint32_t key = 0, known = 0;                               // digits found so far, and their mask
+  uint32_t key = 0, known = 0;                               // bits found so far, and their mask
   if (!none) {
+    // Scores are alike: digits start at the first bit in which the keys differ, which also keeps them off one bin.
+    uint32_t low = ~0u, high = 0;
+    for (int j = from + tid; j < to; j += kSelectThreads) { low = min(low, s_key[j]); high = max(high, s_key[j]); }
+    low = __reduce_min_sync(~0u, low);
+    high = __reduce_max_sync(~0u, high);
+    if (lane == 0) s_range[warp] = make_uint2(low, high);
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kSelectWarps; ++w) { low = min(low, s_range[w].x); high = max(high, s_range[w].y); }
+    int bits = 32 - __clz(low ^ high);                       // still to be found
+    known = bits == 32 ? 0u : ~0u << bits;
+    key = low & known;
 #pragma unroll 1
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      s_bins[tid] = 0;
-      __syncthreads();
+    for (int digit = 0; bits > 0; ++digit) {
+      const int shift = max(0, bits - 8);
+      const uint32_t mask = (1u << (bits - shift)) - 1;
       for (int j = from + tid; j < to; j += kSelectThreads) {
         const uint32_t k = s_key[j];
-        if ((k & known) == key) atomicAdd(&s_bins[k >> shift & 255u], 1u);
+        if ((k & known) == key) atomicAdd(&s_bins[digit][k >> shift & mask], 1u);
       }
       __syncthreads();
-      if (warp == 0) {                                       // bins from the top, eight to a lane
-        uint32_t mine[8];
-        int sum = 0;
+      // every warp looks for the bin in which the count from the top reaches `want`: eight bins to a lane
+      uint32_t mine[8];
+      int sum = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { mine[i] = s_bins[255 - (lane * 8 + i)]; sum += (int)mine[i]; }
-        const int end = warp_inclusive(sum, lane);
-        const int who = __ffs(__ballot_sync(~0u, end >= want)) - 1;          // (all of them together reach `want`)
-        if (lane == who) {
-          int above = end - sum, digit = 0;
-          bool found = false;
+      for (int i = 0; i < 8; ++i) { mine[i] = s_bins[digit][255 - (lane * 8 + i)]; sum += (int)mine[i]; }
+      const int end = warp_inclusive(sum, lane);
+      const int who = __ffs(__ballot_sync(~0u, end >= want)) - 1;            // (all of them together reach `want`)
+      int above = end - sum, at = 0, left = 0, here = 0;
+      bool found = false;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            if (!found && above + (int)mine[i] >= want) { digit = 255 - (lane * 8 + i); found = true; }
-            if (!found) above += (int)mine[i];
-          }
-          s_found = make_int2(digit, want - above);
-        }
+      for (int i = 0; i < 8; ++i) {
+        if (!found && above + (int)mine[i] >= want) { at = 255 - (lane * 8 + i); left = want - above; here = (int)mine[i]; found = true; }
+        above += (int)mine[i];
       }
-      __syncthreads();
-      key |= (uint32_t)s_found.x << shift;
-      known |= 255u << shift;
-      want = s_found.y;
+      key |= (uint32_t)__shfl_sync(~0u, at, who) << shift;
+      known |= mask << shift;
+      want = __shfl_sync(~0u, left, who);
+      if (__shfl_sync(~0u, here, who) == want) break;        // all that share these bits stay
+      bits = shift;
     }
   }
-  // what stays, in order: a thread has `each` neighbouring blocks; `want` of the keys equal to `key` stay
+  // what stays, in order: a thread has `each` neighbouring blocks; `want` of the keys that share the bits of `key` stay
   const int each = (m + kSelectThreads - 1) / kSelectThreads, first = tid * each, end = min(m, first + each);
-  auto stays = [&](int j) { return j < from || j >= to || (!none && s_key[j] > key); };
-  auto equals = [&](int j) { return j >= from && j < to && !none && s_key[j] == key; };
+  auto stays = [&](int j) { return j < from || j >= to || (!none && (s_key[j] & known) > key); };
+  auto equals = [&](int j) { return j >= from && j < to && !none && (s_key[j] & known) == key; };
   uint32_t count = 0;                                        // (at most SSA_MAX_BLOCKS of either)
   for (int j = first; j < end; ++j) count += (uint32_t)stays(j) | (uint32_t)equals(j) << 16;
   const uint32_t upto = (uint32_t)warp_inclusive((int)count, lane);
@@ -311,9 +358,10 @@ static cudaError_t launch_bounds(const BoundsParams& p, dim3 grid, cudaStream_t 
 
 template <typename TQ, int D>
 static cudaError_t launch_select(const SelectParams& p, int B, cudaStream_t st) {
-  // Thread blocks of a token, as long as there are too few for the GPU and each has 64 blocks of positions to score
+  // Thread blocks of a token, as long as there are too few for the GPU and each has a step's blocks of positions to score
+  constexpr int kStep = kSelectWarps * (32 / (2 * D / 8)) * kDeep;
   unsigned ranks = 1;
-  while (ranks < 8 && 2ll * ranks * p.n_q * p.H_kv * B <= sm_count() && p.n_blocks / (2 * (int)ranks) >= 2 * kScored) ranks *= 2;
+  while (ranks < 8 && 2ll * ranks * p.n_q * p.H_kv * B <= 2 * sm_count() && p.n_blocks / (2 * (int)ranks) >= kStep) ranks *= 2;
   const size_t smem = (size_t)p.n_blocks * sizeof(uint32_t);
   auto kernel = block_select_kernel<TQ, D>;
   const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SSA_MAX_BLOCKS * (int)sizeof(uint32_t));

@@ -582,16 +582,21 @@ def make_blocks(n_q: int, block_size: int, budget: int, sinks: int = 0, recent: 
 
 
 def _check_bounds(desc, blocks, bounds):
-    if bounds.shape[0] < desc.B or bounds.shape[1] < desc.H_kv or bounds.shape[2] * blocks.block_size < desc.max_ctx or bounds.shape[4] != desc.D:
+    B, H_kv, n, _, D = bounds.size()
+    if B < desc.B or H_kv < desc.H_kv or n * blocks.block_size < desc.max_ctx or D != desc.D:
         raise ValueError(f"bounds have room for {desc.B} requests, {desc.H_kv} heads and the blocks of {desc.max_ctx} positions")
 
 
+_INT32, _FLOAT32 = torch.int32, torch.float32
+
+
 def _check_lists(desc, blocks, index, counts):
-    rows = desc.B * desc.H_kv * blocks.n_q
-    if index.dtype != torch.int32 or counts.dtype != torch.int32 or not index.is_contiguous() or not counts.is_contiguous():
+    rows, budget = desc.B * desc.H_kv * blocks.n_q, blocks.budget
+    if index.dtype is not _INT32 or counts.dtype is not _INT32 or not index.is_contiguous() or not counts.is_contiguous():
         raise ValueError("lists are contiguous int32 arrays")
-    if index.shape[-1] != blocks.budget or index.numel() < rows * blocks.budget or counts.numel() < rows:
-        raise ValueError(f"lists are {rows} rows of {blocks.budget} blocks, and as many counts")
+    if index.size(-1) != budget or index.numel() < rows * budget or counts.numel() < rows:
+        raise ValueError(f"lists are {rows} rows of {budget} blocks, and as many counts")
+    return rows
 
 
 def block_bounds(desc, blocks, k_cache, ctx_lens, bounds, k_scales=None, dev_status=None, stream=None, check=True):
@@ -605,10 +610,10 @@ def block_select(desc, blocks, q, bounds, ctx_lens, index, counts, scores=None, 
     """ssa_block_select: the blocks that each token attends to -> index[B,H_kv,n_q,budget], counts[B,H_kv,n_q] (and
     scores[B,H_kv,n_q,n], fp32)."""
     _check_bounds(desc, blocks, bounds)
-    _check_lists(desc, blocks, index, counts)
+    rows = _check_lists(desc, blocks, index, counts)
     if scores is not None:
         n = -(-desc.max_ctx // max(1, blocks.block_size))
-        if scores.dtype != torch.float32 or not scores.is_contiguous() or scores.shape[-1] != n or scores.numel() < desc.B * desc.H_kv * blocks.n_q * n:
+        if scores.dtype is not _FLOAT32 or not scores.is_contiguous() or scores.size(-1) != n or scores.numel() < rows * n:
             raise ValueError(f"scores are rows of {n} fp32 values")
     rc = _call.block_select(desc, blocks, q, bounds, ctx_lens, index, counts, scores, dev_status, _stream(stream))
     return _check("ssa_block_select", rc, check)
