@@ -588,11 +588,10 @@ int32_t ssa_cache_compact(const ssa_attn_desc* desc, const ssa_paging* paging, v
  * other than SSA_FP4_E2M1: SSA_ERR_DTYPE; strides of K and V that are no
  * multiples of D, k_cache, v_cache, k_scales, v_scales not 16-byte aligned:
  * SSA_ERR_ALIGN).  Scores, maxima, sums and lse are fp32.  Softmax weights enter
- * the second product as two fp16 parts (22 bits; weights far below the largest
- * to an absolute 2^-38 of it, from tiles 2^-31) - except where more than 24
- * rows per K/V head (tokens x grouped heads; pages of eight rows and more) go to
- * tensor-core tiles and out_dtype is BF16: those round each weight to fp16 once
- * (a relative 2^-11).  A scale that is NaN makes its 16 values NaN.
+ * the second product as fp16, rounded once (a relative 2^-11), where out_dtype is
+ * BF16, which is rounded more; for F32 as two fp16 parts (22 bits).  Those far
+ * below the largest are off by an absolute 2^-38 of it, in tiles of many rows
+ * 2^-31.  A scale that is NaN makes its 16 values NaN.
  */
 size_t ssa_attn_window_fp4_workspace_bytes(const ssa_attn_desc* desc, const ssa_window* window);
 int32_t ssa_attn_window_fp4(const ssa_attn_desc* desc, const ssa_window* window, const void* q, const void* k_cache,
@@ -687,7 +686,8 @@ int32_t ssa_block_select(const ssa_attn_desc* desc, const ssa_blocks* blocks, co
  *              blocks) (0: invalid arguments); one for each of the calls that may
  *              run at the same time
  * Softmax weights enter as two 16-bit parts (fp16 ones far below the largest to an
- * absolute 2^-38 of it), scores and sums are fp32.
+ * absolute 2^-38 of it), over a 4-bit cache with BF16 outputs as one fp16 part;
+ * scores and sums are fp32.
  * Errors: those of ssa_attn_window, SSA_ERR_CAPACITY (budget <= 0) and
  * SSA_ERR_UNSUPPORTED (block_size).
  */
@@ -702,8 +702,9 @@ int32_t ssa_attn_blocks(const ssa_attn_desc* desc, const ssa_blocks* blocks, con
  * its queries rotated (outside the paper, where the caller appends before the
  * call).  ctx_lens counts the step's tokens already: token t of request b goes to
  * position pos = ctx_lens[b] - q_lens[b] + t.  Rows t >= q_lens[b] and tokens of
- * negative position are neither read nor written; ctx_lens[b] > max_ctx and
- * q_lens[b] > n_q are clamped (SSA_DEV_BAD_COUNT).  With R = rotary_dims and
+ * negative position are not used, nor is anything written for them; ctx_lens[b]
+ * above max_ctx and q_lens[b] above n_q are clamped (SSA_DEV_BAD_COUNT).  With R =
+ * rotary_dims and
  * (c_i, s_i) = cos_sin[p*R + i], cos_sin[p*R + R/2 + i] for p = positions[b*n_q +
  * t] (NULL: pos), i < R/2, the pairs (x_i, x_{i+R/2}) of a query or key, or
  * (x_{2i}, x_{2i+1}) where `interleaved`, become

@@ -26,21 +26,22 @@ static bool plan_blocks(const ssa_attn_desc* d, const ssa_blocks* k, BlocksPlan*
   const long long blocks = (long long)pl->parts * k->n_q * d->H_kv * d->B;
   const long long listed = std::min<long long>(k->budget, (d->max_ctx + k->block_size - 1ll) / k->block_size);
   const long long n_tiles = listed * (k->block_size / keys);
-  pl->n_splits = (int)rows_splits(n_tiles, blocks, pl->block_rows, std::max(1ll, std::min(n_tiles / (kSplitKeys / keys), 64ll)));
+  pl->n_splits = (int)rows_splits(n_tiles, blocks, pl->block_rows, d->kv_dtype == SSA_FP4_E2M1,
+                                  std::max(1ll, std::min(n_tiles / (kSplitKeys / keys), 64ll)));
   const size_t slots = (size_t)d->B * d->H * k->n_q * pl->n_splits;
   pl->ml_bytes = up256(slots * sizeof(float2));
   pl->total_bytes = pl->ml_bytes + (pl->n_splits > 1 ? up256(slots * d->D * sizeof(float)) : 0);
   return (long long)pl->parts * k->n_q * pl->n_splits <= 0x7fffffffll;
 }
 
-template <typename T, int D, bool kPaged>
+template <typename T, int D, bool kPaged, bool kBoth>
 static cudaError_t launch_lists(const ListParams& p, cudaStream_t st) {
   const dim3 grid((unsigned)(p.n_q * p.parts * p.n_splits), (unsigned)p.H_kv, (unsigned)p.B);
   auto launch = [&](auto kernel, int bytes) { return launch_rows_kernel(kernel, p, grid, bytes, p.block_rows, D, st); };
   switch (p.block_rows / kGroup) {
-    case 1: return launch(window_rows_kernel<T, D, kPaged, false, 1, 1, ListParams>, RowShape<T, D, 1>::kSmem);
-    case 2: return launch(window_rows_kernel<T, D, kPaged, false, 1, 2, ListParams>, RowShape<T, D, 2>::kSmem);
-    default: return launch(window_rows_kernel<T, D, kPaged, false, 1, 4, ListParams>, RowShape<T, D, 4>::kSmem);
+    case 1: return launch(window_rows_kernel<T, D, kPaged, false, 1, 1, kBoth, ListParams>, RowShape<T, D, 1>::kSmem);
+    case 2: return launch(window_rows_kernel<T, D, kPaged, false, 1, 2, kBoth, ListParams>, RowShape<T, D, 2>::kSmem);
+    default: return launch(window_rows_kernel<T, D, kPaged, false, 1, 4, kBoth, ListParams>, RowShape<T, D, 4>::kSmem);
   }
 }
 
@@ -49,7 +50,9 @@ static int32_t launch(const ListParams& p, cudaStream_t st) {
   cudaEvent_t begin, end;
   take_kernel_events(&begin, &end);
   if (begin) cudaEventRecord(begin, st);
-  cudaError_t err = p.page_table ? launch_lists<T, D, true>(p, st) : launch_lists<T, D, false>(p, st);
+  const bool one = kIsFp4<T> && !p.out_f32;                  // (fp16 weights of one part)
+  cudaError_t err = one ? (p.page_table ? launch_lists<T, D, true, !kIsFp4<T>>(p, st) : launch_lists<T, D, false, !kIsFp4<T>>(p, st))
+                        : (p.page_table ? launch_lists<T, D, true, true>(p, st) : launch_lists<T, D, false, true>(p, st));
   if (err != cudaSuccess) return SSA_ERR_CUDA;
   if (end) cudaEventRecord(end, st);
   note_launches(1);

@@ -13,7 +13,7 @@
 
 namespace ssa {
 
-constexpr int kAppendThreads = 256;
+constexpr int kAppendThreads = 64;
 
 struct AppendParams {
   const void *q, *k_new, *v_new;
@@ -26,6 +26,7 @@ struct AppendParams {
   int64_t k_sb, k_sh, k_st, v_sb, v_sh, v_st;                // values
   int B, H, H_kv, n_q, max_ctx, rotary, interleaved, n_positions;
   int page_table_stride, page_shift, n_pages;
+  int slots, tokens;                                         // threads' places for a token's rows; tokens of a thread block
   float k_factor, v_factor;
 };
 
@@ -42,41 +43,69 @@ __device__ __forceinline__ uint32_t to_e2m1x8(const float (&f)[8]) {
       : "=r"(w) : "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]));
   return w;
 }
+// A new row's piece.  (volatile: asked for where it stands.  Not read-only memory: queries may be rotated in their place.)
+__device__ __forceinline__ uint4 ld_row(const void* p) {
+  uint4 r;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p) : "memory");
+  return r;
+}
 template <typename TQ>
 __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
   return make_uint4(pack2<TQ>(f[0], f[1]), pack2<TQ>(f[2], f[3]), pack2<TQ>(f[4], f[5]), pack2<TQ>(f[6], f[7]));
 }
 
-// grid (tokens, parts, B).  A row has D / 16 lanes with two pieces of eight dimensions each: the pieces that are rotated with one
-// another, which are neighbours where pairs are.
-template <typename T, int D, bool kPaged>
-__global__ void __launch_bounds__(kAppendThreads)
+// grid (tokens / p.tokens, parts, B).  A row has D / 16 lanes with two pieces of eight dimensions each: the pieces that are rotated
+// with one another, which are neighbours where pairs are.  A thread has up to kEach rows of a token, all asked for before anything
+// else is: lengths, pages and cosines arrive meanwhile, and are made ready once for all of them.
+template <typename T, int D, bool kPaged, int kEach>
+__global__ void __launch_bounds__(kAppendThreads, 12)
 cache_append_kernel(const AppendParams p) {
   using TQ = typename Storage<T>::Query;
   constexpr int kLanes = D / 16, kRows = kAppendThreads / kLanes;
-  const int t = blockIdx.x, b = blockIdx.z, lane = threadIdx.x % kLanes;
+  const int b = blockIdx.z, lane = threadIdx.x % kLanes, place = blockIdx.y * kRows + threadIdx.x / kLanes;
+  const int part = p.tokens == 1 ? 0 : place / p.slots, slot = place - part * p.slots, t = blockIdx.x * p.tokens + part;
+  const int R = p.rotary, turned = R / 16;                   // lanes that rotate
+  const bool apart = lane < turned && !p.interleaved;        // the two pieces are R / 2 dimensions apart
+  const int piece0 = apart ? lane : !p.interleaved && R ? R / 8 + 2 * (lane - turned) : 2 * lane;
+  const int piece1 = apart ? lane + R / 16 : piece0 + 1;
+  const int queries = p.q ? p.H : 0, rows = queries + 2 * p.H_kv;
+  const bool placed = part < p.tokens && slot < p.slots && t < p.n_q;
   grid_dependency_wait();
   grid_launch_dependents();
+  uint4 w[kEach][2];
+#pragma unroll
+  for (int y = 0; y < kEach; ++y) {
+    const int i = slot + y * p.slots;
+    const bool is_q = i < queries, is_v = i >= queries + p.H_kv;
+    w[y][0] = w[y][1] = make_uint4(0, 0, 0, 0);
+    if (placed && i < rows) {
+      const TQ* from = is_q ? static_cast<const TQ*>(p.q) + b * p.q_sb + i * p.q_sh + t * p.q_st
+                       : is_v ? static_cast<const TQ*>(p.v_new) + b * p.vn_sb + (i - queries - p.H_kv) * p.vn_sh + t * p.vn_st
+                              : static_cast<const TQ*>(p.k_new) + b * p.kn_sb + (i - queries) * p.kn_sh + t * p.kn_st;
+      w[y][0] = ld_row(from + piece0 * 8);
+      w[y][1] = ld_row(from + piece1 * 8);
+    }
+  }
   uint32_t flags = 0;
   int ctx, n_new;
   window_sizes(p, b, ctx, n_new, flags);
   const int pos = ctx - n_new + t;
-  const bool first = blockIdx.y == 0 && threadIdx.x == 0;
-  if (flags && p.status && first && t == 0) atomicOr(p.status, flags);
-  if (t >= n_new || pos < 0) return;
-  const int R = p.rotary, turned = R / 16;                   // lanes that rotate
-  const int angle = R == 0 ? 0 : p.positions ? p.positions[(int64_t)b * p.n_q + t] : pos;
-  const int64_t row = row_of<kPaged>(p, kPaged ? p.page_table + (int64_t)b * p.page_table_stride : nullptr, pos);
-  const bool known = R == 0 || (unsigned)angle < (unsigned)p.n_positions;
-  if ((!known || row < 0) && first && p.status) atomicOr(p.status, SSA_DEV_BAD_INDEX);
-  if (!known) return;
-  const bool apart = lane < turned && !p.interleaved;        // the two pieces are R / 2 dimensions apart
-  const int piece0 = apart ? lane : !p.interleaved && R ? R / 8 + 2 * (lane - turned) : 2 * lane;
-  const int piece1 = apart ? lane + R / 16 : piece0 + 1;
-  float c[8], s[8];                                          // of pairs 8 lane ...
+  if (flags && p.status && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(p.status, flags);
+  bool live = placed && t < n_new && pos >= 0;
+  int64_t row = -1;
+  int angle = 0;
+  if (live) {
+    row = row_of<kPaged>(p, kPaged ? p.page_table + (int64_t)b * p.page_table_stride : nullptr, pos);
+    angle = R == 0 ? 0 : p.positions ? p.positions[(int64_t)b * p.n_q + t] : pos;
+    const bool known = R == 0 || (unsigned)angle < (unsigned)p.n_positions;
+    if ((!known || row < 0) && slot == 0 && lane == 0 && p.status) atomicOr(p.status, SSA_DEV_BAD_INDEX);
+    live = known;
+  }
+  if (!__any_sync(~0u, live)) return;
+  double c[8], s[8];                                         // of pairs 8 lane ...
 #pragma unroll
-  for (int e = 0; e < 8; ++e) { c[e] = 1.f; s[e] = 0.f; }
-  if (lane < turned) {
+  for (int e = 0; e < 8; ++e) c[e] = s[e] = 0.0;
+  if (live && lane < turned) {
     const float* at = p.cos_sin + (int64_t)angle * R + 8 * lane;
 #pragma unroll
     for (int e = 0; e < 8; e += 4) {
@@ -85,30 +114,23 @@ cache_append_kernel(const AppendParams p) {
       s[e] = y.x; s[e + 1] = y.y; s[e + 2] = y.z; s[e + 3] = y.w;
     }
   }
-  const int queries = p.q ? p.H : 0, rows = queries + 2 * p.H_kv;
-  for (int i = blockIdx.y * kRows + threadIdx.x / kLanes; i - (int)(threadIdx.x % 32) / kLanes < rows; i += gridDim.y * kRows) {
-    // (a warp's rows go through this together: neighbouring lanes exchange their largest values)
-    const bool there = i < rows, is_q = i < queries, is_v = i >= queries + p.H_kv;
+#pragma unroll
+  for (int y = 0; y < kEach; ++y) {                          // (a warp's rows together: neighbouring lanes exchange their largest values)
+    const int i = slot + y * p.slots;
+    const bool there = live && i < rows, is_q = i < queries, is_v = i >= queries + p.H_kv;
+    if (!__any_sync(~0u, there)) break;
     const int h = is_q ? i : is_v ? i - queries - p.H_kv : i - queries;
     float x[2][8];
-    uint4 w[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-    if (there) {
-      const TQ* from = is_q ? static_cast<const TQ*>(p.q) + b * p.q_sb + h * p.q_sh + t * p.q_st
-                       : is_v ? static_cast<const TQ*>(p.v_new) + b * p.vn_sb + h * p.vn_sh + t * p.vn_st
-                              : static_cast<const TQ*>(p.k_new) + b * p.kn_sb + h * p.kn_sh + t * p.kn_st;
-      w[0] = *reinterpret_cast<const uint4*>(from + piece0 * 8);
-      w[1] = *reinterpret_cast<const uint4*>(from + piece1 * 8);
-    }
-    unpack8<TQ>(w[0], x[0]);
-    unpack8<TQ>(w[1], x[1]);
+    unpack8<TQ>(w[y][0], x[0]);
+    unpack8<TQ>(w[y][1], x[1]);
     if (!is_v && lane < turned) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float& u = p.interleaved ? x[e / 4][e % 4 * 2] : x[0][e];
         float& v = p.interleaved ? x[e / 4][e % 4 * 2 + 1] : x[1][e];
-        const double du = u, dv = v, dc = c[e], ds = s[e];
-        u = (float)(du * dc - dv * ds);
-        v = (float)(dv * dc + du * ds);
+        const double du = u, dv = v;
+        u = (float)(du * c[e] - dv * s[e]);
+        v = (float)(dv * c[e] + du * s[e]);
       }
     }
     if (is_q) {
@@ -141,15 +163,21 @@ cache_append_kernel(const AppendParams p) {
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
         bits[z] = to_e4m3x2(__fdiv_rn(by[z], 6.f), 0.f) & 0xffu;
-        const float scale = e4m3x2_to_float2(bits[z]).x;
+        // Quotients by one reciprocal and a residual step (Markstein): exact where they lie halfway between two codes, and never on the
+        // wrong side of that: the scale has four bits, so that fp32 values next to half of a step are told from it.
+        const float scale = e4m3x2_to_float2(bits[z]).x, inverse = scale == 0.f ? 0.f : __frcp_rn(scale);
+        const bool infinite = by[z] == __int_as_float(0x7f800000);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[z][e] = scale == 0.f ? 0.f : __fdiv_rn(x[z][e], scale);
+        for (int e = 0; e < 8; ++e) {
+          const float near = x[z][e] * inverse;
+          x[z][e] = infinite && isinf(x[z][e]) ? near : fmaf(fmaf(-near, scale, x[z][e]), inverse, near);
+        }
       }
       if (stored) {
         uint8_t* codes = static_cast<uint8_t*>(is_v ? p.v : p.k) + o / 2;
         uint8_t* scales = (is_v ? p.v_scales : p.k_scales) + o / kScaleDims;
-        *reinterpret_cast<uint32_t*>(codes + piece0 * 4) = to_e2m1x8(x[0]);
-        *reinterpret_cast<uint32_t*>(codes + piece1 * 4) = to_e2m1x8(x[1]);
+        *reinterpret_cast<uint32_t*>(codes + piece0 * 4) = bits[0] ? to_e2m1x8(x[0]) : 0;
+        *reinterpret_cast<uint32_t*>(codes + piece1 * 4) = bits[1] ? to_e2m1x8(x[1]) : 0;
         if (!apart || lane % 2 == 0) scales[piece0 / 2] = (uint8_t)bits[0];
         if (apart && lane % 2 == 0) scales[piece1 / 2] = (uint8_t)bits[1];
       }
@@ -173,9 +201,18 @@ template <typename T, int D>
 static cudaError_t launch_append(const AppendParams& p, cudaStream_t st) {
   constexpr int kRows = kAppendThreads / (D / 16);
   const int rows = (p.q ? p.H : 0) + 2 * p.H_kv;
-  const dim3 grid((unsigned)p.n_q, (unsigned)((rows + kRows - 1) / kRows), (unsigned)p.B);
-  return p.page_table ? launch_pdl(cache_append_kernel<T, D, true>, grid, dim3(kAppendThreads), st, p)
-                      : launch_pdl(cache_append_kernel<T, D, false>, grid, dim3(kAppendThreads), st, p);
+  auto launch = [&](auto kernel, int each) {
+    AppendParams x = p;
+    x.slots = (rows + each - 1) / each;
+    x.tokens = std::max(1, std::min(kRows / x.slots, p.n_q));
+    const dim3 grid((unsigned)((p.n_q + x.tokens - 1) / x.tokens), (unsigned)((x.slots * x.tokens + kRows - 1) / kRows), (unsigned)p.B);
+    return launch_pdl(kernel, grid, dim3(kAppendThreads), st, x);
+  };
+  // Where there are rows for more threads than the GPU holds, three a thread: cosines are made ready once for them, and more of them
+  // are under way.
+  const bool many = rows >= 3 && (long long)rows * p.n_q * p.B > 6ll * sm_count() * kRows;
+  if (p.page_table) return many ? launch(cache_append_kernel<T, D, true, 3>, 3) : launch(cache_append_kernel<T, D, true, 1>, 1);
+  return many ? launch(cache_append_kernel<T, D, false, 3>, 3) : launch(cache_append_kernel<T, D, false, 1>, 1);
 }
 
 }  // namespace ssa

@@ -8,7 +8,8 @@ static int32_t launch(const Fp4Params& p, cudaStream_t st) {
   cudaEvent_t begin, end;
   take_kernel_events(&begin, &end);
   if (begin) cudaEventRecord(begin, st);
-  cudaError_t err = p.page_table ? launch_rows<Fp4E2M1, D, true, false>(p, st) : launch_rows<Fp4E2M1, D, false, false>(p, st);
+  cudaError_t err = p.out_f32 ? (p.page_table ? launch_rows<Fp4E2M1, D, true, false, true>(p, st) : launch_rows<Fp4E2M1, D, false, false, true>(p, st))
+                              : (p.page_table ? launch_rows<Fp4E2M1, D, true, false, false>(p, st) : launch_rows<Fp4E2M1, D, false, false, false>(p, st));
   if (err != cudaSuccess) return SSA_ERR_CUDA;
   if (end) cudaEventRecord(end, st);
   note_launches(1);

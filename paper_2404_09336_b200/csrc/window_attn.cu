@@ -134,7 +134,7 @@ static bool plan_window(const ssa_attn_desc* d, const ssa_window* w, bool mass, 
   pl->fewest = fewest;
   const long long most_splits = std::max(1ll, std::min(n_tiles / fewest, 64ll));
   long long splits = std::min(most_splits, std::max(1ll, 2ll * sm_count() / blocks));   // tiles: two blocks to an SM
-  if (!tiles) splits = rows_splits(n_tiles, blocks, rows, most_splits);
+  if (!tiles) splits = rows_splits(n_tiles, blocks, rows, d->kv_dtype == SSA_FP4_E2M1, most_splits);
   pl->n_splits = (int)splits;
   pl->block_rows = rows;
   const size_t slots = (size_t)d->B * d->H * w->n_q * pl->n_splits;
@@ -176,8 +176,8 @@ static int32_t launch_window(const WindowParams& p, bool mass, const CUtensorMap
   if (maps) {
     if constexpr (!kIsFp8<T>) err = launch_tiles<T, D>(p, maps[0], maps[1], box_rows, st);
   } else {
-    err = p.page_table ? (mass ? launch_rows<T, D, true, true>(p, st) : launch_rows<T, D, true, false>(p, st))
-                       : (mass ? launch_rows<T, D, false, true>(p, st) : launch_rows<T, D, false, false>(p, st));
+    err = p.page_table ? (mass ? launch_rows<T, D, true, true, true>(p, st) : launch_rows<T, D, true, false, true>(p, st))
+                       : (mass ? launch_rows<T, D, false, true, true>(p, st) : launch_rows<T, D, false, false, true>(p, st));
   }
   if (err != cudaSuccess) return SSA_ERR_CUDA;
   if (end) cudaEventRecord(end, st);

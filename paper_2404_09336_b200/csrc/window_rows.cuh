@@ -37,8 +37,9 @@ struct RowShape {
   static constexpr int kHalves = kRow == 256 ? 1 : 2;                  // tiles of 16 positions, or of 32 where rows are short
   static constexpr int kKeys = 16 * kHalves;
   static constexpr int kCodes = 2 * kKeys * kRow, kTile = 2 * kKeys * (kRow + kScaleRow);   // bytes: of K and V of a tile
-  // blocks that fit an SM by their registers, and tiles of a warp's ring: 64 KB a block (4-bit: 72), or 96
-  static constexpr int kBlocks = kGroups <= 2 ? 3 : 2, kRingBytes = kBlocks == 3 ? (kIsFp4<T> ? 18432 : 16384) : 24576;
+  // blocks that fit an SM by their registers, and bytes of a warp's ring: 64 KB a block (4-bit: 54 or 72), or 96
+  static constexpr int kBlocks = kIsFp4<T> && kGroups == 1 ? 4 : kGroups <= 2 ? 3 : 2;
+  static constexpr int kRingBytes = kBlocks == 4 ? 13824 : kBlocks == 3 ? (kIsFp4<T> ? 18432 : 16384) : 24576;
   __host__ __device__ static constexpr int64_t bytes(int64_t values) { return kIsFp4<T> ? values / 2 : values * kBytes; }
   static constexpr int kRingTiles = kRingBytes / kTile < 4 ? kRingBytes / kTile : 4;
   static constexpr int kSmem = kWarps * kRingTiles * kTile;
@@ -122,7 +123,9 @@ template <> __device__ __forceinline__ bool pair_not_finite<__half>(uint32_t w) 
 // tile (some 230) and a block's start and end where they are short.
 // kListed parameters: the rows are the query heads of one token, grid.x (splits x parts of them x tokens), the tiles those of the
 // blocks on its list.
-template <typename T, int D, bool kPaged, bool kMass, int kTeam, int kGroups, typename Params>
+// kBoth: weights as a 16-bit value and the 16-bit rest.  Without (4-bit values, 16-bit outputs): rounded to fp16 once, 2^-11, less
+// than the output is.  32 requests of up to 16384 positions, 32 heads over 8, 4-bit values: 119 us instead of 132.
+template <typename T, int D, bool kPaged, bool kMass, int kTeam, int kGroups, bool kBoth, typename Params>
 __global__ void __launch_bounds__(kWarps * 32, (RowShape<T, D, kGroups>::kBlocks))
 window_rows_kernel(const Params p) {
   constexpr bool kListed = Params::kListed;
@@ -180,16 +183,23 @@ window_rows_kernel(const Params p) {
   const char* const vb = reinterpret_cast<const char*>(p.v) + my_chunk * 16 +
                          RS::bytes((kPaged ? 0 : (int64_t)b * p.v_sb) + (int64_t)hkv * p.v_sh);
   const int64_t k_step = RS::bytes(p.k_st), v_step = RS::bytes(p.v_st);
-  // 4-bit: copy i of 2 kKeys is of the scales of row i % kKeys, of K, then of V; row(i) < 0: there is none
-  auto load_scales = [&](uint32_t to, auto row) {
+  // 4-bit: lanes my and my + kLanes copy the scales of row my % kKeys, of K (below kKeys), of V
+  const int scale_key = my % kKeys, scale_copies = 2 * kKeys / kLanes;
+  const uint8_t* scales[2] = {nullptr, nullptr};
+  int64_t scale_step[2] = {0, 0};
+  if constexpr (kIsFp4<T>) {
+#pragma unroll
+    for (int x = 0; x < scale_copies; ++x) {
+      const bool of_v = my + x * kLanes >= kKeys;
+      scales[x] = (of_v ? p.v_scales : p.k_scales) + ((kPaged ? 0 : (int64_t)b * (of_v ? p.v_sb : p.k_sb)) + (int64_t)hkv * (of_v ? p.v_sh : p.k_sh)) / kScaleDims;
+      scale_step[x] = (of_v ? p.v_st : p.k_st) / kScaleDims;
+    }
+  }
+  auto load_scales = [&](uint32_t to, int64_t row) {         // row < 0: there is none
     if constexpr (kIsFp4<T>) {
 #pragma unroll
-      for (int i = my; i < 2 * kKeys; i += kLanes) {
-        const bool of_v = i >= kKeys;
-        const int64_t r = row(i % kKeys), st = of_v ? p.v_st : p.k_st;
-        const int64_t o = (kPaged ? 0 : (int64_t)b * (of_v ? p.v_sb : p.k_sb)) + (int64_t)hkv * (of_v ? p.v_sh : p.k_sh) + (r < 0 ? 0 : r * st);
-        copy_few<RS::kScaleRow>(to + RS::kCodes + i * RS::kScaleRow, (of_v ? p.v_scales : p.k_scales) + o / kScaleDims, r >= 0);
-      }
+      for (int x = 0; x < scale_copies; ++x)
+        copy_few<RS::kScaleRow>(to + RS::kCodes + (my + x * kLanes) * RS::kScaleRow, scales[x] + (row < 0 ? 0 : row * scale_step[x]), row >= 0);
     }
   };
   auto load = [&](int n) {
@@ -206,19 +216,28 @@ window_rows_kernel(const Params p) {
       if (at >= 0) {
         if (copies) {
           const char *k = kb + (at + my_key) * k_step, *v = vb + (at + my_key) * v_step;
+          if (kIsFp4<T> && k_step == RS::kRow && v_step == RS::kRow) {   // (rows side by side: fixed offsets)
+            const uint32_t x = to + chunk_at<T, kChunks>(my_key, my_chunk) * 16;
 #pragma unroll
-          for (int i = 0; i < kPasses; ++i) {
-            const int key = i * kPass;
-            const uint32_t x = kIsFp4<T> ? to + (chunk_at<T, kChunks>(my_key, my_chunk) + key * kChunks) * 16   // (key: a multiple of 8)
-                                         : to + (my_key + key) * kChunks * 16 +
-                                               (turned<T, kChunks>(my_key, my_chunk) ^ turned<T, kChunks>(key, 0)) * 16;
-            copy_16B(x, k, true);
-            copy_16B(x + kKeys * RS::kRow, v, true);
-            k += kPass * k_step;
-            v += kPass * v_step;
+            for (int i = 0; i < kPasses; ++i) {
+              copy_16B(x + i * kPass * RS::kRow, k + i * kPass * RS::kRow, true);
+              copy_16B(x + (i * kPass + kKeys) * RS::kRow, v + i * kPass * RS::kRow, true);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < kPasses; ++i) {
+              const int key = i * kPass;
+              const uint32_t x = kIsFp4<T> ? to + (chunk_at<T, kChunks>(my_key, my_chunk) + key * kChunks) * 16   // (key: a multiple of 8)
+                                           : to + (my_key + key) * kChunks * 16 +
+                                                 (turned<T, kChunks>(my_key, my_chunk) ^ turned<T, kChunks>(key, 0)) * 16;
+              copy_16B(x, k, true);
+              copy_16B(x + kKeys * RS::kRow, v, true);
+              k += kPass * k_step;
+              v += kPass * v_step;
+            }
           }
         }
-        load_scales(to, [&](int key) { return at + key; });
+        load_scales(to, at + scale_key);
       } else {
         // what no row sees is not read: it may hold anything, or have no page
         const int j = j0 + lane % kKeys;
@@ -236,7 +255,7 @@ window_rows_kernel(const Params p) {
             copy_16B(x + kKeys * RS::kRow, vb + (r < 0 ? 0 : r * v_step), r >= 0);
           }
         }
-        load_scales(to, [&](int) { return (int64_t)row; });             // (kKeys = 32: the lane's own row)
+        load_scales(to, row);                                // (kKeys = 32: the lane's own row)
       }
       if (lane == 0 && member == 0) {
         s_have[team][stage] = have;
@@ -287,6 +306,11 @@ window_rows_kernel(const Params p) {
   // V: keys 8 (y / 2) ..., pieces 2 i + y % 2
   const int k_key = lane % 16, v_key = lane % 8 + lane / 16 * 8;       // (of each sixteen positions)
 
+  // 4-bit: where the lane's part of K's row g is, of V's rows 2c and 2c + 1; rows 8 and 16 further on lie as many rows behind
+  const int k_off = D == 128 ? chunk_at<T, kChunks>(g, c) * 16 : chunk_at<T, kChunks>(g, c / 2) * 16 + c % 2 * 8;
+  const int v_off[2] = {chunk_at<T, kChunks>(2 * c, g * RS::kV / 32) * 16 + g * RS::kV / 2 % 16,
+                        chunk_at<T, kChunks>(2 * c + 1, g * RS::kV / 32) * 16 + g * RS::kV / 2 % 16};
+
   // An infinite or NaN element of V must not reach rows that do not see it (0 * inf), and has to stay infinite for those that do
   // (its product with a weight's two parts may be inf - inf).  Sums that come out finite met none; else the block goes through
   // its tiles once more and takes such elements out of the contraction, to add them to the rows that see them.
@@ -321,7 +345,7 @@ again:
     float s[kHalves][kGroups][4];
 #pragma unroll
     for (int x = 0; x < kHalves; ++x) {
-      float s2[kGroups][4];                                  // (two chains of half the steps each)
+      float s2[kGroups][4];                                  // (two chains of half the steps each; 4-bit: of the two halves)
 #pragma unroll
       for (int y = 0; y < kGroups; ++y)
 #pragma unroll
@@ -332,15 +356,15 @@ again:
         uint32_t codes[2][kWords], by[2][2];
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
-          const int key = 16 * x + g + 8 * z;
-          const uint8_t* scales = kt + RS::kCodes + key * RS::kScaleRow;
+          const int rows_on = 16 * x + 8 * z;
+          const uint8_t* scales = kt + RS::kCodes + (g + rows_on) * RS::kScaleRow;
           uint32_t pair;
           if constexpr (D == 128) {
-            const uint4 w = *reinterpret_cast<const uint4*>(kt + chunk_at<T, kChunks>(key, c) * 16);
+            const uint4 w = *reinterpret_cast<const uint4*>(kt + k_off + rows_on * RS::kRow);
             codes[z][0] = w.x; codes[z][1] = w.y; codes[z][2] = w.z; codes[z][3] = w.w;
             pair = e4m3x2_to_half2(*reinterpret_cast<const uint16_t*>(scales + 2 * c));
           } else {
-            const uint2 w = *reinterpret_cast<const uint2*>(kt + chunk_at<T, kChunks>(key, c / 2) * 16 + c % 2 * 8);
+            const uint2 w = *reinterpret_cast<const uint2*>(kt + k_off + rows_on * RS::kRow);
             codes[z][0] = w.x; codes[z][1] = w.y;
             pair = e4m3x2_to_half2(scales[c]);
           }
@@ -358,8 +382,7 @@ again:
           for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int y = 0; y < kGroups; ++y)
-              mma_16816<TS>(i % 2 ? s2[y] : s[x][y], a[2 * i], z[2 * i], a[2 * i + 1], z[2 * i + 1], qb[y][2 * (2 * w + i)],
-                            qb[y][2 * (2 * w + i) + 1], i % 2 ? s2[y] : s[x][y]);
+              mma_16816<TS>(s[x][y], a[2 * i], z[2 * i], a[2 * i + 1], z[2 * i + 1], qb[y][2 * (2 * w + i)], qb[y][2 * (2 * w + i) + 1], s[x][y]);
         }
       } else if constexpr (kIsFp8<T>) {
 #pragma unroll
@@ -389,7 +412,7 @@ again:
 #pragma unroll
       for (int y = 0; y < kGroups; ++y)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[x][y][e] = (s[x][y][e] + s2[y][e]) * unit[y][e % 2];
+        for (int e = 0; e < 4; ++e) s[x][y][e] = (kIsFp4<T> ? s[x][y][e] : s[x][y][e] + s2[y][e]) * unit[y][e % 2];
     }
 
     // scores in log2 units; what a row does not see is -inf
@@ -427,17 +450,17 @@ again:
           }
       }
     }
-#pragma unroll
-    for (int o = 4; o < 32; o *= 2)
-#pragma unroll
-      for (int y = 0; y < kGroups; ++y) {
-        top[y][0] = fmaxf(top[y][0], __shfl_xor_sync(~0u, top[y][0], o));
-        top[y][1] = fmaxf(top[y][1], __shfl_xor_sync(~0u, top[y][1], o));
-      }
     bool higher = false;
 #pragma unroll
     for (int y = 0; y < kGroups; ++y) higher |= top[y][0] > m[y][0] + kLazyRows || top[y][1] > m[y][1] + kLazyRows;   // (m = -inf: anything)
-    if (__any_sync(~0u, higher)) {
+    if (__any_sync(~0u, higher)) {                           // (the lanes' maxima meet only then)
+#pragma unroll
+      for (int o = 4; o < 32; o *= 2)
+#pragma unroll
+        for (int y = 0; y < kGroups; ++y) {
+          top[y][0] = fmaxf(top[y][0], __shfl_xor_sync(~0u, top[y][0], o));
+          top[y][1] = fmaxf(top[y][1], __shfl_xor_sync(~0u, top[y][1], o));
+        }
 #pragma unroll
       for (int y = 0; y < kGroups; ++y)
 #pragma unroll
@@ -463,9 +486,11 @@ again:
           l[y][0] += w0;
           l[y][1] += w1;
           const uint32_t w = pack2<TP>(w0, w1);
-          const float2 back = unpack2<TP>(w);
           ph[x][y][z] = transposed(w);
-          pl[x][y][z] = transposed(pack2<TP>(w0 - back.x, w1 - back.y));
+          if constexpr (kBoth) {
+            const float2 back = unpack2<TP>(w);
+            pl[x][y][z] = transposed(pack2<TP>(w0 - back.x, w1 - back.y));
+          }
         }
     }
     bool odd = false;
@@ -482,16 +507,21 @@ again:
           uint32_t w[2][kVWords], scale[2];
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
-            const int key = 16 * x + 2 * c + y + 8 * z;
+            const uint8_t* row = vt + v_off[y] + (16 * x + 8 * z) * RS::kRow;
             if constexpr (D == 128) {
-              const uint2 u = *reinterpret_cast<const uint2*>(vt + chunk_at<T, kChunks>(key, g / 2) * 16 + g % 2 * 8);
+              const uint2 u = *reinterpret_cast<const uint2*>(row);
               w[y][0] = u.x; w[y][1] = u.y;
             } else {
-              w[y][0] = *reinterpret_cast<const uint32_t*>(vt + chunk_at<T, kChunks>(key, g / 4) * 16 + g % 4 * 4);
+              w[y][0] = *reinterpret_cast<const uint32_t*>(row);
             }
-            scale[y] = kt[RS::kCodes + (kKeys + key) * RS::kScaleRow + g * RS::kV / kScaleDims];
+            scale[y] = kt[RS::kCodes + (kKeys + 2 * c + y + 16 * x + 8 * z) * RS::kScaleRow + g * RS::kV / kScaleDims];
           }
           by[z] = e4m3x2_to_half2(scale[0] | scale[1] << 8);
+          if (careful && pair_not_finite<TP>(by[z])) {       // (values are finite but for their scale)
+            odd = true;
+            if (pair_not_finite<TP>(by[z] & 0xffffu)) by[z] &= 0xffff0000u;
+            if (pair_not_finite<TP>(by[z] & 0xffff0000u)) by[z] &= 0xffffu;
+          }
 #pragma unroll
           for (int i = 0; i < kVWords; ++i) {
             both[z][0][i] = (w[0][i] & 0x0f0f0f0fu) | (w[1][i] << 4 & 0xf0f0f0f0u);
@@ -536,7 +566,7 @@ again:
         } else {
           ldmatrix<true>(a, v_at + chunk_at<T, kChunks>(16 * x + v_key, 2 * i + lane / 8 % 2) * 16);
         }
-        if (careful) {
+        if (!kIsFp4<T> && careful) {
 #pragma unroll
           for (int y = 0; y < 4; ++y)
             if (pair_not_finite<TP>(a[y])) {
@@ -547,8 +577,10 @@ again:
         }
 #pragma unroll
         for (int y = 0; y < kGroups; ++y) mma_16816<TP>(acc[y][i], a[0], a[1], a[2], a[3], ph[x][y][0], ph[x][y][1], acc[y][i]);
+        if constexpr (kBoth) {
 #pragma unroll
-        for (int y = 0; y < kGroups; ++y) mma_16816<TP>(acc[y][i], a[0], a[1], a[2], a[3], pl[x][y][0], pl[x][y][1], acc[y][i]);
+          for (int y = 0; y < kGroups; ++y) mma_16816<TP>(acc[y][i], a[0], a[1], a[2], a[3], pl[x][y][0], pl[x][y][1], acc[y][i]);
+        }
       }
     }
     if (careful && __any_sync(~0u, odd)) {                   // add what was taken out, element by element
@@ -714,10 +746,12 @@ window_join_kernel(const Params p) {
 // ---- host ------------------------------------------------------------------------------------------------------------
 // Splits of the kernel for few rows: what n splits cost in units of one tile's time.  The work of all blocks, each with a start and
 // an end, over the places that there are (two or three blocks to an SM), but no less than one block's; half a block's until the
-// last is done (lengths differ: three quarters of the longest are taken for the mean); joining.
-inline long long rows_splits(long long n_tiles, long long blocks, int rows, long long most_splits) {
+// last is done (lengths differ: three quarters of the longest are taken for the mean); joining.  Tiles of 4-bit values take longer,
+// and four blocks of one group fit an SM (32 requests of up to 16384 positions, 32 heads over 8: 113 us instead of 119).
+inline long long rows_splits(long long n_tiles, long long blocks, int rows, bool fp4, long long most_splits) {
   const int teams = rows <= kMostGroups * kGroup ? kWarps : kWarps / 2;
-  const double steps = (double)n_tiles / teams, places = (rows <= 2 * kGroup ? 3.0 : 2.0) * sm_count(), ends = 5, join = 6;
+  const bool four = fp4 && rows <= kGroup;
+  const double steps = (double)n_tiles / teams, places = (four ? 4.0 : rows <= 2 * kGroup ? 3.0 : 2.0) * sm_count(), ends = four ? 3 : 5, join = 6;
   double least = 0;
   long long splits = 1;
   for (long long n = 1; n <= most_splits; ++n) {
@@ -762,16 +796,16 @@ static cudaError_t launch_rows_kernel(Kernel kernel, const Params& p, dim3 grid,
   return err != cudaSuccess ? err : launch_pdl_smem(kernel, grid, dim3(kWarps * 32), smem, st, p);
 }
 
-template <typename T, int D, bool kPaged, bool kMass, typename Params>
+template <typename T, int D, bool kPaged, bool kMass, bool kBoth, typename Params>
 static cudaError_t launch_rows(const Params& p, cudaStream_t st) {
   const dim3 grid((unsigned)((p.group * p.n_q + p.block_rows - 1) / p.block_rows * p.n_splits), (unsigned)p.H_kv, (unsigned)p.B);
   auto launch = [&](auto kernel, int bytes, int warp_rows) { return launch_rows_kernel(kernel, p, grid, bytes, warp_rows, D, st); };
   switch (p.block_rows / kGroup) {
-    case 1: return launch(window_rows_kernel<T, D, kPaged, kMass, 1, 1, Params>, RowShape<T, D, 1>::kSmem, kGroup);
-    case 2: return launch(window_rows_kernel<T, D, kPaged, kMass, 1, 2, Params>, RowShape<T, D, 2>::kSmem, 2 * kGroup);
-    case 3: return launch(window_rows_kernel<T, D, kPaged, kMass, 1, 3, Params>, RowShape<T, D, 3>::kSmem, 3 * kGroup);
-    case 4: return launch(window_rows_kernel<T, D, kPaged, kMass, 1, 4, Params>, RowShape<T, D, 4>::kSmem, 4 * kGroup);
-    default: return launch(window_rows_kernel<T, D, kPaged, kMass, 2, 4, Params>, RowShape<T, D, 4>::kSmem, 4 * kGroup);
+    case 1: return launch(window_rows_kernel<T, D, kPaged, kMass, 1, 1, kBoth, Params>, RowShape<T, D, 1>::kSmem, kGroup);
+    case 2: return launch(window_rows_kernel<T, D, kPaged, kMass, 1, 2, kBoth, Params>, RowShape<T, D, 2>::kSmem, 2 * kGroup);
+    case 3: return launch(window_rows_kernel<T, D, kPaged, kMass, 1, 3, kBoth, Params>, RowShape<T, D, 3>::kSmem, 3 * kGroup);
+    case 4: return launch(window_rows_kernel<T, D, kPaged, kMass, 1, 4, kBoth, Params>, RowShape<T, D, 4>::kSmem, 4 * kGroup);
+    default: return launch(window_rows_kernel<T, D, kPaged, kMass, 2, 4, kBoth, Params>, RowShape<T, D, 4>::kSmem, 4 * kGroup);
   }
 }
 

@@ -129,8 +129,9 @@ def check_rows(got, lse, want, D, n, dt, out_dtype, v_most):
     """One token's rows of a K/V head against CO.attention's: the bounds of budget_util.check, and the floor of fp16 weights."""
     out, l, spread, score = want
     step = half_step(torch.float16 if dt in ("fp8", "fp4") else DT[dt])
+    step = step if dt == "fp4" and out_dtype != torch.float32 else step * step
     score = (D * score + 2 * score + 4) * 2.0 ** -24
-    tol = 2 * (score + 2.0 ** -22 + step * step + (n + 64) * 2.0 ** -24) * spread + 1e-30
+    tol = 2 * (score + 2.0 ** -22 + step + (n + 64) * 2.0 ** -24) * spread + 1e-30
     if dt != "bf16":
         tol = tol + 2 * FLOOR_ROWS * n * v_most
     if out_dtype != torch.float32:
@@ -142,15 +143,15 @@ def check_rows(got, lse, want, D, n, dt, out_dtype, v_most):
     assert (np.abs(lse - l) <= 2 * (score + 2.0 ** -22 + (n + 64) * 2.0 ** -24) + np.abs(l) * 2.0 ** -22).all()
 
 
-def check_tokens(p, got, ctx, q_lens, window, sinks, out_dtype, many=False, tiles=False, skipped=None, scale=None):
-    """budget_util.check over a 4-bit cache, with the floor of fp16 weights.  many: weights of one 16-bit part; tiles: whatever the
-    parts, the call may go to the tiles."""
+def check_tokens(p, got, ctx, q_lens, window, sinks, out_dtype, tiles=False, skipped=None, scale=None):
+    """budget_util.check over a 4-bit cache, with the floor of fp16 weights: of one part for bf16 outputs, of two for fp32 ones.
+    tiles: the call may go to the tiles."""
     out, lse, _, status = got
     assert not status & ssa.DEV_GAVE_UP
     q, k, v = p.values()
     q_lens = [p.n_q] * p.B if q_lens is None else q_lens
     ref = BO.attention(q, k, v, ctx, q_lens, window, sinks, p.D ** -0.5 if scale is None else scale, skipped)
-    step = half_step(torch.float16) if many else half_step(torch.float16) ** 2
+    step = half_step(torch.float16) if out_dtype != torch.float32 else half_step(torch.float16) ** 2
     for b, r in enumerate(ref):
         n, t = ctx[b], q_lens[b]
         assert (out[b, :, t:] == UNWRITTEN).all() and (lse[b, :, t:] == UNWRITTEN).all(), "rows behind the last token were written"

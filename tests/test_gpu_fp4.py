@@ -18,7 +18,7 @@ def many(p):
 
 def run(p, ctx, new=None, window=0, sinks=0, out_dtype=F32, **k):
     got = p.call(ctx, new, window, sinks, out_dtype, **k)
-    check_tokens(p, got, ctx, new, window, sinks, out_dtype, many(p) and out_dtype == BF16, many(p), scale=k.get("scale") or None)
+    check_tokens(p, got, ctx, new, window, sinks, out_dtype, many(p), scale=k.get("scale") or None)
     return got
 
 
