@@ -140,6 +140,12 @@ __device__ __forceinline__ void e2m1x8_to_half2(uint32_t w, uint32_t (&h)[4]) {
       "cvt.rn.f16x2.e2m1x2 %2, b2; cvt.rn.f16x2.e2m1x2 %3, b3; }"
       : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
 }
+// One such byte -> two floats.  (In all four places: alone in a register that was loaded as a byte it came out as zeros, nvcc 12.9.)
+__device__ __forceinline__ float2 e2m1x2_to_float2(uint8_t byte) {
+  uint32_t h[4];
+  e2m1x8_to_half2(byte * 0x01010101u, h);
+  return __half22float2(*reinterpret_cast<const __half2*>(&h[0]));
+}
 // Two e4m3 values -> two fp16 values (exact).
 __device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t pair) {
   uint32_t h2;

@@ -115,8 +115,8 @@ static int32_t check_window(const ssa_attn_desc* d, const ssa_window* w, bool ma
 
 // Whether the tiles of 128 rows serve a call.
 static bool tiles_pay(const ssa_attn_desc* d, const ssa_window* w, bool mass) {
-  return !mass && d->kv_dtype != SSA_FP8_E4M3 && d->kv_dtype != SSA_FP4_E2M1 && (long long)(d->H / d->H_kv) * w->n_q > kFewRows &&
-         (!w->paging || w->paging->page_size >= 8);          // (a box of a copy is eight rows at least)
+  return !mass && d->kv_dtype != SSA_FP8_E4M3 && (long long)(d->H / d->H_kv) * w->n_q > kFewRows &&
+         (!w->paging || w->paging->page_size >= 8);          // (a box of a copy is eight rows at least, or a lane's run of 4-bit ones)
 }
 
 static bool plan_window(const ssa_attn_desc* d, const ssa_window* w, bool mass, bool tiles, WindowPlan* pl) {
@@ -153,17 +153,6 @@ static size_t window_bytes(const ssa_attn_desc* d, const ssa_window* w, bool mas
   const size_t few = pl.total_bytes;
   if (!tiles_pay(d, w, mass) || !plan_window(d, w, mass, true, &pl)) return few;
   return std::max(few, pl.total_bytes);
-}
-
-template <typename T, int D>
-static cudaError_t launch_tiles(const WindowParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, int box_rows, cudaStream_t st) {
-  const dim3 grid((unsigned)((p.group * p.n_q + kTileRows - 1) / kTileRows * p.n_splits), (unsigned)p.H_kv, (unsigned)p.B);
-  auto kernel = p.page_table ? (p.out_f32 ? window_tile_kernel<T, D, true, true> : window_tile_kernel<T, D, true, false>)
-                             : (p.out_f32 ? window_tile_kernel<T, D, false, true> : window_tile_kernel<T, D, false, false>);
-  constexpr int kSmem = TileShape<D>::kSmem;
-  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-  if (err != cudaSuccess) return err;
-  return launch_pdl_smem(kernel, grid, dim3(kTileThreads), kSmem, st, p, k_map, v_map, box_rows);
 }
 
 template <typename T, int D>
@@ -212,11 +201,12 @@ static int32_t run_window(const ssa_attn_desc* d, const ssa_window* w, const voi
   const int box_rows = pg ? std::min(pg->page_size, kTileKeys) : kTileKeys;
   const int64_t pool_rows = pg ? (int64_t)pg->n_pages * pg->page_size : d->max_ctx;
   WindowPlan pl;
+  auto mapped = [&](CUtensorMap* map, const void* cache, int64_t st, int64_t sh, int64_t sb) {
+    return tile_map(map, cache, d->kv_dtype, d->D, pool_rows, st, d->H_kv, sh, pg ? 1 : d->B, sb, box_rows);
+  };
   const bool tiles = tiles_pay(d, w, mass) && plan_window(d, w, mass, true, &pl) &&
-                     tile_map(&maps[0], k, d->kv_dtype, d->D, pool_rows, d->k_stride_t, d->H_kv, d->k_stride_h, pg ? 1 : d->B,
-                              d->k_stride_b, box_rows) &&
-                     tile_map(&maps[1], v, d->kv_dtype, d->D, pool_rows, d->v_stride_t, d->H_kv, d->v_stride_h, pg ? 1 : d->B,
-                              d->v_stride_b, box_rows);
+                     (fp4 || (mapped(&maps[0], k, d->k_stride_t, d->k_stride_h, d->k_stride_b) &&
+                              mapped(&maps[1], v, d->v_stride_t, d->v_stride_h, d->v_stride_b)));
   if (!tiles && !plan_window(d, w, mass, false, &pl)) return SSA_ERR_SHAPE;
   WindowParams p;
   p.block_rows = pl.block_rows;
@@ -239,7 +229,7 @@ static int32_t run_window(const ssa_attn_desc* d, const ssa_window* w, const voi
     static_cast<WindowParams&>(f) = p;
     f.k_scales = static_cast<const uint8_t*>(k_scales);
     f.v_scales = static_cast<const uint8_t*>(v_scales);
-    return launch_window_fp4(f, d->D, st);
+    return launch_window_fp4(f, d->D, tiles ? box_rows : 0, st);
   }
   const CUtensorMap* m = tiles ? maps : nullptr;
   if (d->kv_dtype == SSA_FP8_E4M3)

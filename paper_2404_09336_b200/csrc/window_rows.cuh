@@ -84,9 +84,9 @@ template <int kLeft>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
 // A row of bf16 queries over an 8-bit cache as fp16 values times a power of two that brings its largest to 2^14: what the others
-// lose is below 2^-39 of that.  w: the row's part of this lane, the rest in the three neighbouring lanes.  Returns the power's
+// lose is below 2^-39 of that.  w: the row's part of this lane, the rest in the kLanes - 1 neighbouring lanes.  Returns the power's
 // inverse.
-template <int N>
+template <int N, int kLanes = 4>
 __device__ __forceinline__ float rows_to_half(uint32_t (&w)[N]) {
   uint32_t most = 0;                                         // bits of the largest finite magnitude
 #pragma unroll
@@ -94,8 +94,8 @@ __device__ __forceinline__ float rows_to_half(uint32_t (&w)[N]) {
     const uint32_t a = w[i] & 0x7fffu, z = w[i] >> 16 & 0x7fffu;
     most = max(most, max(a < 0x7f80u ? a : 0u, z < 0x7f80u ? z : 0u));
   }
-  most = max(most, __shfl_xor_sync(~0u, most, 1));
-  most = max(most, __shfl_xor_sync(~0u, most, 2));
+#pragma unroll
+  for (int o = 1; o < kLanes; o *= 2) most = max(most, __shfl_xor_sync(~0u, most, o));
   const int up = min(141 - (int)(most >> 7), 126);           // 2^up: the exponent 127 + 14 - that of the largest
   const float by = __int_as_float((127 + up) << 23), back = __int_as_float((127 - up) << 23);
 #pragma unroll
@@ -594,9 +594,7 @@ again:
             const uint8_t* v = vt + chunk_at<T, kChunks>(key, at / 16) * 16 + at % 16;
             float f;
             if constexpr (kIsFp4<T>) {                       // (finite but for its scale)
-              uint32_t h[4];
-              e2m1x8_to_half2(*v, h);
-              const float2 pair = unpack2<__half>(h[0]);
+              const float2 pair = e2m1x2_to_float2(*v);
               f = (z ? pair.y : pair.x) * e4m3x2_to_float2(kt[RS::kCodes + (kKeys + key) * RS::kScaleRow + d / kScaleDims]).x;
             } else if constexpr (kIsFp8<T>) f = e4m3x2_to_float2(*v).x;
             else f = to_float(*reinterpret_cast<const TQ*>(v));
@@ -762,7 +760,8 @@ inline long long rows_splits(long long n_tiles, long long blocks, int rows, bool
   return splits;
 }
 inline size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-int32_t launch_window_fp4(const Fp4Params& p, int D, cudaStream_t st);       // (defined in fp4_attn.cu)
+// (defined in fp4_attn.cu; box_rows: rows side by side for certain, for the tiles of 128 rows; 0: the kernel for few rows)
+int32_t launch_window_fp4(const Fp4Params& p, int D, int box_rows, cudaStream_t st);
 
 // What the calls' parameters have in common.
 inline void fill_params(WindowParams& p, const ssa_attn_desc* d, int32_t n_q, int64_t q_stride_t, int64_t o_stride_t,

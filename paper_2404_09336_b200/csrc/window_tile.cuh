@@ -1,4 +1,5 @@
-// Window attention of many query rows per K/V head (prompt chunks): tcgen05 tiles.  Included by window_attn.cu.
+// Window attention of many query rows per K/V head (prompt chunks): tcgen05 tiles.  Included by window_attn.cu and, for caches of
+// 4-bit values, by fp4_attn.cu.
 //
 // A block serves 128 (token, head of the group) rows of one K/V head and goes through the tiles of 128 positions that they see
 // between them.  Both contractions are tcgen05.mma in steps of 16 with fp32 accumulators:
@@ -21,28 +22,36 @@
 // as that output is rounded.  An fp32 output keeps the rest of each weight as a second 16-bit part, over the other half of S, with
 // a contraction of its own, as in the kernel for few rows.  (Instructions, not the special function unit, bound the softmax: with a
 // quarter of the powers on the FMA units prompts took 7 % longer.)
+//
+// 4-bit values become fp16 on their way into shared memory (exactly: six significant bits), by warps 5 to 7: codes arrive by
+// asynchronous copies, a K or V tile ahead, each thread converts the pieces that it asked for, scales them and writes them where a
+// TMA copy with its swizzle would have put them, zeros for what no token sees.  Query rows become fp16 times a power of two of their
+// own (rows_to_half), weights are fp16.
 #pragma once
 #include <cuda.h>
 
 #include <type_traits>
 
-#include "mma.cuh"
-#include "window.cuh"
+#include "window_rows.cuh"
 
 namespace ssa {
 
 constexpr int kTileRows = 128, kTileKeys = 128;
 constexpr int kTileThreads = 256;
-constexpr int kSoftmaxRegs = 200, kOtherRegs = 56;  // of a thread; 128 x 200 + 128 x 56 = 256 x 128, what the launch has
+// registers of a thread; 128 x 200 + 128 x 56 (4-bit: 192, 64) = 256 x 128, what the launch has
+template <typename T> constexpr int kSoftmaxRegs = kIsFp4<T> ? 192 : 200;
+template <typename T> constexpr int kOtherRegs = kIsFp4<T> ? 64 : 56;
+constexpr int kConverters = 96;                     // threads of warps 5 to 7
 constexpr int kTileSplit = 4;                       // fewest tiles worth a split of their own
 constexpr float kLazy = 8.f;                        // log2 of how far weights may exceed 1
 
-template <int D>
+template <typename T, int D>
 struct TileShape {
   static constexpr int kQHalf = kTileRows * 128, kHalf = kTileKeys * 128;   // bytes of 64 dimensions of a Q tile, of a K or V tile
   static constexpr int kQBytes = kQHalf * (D / 64), kTileBytes = kHalf * (D / 64);
   static constexpr int kStages = D == 64 ? 4 : 2;                   // K and V tiles of the ring: two blocks fit an SM
-  static constexpr int kSmem = kQBytes + kStages * kTileBytes + 1024;   // (1024: room to align)
+  static constexpr int kPieces = kIsFp4<T> ? kTileKeys * D / 32 : 0;     // of 16 bytes of codes, of a K or V tile
+  static constexpr int kSmem = kQBytes + kStages * kTileBytes + kPieces * 16 + 1024;   // (1024: room to align)
 };
 
 // ---- PTX ------------------------------------------------------------------------------------------------------------
@@ -149,16 +158,34 @@ __device__ constexpr uint32_t tile_idesc() {
 }
 
 // One row again in fp32, by a warp, with the infinities and NaNs of V kept to where they are seen: lane i's dimensions i D/32 ...
-template <typename T, int D, bool kPaged>
-__device__ __noinline__ void careful_row(const WindowParams& p, const Seen& seen, int2 range, int b, int h, int t, int pos, float& m,
+template <typename T, int D, bool kPaged, typename Params>
+__device__ __noinline__ void careful_row(const Params& p, const Seen& seen, int2 range, int b, int h, int t, int pos, float& m,
                                          float& l, float (&acc)[D / 32]) {
   constexpr int kN = D / 32;
+  using TQ = typename Storage<T>::Query;
   const int lane = threadIdx.x % 32, hkv = h / p.group;
-  const T* q = reinterpret_cast<const T*>(p.q) + (int64_t)b * p.q_sb + (int64_t)h * p.q_sh + (int64_t)t * p.q_st + lane * kN;
-  const T* k = reinterpret_cast<const T*>(p.k) + (kPaged ? 0 : (int64_t)b * p.k_sb) + (int64_t)hkv * p.k_sh + lane * kN;
-  const T* v = reinterpret_cast<const T*>(p.v) + (kPaged ? 0 : (int64_t)b * p.v_sb) + (int64_t)hkv * p.v_sh + lane * kN;
+  const TQ* q = reinterpret_cast<const TQ*>(p.q) + (int64_t)b * p.q_sb + (int64_t)h * p.q_sh + (int64_t)t * p.q_st + lane * kN;
+  const int64_t k0 = (kPaged ? 0 : (int64_t)b * p.k_sb) + (int64_t)hkv * p.k_sh + lane * kN;
+  const int64_t v0 = (kPaged ? 0 : (int64_t)b * p.v_sb) + (int64_t)hkv * p.v_sh + lane * kN;
   const int32_t* table = kPaged ? p.page_table + (int64_t)b * p.page_table_stride : nullptr;
-  float odd[kN], qf[kN];
+  // the lane's dimensions of the row whose part starts at value o
+  auto load = [&](const void* cache, const uint8_t* scales, int64_t o, float (&f)[kN]) {
+    if constexpr (kIsFp4<T>) {
+      const float scale = e4m3x2_to_float2(scales[o / kScaleDims]).x;
+#pragma unroll
+      for (int i = 0; i < kN; i += 2) {
+        const float2 x = e2m1x2_to_float2(static_cast<const uint8_t*>(cache)[(o + i) / 2]);
+        f[i] = x.x * scale;
+        f[i + 1] = x.y * scale;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kN; ++i) f[i] = to_float(static_cast<const T*>(cache)[o + i]);
+    }
+  };
+  const uint8_t *k_scales = nullptr, *v_scales = nullptr;
+  if constexpr (kIsFp4<T>) { k_scales = p.k_scales; v_scales = p.v_scales; }
+  float odd[kN], qf[kN], x[kN];
   m = neg_inf();
   l = 0.f;
 #pragma unroll
@@ -169,19 +196,20 @@ __device__ __noinline__ void careful_row(const WindowParams& p, const Seen& seen
       const int64_t row = row_of<kPaged>(p, table, j);
       if (row < 0) continue;
       float s = 0.f;
+      load(p.k, k_scales, k0 + row * p.k_st, x);
 #pragma unroll
-      for (int i = 0; i < kN; ++i) s = fmaf(qf[i], to_float(k[row * p.k_st + i]), s);
+      for (int i = 0; i < kN; ++i) s = fmaf(qf[i], x[i], s);
 #pragma unroll
       for (int o = 16; o; o /= 2) s += __shfl_xor_sync(~0u, s, o);
       s *= p.scale_log2;
       const float top = fmaxf(m, s), base = top == neg_inf() ? 0.f : top, a = fast_exp2(m - base), w = fast_exp2(s - base);
       m = top;
       l = fmaf(l, a, w);
+      load(p.v, v_scales, v0 + row * p.v_st, x);
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
-        const float x = to_float(v[row * p.v_st + i]);
-        if (isfinite(x)) acc[i] = fmaf(acc[i], a, w * x);
-        else { acc[i] *= a; odd[i] += x; }
+        if (isfinite(x[i])) acc[i] = fmaf(acc[i], a, w * x[i]);
+        else { acc[i] *= a; odd[i] += x[i]; }
       }
     }
 #pragma unroll
@@ -189,17 +217,21 @@ __device__ __noinline__ void careful_row(const WindowParams& p, const Seen& seen
 }
 
 // grid (splits x row blocks, H_kv, B), the last row blocks first: they see most.  kBoth: weights in two 16-bit parts.
-template <typename T, int D, bool kPaged, bool kBoth>
+// box_rows: rows that lie side by side for certain, of a copy or (4-bit, which has no use for the maps) of a page.
+template <typename T, int D, bool kPaged, bool kBoth, typename Params>
 __global__ void __launch_bounds__(kTileThreads, 2)
-window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+window_tile_kernel(const Params p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                    const int box_rows) {
-  using Shape = TileShape<D>;
+  using Shape = TileShape<T, D>;
+  using TQ = typename Storage<T>::Query;
+  using TM = std::conditional_t<kIsFp4<T>, __half, T>;                 // of the contractions
   constexpr int kStages = Shape::kStages;
-  constexpr float kShift = std::is_same<T, __half>::value ? 6.f : 0.f;
+  constexpr float kShift = std::is_same<TM, __half>::value ? 6.f : 0.f;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t s_bar[3 * kStages + 4];
   __shared__ uint32_t s_tmem;
   __shared__ int64_t s_row[2][kTileRows];                              // where a row starts in q and in out
+  __shared__ float s_unit[kIsFp4<T> ? kTileRows : 1];                  // 4-bit: what a row's scores are to be multiplied with
   __shared__ int s_dead, s_asked;                                      // the block has given up; copies asked for
   const uint32_t base = (smem_at(smem_raw) + 1023) & ~1023u;
   uint8_t* const smem = smem_raw + (base - smem_at(smem_raw));
@@ -272,9 +304,68 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
       mbar_arrive(fixed + 8 * stage);
     }
   };
+  // ---- 4-bit: pieces of 16 bytes of codes, by warps 5 to 7.  A lane's are of kMine rows and the same dimensions 32 my_c ...; eight
+  // neighbouring lanes have eight rows, which the swizzle spreads over all banks.  Three pieces at a time are converted, and the same
+  // three of the next K or V tile asked for. ----
+  constexpr int kC = D / 32, kRowsAtOnce = kConverters / kC, kMine = kIsFp4<T> ? (kTileKeys + kRowsAtOnce - 1) / kRowsAtOnce : 1;
+  constexpr int kTurn = 3, kWarpRows = 32 / kC;
+  static_assert(!kIsFp4<T> || kMine % kTurn == 0, "");
+  const int me = (int)threadIdx.x - (kTileThreads - kConverters), my_c = lane / kWarpRows, box_shift = 31 - __clz(box_rows);
+  const int my_row = (warp - (kTileThreads - kConverters) / 32) * kWarpRows + lane % kWarpRows;
+  uint8_t* const raw = smem + Shape::kQBytes + kStages * Shape::kTileBytes;
+  uint32_t scale_pair[kMine];
+  // where the thread's part of row 0 would be, in K and in V
+  const int64_t my_k = (kPaged ? 0 : (int64_t)b * p.k_sb) + (int64_t)hkv * p.k_sh + my_c * 32;
+  const int64_t my_v = (kPaged ? 0 : (int64_t)b * p.v_sb) + (int64_t)hkv * p.v_sh + my_c * 32;
+  // the pool row of the lane's run of box_rows rows of a tile; -1: no page, or none that a token sees a position of
+  auto page_of = [&](int it) {
+    if constexpr (!kPaged) return 0;
+    const int ja = seen.position(it) + lane * box_rows;
+    const bool used = lane < kTileKeys >> box_shift && ja <= hi && (ja + box_rows - 1 >= from || ja < p.sinks);
+    return used ? (int)row_of<true>(p, p.page_table + (int64_t)b * p.page_table_stride, ja) : -1;
+  };
+  auto ask = [&](int x, int j0, int of_v, int page_row, bool whole) {  // piece x of the tile from position j0 on
+    const int r = my_row + x * kRowsAtOnce, j = j0 + r;
+    int row = j;
+    if constexpr (kPaged) {
+      row = __shfl_sync(~0u, page_row, r >> box_shift & 31);
+      row = row < 0 ? -1 : row + (r & (box_rows - 1));
+    }
+    if (!whole && (j > hi || !(j >= from || j < p.sinks))) row = -1;
+    if (r < kTileKeys) {
+      if constexpr (kIsFp4<T>) {
+        const int64_t at = (of_v ? my_v : my_k) + (row < 0 ? 0 : row) * (int64_t)(of_v ? p.v_st : p.k_st);
+        copy_16B(smem_at(raw) + (me + x * kConverters) * 16, static_cast<const uint8_t*>(of_v ? p.v : p.k) + at / 2, row >= 0);
+        scale_pair[x] = row >= 0 ? *reinterpret_cast<const uint16_t*>((of_v ? p.v_scales : p.k_scales) + at / kScaleDims) : 0u;
+      }
+    }
+    copies_commit();
+  };
+  auto convert = [&](int x0, uint8_t* to) {                  // pieces x0 ... x0 + kTurn - 1
+    uint4 w[kTurn];
+#pragma unroll
+    for (int x = x0; x < x0 + kTurn; ++x)                    // (a place in shared memory for every lane's piece but the last ones)
+      if (my_row + x * kRowsAtOnce < kTileKeys) w[x - x0] = *reinterpret_cast<const uint4*>(raw + (me + x * kConverters) * 16);
+#pragma unroll
+    for (int x = x0; x < x0 + kTurn; ++x) {
+      const int r = my_row + x * kRowsAtOnce;
+      if (r >= kTileKeys) continue;
+      const uint32_t pair = e4m3x2_to_half2(scale_pair[x]), by[2] = {__byte_perm(pair, 0, 0x1010), __byte_perm(pair, 0, 0x3232)};
+      const uint32_t words[4] = {w[x - x0].x, w[x - x0].y, w[x - x0].z, w[x - x0].w};
+      uint8_t* const row = to + my_c / 2 * Shape::kHalf + r * 128;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        uint32_t h[4];
+        e2m1x8_to_half2(words[y], h);
+        *reinterpret_cast<uint4*>(row + ((my_c % 2 * 4 + y) ^ (r & 7)) * 16) =
+            make_uint4(half2_mul(h[0], by[y / 2]), half2_mul(h[1], by[y / 2]), half2_mul(h[2], by[y / 2]), half2_mul(h[3], by[y / 2]));
+      }
+    }
+  };
+  int page_row = 0;
   if (warp == 5) {
     if (lane == 0) {
-      for (int i = 0; i < kStages; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); mbar_init(fixed + 8 * i, 32); }
+      for (int i = 0; i < kStages; ++i) { mbar_init(full + 8 * i, kIsFp4<T> ? kConverters : 1); mbar_init(empty + 8 * i, 1); mbar_init(fixed + 8 * i, 32); }
       mbar_init(s_full, 1);
       mbar_init(o_full, 1);
       for (int half = 0; half < 2; ++half) mbar_init(p_full + 8 * half, kTileRows);
@@ -283,7 +374,15 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
-    for (int i = 0; i < min(kStages, n_loads); ++i) load(i);
+    if constexpr (!kIsFp4<T>)
+      for (int i = 0; i < min(kStages, n_loads); ++i) load(i);
+  }
+  if constexpr (kIsFp4<T>) {
+    if (warp >= 5 && n_loads > 0) {
+      page_row = page_of(range.x);
+#pragma unroll
+      for (int x = 0; x < kMine; ++x) ask(x, seen.position(range.x), 0, page_row, false);
+    }
   }
   if (warp == 4) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&s_tmem)), "n"(256) : "memory");
@@ -303,7 +402,16 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
     for (int y = 0; y < 32 / kAtOnce; ++y) {
       const int r = warp * 32 + y * kAtOnce + lane / kLanes;
       w[y] = make_uint4(0, 0, 0, 0);
-      if (r < rows) w[y] = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.q) + s_row[0][r] + i * 8);
+      if (r < rows) w[y] = *reinterpret_cast<const uint4*>(reinterpret_cast<const TQ*>(p.q) + s_row[0][r] + i * 8);
+    }
+    if constexpr (kIsFp4<T>) {
+#pragma unroll
+      for (int y = 0; y < 32 / kAtOnce; ++y) {
+        uint32_t x[4] = {w[y].x, w[y].y, w[y].z, w[y].w};
+        const float back = rows_to_half<4, kLanes>(x);
+        w[y] = make_uint4(x[0], x[1], x[2], x[3]);
+        if (i == 0) s_unit[warp * 32 + y * kAtOnce + lane / kLanes] = p.scale_log2 * back;
+      }
     }
 #pragma unroll
     for (int y = 0; y < 32 / kAtOnce; ++y) {
@@ -317,8 +425,34 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
   tc_after();
   const uint32_t tmem = s_tmem;
 
-  if (warp == 5) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+  if (kIsFp4<T> && warp >= 5) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs<T>));
+    if constexpr (kIsFp4<T>) {
+      int next_row = n_tiles > 1 ? page_of(range.x + 1) : 0;
+      for (int i = 0; i < n_loads; ++i) {
+        if (i >= kStages && !__all_sync(~0u, mbar_wait(empty + 8 * (i % kStages), (i / kStages - 1) & 1, dead))) break;
+        uint8_t* const to = smem + Shape::kQBytes + i % kStages * Shape::kTileBytes;
+        const int it = range.x + (i + 1) / 2, j0 = seen.position(it);  // of the next load
+        const bool more = i + 1 < n_loads, whole = more && !unseen(it);
+        if (i & 1) page_row = next_row;
+#pragma unroll
+        for (int x0 = 0; x0 < kMine; x0 += kTurn) {
+          copies_wait<kMine - kTurn>();                      // (a thread reads what it asked for itself)
+          convert(x0, to);
+#pragma unroll
+          for (int x = x0; x < x0 + kTurn; ++x) {
+            if (more) ask(x, j0, (i + 1) & 1, page_row, whole);
+            else copies_commit();
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        mbar_arrive(full + 8 * (i % kStages));
+        if ((i & 1) && i + 3 < n_loads) next_row = page_of(range.x + (i + 3) / 2);
+      }
+      copies_wait<0>();
+    }
+  } else if (!kIsFp4<T> && warp == 5) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs<T>));
     settle(min(kStages, n_loads) - 2);
     for (int i = kStages; i < n_loads; ++i) {
       if (!__all_sync(~0u, mbar_wait(empty + 8 * (i % kStages), (i / kStages - 1) & 1, dead))) {
@@ -331,8 +465,8 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
     settle(n_loads - 1);
   } else if (warp == 4) {
     // ---- matrix instructions: the whole warp goes through this, so that addresses stay in uniform registers; one lane issues ----
-    constexpr uint32_t kIdS = tile_idesc<T, kTileKeys, false>(), kIdO = tile_idesc<T, D, true>();
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    constexpr uint32_t kIdS = tile_idesc<TM, kTileKeys, false>(), kIdO = tile_idesc<TM, D, true>();
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs<T>));
     const bool leader = elect_one();
     uint32_t fixes = 0;                                      // phases of `fixed`
     const uint64_t q_desc = tile_desc(base, 16), k_desc = tile_desc(kv, 16), v_desc = tile_desc(kv, Shape::kHalf);
@@ -355,7 +489,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
     for (int tile = 0; tile < n_tiles; ++tile) {
       const int i = 2 * tile + 1, stage = i % kStages;
       wait_full(i);
-      if (unseen(range.x + tile)) {
+      if (!kIsFp4<T> && unseen(range.x + tile)) {
         mbar_wait(fixed + 8 * stage, fixes >> stage & 1, dead);
         fixes ^= 1u << stage;
       }
@@ -381,7 +515,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
     }
   } else if (warp < 4) {
     // ---- softmax: a thread per row ----
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs<T>));
     const int row = row0 + (int)threadIdx.x;
     const bool there = (int)threadIdx.x < rows;
     const int t = token_of(p, row), h = hkv * p.group + row - t * p.group, pos = there ? first + t : -1;
@@ -389,7 +523,8 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
     const int all_lo = p.window == 0 ? 0 : hi - p.window + 1;          // every row sees [all_lo, lo]
     const int window_lo = p.window == 0 ? 0 : pos - p.window + 1;
     const int32_t* table = kPaged ? p.page_table + (int64_t)b * p.page_table_stride : nullptr;
-    float m = neg_inf(), l = 0.f;
+    float m = neg_inf(), l = 0.f, unit = p.scale_log2;
+    if constexpr (kIsFp4<T>) unit = s_unit[threadIdx.x];
     int n = 0;                                               // tiles so far
     for (int it = range.x; it < range.y; ++it) {
       const int j0 = seen.position(it);
@@ -431,7 +566,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
 #pragma unroll
       for (int c = 0; c < 128; c += 2)
         top[c / 2 % 4] = max3(top[c / 2 % 4], __uint_as_float(s[c / 32][c % 32]), __uint_as_float(s[c / 32][c % 32 + 1]));
-      const float now = fmaxf(max3(top[0], top[1], top[2]), top[3]) * p.scale_log2;
+      const float now = fmaxf(max3(top[0], top[1], top[2]), top[3]) * unit;
       const bool higher = now > m + kLazy;                   // (m = -inf: anything)
       if (__any_sync(~0u, higher)) {
         const float to = higher ? now : m;
@@ -451,7 +586,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
         }
       }
       const float off1 = (m == neg_inf() ? 0.f : -m) + kShift;
-      const float2 off = make_float2(off1, off1), by = make_float2(p.scale_log2, p.scale_log2);
+      const float2 off = make_float2(off1, off1), by = make_float2(unit, unit);
       float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
@@ -462,10 +597,10 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
           float2 y = fma2(make_float2(__uint_as_float(s[e / 32][e % 32]), __uint_as_float(s[e / 32][e % 32 + 1])), by, off);
           y = make_float2(fast_exp2(y.x), fast_exp2(y.y));
           sum[i & 1] = add2(sum[i & 1], y);
-          w[i] = pack2<T>(y.x, y.y);
+          w[i] = pack2<TM>(y.x, y.y);
           if constexpr (kBoth) {
-            const float2 back = unpack2<T>(w[i]);
-            rest[i] = pack2<T>(y.x - back.x, y.y - back.y);
+            const float2 back = unpack2<TM>(w[i]);
+            rest[i] = pack2<TM>(y.x - back.x, y.y - back.y);
           }
         }
         tc_st32(s_at + half * 32, w);
@@ -507,7 +642,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
         for (int i = 0; i < 32; i += 8) {
           const int at16 = c * 4 + i / 8;
           *reinterpret_cast<uint4*>(stage + at16 / 8 * Shape::kQHalf + rw * 128 + ((at16 % 8) ^ (rw & 7)) * 16) =
-              make_uint4(pack2<T>(f[i], f[i + 1]), pack2<T>(f[i + 2], f[i + 3]), pack2<T>(f[i + 4], f[i + 5]), pack2<T>(f[i + 6], f[i + 7]));
+              make_uint4(pack2<TQ>(f[i], f[i + 1]), pack2<TQ>(f[i + 2], f[i + 3]), pack2<TQ>(f[i + 4], f[i + 5]), pack2<TQ>(f[i + 6], f[i + 7]));
         }
       } else if (there) {
 #pragma unroll
@@ -527,7 +662,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
 #pragma unroll
       for (int y = 0; y < 32 / kAtOnce; ++y) {
         const int yr = warp * 32 + y * kAtOnce + lane / kLanes;
-        if (yr < rows) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.out) + s_row[1][yr] + i * 8) = w[y];
+        if (yr < rows) *reinterpret_cast<uint4*>(reinterpret_cast<TQ*>(p.out) + s_row[1][yr] + i * 8) = w[y];
       }
     }
     if (there) {
@@ -549,7 +684,7 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
       __syncwarp();
 #pragma unroll
       for (int d = 0; d < D / 32; ++d) {
-        if (finished) store_window_value<T>(p, b, rh, rt, lane * (D / 32) + d, rl == 0.f ? 0.f : acc[d] / rl);
+        if (finished) store_window_value<TQ>(p, b, rh, rt, lane * (D / 32) + d, rl == 0.f ? 0.f : acc[d] / rl);
         else p.ws_acc[rslot * D + lane * (D / 32) + d] = acc[d];
       }
       if (lane == 0) {
@@ -559,13 +694,13 @@ window_tile_kernel(const WindowParams p, const __grid_constant__ CUtensorMap k_m
     }
     if (kPaged && p.status && (flags & SSA_DEV_BAD_INDEX)) atomicOr(p.status, SSA_DEV_BAD_INDEX);
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs<T>));
   }
   tc_before();
   __syncthreads();
   tc_after();
   if (s_dead) {                                              // (otherwise all that was asked for has been waited for)
-    for (int i = max(0, s_asked - kStages); i < s_asked; ++i) mbar_drain(full + 8 * (i % kStages), (i / kStages) & 1);
+    for (int i = kIsFp4<T> ? s_asked : max(0, s_asked - kStages); i < s_asked; ++i) mbar_drain(full + 8 * (i % kStages), (i / kStages) & 1);
     if (n_tiles > 0) mbar_drain(o_full, 0);                  // instructions end in order: these have all
     if (threadIdx.x == 0 && p.status) atomicOr(p.status, SSA_DEV_GAVE_UP);
     __syncthreads();
@@ -603,6 +738,17 @@ inline bool tile_map(CUtensorMap* map, const void* base, int32_t dtype, int D, i
   return encode(map, dtype == SSA_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(base),
                 dims, steps, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                 CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int D, typename Params>
+static cudaError_t launch_tiles(const Params& p, const CUtensorMap& k_map, const CUtensorMap& v_map, int box_rows, cudaStream_t st) {
+  const dim3 grid((unsigned)((p.group * p.n_q + kTileRows - 1) / kTileRows * p.n_splits), (unsigned)p.H_kv, (unsigned)p.B);
+  auto kernel = p.page_table ? (p.out_f32 ? window_tile_kernel<T, D, true, true, Params> : window_tile_kernel<T, D, true, false, Params>)
+                             : (p.out_f32 ? window_tile_kernel<T, D, false, true, Params> : window_tile_kernel<T, D, false, false, Params>);
+  constexpr int kSmem = TileShape<T, D>::kSmem;
+  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  if (err != cudaSuccess) return err;
+  return launch_pdl_smem(kernel, grid, dim3(kTileThreads), kSmem, st, p, k_map, v_map, box_rows);
 }
 
 }  // namespace ssa
