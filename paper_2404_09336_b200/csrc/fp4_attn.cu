@@ -3,6 +3,82 @@
 
 namespace ssa {
 
+// ---- the seen part of a 4-bit cache in bf16 ---------------------------------------------------------------------------------
+// Every block of 128 query rows that works on tiles converts the K and V rows that it sees.  Where many share them (prompt chunks)
+// they are converted once instead, into pages of the workspace that the tiles of a bf16 cache then read: products of a code and a
+// scale have six significant bits, so that nothing is rounded.  HBM bounds it: 2.56 bytes a value.
+constexpr int kExpandThreads = 256;
+
+// grid (tiles of 128 positions that a request's tokens see between them, H_kv, B).  Page tables of the pages made: tile i of request b
+// is rows (b most_tiles + i) 128 ...; where the cache has smaller pages these are as small, and missing where they are.
+template <int D, bool kPaged>
+__global__ void __launch_bounds__(kExpandThreads)
+fp4_expand_kernel(const Fp4Params p, const Fp4Expanded x) {
+  constexpr int kC = D / 32, kEach = 2 * kTileKeys * kC / kExpandThreads;    // 16-byte pieces of a row; of K and V, of a thread
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int b = blockIdx.z, hkv = blockIdx.y, tile = blockIdx.x, tid = threadIdx.x;
+  uint32_t flags = 0;
+  int ctx, n_new;
+  window_sizes(p, b, ctx, n_new, flags);
+  const int first = ctx - n_new, hi = ctx - 1, from = p.window == 0 ? 0 : max(0, first - p.window + 1);
+  const Seen seen(p, kTileKeys, first, 0, n_new - 1);
+  if (tile >= seen.tiles) return;
+  const int j0 = seen.position(tile);
+  const int64_t to_row = ((int64_t)b * x.most_tiles + tile) * kTileKeys;
+  const int32_t* table = kPaged ? p.page_table + (int64_t)b * p.page_table_stride : nullptr;
+  auto is_seen = [&](int j) { return j <= hi && (j >= from || j < p.sinks); };
+  if (hkv == 0 && tid < kTileKeys >> x.page_shift) {
+    const int ja = j0 + (tid << x.page_shift), jz = ja + (1 << x.page_shift) - 1;
+    const bool used = ja <= hi && (jz >= from || ja < p.sinks);
+    if (used) x.table[(int64_t)b * x.table_stride + (ja >> x.page_shift)] = row_of<kPaged>(p, table, ja) < 0 ? -1 : (int)(to_row >> x.page_shift) + tid;
+  }
+  uint4 w[kEach];
+  uint32_t pair[kEach];
+#pragma unroll
+  for (int y = 0; y < kEach; ++y) {
+    const int piece = tid + y * kExpandThreads, of_v = piece / (kTileKeys * kC), r = piece / kC % kTileKeys, c = piece % kC;
+    const int64_t row = is_seen(j0 + r) ? row_of<kPaged>(p, table, j0 + r) : -1;
+    const int64_t o = (kPaged ? 0 : (int64_t)b * (of_v ? p.v_sb : p.k_sb)) + (int64_t)hkv * (of_v ? p.v_sh : p.k_sh) +
+                      (row < 0 ? 0 : row) * (of_v ? p.v_st : p.k_st) + c * 32;
+    w[y] = make_uint4(0, 0, 0, 0);
+    pair[y] = 0;
+    if (row >= 0) {
+      w[y] = ld_stream_16B(static_cast<const uint8_t*>(of_v ? p.v : p.k) + o / 2);
+      pair[y] = *reinterpret_cast<const uint16_t*>((of_v ? p.v_scales : p.k_scales) + o / kScaleDims);
+    }
+  }
+#pragma unroll
+  for (int y = 0; y < kEach; ++y) {
+    const int piece = tid + y * kExpandThreads, of_v = piece / (kTileKeys * kC), r = piece / kC % kTileKeys, c = piece % kC;
+    if (!is_seen(j0 + r)) continue;                          // (may hold anything: the tiles do not use it)
+    const float2 scale = unpack2<__half>(e4m3x2_to_half2(pair[y]));
+    const uint32_t words[4] = {w[y].x, w[y].y, w[y].z, w[y].w};
+    uint4* to = reinterpret_cast<uint4*>((of_v ? x.v : x.k) + ((int64_t)hkv * x.head_rows + to_row + r) * D + c * 32);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float by = i < 2 ? scale.x : scale.y;
+      uint32_t h[4];
+      e2m1x8_to_half2(words[i], h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = unpack2<__half>(h[e]);
+        h[e] = pack2<__nv_bfloat16>(f.x * by, f.y * by);
+      }
+      to[i] = make_uint4(h[0], h[1], h[2], h[3]);
+    }
+  }
+}
+
+int32_t launch_expand(const Fp4Params& p, const Fp4Expanded& x, int D, cudaStream_t st) {
+  const dim3 grid((unsigned)x.most_tiles, (unsigned)p.H_kv, (unsigned)p.B);
+  auto kernel = p.page_table ? (D == 128 ? fp4_expand_kernel<128, true> : fp4_expand_kernel<64, true>)
+                             : (D == 128 ? fp4_expand_kernel<128, false> : fp4_expand_kernel<64, false>);
+  if (launch_pdl(kernel, grid, dim3(kExpandThreads), st, p, x) != cudaSuccess) return SSA_ERR_CUDA;
+  note_launches(1);
+  return SSA_OK;
+}
+
 template <int D>
 static int32_t launch(const Fp4Params& p, int box_rows, cudaStream_t st) {
   cudaEvent_t begin, end;

@@ -113,9 +113,19 @@ static int32_t check_window(const ssa_attn_desc* d, const ssa_window* w, bool ma
   return w->paging ? check_paging(w->paging, d->max_ctx) : SSA_OK;
 }
 
+// Rows of a K/V head up to which the kernel for few rows serves a 4-bit cache: with 32 it takes 92, 58, 102 and 39 us, the tiles 124,
+// 56, 131 and 37 (8 requests of 4100 to 16384 positions, those within a window of 4096, 32 requests of up to 4096, one of 16384; 8 K/V
+// heads); with 48 rows 149, 73, 150 and 46 against 134, 56, 124 and 34.
+constexpr int kFewRowsFp4 = 32;
+// Rows above which it is converted once for all of them, instead of by every block of 128 rows: with 256 that takes 222, 106, 224 and
+// 43 us for the same requests, each block for itself 227, 91, 194 and 40; with 384 324, 127, 233 and 58 against 396, 139, 216 and 56;
+// with 768 342, 133, 304 and 66 against 412, 143, 335 and 78.
+constexpr int kExpandRows = 256;
+
 // Whether the tiles of 128 rows serve a call.
 static bool tiles_pay(const ssa_attn_desc* d, const ssa_window* w, bool mass) {
-  return !mass && d->kv_dtype != SSA_FP8_E4M3 && (long long)(d->H / d->H_kv) * w->n_q > kFewRows &&
+  return !mass && d->kv_dtype != SSA_FP8_E4M3 &&
+         (long long)(d->H / d->H_kv) * w->n_q > (d->kv_dtype == SSA_FP4_E2M1 ? kFewRowsFp4 : kFewRows) &&
          (!w->paging || w->paging->page_size >= 8);          // (a box of a copy is eight rows at least, or a lane's run of 4-bit ones)
 }
 
@@ -146,6 +156,24 @@ static bool plan_window(const ssa_attn_desc* d, const ssa_window* w, bool mass, 
   return row_tiles * pl->n_splits <= 0x7fffffffll;
 }
 
+// Where the rows of a 4-bit cache that the tokens see have places in bf16; bytes of all of it, 0 where the call has no use for that.
+// Few blocks of 128 rows convert what they see themselves.
+static size_t plan_expanded(const ssa_attn_desc* d, const ssa_window* w, Fp4Expanded* x) {
+  const long long rows = (long long)(d->H / d->H_kv) * w->n_q;
+  if (rows <= kExpandRows) return 0;
+  const long long all = (d->max_ctx + kTileKeys - 1ll) / kTileKeys;
+  const long long seen = ((long long)w->sinks + kTileKeys - 1) / kTileKeys + ((long long)w->window + w->n_q + kTileKeys - 1) / kTileKeys + 1;
+  const long long tiles = w->window == 0 ? all : std::min(all, seen);
+  if (tiles * d->B * kTileKeys > 0x7fffffffll) return 0;
+  const int page = w->paging ? std::min(w->paging->page_size, kTileKeys) : kTileKeys;
+  x->most_tiles = (int)tiles;
+  x->head_rows = tiles * d->B * kTileKeys;
+  x->page_shift = 0;
+  while ((1 << x->page_shift) < page) ++x->page_shift;
+  x->table_stride = (int)((d->max_ctx + (long long)page - 1) / page);
+  return up256((size_t)d->B * x->table_stride * sizeof(int32_t)) + 2 * up256((size_t)x->head_rows * d->H_kv * d->D * 2);
+}
+
 // Room for either kernel: which one runs may depend on the cache's strides.
 static size_t window_bytes(const ssa_attn_desc* d, const ssa_window* w, bool mass, bool fp4) {
   WindowPlan pl;
@@ -153,6 +181,10 @@ static size_t window_bytes(const ssa_attn_desc* d, const ssa_window* w, bool mas
   const size_t few = pl.total_bytes;
   if (!tiles_pay(d, w, mass) || !plan_window(d, w, mass, true, &pl)) return few;
   return std::max(few, pl.total_bytes);
+}
+static size_t expanded_bytes(const ssa_attn_desc* d, const ssa_window* w) {
+  Fp4Expanded x;
+  return tiles_pay(d, w, false) ? plan_expanded(d, w, &x) : 0;
 }
 
 template <typename T, int D>
@@ -224,6 +256,31 @@ static int32_t run_window(const ssa_attn_desc* d, const ssa_window* w, const voi
   p.n_splits = pl.n_splits; p.s_pitch = pl.s_pitch;
   p.decay = decay;
   cudaStream_t st = (cudaStream_t)stream;
+  Fp4Expanded x;
+  if (const size_t more = fp4 && tiles ? plan_expanded(d, w, &x) : 0; more && ws_bytes >= window_bytes(d, w, mass, fp4) + more) {
+    // the rows that are seen in bf16, behind the partial results, and the tiles of a cache of such rows in pages
+    char* to = static_cast<char*>(ws) + window_bytes(d, w, mass, fp4);
+    x.table = reinterpret_cast<int32_t*>(to);
+    to += up256((size_t)d->B * x.table_stride * sizeof(int32_t));
+    x.k = reinterpret_cast<__nv_bfloat16*>(to);
+    x.v = reinterpret_cast<__nv_bfloat16*>(to + up256((size_t)x.head_rows * d->H_kv * d->D * 2));
+    const int page = 1 << x.page_shift;
+    const int64_t head = x.head_rows * d->D;
+    if (tile_map(&maps[0], x.k, SSA_BF16, d->D, x.head_rows, d->D, d->H_kv, head, 1, 0, page) &&
+        tile_map(&maps[1], x.v, SSA_BF16, d->D, x.head_rows, d->D, d->H_kv, head, 1, 0, page)) {
+      Fp4Params f;
+      static_cast<WindowParams&>(f) = p;
+      f.k_scales = static_cast<const uint8_t*>(k_scales);
+      f.v_scales = static_cast<const uint8_t*>(v_scales);
+      const int32_t rc = launch_expand(f, x, d->D, st);
+      if (rc != SSA_OK) return rc;
+      p.k = x.k; p.v = x.v;
+      p.page_table = x.table; p.page_table_stride = x.table_stride; p.page_shift = x.page_shift;
+      p.n_pages = (int)(x.head_rows >> x.page_shift);
+      p.k_sb = p.v_sb = 0; p.k_sh = p.v_sh = head; p.k_st = p.v_st = d->D;
+      return d->D == 128 ? launch_window<__nv_bfloat16, 128>(p, false, maps, page, st) : launch_window<__nv_bfloat16, 64>(p, false, maps, page, st);
+    }
+  }
   if (fp4) {
     Fp4Params f;
     static_cast<WindowParams&>(f) = p;
@@ -268,7 +325,8 @@ int32_t ssa_attn_mass(const ssa_attn_desc* desc, const ssa_window* window, const
 }
 
 size_t ssa_attn_window_fp4_workspace_bytes(const ssa_attn_desc* desc, const ssa_window* window) {
-  return ssa::window_bytes(desc, window, false, true);
+  const size_t need = ssa::window_bytes(desc, window, false, true);
+  return need ? need + ssa::expanded_bytes(desc, window) : 0;
 }
 
 int32_t ssa_attn_window_fp4(const ssa_attn_desc* desc, const ssa_window* window, const void* q, const void* k_cache,

@@ -103,7 +103,8 @@ class Fp4Tokens(Tokens):
     def values(self):
         return [self.q.cpu().double().numpy(), self.cache.values("k"), self.cache.values("v")]
 
-    def call(self, ctx, q_lens=None, window=0, sinks=0, out_dtype=torch.float32, scale=0.0, stream=None, table=None):
+    def call(self, ctx, q_lens=None, window=0, sinks=0, out_dtype=torch.float32, scale=0.0, stream=None, table=None, less=0):
+        """less: bytes that the workspace lacks of what the library asks for."""
         c = self.cache
         d_ctx = torch.tensor(ctx, dtype=torch.int32, device=DEV)
         d_new = None if q_lens is None else torch.tensor(q_lens, dtype=torch.int32, device=DEV)
@@ -112,7 +113,7 @@ class Fp4Tokens(Tokens):
         status = torch.zeros(1, dtype=torch.int32, device=DEV)
         desc = c.desc(self.q, out, scale)
         win = ssa.make_window(self.q, out, window, sinks, d_new, c.paging(table))
-        ws = torch.full((ssa.attn_window_fp4_workspace_bytes(desc, win),), 0xff, dtype=torch.uint8, device=DEV)
+        ws = torch.full((ssa.attn_window_fp4_workspace_bytes(desc, win) - less,), 0xff, dtype=torch.uint8, device=DEV)
         ssa.attn_window_fp4(desc, win, self.q, c.parts["k"], c.parts["v"], c.scales("k"), c.scales("v"), d_ctx, out, lse, ws, status, stream)
         torch.cuda.synchronize()
         f64 = lambda x: x.double().cpu().numpy()
@@ -143,15 +144,16 @@ def check_rows(got, lse, want, D, n, dt, out_dtype, v_most):
     assert (np.abs(lse - l) <= 2 * (score + 2.0 ** -22 + (n + 64) * 2.0 ** -24) + np.abs(l) * 2.0 ** -22).all()
 
 
-def check_tokens(p, got, ctx, q_lens, window, sinks, out_dtype, tiles=False, skipped=None, scale=None):
+def check_tokens(p, got, ctx, q_lens, window, sinks, out_dtype, tiles=False, shared=False, skipped=None, scale=None):
     """budget_util.check over a 4-bit cache, with the floor of fp16 weights: of one part for bf16 outputs, of two for fp32 ones.
-    tiles: the call may go to the tiles."""
+    tiles: the call may go to the tiles; shared: to those of a bf16 cache, whose weights are bf16 of as many parts (and have no floor)."""
     out, lse, _, status = got
     assert not status & ssa.DEV_GAVE_UP
     q, k, v = p.values()
     q_lens = [p.n_q] * p.B if q_lens is None else q_lens
     ref = BO.attention(q, k, v, ctx, q_lens, window, sinks, p.D ** -0.5 if scale is None else scale, skipped)
-    step = half_step(torch.float16) if out_dtype != torch.float32 else half_step(torch.float16) ** 2
+    one = torch.bfloat16 if shared else torch.float16
+    step = half_step(one) if out_dtype != torch.float32 else half_step(one) ** 2
     for b, r in enumerate(ref):
         n, t = ctx[b], q_lens[b]
         assert (out[b, :, t:] == UNWRITTEN).all() and (lse[b, :, t:] == UNWRITTEN).all(), "rows behind the last token were written"

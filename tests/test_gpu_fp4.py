@@ -14,12 +14,12 @@ BF16, F32 = torch.bfloat16, torch.float32
 
 def many(p):
     """Whether the tiles of 128 rows may serve the call."""
-    return p.H // p.H_kv * p.n_q > 24
+    return p.H // p.H_kv * p.n_q > 32
 
 
 def run(p, ctx, new=None, window=0, sinks=0, out_dtype=F32, **k):
     got = p.call(ctx, new, window, sinks, out_dtype, **k)
-    check_tokens(p, got, ctx, new, window, sinks, out_dtype, many(p), scale=k.get("scale") or None)
+    check_tokens(p, got, ctx, new, window, sinks, out_dtype, many(p), shared=p.H // p.H_kv * p.n_q > 256 and not k.get("less"), scale=k.get("scale") or None)
     return got
 
 
@@ -78,6 +78,19 @@ def test_long_contexts_in_splits(n_q):
     run(Fp4Tokens(1, 2, 2, 9001, 64, n_q, page=64), [9001], out_dtype=BF16)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("layout", ["spaced", 8, 16, 256])
+@pytest.mark.parametrize("less", [0, 1])
+def test_chunks_that_share_a_conversion(D, layout, less):
+    """More than 256 rows a K/V head, with and without room for the seen part of the cache in bf16."""
+    page = layout if isinstance(layout, int) else 0
+    p = Fp4Tokens(3, 5, 1, 500, D, 60, layout="bhtd" if page else layout, page=page)
+    run(p, [500, 333, 60], None, out_dtype=BF16 if less else F32, less=less)
+    run(p, [477, 130, 50], [60, 5, 0], window=150, sinks=9, out_dtype=F32 if less else BF16, less=less)
+    run(p, [499, 340, 60], [40, 60, 1], window=128, sinks=200, less=less)
+    run(p, [40, 0, 60], [40, 0, 60], window=5000, less=less)
+
+
 def test_large_queries_and_scales():
     run(Fp4Tokens(2, 4, 2, 300, 128, 2, spread=30.0), [300, 200])
     run(Fp4Tokens(2, 4, 2, 300, 128, 40, spread=30.0), [300, 200], out_dtype=BF16)
@@ -93,7 +106,7 @@ def test_tokens_of_negative_position_and_clamped_lengths():
         assert not out[1].any() and np.isneginf(lse[1]).all() and np.isfinite(lse[2]).all()
 
 
-@pytest.mark.parametrize("n_q", [2, 40])
+@pytest.mark.parametrize("n_q", [2, 40, 140])
 def test_missing_pages(n_q):
     p = Fp4Tokens(2, 4, 2, 256, 128, n_q, page=16)
     table = p.cache.table.clone()
@@ -130,6 +143,20 @@ def test_nan_scales_reach_the_tokens_that_see_them(n_q, out_dtype):
     # weights off by 2^-11 and scores by D 2^-24 of theirs, below another 2^-11, in numerator and denominator; the output's rounding
     tol = 4 * 2.0 ** -11 * ref["spread"] + half_step(out_dtype) * np.abs(ref["out"])
     assert 130 * ref["score"] * 2.0 ** -24 < 2.0 ** -11 and (np.abs(out[0, 2:, 1:] - ref["out"][2:, 1:]) <= tol[2:, 1:]).all()
+
+
+def test_nan_scales_in_a_chunk_that_shares_a_conversion():
+    p = Fp4Tokens(1, 4, 2, 500, 64, 150)
+    want = p.call([400], None, window=60, out_dtype=BF16)
+    for row in (20, 400, 499):                               # before every window; behind the context
+        for name in ("k_scales", "v_scales"):
+            p.cache.parts[name][0, :, row] = 0xff
+    got = p.call([400], None, window=60, out_dtype=BF16)
+    assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
+    p.cache.parts["v_scales"][0, 1, 300, 3] = 0x7f           # tokens at 300 ... 359 see it
+    out = p.call([400], None, window=60, out_dtype=BF16)[0]
+    assert np.isnan(out[0, 2:, 50:110, 48:]).all() and np.isfinite(out[0, 2:, 50:110, :48]).all()
+    assert np.isfinite(out[0, 2:, :50]).all() and np.isfinite(out[0, 2:, 110:]).all() and np.array_equal(out[0, :2], want[0][0, :2])
 
 
 def test_offsets_past_32_bits():
