@@ -645,8 +645,9 @@ typedef struct {
  *            any; bounds (dev, written) have the type of the queries
  *   k_scales dev, 4-bit caches only
  * Errors: SSA_ERR_NULL, SSA_ERR_SHAPE (n_q <= 0; n above SSA_MAX_BLOCKS; negative
- * strides), SSA_ERR_UNSUPPORTED (block_size), SSA_ERR_DTYPE, SSA_ERR_ALIGN (the
- * bounds and their strides: 16 bytes), SSA_ERR_CUDA.
+ * strides), SSA_ERR_UNSUPPORTED (block_size; bounds that requests or heads share),
+ * SSA_ERR_DTYPE, SSA_ERR_ALIGN (the bounds and their strides: 16 bytes),
+ * SSA_ERR_CUDA.
  */
 int32_t ssa_block_bounds(const ssa_attn_desc* desc, const ssa_blocks* blocks, const void* k_cache, const void* k_scales,
                          const int32_t* ctx_lens, void* bounds, uint32_t* dev_status, void* stream);
@@ -731,7 +732,7 @@ int32_t ssa_attn_blocks(const ssa_attn_desc* desc, const ssa_blocks* blocks, con
  * Errors: SSA_ERR_NULL, SSA_ERR_SHAPE (n_q, R no multiple of 32 in [0, D],
  * n_positions), SSA_ERR_DTYPE, SSA_ERR_ALIGN (all rows: 16 bytes; cos_sin too),
  * SSA_ERR_UNSUPPORTED (K and V in one place, strides of zero between the cache's
- * rows, heads or requests), SSA_ERR_CUDA.
+ * rows, heads or requests, or those of q_out), SSA_ERR_CUDA.
  */
 typedef struct {
   int32_t n_q;                 /* rows laid out per head and request; H*n_q <= 2^24 */

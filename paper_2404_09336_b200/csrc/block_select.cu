@@ -385,6 +385,7 @@ int32_t ssa_block_bounds(const ssa_attn_desc* desc, const ssa_blocks* blocks, co
   if (rc == SSA_OK && blocks->paging) rc = check_paging(blocks->paging, desc->max_ctx);
   if (rc != SSA_OK) return rc;
   if (!aligned16(k_cache) || (fp4 && !aligned16(k_scales))) return SSA_ERR_ALIGN;
+  if ((desc->B > 1 && blocks->bounds_stride_b == 0) || (desc->H_kv > 1 && blocks->bounds_stride_h == 0)) return SSA_ERR_UNSUPPORTED;
   const ssa_paging* pg = blocks->paging;
   BoundsParams p = {};
   p.k = static_cast<const char*>(k_cache);

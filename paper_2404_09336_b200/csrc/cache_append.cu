@@ -243,7 +243,8 @@ extern "C" int32_t ssa_cache_append(const ssa_attn_desc* desc, const ssa_append*
   // rows that several heads or requests share, or that K and V do, would be written more than once
   if (k_cache == v_cache || (fp4 && k_scales == v_scales) || desc->k_stride_t == 0 || desc->v_stride_t == 0 ||
       (desc->H_kv > 1 && (desc->k_stride_h == 0 || desc->v_stride_h == 0)) ||
-      (desc->B > 1 && !a->paging && (desc->k_stride_b == 0 || desc->v_stride_b == 0)))
+      (desc->B > 1 && !a->paging && (desc->k_stride_b == 0 || desc->v_stride_b == 0)) ||
+      (q && ((desc->B > 1 && a->qo_stride_b == 0) || (desc->H > 1 && a->qo_stride_h == 0) || (a->n_q > 1 && a->qo_stride_t == 0))))
     return SSA_ERR_UNSUPPORTED;
   const ssa_paging* pg = a->paging;
   AppendParams p = {};

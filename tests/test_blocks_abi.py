@@ -182,6 +182,14 @@ def test_appending():
         d = desc()
         setattr(d, field, 0)
         assert append(d, good_append()) == ssa.ERR_UNSUPPORTED, field
+    for field in ("qo_stride_b", "qo_stride_h", "qo_stride_t"):
+        a = good_append()
+        setattr(a, field, 0)
+        assert append(desc(), a) == ssa.ERR_UNSUPPORTED, field
+    for field in ("bounds_stride_b", "bounds_stride_h"):
+        k = good_blocks()
+        setattr(k, field, 0)
+        assert bounds(desc(), k) == ssa.ERR_UNSUPPORTED, field
     assert ssa.launch_count() == before
 
 
