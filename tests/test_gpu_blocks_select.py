@@ -124,7 +124,8 @@ class Choice:
                         with np.errstate(invalid="ignore"):
                             assert (np.abs(scores[b, h, i, :m] - s) <= 2.0 ** -24 * np.abs(s) + 2.0 ** -40 * size)[np.isfinite(s)].all()
                         assert np.array_equal(np.isnan(s), np.isnan(scores[b, h, i, :m])) and (scores[b, h, i, m:] == 777).all()
-                    kept = BO.kept(s.astype(np.float32), m, budget, sinks, recent)
+                    with np.errstate(over="ignore"):
+                        kept = BO.kept(s.astype(np.float32), m, budget, sinks, recent)
                     assert counts[b, h, i] == len(kept) and np.array_equal(index[b, h, i, : len(kept)], kept)
                     assert (index[b, h, i, len(kept):] == -7).all()
         return status
@@ -164,6 +165,30 @@ def test_equal_scores_go_to_the_lowest_blocks():
     c.check([2048], None, 17, 1, 4)
     c.q[:] = 0
     c.check([1999], None, 17, 0, 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_scores_that_fp32_sums_do_not_tell_apart(dtype, D):
+    """Blocks that differ in one value, by less and less: down to ties after rounding, whatever the order of summation."""
+    for seed, (T, block) in enumerate(((2048, 32), (20000, 64), (40000, 32))):
+        c = Choice(2, 8, 2, T, D, block, dtype=dtype, seed=seed)
+        n = c.n
+        c.bounds[:, :, 2:] = c.bounds[:, :, 2:3]
+        steps = 2.0 ** -(torch.arange(n - 2) % 23) * (1 + (torch.arange(n - 2) % 7) / 8)
+        c.bounds[:, :, 2:, 1, 5] = steps.to(c.dt)
+        c.bounds[:, :, 2:, 0, 5] = -1
+        for budget in (1, 7, n // 3, n - 1):
+            c.check([T, T - 700], None, budget, min(1, budget - 1), 0, with_scores=seed == 0)
+
+
+def test_scores_beyond_fp32():
+    c = Choice(1, 2, 1, 2048, 64, 32)
+    c.bounds[:, :, 3:30] *= 2.0 ** 100
+    c.q *= 2.0 ** 30                                         # sums of 2^130: infinite after rounding, of either sign
+    c.check([2048], None, 20, 1, 1, with_scores=False)
+    c.bounds[:], c.q[:] = c.bounds * 2.0 ** -60, c.q * 2.0 ** -130
+    c.check([2048], None, 20, 1, 1, with_scores=False)
 
 
 def test_nan_ranks_below_everything():
