@@ -151,9 +151,9 @@ cache_append_kernel(const AppendParams p) {
       float top[2], by[2];
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
-        top[z] = fabsf(x[z][0]);
-#pragma unroll
-        for (int e = 1; e < 8; ++e) top[z] = max_or_nan(top[z], fabsf(x[z][e]));
+        top[z] = max3_or_nan(fabsf(x[z][0]), fabsf(x[z][1]), fabsf(x[z][2]));
+        top[z] = max3_or_nan(top[z], fabsf(x[z][3]), fabsf(x[z][4]));
+        top[z] = max3_or_nan(top[z], fabsf(x[z][5]), max_or_nan(fabsf(x[z][6]), fabsf(x[z][7])));
       }
       // sixteen dimensions are a neighbouring lane's piece, or both of this lane's
       const float their0 = __shfl_xor_sync(~0u, top[0], 1), their1 = __shfl_xor_sync(~0u, top[1], 1);
@@ -166,11 +166,15 @@ cache_append_kernel(const AppendParams p) {
         // Quotients by one reciprocal and a residual step (Markstein): exact where they lie halfway between two codes, and never on the
         // wrong side of that: the scale has four bits, so that fp32 values next to half of a step are told from it.
         const float scale = e4m3x2_to_float2(bits[z]).x, inverse = scale == 0.f ? 0.f : __frcp_rn(scale);
-        const bool infinite = by[z] == __int_as_float(0x7f800000);
+        if (by[z] == __int_as_float(0x7f800000)) {           // (an infinity has no residual)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (isinf(x[z][e])) { x[z][e] = copysignf(6.f * scale, x[z][e]); }
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float near = x[z][e] * inverse;
-          x[z][e] = infinite && isinf(x[z][e]) ? near : fmaf(fmaf(-near, scale, x[z][e]), inverse, near);
+          x[z][e] = fmaf(fmaf(-near, scale, x[z][e]), inverse, near);
         }
       }
       if (stored) {

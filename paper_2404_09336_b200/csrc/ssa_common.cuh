@@ -204,6 +204,13 @@ __device__ __forceinline__ float fast_exp2(float x) {
   return y;
 }
 
+// The largest of three values, NaN if one of them is.
+__device__ __forceinline__ float max3_or_nan(float a, float b, float c) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+
 // The larger of two values, NaN if one of them is.
 __device__ __forceinline__ float max_or_nan(float a, float b) {
   float y;
