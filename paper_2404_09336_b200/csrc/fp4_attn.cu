@@ -6,7 +6,8 @@ namespace ssa {
 // ---- the seen part of a 4-bit cache in bf16 ---------------------------------------------------------------------------------
 // Every block of 128 query rows that works on tiles converts the K and V rows that it sees.  Where many share them (prompt chunks)
 // they are converted once instead, into pages of the workspace that the tiles of a bf16 cache then read: products of a code and a
-// scale have six significant bits, so that nothing is rounded.  HBM bounds it: 2.56 bytes a value.
+// scale have six significant bits, so that nothing is rounded.  HBM bounds it: 2.56 bytes a value.  8 requests' chunks of up to 509
+// tokens within a window of 4096, 8 K/V heads: some 45 us, and 166 for the tiles.
 constexpr int kExpandThreads = 256;
 
 // grid (tiles of 128 positions that a request's tokens see between them, H_kv, B).  Page tables of the pages made: tile i of request b

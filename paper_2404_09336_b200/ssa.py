@@ -527,6 +527,15 @@ def cache_compact(desc, k_cache, v_cache, ctx_lens, index, counts, max_selected,
     return _check("ssa_cache_compact", rc, check)
 
 
+_QUERIES = {F16: torch.float16, BF16: torch.bfloat16, FP8_E4M3: torch.bfloat16, FP4_E2M1: torch.bfloat16}
+
+
+def _check_type(desc, x):
+    """x has the type of the queries that go with the cache."""
+    if x is not None and x.dtype is not _QUERIES.get(desc.kv_dtype):
+        raise ValueError(f"{x.dtype} where the cache goes with {_QUERIES.get(desc.kv_dtype)}")
+
+
 def make_desc_fp4(q, k, v, k_scales, v_scales, out, max_ctx=None, scale: float = 0.0, paged: bool = False) -> AttnDesc:
     """Descriptor for q[B,H,D], out[B,H,D] over a cache of 4-bit values: codes k, v [B,H_kv,T,D/2] (any strides) and their scales
     [B,H_kv,T,D/16]; paged: pools [n_pages, page_size, H_kv, D/2] and [n_pages, page_size, H_kv, D/16], max_ctx given."""
@@ -552,6 +561,7 @@ def attn_window_fp4_workspace_bytes(desc: AttnDesc, window: Window) -> int:
 def attn_window_fp4(desc, window, q, k_cache, v_cache, k_scales, v_scales, ctx_lens, out, lse=None, workspace=None, dev_status=None,
                     stream=None, check=True):
     """ssa_attn_window_fp4: attn_window over a cache of 4-bit values (make_desc_fp4)."""
+    _check_type(desc, q)
     rc = _call.attn_window_fp4(desc, window, q, k_cache, v_cache, k_scales, v_scales, ctx_lens, out, lse, workspace, dev_status,
                                _stream(stream))
     return _check("ssa_attn_window_fp4", rc, check)
@@ -602,6 +612,7 @@ def _check_lists(desc, blocks, index, counts):
 def block_bounds(desc, blocks, k_cache, ctx_lens, bounds, k_scales=None, dev_status=None, stream=None, check=True):
     """ssa_block_bounds: least and largest values over the keys of the blocks of the newest positions -> bounds[B,H_kv,n,2,D]."""
     _check_bounds(desc, blocks, bounds)
+    _check_type(desc, bounds)
     rc = _call.block_bounds(desc, blocks, k_cache, k_scales, ctx_lens, bounds, dev_status, _stream(stream))
     return _check("ssa_block_bounds", rc, check)
 
@@ -610,6 +621,8 @@ def block_select(desc, blocks, q, bounds, ctx_lens, index, counts, scores=None, 
     """ssa_block_select: the blocks that each token attends to -> index[B,H_kv,n_q,budget], counts[B,H_kv,n_q] (and
     scores[B,H_kv,n_q,n], fp32)."""
     _check_bounds(desc, blocks, bounds)
+    _check_type(desc, bounds)
+    _check_type(desc, q)
     rows = _check_lists(desc, blocks, index, counts)
     if scores is not None:
         n = -(-desc.max_ctx // max(1, blocks.block_size))
@@ -627,6 +640,7 @@ def attn_blocks(desc, blocks, q, k_cache, v_cache, ctx_lens, index, counts, out,
                 workspace=None, dev_status=None, stream=None, check=True):
     """ssa_attn_blocks: every token over the blocks of its list; out (and lse[B,H,n_q]) are written."""
     _check_lists(desc, blocks, index, counts)
+    _check_type(desc, q)
     rc = _call.attn_blocks(desc, blocks, q, k_cache, v_cache, k_scales, v_scales, ctx_lens, index, counts, out, lse, workspace,
                            dev_status, _stream(stream))
     return _check("ssa_attn_blocks", rc, check)
@@ -664,6 +678,7 @@ def make_append(k_new, v_new, q=None, q_out=None, cos_sin=None, interleaved: boo
 def cache_append(desc, append, k_new, v_new, ctx_lens, k_cache, v_cache, q=None, q_out=None, k_scales=None, v_scales=None,
                  dev_status=None, stream=None, check=True):
     """ssa_cache_append: the step's keys and values into the cache, rotated by position, and its queries rotated into q_out."""
+    _check_type(desc, k_new)
     rc = _call.cache_append(desc, append, k_new, v_new, ctx_lens, k_cache, v_cache, q, q_out, k_scales, v_scales, dev_status,
                             _stream(stream))
     return _check("ssa_cache_append", rc, check)

@@ -251,14 +251,21 @@ def test_arguments_arrive(name, through):
 
 
 def test_errors_raise_through_the_binding():
-    d, x = desc(), torch.zeros(2, 8, 4, 128)
-    b, i = torch.zeros(2, 2, 8, 2, 128), torch.zeros(2, 2, 4, 4, dtype=torch.int32)
+    d, x = desc(), torch.zeros(2, 8, 4, 128).bfloat16()
+    b, i = torch.zeros(2, 2, 8, 2, 128).bfloat16(), torch.zeros(2, 2, 4, 4, dtype=torch.int32)
     k = good_blocks()
     for f, args in ((ssa.attn_window_fp4, (d, good_window(), *[None] * 7)), (ssa.block_bounds, (d, k, None, None, b)), (ssa.block_select, (d, k, None, b, None, i, i[..., 0].contiguous())),
                     (ssa.attn_blocks, (d, k, None, None, None, None, i, i[..., 0].contiguous(), None)), (ssa.cache_append, (d, good_append(), *[None] * 5))):
         with pytest.raises(ssa.SsaError, match=f.__name__):
             f(*args, stream=0)
         assert f(*args, stream=0, check=False) != ssa.OK
+    other, c = x.half(), i[..., 0].contiguous()              # another type than the cache's queries have
+    for call in (lambda: ssa.attn_window_fp4(d, good_window(), other, *[None] * 6, stream=0), lambda: ssa.block_bounds(d, k, None, None, b.half(), stream=0),
+                 lambda: ssa.block_select(d, k, other, b, None, i, c, stream=0), lambda: ssa.block_select(d, k, x, b.float(), None, i, c, stream=0),
+                 lambda: ssa.attn_blocks(d, k, other, None, None, None, i, c, None, stream=0), lambda: ssa.cache_append(d, good_append(), other, *[None] * 4, stream=0),
+                 lambda: ssa.cache_append(desc(ssa.F16), good_append(), x, *[None] * 4, stream=0)):
+        with pytest.raises(ValueError, match="where the cache goes with"):
+            call()
     few = [(b[:1], "bounds"), (b[:, :1], "bounds"), (b[:, :, :7], "bounds"), (b[..., :64], "bounds")]
     for bad, word in few:
         with pytest.raises(ValueError, match=word):
