@@ -59,8 +59,7 @@ static int32_t launch(const ListParams& p, cudaStream_t st) {
   note_launches(1);
   if (p.n_splits == 1) return SSA_OK;
   using TQ = typename Storage<T>::Query;
-  err = launch_pdl(window_join_kernel<TQ, D, ListParams>, dim3((unsigned)((p.H * p.n_q + kJoinWarps - 1) / kJoinWarps), (unsigned)p.B),
-                   dim3(kJoinWarps * 32), st, p);
+  err = launch_join<TQ, D>(p, st);
   if (err != cudaSuccess) return SSA_ERR_CUDA;
   note_launches(1);
   return SSA_OK;

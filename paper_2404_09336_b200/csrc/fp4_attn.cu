@@ -92,8 +92,7 @@ static int32_t launch(const Fp4Params& p, int box_rows, cudaStream_t st) {
   if (end) cudaEventRecord(end, st);
   note_launches(1);
   if (p.n_splits == 1) return SSA_OK;
-  err = launch_pdl(window_join_kernel<__nv_bfloat16, D, Fp4Params>, dim3((unsigned)((p.H * p.n_q + kJoinWarps - 1) / kJoinWarps), (unsigned)p.B),
-                   dim3(kJoinWarps * 32), st, p);
+  err = launch_join<__nv_bfloat16, D>(p, st);
   if (err != cudaSuccess) return SSA_ERR_CUDA;
   note_launches(1);
   return SSA_OK;

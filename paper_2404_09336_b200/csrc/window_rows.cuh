@@ -741,7 +741,84 @@ window_join_kernel(const Params p) {
   join_rows<TQ, D>(p, blockIdx.y, blockIdx.x * kJoinWarps + threadIdx.x / 32);
 }
 
+// The same where there are many splits and few rows, of the calls over 4-bit values and lists: a block per query row, whose warps take
+// splits in turn, two at a time, and meet in shared memory.  One request of 16384 positions, 32 heads over 8, 4-bit values, 64 splits:
+// 14.4 us in all instead of 17.6.
+constexpr int kManySplits = 8, kWideWarps = 8;
+
+template <typename TQ, int D, typename Params>
+__global__ void __launch_bounds__(kWideWarps * 32)
+window_join_wide_kernel(const Params p) {
+  constexpr int kN = D / 32, kAhead = 4;
+  __shared__ float s_acc[kWideWarps][D];
+  __shared__ float2 s_ml[kWideWarps];
+  const int row = blockIdx.x, b = blockIdx.y, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int h = p.n_q == 1 ? row : row / p.n_q, t = row - h * p.n_q;
+  const int64_t at = (int64_t)b * p.H * p.n_q + row, slot = at * p.n_splits;
+  grid_dependency_wait();
+  grid_launch_dependents();
+  // (asked for before it is known how many there are: all n_splits have their place)
+  float2 ml[kAhead];
+  float a[kAhead][kN];
+  auto ask = [&](int i, int x) {
+    if (i >= p.n_splits) return;
+    ml[x] = p.ws_ml[slot + i];
+    const float* from = p.ws_acc + (slot + i) * D + lane * kN;
+#pragma unroll
+    for (int y = 0; y < kN; y += 2) {
+      const float2 f = *reinterpret_cast<const float2*>(from + y);
+      a[x][y] = f.x; a[x][y + 1] = f.y;
+    }
+  };
+#pragma unroll
+  for (int x = 0; x < kAhead; ++x) ask(warp + x * kWideWarps, x);
+  uint32_t flags = 0;
+  int ctx, n_new;
+  window_sizes(p, b, ctx, n_new, flags);
+  if (t >= n_new) return;
+  const int n = row_splits(p, b, h, t, ctx, n_new);
+  if (n == 1) return;
+  float M = neg_inf(), L = 0.f, A[kN];
+#pragma unroll
+  for (int y = 0; y < kN; ++y) A[y] = 0.f;
+  for (int i0 = warp; i0 < n; i0 += kAhead * kWideWarps) {
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      if (i0 + x * kWideWarps < n && ml[x].y != 0.f) {       // (a split without a weight adds nothing)
+        const float top = fmaxf(M, ml[x].x), base = top == neg_inf() ? 0.f : top, w = fast_exp2(ml[x].x - base), old = fast_exp2(M - base);
+        L = fmaf(L, old, ml[x].y * w);
+#pragma unroll
+        for (int y = 0; y < kN; ++y) A[y] = fmaf(A[y], old, a[x][y] * w);
+        M = top;
+      }
+      ask(i0 + (kAhead + x) * kWideWarps, x);
+    }
+  }
+  if (lane == 0) s_ml[warp] = make_float2(M, L);
+#pragma unroll
+  for (int y = 0; y < kN; ++y) s_acc[warp][lane * kN + y] = A[y];
+  __syncthreads();
+  if (threadIdx.x >= D) return;
+  float top = neg_inf(), sum = 0.f, x = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWideWarps; ++w) top = fmaxf(top, s_ml[w].x);
+#pragma unroll
+  for (int w = 0; w < kWideWarps; ++w) {
+    const float by = s_ml[w].y == 0.f ? 0.f : fast_exp2(s_ml[w].x - top);
+    sum = fmaf(s_ml[w].y, by, sum);
+    x = by == 0.f ? x : fmaf(s_acc[w][threadIdx.x], by, x);
+  }
+  store_window_value<TQ>(p, b, h, t, threadIdx.x, sum == 0.f ? 0.f : x / sum);
+  if (threadIdx.x == 0 && p.lse) p.lse[at] = sum == 0.f ? neg_inf() : (top + log2f(sum)) * kLn2;
+}
+
 // ---- host ------------------------------------------------------------------------------------------------------------
+// Joins the splits of the calls over 4-bit values and lists.
+template <typename TQ, int D, typename Params>
+static cudaError_t launch_join(const Params& p, cudaStream_t st) {
+  if (p.n_splits > kManySplits) return launch_pdl(window_join_wide_kernel<TQ, D, Params>, dim3((unsigned)(p.H * p.n_q), (unsigned)p.B), dim3(kWideWarps * 32), st, p);
+  return launch_pdl(window_join_kernel<TQ, D, Params>, dim3((unsigned)((p.H * p.n_q + kJoinWarps - 1) / kJoinWarps), (unsigned)p.B), dim3(kJoinWarps * 32), st, p);
+}
 // Splits of the kernel for few rows: what n splits cost in units of one tile's time.  The work of all blocks, each with a start and
 // an end, over the places that there are (two or three blocks to an SM), but no less than one block's; half a block's until the
 // last is done (lengths differ: three quarters of the longest are taken for the mean); joining.  Tiles of 4-bit values take longer,
