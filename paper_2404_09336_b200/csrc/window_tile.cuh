@@ -38,9 +38,9 @@ namespace ssa {
 
 constexpr int kTileRows = 128, kTileKeys = 128;
 constexpr int kTileThreads = 256;
-// registers of a thread; 128 x 200 + 128 x 56 (4-bit: 192, 64) = 256 x 128, what the launch has
-template <typename T> constexpr int kSoftmaxRegs = kIsFp4<T> ? 192 : 200;
-template <typename T> constexpr int kOtherRegs = kIsFp4<T> ? 64 : 56;
+// registers of a thread; 128 x 200 + 128 x 56 (4-bit: 184, 72) = 256 x 128, what the launch has
+template <typename T> constexpr int kSoftmaxRegs = kIsFp4<T> ? 184 : 200;
+template <typename T> constexpr int kOtherRegs = kIsFp4<T> ? 72 : 56;
 constexpr int kConverters = 96;                     // threads of warps 5 to 7
 constexpr int kTileSplit = 4;                       // fewest tiles worth a split of their own
 constexpr float kLazy = 8.f;                        // log2 of how far weights may exceed 1
@@ -324,22 +324,35 @@ window_tile_kernel(const Params p, const __grid_constant__ CUtensorMap k_map, co
     const bool used = lane < kTileKeys >> box_shift && ja <= hi && (ja + box_rows - 1 >= from || ja < p.sinks);
     return used ? (int)row_of<true>(p, p.page_table + (int64_t)b * p.page_table_stride, ja) : -1;
   };
-  auto ask = [&](int x, int j0, int of_v, int page_row, bool whole) {  // piece x of the tile from position j0 on
-    const int r = my_row + x * kRowsAtOnce, j = j0 + r;
-    int row = j;
-    if constexpr (kPaged) {
-      row = __shfl_sync(~0u, page_row, r >> box_shift & 31);
-      row = row < 0 ? -1 : row + (r & (box_rows - 1));
-    }
-    if (!whole && (j > hi || !(j >= from || j < p.sinks))) row = -1;
-    if (r < kTileKeys) {
-      if constexpr (kIsFp4<T>) {
-        const int64_t at = (of_v ? my_v : my_k) + (row < 0 ? 0 : row) * (int64_t)(of_v ? p.v_st : p.k_st);
-        copy_16B(smem_at(raw) + (me + x * kConverters) * 16, static_cast<const uint8_t*>(of_v ? p.v : p.k) + at / 2, row >= 0);
-        scale_pair[x] = row >= 0 ? *reinterpret_cast<const uint16_t*>((of_v ? p.v_scales : p.k_scales) + at / kScaleDims) : 0u;
+  // pieces x0 ... x0 + kTurn - 1 of the tile from position j0 on: addresses first, of all of them, so that none waits for another's
+  auto ask = [&](int x0, int j0, bool of_v, int page_row, bool whole) {
+    if constexpr (kIsFp4<T>) {
+      const int64_t my = of_v ? my_v : my_k, st = of_v ? p.v_st : p.k_st;
+      const uint8_t* const codes = static_cast<const uint8_t*>(of_v ? p.v : p.k) + my / 2;
+      const uint8_t* const scales = (of_v ? p.v_scales : p.k_scales) + my / kScaleDims;
+      int row[kTurn];
+#pragma unroll
+      for (int y = 0; y < kTurn; ++y) {
+        const int r = my_row + (x0 + y) * kRowsAtOnce;
+        row[y] = kPaged ? __shfl_sync(~0u, page_row, r >> box_shift & 31) : j0 + r;
       }
+      int64_t at[kTurn];
+#pragma unroll
+      for (int y = 0; y < kTurn; ++y) {
+        const int r = my_row + (x0 + y) * kRowsAtOnce;
+        if (kPaged && row[y] >= 0) row[y] += r & (box_rows - 1);
+        if (!whole && (j0 + r > hi || !(j0 + r >= from || j0 + r < p.sinks))) row[y] = -1;
+        at[y] = max(row[y], 0) * st;
+      }
+#pragma unroll
+      for (int y = 0; y < kTurn; ++y) {
+        if (my_row + (x0 + y) * kRowsAtOnce < kTileKeys) {
+          scale_pair[x0 + y] = row[y] >= 0 ? *reinterpret_cast<const uint16_t*>(scales + at[y] / kScaleDims) : 0u;
+          copy_16B(smem_at(raw) + (me + (x0 + y) * kConverters) * 16, codes + at[y] / 2, row[y] >= 0);
+        }
+      }
+      copies_commit();
     }
-    copies_commit();
   };
   auto convert = [&](int x0, uint8_t* to) {                  // pieces x0 ... x0 + kTurn - 1
     uint4 w[kTurn];
@@ -381,7 +394,7 @@ window_tile_kernel(const Params p, const __grid_constant__ CUtensorMap k_map, co
     if (warp >= 5 && n_loads > 0) {
       page_row = page_of(range.x);
 #pragma unroll
-      for (int x = 0; x < kMine; ++x) ask(x, seen.position(range.x), 0, page_row, false);
+      for (int x = 0; x < kMine; x += kTurn) ask(x, seen.position(range.x), false, page_row, false);
     }
   }
   if (warp == 4) {
@@ -437,13 +450,10 @@ window_tile_kernel(const Params p, const __grid_constant__ CUtensorMap k_map, co
         if (i & 1) page_row = next_row;
 #pragma unroll
         for (int x0 = 0; x0 < kMine; x0 += kTurn) {
-          copies_wait<kMine - kTurn>();                      // (a thread reads what it asked for itself)
+          copies_wait<kMine / kTurn - 1>();                  // (a thread reads what it asked for itself)
           convert(x0, to);
-#pragma unroll
-          for (int x = x0; x < x0 + kTurn; ++x) {
-            if (more) ask(x, j0, (i + 1) & 1, page_row, whole);
-            else copies_commit();
-          }
+          if (more) ask(x0, j0, (i + 1) & 1, page_row, whole);
+          else copies_commit();
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         mbar_arrive(full + 8 * (i % kStages));
