@@ -113,14 +113,15 @@ static int32_t check_window(const ssa_attn_desc* d, const ssa_window* w, bool ma
   return w->paging ? check_paging(w->paging, d->max_ctx) : SSA_OK;
 }
 
-// Rows of a K/V head up to which the kernel for few rows serves a 4-bit cache: with 32 it takes 92, 58, 102 and 39 us, the tiles 124,
-// 56, 131 and 37 (8 requests of 4100 to 16384 positions, those within a window of 4096, 32 requests of up to 4096, one of 16384; 8 K/V
-// heads); with 48 rows 149, 73, 150 and 46 against 134, 56, 124 and 34.
+// Rows of a K/V head up to which the kernel for few rows serves a 4-bit cache: with 32 it takes 91, 57, 102 and 36 us, the tiles 98, 48,
+// 106 and 32 (8 requests of 4100 to 16384 positions, those within a window of 4096, 32 requests of up to 4096, one of 16384; 8 K/V
+// heads); with 24 rows 69, 42, 70 and 16 against 105, 48, 99 and 25, with 48 154, 73, 150 and 43 against 111, 48, 100 and 29.
 constexpr int kFewRowsFp4 = 32;
-// Rows above which it is converted once for all of them, instead of by every block of 128 rows: with 256 that takes 222, 106, 224 and
-// 43 us for the same requests, each block for itself 227, 91, 194 and 40; with 384 324, 127, 233 and 58 against 396, 139, 216 and 56;
-// with 768 342, 133, 304 and 66 against 412, 143, 335 and 78.
-constexpr int kExpandRows = 256;
+// Rows above which it is converted once for all of them, instead of by every block of 128 rows: for the same requests that takes 222,
+// 107, 224 and 43 us with 256 rows, 343, 133, 304 and 66 with 768, each block for itself 175, 79, 159 and 40, and 336, 119, 278 and 67.
+// In pages, where a block fetches its rows one address each, 235 against 235 with 256 rows (the first requests), 339 against 414 with
+// 384, 359 against 445 with 768.
+constexpr int kExpandRows = 768, kExpandRowsPaged = 256;
 
 // Whether the tiles of 128 rows serve a call.
 static bool tiles_pay(const ssa_attn_desc* d, const ssa_window* w, bool mass) {
@@ -160,7 +161,7 @@ static bool plan_window(const ssa_attn_desc* d, const ssa_window* w, bool mass, 
 // Few blocks of 128 rows convert what they see themselves.
 static size_t plan_expanded(const ssa_attn_desc* d, const ssa_window* w, Fp4Expanded* x) {
   const long long rows = (long long)(d->H / d->H_kv) * w->n_q;
-  if (rows <= kExpandRows) return 0;
+  if (rows <= (w->paging ? kExpandRowsPaged : kExpandRows)) return 0;
   const long long all = (d->max_ctx + kTileKeys - 1ll) / kTileKeys;
   const long long seen = ((long long)w->sinks + kTileKeys - 1) / kTileKeys + ((long long)w->window + w->n_q + kTileKeys - 1) / kTileKeys + 1;
   const long long tiles = w->window == 0 ? all : std::min(all, seen);

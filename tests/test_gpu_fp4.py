@@ -17,9 +17,14 @@ def many(p):
     return p.H // p.H_kv * p.n_q > 32
 
 
+def shares(p):
+    """Whether the seen part of the cache is converted once for all of the call's blocks, where there is room."""
+    return p.H // p.H_kv * p.n_q > (256 if p.cache.page else 768)
+
+
 def run(p, ctx, new=None, window=0, sinks=0, out_dtype=F32, **k):
     got = p.call(ctx, new, window, sinks, out_dtype, **k)
-    check_tokens(p, got, ctx, new, window, sinks, out_dtype, many(p), shared=p.H // p.H_kv * p.n_q > 256 and not k.get("less"), scale=k.get("scale") or None)
+    check_tokens(p, got, ctx, new, window, sinks, out_dtype, many(p), shared=shares(p) and not k.get("less"), scale=k.get("scale") or None)
     return got
 
 
@@ -82,13 +87,22 @@ def test_long_contexts_in_splits(n_q):
 @pytest.mark.parametrize("layout", ["spaced", 8, 16, 256])
 @pytest.mark.parametrize("less", [0, 1])
 def test_chunks_that_share_a_conversion(D, layout, less):
-    """More than 256 rows a K/V head, with and without room for the seen part of the cache in bf16."""
+    """More than 256 rows a K/V head of a paged cache, 768 of another, with and without room for the seen part of it in bf16."""
     page = layout if isinstance(layout, int) else 0
-    p = Fp4Tokens(3, 5, 1, 500, D, 60, layout="bhtd" if page else layout, page=page)
-    run(p, [500, 333, 60], None, out_dtype=BF16 if less else F32, less=less)
-    run(p, [477, 130, 50], [60, 5, 0], window=150, sinks=9, out_dtype=F32 if less else BF16, less=less)
-    run(p, [499, 340, 60], [40, 60, 1], window=128, sinks=200, less=less)
-    run(p, [40, 0, 60], [40, 0, 60], window=5000, less=less)
+    n = 60 if page else 160
+    p = Fp4Tokens(3, 5, 1, 500, D, n, layout="bhtd" if page else layout, page=page)
+    run(p, [500, 333, n], None, out_dtype=BF16 if less else F32, less=less)
+    run(p, [477, 130, n - 10], [n, 5, 0], window=150, sinks=9, out_dtype=F32 if less else BF16, less=less)
+    run(p, [499, 340, n], [n - 20, n, 1], window=128, sinks=200, less=less)
+    run(p, [40, 0, n], [40, 0, n], window=5000, less=less)
+
+
+@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("rows", [256, 257, 768, 769])
+def test_rows_on_both_sides_of_a_shared_conversion(page, rows):
+    p = Fp4Tokens(2, 1, 1, 900, 128, rows, page=page)
+    run(p, [900, rows], [rows, rows - 1])
+    run(p, [899, 700], [rows, 3], window=100, sinks=2, out_dtype=BF16)
 
 
 def test_large_queries_and_scales():
