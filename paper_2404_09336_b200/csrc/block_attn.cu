@@ -16,7 +16,7 @@ static int32_t check_blocks(const ssa_attn_desc* d, const ssa_blocks* k) {
   if (rc != SSA_OK) return rc;
   if (k->q_stride_t < 0 || k->o_stride_t < 0 || (long long)d->H * k->n_q > 1ll << 24) return SSA_ERR_SHAPE;
   if (k->q_stride_t % 8 != 0 || k->o_stride_t % 8 != 0) return SSA_ERR_ALIGN;
-  if (k->budget <= 0) return SSA_ERR_CAPACITY;
+  if (k->budget <= 0 || (long long)k->budget * k->block_size > 0x7fffffffll) return SSA_ERR_CAPACITY;
   return k->paging ? check_paging(k->paging, d->max_ctx) : SSA_OK;
 }
 

@@ -166,6 +166,10 @@ def test_blocks(call):
         assert attend(desc(), good_blocks(), ws=ODD) == ssa.ERR_ALIGN
         k.block_size = 31
         assert ssa.attn_blocks_workspace_bytes(desc(), k) == 0
+        k.block_size, k.budget = 64, 1 << 25                 # (2^31 positions: tiles and positions of a list are counted in 32 bits)
+        assert attend(desc(), k) == ssa.ERR_CAPACITY and ssa.attn_blocks_workspace_bytes(desc(), k) == 0
+        k.budget -= 1
+        assert ssa.attn_blocks_workspace_bytes(desc(), k) > 0
     assert ssa.launch_count() == before
 
 
