@@ -93,6 +93,17 @@ class Cache:
         return (ssa.make_desc_paged if self.page else ssa.make_desc)(q[:, :, 0], k, v, *args, scale=scale)
 
 
+def far_apart(c):
+    """The cache's requests (two) more than 2^32 values apart."""
+    for name, x in c.parts.items():
+        B, H, T, n = x.shape
+        far = ((1 << 32) + 128) // (c.D // n)
+        y = torch.zeros(far + H * T * n, dtype=x.dtype, device=DEV).as_strided((B, H, T, n), (far, T * n, n, 1))
+        y.copy_(x)
+        c.parts[name] = y
+    return c
+
+
 class Fp4Tokens(Tokens):
     """budget_util.Tokens over a 4-bit cache (weights are fp16 pairs, as over an 8-bit one)."""
 

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from budget_util import DEV, UNWRITTEN
-from cache_util import DTYPES, Cache, check_rows, query_type
+from cache_util import DTYPES, Cache, check_rows, far_apart, query_type
 from oracle import cache_oracle as CO
 from paper_2404_09336_b200 import ssa
 
@@ -164,3 +164,10 @@ def test_infinities_and_nan_reach_the_tokens_that_see_them(dtype, D):
     seen[17] = True
     assert np.isfinite(out[0, :, 0]).all() and np.isfinite(lse).all()
     assert np.isnan(out[0, :, 1, seen]).all() and np.isfinite(out[0, :, 1, ~seen]).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_offsets_past_32_bits(dtype):
+    p = Lists(2, 4, 2, 200, 128, 32, 3, dtype=dtype)
+    far_apart(p.c)
+    assert p.check([200, 150]) == 0

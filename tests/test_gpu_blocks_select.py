@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from budget_util import DEV
-from cache_util import DTYPES, Cache, query_type
+from cache_util import DTYPES, Cache, far_apart, query_type
 from oracle import budget_oracle as BO
 from oracle import cache_oracle as CO
 from paper_2404_09336_b200 import ssa
@@ -203,3 +203,15 @@ def test_scores_need_not_be_asked_for():
     c = Choice(2, 8, 4, 3000, 128, 64)
     with_them, without = c.call([3000, 1234], None, 9, 1, 1), c.call([3000, 1234], None, 9, 1, 1, with_scores=False)
     assert np.array_equal(with_them[0], without[0]) and np.array_equal(with_them[1], without[1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_keys_past_32_bits(dtype):
+    c = far_apart(Cache(2, 2, 100, 128, dtype))
+    got, status = bounds_of(c, 2, [100, 70], None, 100, 32)
+    K = c.values("k")
+    for b, n in ((0, 100), (1, 70)):
+        for h in range(2):
+            least, most = CO.bounds(K[b, h], n, 32)
+            assert np.array_equal(got[b, h, : len(least), 0], least) and np.array_equal(got[b, h, : len(most), 1], most)
+    assert status == 0

@@ -3,8 +3,8 @@ import numpy as np
 import pytest
 import torch
 
-from budget_util import DEV, half_step
-from cache_util import Fp4Tokens, check_tokens
+from budget_util import half_step
+from cache_util import Fp4Tokens, check_tokens, far_apart
 from oracle import budget_oracle as BO
 from paper_2404_09336_b200 import ssa
 
@@ -173,18 +173,10 @@ def test_nan_scales_in_a_chunk_that_shares_a_conversion():
     assert np.isfinite(out[0, 2:, :50]).all() and np.isfinite(out[0, 2:, 110:]).all() and np.array_equal(out[0, :2], want[0][0, :2])
 
 
-def test_offsets_past_32_bits():
+@pytest.mark.parametrize("n_q", [2, 40, 400])
+def test_offsets_past_32_bits(n_q):
     """Codes of the second request lie beyond 2^32 values, scales beyond 2^28 bytes."""
-    far = (1 << 32) + 128                                    # values from request to request
-    T, D = 70, 128
-    p = Fp4Tokens(2, 4, 2, T, D, 2)
-    big = {}
-    for name in "kv":
-        codes, scales = torch.zeros(far // 2 + 2 * T * D, dtype=torch.uint8, device=DEV), torch.zeros(far // 16 + 2 * T * D, dtype=torch.uint8, device=DEV)
-        big[name] = codes.as_strided((2, 2, T, D // 2), (far // 2, T * D // 2, D // 2, 1))
-        big[name + "_scales"] = scales.as_strided((2, 2, T, D // 16), (far // 16, T * D // 16, D // 16, 1))
-    for name, x in big.items():
-        x.copy_(p.cache.parts[name])
-        p.cache.parts[name] = x
-    p.cache.get = lambda name: big[name].cpu().contiguous()
-    run(p, [70, 55])
+    T = max(70, n_q)
+    p = Fp4Tokens(2, 4, 2, T, 128, n_q)
+    far_apart(p.cache)
+    run(p, [T, T])
