@@ -7,7 +7,8 @@ namespace ssa {
 // Every block of 128 query rows that works on tiles converts the K and V rows that it sees.  Where many share them (prompt chunks)
 // they are converted once instead, into pages of the workspace that the tiles of a bf16 cache then read: products of a code and a
 // scale have six significant bits, so that nothing is rounded.  HBM bounds it: 2.56 bytes a value.  8 requests' chunks of up to 509
-// tokens within a window of 4096, 8 K/V heads: some 45 us, and 166 for the tiles.
+// tokens within a window of 4096, 8 K/V heads: some 36 us (5.4 TB/s), and 166 for the tiles; 49 with 16 bytes of codes to a thread,
+// whose stores then lie 64 bytes apart.
 constexpr int kExpandThreads = 256;
 
 // grid (tiles of 128 positions that a request's tokens see between them, H_kv, B).  Page tables of the pages made: tile i of request b
@@ -15,7 +16,7 @@ constexpr int kExpandThreads = 256;
 template <int D, bool kPaged>
 __global__ void __launch_bounds__(kExpandThreads)
 fp4_expand_kernel(const Fp4Params p, const Fp4Expanded x) {
-  constexpr int kC = D / 32, kEach = 2 * kTileKeys * kC / kExpandThreads;    // 16-byte pieces of a row; of K and V, of a thread
+  constexpr int kC = D / 8, kStep = kExpandThreads / kC, kEach = kTileKeys / kStep;    // pieces of a row; rows at a time; of a thread
   grid_dependency_wait();
   grid_launch_dependents();
   const int b = blockIdx.z, hkv = blockIdx.y, tile = blockIdx.x, tid = threadIdx.x;
@@ -34,39 +35,38 @@ fp4_expand_kernel(const Fp4Params p, const Fp4Expanded x) {
     const bool used = ja <= hi && (jz >= from || ja < p.sinks);
     if (used) x.table[(int64_t)b * x.table_stride + (ja >> x.page_shift)] = row_of<kPaged>(p, table, ja) < 0 ? -1 : (int)(to_row >> x.page_shift) + tid;
   }
-  uint4 w[kEach];
-  uint32_t pair[kEach];
+  // a thread has eight values of every kStep-th row, so that a warp stores whole lines
+  const int r0 = tid / kC, c = tid % kC;
+  uint32_t w[2][kEach], scale[2][kEach];
 #pragma unroll
   for (int y = 0; y < kEach; ++y) {
-    const int piece = tid + y * kExpandThreads, of_v = piece / (kTileKeys * kC), r = piece / kC % kTileKeys, c = piece % kC;
+    const int r = r0 + y * kStep;
     const int64_t row = is_seen(j0 + r) ? row_of<kPaged>(p, table, j0 + r) : -1;
-    const int64_t o = (kPaged ? 0 : (int64_t)b * (of_v ? p.v_sb : p.k_sb)) + (int64_t)hkv * (of_v ? p.v_sh : p.k_sh) +
-                      (row < 0 ? 0 : row) * (of_v ? p.v_st : p.k_st) + c * 32;
-    w[y] = make_uint4(0, 0, 0, 0);
-    pair[y] = 0;
-    if (row >= 0) {
-      w[y] = ld_stream_16B(static_cast<const uint8_t*>(of_v ? p.v : p.k) + o / 2);
-      pair[y] = *reinterpret_cast<const uint16_t*>((of_v ? p.v_scales : p.k_scales) + o / kScaleDims);
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      w[z][y] = scale[z][y] = 0;
+      if (row >= 0) {
+        const int64_t o = (kPaged ? 0 : (int64_t)b * (z ? p.v_sb : p.k_sb)) + (int64_t)hkv * (z ? p.v_sh : p.k_sh) + row * (z ? p.v_st : p.k_st) + c * 8;
+        w[z][y] = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(z ? p.v : p.k) + o / 2);
+        scale[z][y] = (z ? p.v_scales : p.k_scales)[o / kScaleDims];
+      }
     }
   }
 #pragma unroll
   for (int y = 0; y < kEach; ++y) {
-    const int piece = tid + y * kExpandThreads, of_v = piece / (kTileKeys * kC), r = piece / kC % kTileKeys, c = piece % kC;
+    const int r = r0 + y * kStep;
     if (!is_seen(j0 + r)) continue;                          // (may hold anything: the tiles do not use it)
-    const float2 scale = unpack2<__half>(e4m3x2_to_half2(pair[y]));
-    const uint32_t words[4] = {w[y].x, w[y].y, w[y].z, w[y].w};
-    uint4* to = reinterpret_cast<uint4*>((of_v ? x.v : x.k) + ((int64_t)hkv * x.head_rows + to_row + r) * D + c * 32);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float by = i < 2 ? scale.x : scale.y;
+    for (int z = 0; z < 2; ++z) {
+      const float by = e4m3x2_to_float2(scale[z][y]).x;
       uint32_t h[4];
-      e2m1x8_to_half2(words[i], h);
+      e2m1x8_to_half2(w[z][y], h);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float2 f = unpack2<__half>(h[e]);
         h[e] = pack2<__nv_bfloat16>(f.x * by, f.y * by);
       }
-      to[i] = make_uint4(h[0], h[1], h[2], h[3]);
+      *reinterpret_cast<uint4*>((z ? x.v : x.k) + ((int64_t)hkv * x.head_rows + to_row + r) * D + c * 8) = make_uint4(h[0], h[1], h[2], h[3]);
     }
   }
 }
