@@ -117,10 +117,10 @@ static int32_t check_window(const ssa_attn_desc* d, const ssa_window* w, bool ma
 // 106 and 32 (8 requests of 4100 to 16384 positions, those within a window of 4096, 32 requests of up to 4096, one of 16384; 8 K/V
 // heads); with 24 rows 69, 42, 70 and 16 against 105, 48, 99 and 25, with 48 154, 73, 150 and 43 against 111, 48, 100 and 29.
 constexpr int kFewRowsFp4 = 32;
-// Rows above which it is converted once for all of them, instead of by every block of 128 rows: for the same requests that takes 222,
-// 107, 224 and 43 us with 256 rows, 343, 133, 304 and 66 with 768, each block for itself 175, 79, 159 and 40, and 336, 119, 278 and 67.
-// In pages, where a block fetches its rows one address each, 235 against 235 with 256 rows (the first requests), 339 against 414 with
-// 384, 359 against 445 with 768.
+// Rows above which it is converted once for all of them, instead of by every block of 128 rows: for the same requests that takes 199,
+// 94, 197 and 40 us with 256 rows, 280, 116, 214 and 54 with 512, 314, 121, 277 and 65 with 768, each block for itself 176, 79, 160 and
+// 40, then 283, 117, 199 and 61, then 336, 119, 276 and 66.  In pages each piece of a row costs a block more instructions: 212, 99, 213
+// and 41 against 235, 97, 207 and 45 with 256 rows, 314, 121, 222 and 53 against 416, 149, 232 and 64 with 384.
 constexpr int kExpandRows = 768, kExpandRowsPaged = 256;
 
 // Whether the tiles of 128 rows serve a call.
