@@ -547,7 +547,9 @@ int32_t ssa_mass_to_index(const float* mass, int64_t mass_stride, const int32_t*
  * head and i < counts[b], row index[b*index_stride + i] of K and of V becomes
  * row i, and entry i of mass (dev float, rows mass_stride >= max_ctx apart, or
  * NULL) likewise.  Afterwards counts[b] is the request's context length.  Rows
- * from counts[b] on keep what they held.  The lists must ascend strictly
+ * from counts[b] on keep what they held, and so do entries of mass: a caller
+ * who appends tokens that no ssa_attn_mass has as its step's makes theirs zero.
+ * The lists must ascend strictly
  * within [0, ctx_lens[b]), as ssa_mass_to_index and ssa_spans_to_index write
  * them; an entry outside that range moves nothing (SSA_DEV_BAD_INDEX), and
  * lists in another order leave unspecified rows.  counts[b] above max_selected

@@ -239,8 +239,11 @@ class DecodeStep:
     def append(self, k_new, v_new, q=None, cos_sin=None, interleaved=False, positions=None, stream=None):
         """A new token of every request: contexts are one longer, its key k_new[B,H,D], rotated by position (cos_sin, positions as for
         make_append), and its value v_new are in every copy of the cache (the 4-bit one too), its query q, rotated, in self.q; the
-        bounds of its block are made anew.  What bounds lists on the host (max_selected, spans) stays."""
+        bounds of its block are made anew, its position's sum (attend_mass) starts from nothing.  What bounds lists on the host
+        (max_selected, spans) stays."""
         with self._on(stream):
+            # (the sum may be that of a position which was here before a compaction)
+            self.mass.scatter_(1, self.ctx_lens.clamp(0, self.wl.max_ctx - 1).long().unsqueeze(1), 0.0)
             self.ctx_lens.add_(1)
         new = ssa.make_append(k_new.unsqueeze(2), v_new.unsqueeze(2), None if q is None else q.unsqueeze(2),
                               None if q is None else self.q.unsqueeze(2), cos_sin, interleaved, positions)
