@@ -711,7 +711,9 @@ int32_t ssa_attn_blocks(const ssa_attn_desc* desc, const ssa_blocks* blocks, con
  * call).  ctx_lens counts the step's tokens already: token t of request b goes to
  * position pos = ctx_lens[b] - q_lens[b] + t.  Rows t >= q_lens[b] and tokens of
  * negative position are not used, nor is anything written for them; ctx_lens[b]
- * above max_ctx and q_lens[b] above n_q are clamped (SSA_DEV_BAD_COUNT).  With R =
+ * above max_ctx and q_lens[b] above n_q are clamped (SSA_DEV_BAD_COUNT): the step's
+ * tokens are then the cache's last rows, and a caller whose cache may be full gives
+ * that request a q_lens[b] of 0.  With R =
  * rotary_dims and
  * (c_i, s_i) = cos_sin[p*R + i], cos_sin[p*R + R/2 + i] for p = positions[b*n_q +
  * t] (NULL: pos), i < R/2, the pairs (x_i, x_{i+R/2}) of a query or key, or

@@ -127,6 +127,7 @@ class DecodeStep:
             raise RuntimeError("ssa_decode_workspace_bytes rejected the descriptor")
         self.workspace = torch.empty(need, dtype=torch.uint8, device=dev)
         self._rooms, self._outgrown = [], []
+        self._next_lens, self._new_lens = (torch.zeros_like(self.ctx_lens) for _ in range(2))    # of append
         self._steps = {}
         if dev.type == "cuda":                               # calls may come on any stream: what was filled above is there
             torch.cuda.current_stream(dev).synchronize()
@@ -237,25 +238,31 @@ class DecodeStep:
 
     # ---- filling the cache ----------------------------------------------------------------
     def append(self, k_new, v_new, q=None, cos_sin=None, interleaved=False, positions=None, stream=None):
-        """A new token of every request: contexts are one longer, its key k_new[B,H,D], rotated by position (cos_sin, positions as for
-        make_append), and its value v_new are in every copy of the cache (the 4-bit one too), its query q, rotated, in self.q; the
-        bounds of its block are made anew, its position's sum (attend_mass) starts from nothing.  What bounds lists on the host
-        (max_selected, spans) stays."""
-        with self._on(stream):
-            # (the sum may be that of a position which was here before a compaction)
-            self.mass.scatter_(1, self.ctx_lens.clamp(0, self.wl.max_ctx - 1).long().unsqueeze(1), 0.0)
-            self.ctx_lens.add_(1)
-        new = ssa.make_append(k_new.unsqueeze(2), v_new.unsqueeze(2), None if q is None else q.unsqueeze(2),
-                              None if q is None else self.q.unsqueeze(2), cos_sin, interleaved, positions)
+        """A new token of every request that has room for one: contexts are one longer, its key k_new[B,H,D], rotated by position
+        (cos_sin, positions as for make_append), and its value v_new are in every copy of the cache (the 4-bit one too), its query q,
+        rotated, in self.q; the bounds of its block are made anew, its position's sum (attend_mass) starts from nothing.  A request
+        whose context is max_ctx long already stays as it is, its row of self.q too (DEV_BAD_COUNT in self.status).  Refused arguments
+        raise and change nothing.  What bounds lists on the host (max_selected, spans) stays."""
+        k_new, v_new = k_new.unsqueeze(2), v_new.unsqueeze(2)
+        q_new, q_out = (None, None) if q is None else (q.unsqueeze(2), self.q.unsqueeze(2))
+        how = dict(cos_sin=cos_sin, interleaved=interleaved, positions=positions, q_lens=self._new_lens)
+        first, others = ssa.make_append(k_new, v_new, q_new, q_out, **how), ssa.make_append(k_new, v_new, **how)
+        desc = self.desc if q is None else ssa.make_desc(q, self.k, self.v, self.out, max_ctx=self.wl.max_ctx)
         caches = [(*self._copy(c), None, None) for c in range(len(self.k_store))]
         if hasattr(self, "fp4"):
             caches.append(self.fp4)
-        desc = self.desc if q is None else ssa.make_desc(q, self.k, self.v, self.out, max_ctx=self.wl.max_ctx)
-        for i, (k, v, k_scales, v_scales) in enumerate(caches):
-            if i == 1:                                       # (queries are rotated once)
-                q, new = None, ssa.make_append(k_new.unsqueeze(2), v_new.unsqueeze(2), None, None, cos_sin, interleaved, positions)
-            ssa.cache_append(desc if k_scales is None else self.desc_fp4, new, k_new, v_new, self.ctx_lens, k, v, q,
-                             None if q is None else self.q, k_scales, v_scales, self.status, stream)
+        with self._on(stream):
+            torch.add(self.ctx_lens, 1, out=self._next_lens)
+            self._new_lens.copy_(self.ctx_lens < self.wl.max_ctx)
+        for i, (k, v, k_scales, v_scales) in enumerate(caches):          # (queries are rotated once)
+            ssa.cache_append(desc if i == 0 else self.desc if k_scales is None else self.desc_fp4, others if i else first, k_new, v_new,
+                             self._next_lens, k, v, None if i else q, None if i or q is None else self.q, k_scales, v_scales,
+                             self.status, stream)
+        with self._on(stream):
+            # (the sum may be that of a position which was here before a compaction)
+            at, new = self.ctx_lens.clamp(0, self.wl.max_ctx - 1).long().unsqueeze(1), self._new_lens.unsqueeze(1) > 0
+            self.mass.scatter_(1, at, self.mass.gather(1, at).masked_fill(new, 0.0))
+            self.ctx_lens.add_(self._new_lens)
         if hasattr(self, "bounds"):
             self.refresh_bounds(1, stream)
         return ssa.OK

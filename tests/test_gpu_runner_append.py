@@ -54,3 +54,72 @@ def test_tokens_appended_behind_a_compaction_have_sums_of_their_own(last):
         assert (np.abs(got[b, :n] - want) <= tol).all()
         kept = BO.kept(got[b, :n].astype(np.float32), n, budget, sinks, recent)
         assert ds.counts[b] == len(kept) and np.array_equal(ds.index[b, : len(kept)].cpu().numpy(), kept)
+
+
+@pytest.mark.parametrize("layout", ["bhtd", "bthd"])
+def test_full_contexts_keep_their_rows(layout):
+    ds = made(layout=layout, kv_copies=2)
+    ds.enable_fp4()
+    ds.enable_blocks(32, 4)
+    T = ds.wl.max_ctx
+    ds.attend_mass()
+    ds.ctx_lens.copy_(torch.tensor([T, T - 1, 9], dtype=torch.int32))
+    ds.refresh_bounds()
+    torch.cuda.synchronize()
+    kept = [x.clone() for x in (*ds.k_store, *ds.v_store, *ds.fp4, ds.bounds, ds.mass, ds.q)]
+    x = rows(ds, 1)[0]
+    ds.append(x, x, x)
+    torch.cuda.synchronize()
+    assert ds.ctx_lens.tolist() == [T, T, 10] and int(ds.status) == ssa.DEV_BAD_COUNT
+    now = (*ds.k_store, *ds.v_store, *ds.fp4, ds.bounds, ds.mass, ds.q)
+    assert all(torch.equal(a[0], b[0]) for a, b in zip(now, kept))
+    for c in range(2):
+        ds.select_copy(c)
+        for b, n in ((1, T), (2, 10)):
+            assert torch.equal(ds.k[b, :, n - 1], x[b]) and torch.equal(ds.v[b, :, n - 1], x[b]) and torch.equal(ds.q[b], x[b])
+            was = kept[c][b] if layout == "bhtd" else kept[c][b].transpose(0, 1)
+            assert torch.equal(ds.k[b, :, : n - 1], was[:, : n - 1])
+    ds.append(x, x)
+    torch.cuda.synchronize()
+    assert ds.ctx_lens.tolist() == [T, T, 11]
+
+
+def test_a_refused_token_changes_nothing():
+    ds = made()
+    ds.enable_fp4()
+    x = rows(ds, 1)[0]
+    torch.cuda.synchronize()
+    ctx, k, q = ds.ctx_lens.clone(), ds.k_store[0].clone(), ds.q.clone()
+    for R in (40, 160):                                      # no multiple of 32; more than a row has
+        with pytest.raises(ssa.SsaError):
+            ds.append(x, x, x, torch.zeros(ds.wl.max_ctx, R, device=ds.device))
+    with pytest.raises(ValueError):
+        ds.append(x.half(), x, x)
+    torch.cuda.synchronize()
+    assert torch.equal(ds.ctx_lens, ctx) and torch.equal(ds.k_store[0], k) and torch.equal(ds.q, q) and int(ds.status) == 0
+
+
+def test_captured_appends_fill_a_cache_up():
+    """A graph of one token, replayed past the end of the shortest room, gives what eager calls give."""
+    eager, captured = made(), made()
+    T = eager.wl.max_ctx
+    for ds in (eager, captured):
+        ds.enable_fp4()
+        ds.enable_blocks(32, 5)
+        ds.ctx_lens.copy_(torch.tensor([T - 2, T, 3], dtype=torch.int32))
+        ds.refresh_bounds()
+    xs = rows(eager, 4)
+    k = xs[0].clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured.append(k, k, k)
+    for x in xs:
+        k.copy_(x)
+        graph.replay()
+        eager.append(x, x, x)
+    torch.cuda.synchronize()
+    assert eager.ctx_lens.tolist() == captured.ctx_lens.tolist() == [T, T, 7]
+    for a, b in zip((*eager.k_store, *eager.v_store, *eager.fp4, eager.bounds, eager.q), (*captured.k_store, *captured.v_store, *captured.fp4, captured.bounds, captured.q)):
+        assert torch.equal(a, b)
+    assert int(eager.status) == int(captured.status) == ssa.DEV_BAD_COUNT

@@ -20,3 +20,41 @@ def test_an_appended_position_has_no_sum_yet(made):          # noqa: F811
     ds.append(k, v)
     for b, n in enumerate(ctx.tolist()):
         assert not ds.mass[b, n:n + 2].any() and (ds.mass[b, :n] == 7).all() and (ds.mass[b, n + 2:] == 7).all()
+
+
+def test_a_refused_token_changes_nothing(made, monkeypatch):             # noqa: F811
+    ds = small()
+    ds.enable_blocks(64, 8)
+    ds.mass.fill_(7.0)
+    ctx = ds.ctx_lens.clone()
+    k, v, q = rows(ds)
+    for bad in ((k.half(), v, q), (k, v.float(), q), (k[:2], v, q), (k, v, q.half()), (k, v, q, torch.zeros(9, 64).double())):
+        with pytest.raises(ValueError):
+            ds.append(*bad)
+
+    def refuse(*a, **kw):
+        raise ssa.SsaError("ssa_cache_append", 2)
+    monkeypatch.setattr(ssa, "cache_append", refuse)
+    with pytest.raises(ssa.SsaError):
+        ds.append(k, v, q)
+    assert torch.equal(ds.ctx_lens, ctx) and (ds.mass == 7).all()
+
+
+def test_full_contexts_stay_as_they_are(made):               # noqa: F811
+    """The library is told of their token (it flags it), but not to store one."""
+    ds = small(kv_copies=2)
+    T = ds.wl.max_ctx
+    ds.ctx_lens.copy_(torch.tensor([T, T - 1, 5]))
+    ds.mass.fill_(7.0)
+    k, v, q = rows(ds)
+    for want, stored in (([T, T, 6], [0, 1, 1]), ([T, T, 7], [0, 0, 1])):
+        made.clear()
+        before = ds.ctx_lens.clone()
+        ds.append(k, v, q)
+        calls = [a for n, a in made if n == "cache_append"]
+        assert len(calls) == 2 and ds.ctx_lens.tolist() == want
+        for a in calls:
+            assert torch.equal(a["ctx_lens"], before + 1) and a["append"].q_lens == ds._new_lens.data_ptr()
+        assert ds._new_lens.tolist() == stored
+    assert (ds.mass[0] == 7).all() and ds.mass[1, T - 1] == 0 and (ds.mass[1, : T - 1] == 7).all()
+    assert not ds.mass[2, 5:7].any() and (ds.mass[2, :5] == 7).all() and (ds.mass[2, 7:] == 7).all()
