@@ -595,9 +595,9 @@ int32_t ssa_cache_compact(const ssa_attn_desc* desc, const ssa_paging* paging, v
  * below the largest are off by an absolute 2^-38 of it, in tiles of many rows
  * 2^-31.  Above 768 rows per K/V head (tokens x grouped heads), 256 of a paged
  * cache (pages of eight rows and more), the part of the cache that the tokens see is
- * converted to bf16 once, exactly, in the workspace; weights are then bf16 as over a
- * bf16 cache.  The size has room for that; a call given less converts it in every
- * block of 128 rows, if the rest fits, and refuses otherwise.  A scale that is NaN
+ * converted to fp16 once, exactly, in the workspace.  The size has room for that; a
+ * call given less converts it in every block of 128 rows, if the rest fits, and
+ * refuses otherwise: the results are the same.  A scale that is NaN
  * makes its 16 values NaN.
  */
 size_t ssa_attn_window_fp4_workspace_bytes(const ssa_attn_desc* desc, const ssa_window* window);

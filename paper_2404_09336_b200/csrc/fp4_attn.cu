@@ -3,10 +3,10 @@
 
 namespace ssa {
 
-// ---- the seen part of a 4-bit cache in bf16 ---------------------------------------------------------------------------------
+// ---- the seen part of a 4-bit cache in fp16 ---------------------------------------------------------------------------------
 // Every block of 128 query rows that works on tiles converts the K and V rows that it sees.  Where many share them (prompt chunks)
-// they are converted once instead, into pages of the workspace that the tiles of a bf16 cache then read: products of a code and a
-// scale have six significant bits, so that nothing is rounded.  HBM bounds it: 2.56 bytes a value.  8 requests' chunks of up to 509
+// they are converted once instead, into pages of the workspace that the tiles then read: products of a code and a scale have six
+// significant bits and are multiples of 2^-10 up to 2688, so that nothing is rounded, and outputs are those of tiles that convert.  HBM bounds it: 2.56 bytes a value.  8 requests' chunks of up to 509
 // tokens within a window of 4096, 8 K/V heads: some 36 us (5.4 TB/s), and 166 for the tiles; 49 with 16 bytes of codes to a thread,
 // whose stores then lie 64 bytes apart.
 constexpr int kExpandThreads = 256;
@@ -58,26 +58,47 @@ fp4_expand_kernel(const Fp4Params p, const Fp4Expanded x) {
     if (!is_seen(j0 + r)) continue;                          // (may hold anything: the tiles do not use it)
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
-      const float by = e4m3x2_to_float2(scale[z][y]).x;
+      const uint32_t by = __byte_perm(e4m3x2_to_half2(scale[z][y]), 0, 0x1010);
       uint32_t h[4];
       e2m1x8_to_half2(w[z][y], h);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 f = unpack2<__half>(h[e]);
-        h[e] = pack2<__nv_bfloat16>(f.x * by, f.y * by);
-      }
+      for (int e = 0; e < 4; ++e) h[e] = half2_mul(h[e], by);
       *reinterpret_cast<uint4*>((z ? x.v : x.k) + ((int64_t)hkv * x.head_rows + to_row + r) * D + c * 8) = make_uint4(h[0], h[1], h[2], h[3]);
     }
   }
 }
 
-int32_t launch_expand(const Fp4Params& p, const Fp4Expanded& x, int D, cudaStream_t st) {
+template <int D>
+static int32_t launch_expanded(const Fp4Params& p, const Fp4Expanded& x, cudaStream_t st) {
+  const int page = 1 << x.page_shift;
+  const int64_t head = x.head_rows * D;
+  CUtensorMap maps[2];
+  if (!tile_map(&maps[0], x.k, SSA_F16, D, x.head_rows, D, p.H_kv, head, 1, 0, page) ||
+      !tile_map(&maps[1], x.v, SSA_F16, D, x.head_rows, D, p.H_kv, head, 1, 0, page))
+    return SSA_ERR_CUDA;
   const dim3 grid((unsigned)x.most_tiles, (unsigned)p.H_kv, (unsigned)p.B);
-  auto kernel = p.page_table ? (D == 128 ? fp4_expand_kernel<128, true> : fp4_expand_kernel<64, true>)
-                             : (D == 128 ? fp4_expand_kernel<128, false> : fp4_expand_kernel<64, false>);
-  if (launch_pdl(kernel, grid, dim3(kExpandThreads), st, p, x) != cudaSuccess) return SSA_ERR_CUDA;
+  if (launch_pdl(p.page_table ? fp4_expand_kernel<D, true> : fp4_expand_kernel<D, false>, grid, dim3(kExpandThreads), st, p, x) != cudaSuccess)
+    return SSA_ERR_CUDA;
+  note_launches(1);
+  WindowParams t = p;
+  t.k = x.k; t.v = x.v;
+  t.page_table = x.table; t.page_table_stride = x.table_stride; t.page_shift = x.page_shift;
+  t.n_pages = (int)(x.head_rows >> x.page_shift);
+  t.k_sb = t.v_sb = 0; t.k_sh = t.v_sh = head; t.k_st = t.v_st = D;
+  cudaEvent_t begin, end;
+  take_kernel_events(&begin, &end);
+  if (begin) cudaEventRecord(begin, st);
+  if (launch_tiles<Fp4AsHalf, D>(t, maps[0], maps[1], page, st) != cudaSuccess) return SSA_ERR_CUDA;
+  if (end) cudaEventRecord(end, st);
+  note_launches(1);
+  if (p.n_splits == 1) return SSA_OK;
+  if (launch_join<__nv_bfloat16, D>(t, st) != cudaSuccess) return SSA_ERR_CUDA;
   note_launches(1);
   return SSA_OK;
+}
+
+int32_t launch_expanded(const Fp4Params& p, const Fp4Expanded& x, int D, cudaStream_t st) {
+  return D == 128 ? launch_expanded<128>(p, x, st) : launch_expanded<64>(p, x, st);
 }
 
 template <int D>

@@ -124,6 +124,11 @@ struct Fp4E2M1 { uint8_t bits; };
 template <> struct Storage<Fp4E2M1> { using Query = __nv_bfloat16; };
 template <typename T> constexpr bool kIsFp4 = false;
 template <> constexpr bool kIsFp4<Fp4E2M1> = true;
+// The values of such a cache as fp16 ones (exactly), whose queries are bf16 all the same.
+struct Fp4AsHalf { __half x; };
+template <> struct Storage<Fp4AsHalf> { using Query = __nv_bfloat16; };
+template <typename T> constexpr bool kIsFp4AsHalf = false;
+template <> constexpr bool kIsFp4AsHalf<Fp4AsHalf> = true;
 template <typename T> constexpr bool kIsNarrow = kIsFp8<T> || kIsFp4<T>;     // values that are converted to fp16 where they are used
 constexpr int kScaleDims = 16;         // dimensions of a scale
 

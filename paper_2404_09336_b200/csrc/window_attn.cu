@@ -157,7 +157,7 @@ static bool plan_window(const ssa_attn_desc* d, const ssa_window* w, bool mass, 
   return row_tiles * pl->n_splits <= 0x7fffffffll;
 }
 
-// Where the rows of a 4-bit cache that the tokens see have places in bf16; bytes of all of it, 0 where the call has no use for that.
+// Where the rows of a 4-bit cache that the tokens see have places in fp16; bytes of all of it, 0 where the call has no use for that.
 // Few blocks of 128 rows convert what they see themselves.
 static size_t plan_expanded(const ssa_attn_desc* d, const ssa_window* w, Fp4Expanded* x) {
   const long long rows = (long long)(d->H / d->H_kv) * w->n_q;
@@ -257,36 +257,21 @@ static int32_t run_window(const ssa_attn_desc* d, const ssa_window* w, const voi
   p.n_splits = pl.n_splits; p.s_pitch = pl.s_pitch;
   p.decay = decay;
   cudaStream_t st = (cudaStream_t)stream;
-  Fp4Expanded x;
-  if (const size_t more = fp4 && tiles ? plan_expanded(d, w, &x) : 0; more && ws_bytes >= window_bytes(d, w, mass, fp4) + more) {
-    // the rows that are seen in bf16, behind the partial results, and the tiles of a cache of such rows in pages
-    char* to = static_cast<char*>(ws) + window_bytes(d, w, mass, fp4);
-    x.table = reinterpret_cast<int32_t*>(to);
-    to += up256((size_t)d->B * x.table_stride * sizeof(int32_t));
-    x.k = reinterpret_cast<__nv_bfloat16*>(to);
-    x.v = reinterpret_cast<__nv_bfloat16*>(to + up256((size_t)x.head_rows * d->H_kv * d->D * 2));
-    const int page = 1 << x.page_shift;
-    const int64_t head = x.head_rows * d->D;
-    if (tile_map(&maps[0], x.k, SSA_BF16, d->D, x.head_rows, d->D, d->H_kv, head, 1, 0, page) &&
-        tile_map(&maps[1], x.v, SSA_BF16, d->D, x.head_rows, d->D, d->H_kv, head, 1, 0, page)) {
-      Fp4Params f;
-      static_cast<WindowParams&>(f) = p;
-      f.k_scales = static_cast<const uint8_t*>(k_scales);
-      f.v_scales = static_cast<const uint8_t*>(v_scales);
-      const int32_t rc = launch_expand(f, x, d->D, st);
-      if (rc != SSA_OK) return rc;
-      p.k = x.k; p.v = x.v;
-      p.page_table = x.table; p.page_table_stride = x.table_stride; p.page_shift = x.page_shift;
-      p.n_pages = (int)(x.head_rows >> x.page_shift);
-      p.k_sb = p.v_sb = 0; p.k_sh = p.v_sh = head; p.k_st = p.v_st = d->D;
-      return d->D == 128 ? launch_window<__nv_bfloat16, 128>(p, false, maps, page, st) : launch_window<__nv_bfloat16, 64>(p, false, maps, page, st);
-    }
-  }
   if (fp4) {
     Fp4Params f;
     static_cast<WindowParams&>(f) = p;
     f.k_scales = static_cast<const uint8_t*>(k_scales);
     f.v_scales = static_cast<const uint8_t*>(v_scales);
+    Fp4Expanded x;
+    if (const size_t more = tiles ? plan_expanded(d, w, &x) : 0; more && ws_bytes >= window_bytes(d, w, mass, fp4) + more) {
+      // the rows that are seen in fp16, behind the partial results, and the tiles of a cache of such rows in pages
+      char* to = static_cast<char*>(ws) + window_bytes(d, w, mass, fp4);
+      x.table = reinterpret_cast<int32_t*>(to);
+      to += up256((size_t)d->B * x.table_stride * sizeof(int32_t));
+      x.k = reinterpret_cast<__half*>(to);
+      x.v = reinterpret_cast<__half*>(to + up256((size_t)x.head_rows * d->H_kv * d->D * 2));
+      return launch_expanded(f, x, d->D, st);
+    }
     return launch_window_fp4(f, d->D, tiles ? box_rows : 0, st);
   }
   const CUtensorMap* m = tiles ? maps : nullptr;

@@ -837,14 +837,15 @@ inline long long rows_splits(long long n_tiles, long long blocks, int rows, bool
   return splits;
 }
 inline size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-// The seen part of a 4-bit cache as pages of a bf16 one, in the workspace.
+// The seen part of a 4-bit cache as pages of an fp16 one, in the workspace.
 struct Fp4Expanded {
-  __nv_bfloat16 *k, *v;          // [H_kv][head_rows][D]
+  __half *k, *v;                 // [H_kv][head_rows][D]
   int32_t* table;                // [B][table_stride]
   int64_t head_rows;             // B most_tiles 128
   int most_tiles, table_stride, page_shift;
 };
-int32_t launch_expand(const Fp4Params& p, const Fp4Expanded& x, int D, cudaStream_t st);   // (defined in fp4_attn.cu)
+// Converts it, and attends to it (defined in fp4_attn.cu).
+int32_t launch_expanded(const Fp4Params& p, const Fp4Expanded& x, int D, cudaStream_t st);
 // (defined in fp4_attn.cu; box_rows: rows side by side for certain, for the tiles of 128 rows; 0: the kernel for few rows)
 int32_t launch_window_fp4(const Fp4Params& p, int D, int box_rows, cudaStream_t st);
 

@@ -26,7 +26,8 @@
 // 4-bit values become fp16 on their way into shared memory (exactly: six significant bits), by warps 5 to 7: codes arrive by
 // asynchronous copies, a K or V tile ahead, each thread converts the pieces that it asked for, scales them and writes them where a
 // TMA copy with its swizzle would have put them, zeros for what no token sees.  Query rows become fp16 times a power of two of their
-// own (rows_to_half), weights are fp16.
+// own (rows_to_half), weights are fp16.  Where a call has converted the values before (fp4_attn.cu) they arrive as fp16, by TMA, and all
+// else is the same.
 #pragma once
 #include <cuda.h>
 
@@ -39,6 +40,7 @@ namespace ssa {
 constexpr int kTileRows = 128, kTileKeys = 128;
 constexpr int kTileThreads = 256;
 // registers of a thread; 128 x 200 + 128 x 56 (4-bit: 184, 72) = 256 x 128, what the launch has
+template <typename T> constexpr bool kHalfQueries = kIsFp4<T> || kIsFp4AsHalf<T>;    // bf16 ones, brought to fp16
 template <typename T> constexpr int kSoftmaxRegs = kIsFp4<T> ? 184 : 200;
 template <typename T> constexpr int kOtherRegs = kIsFp4<T> ? 72 : 56;
 constexpr int kConverters = 96;                     // threads of warps 5 to 7
@@ -163,6 +165,7 @@ __device__ __noinline__ void careful_row(const Params& p, const Seen& seen, int2
                                          float& l, float (&acc)[D / 32]) {
   constexpr int kN = D / 32;
   using TQ = typename Storage<T>::Query;
+  using TV = std::conditional_t<kIsFp4AsHalf<T>, __half, T>;
   const int lane = threadIdx.x % 32, hkv = h / p.group;
   const TQ* q = reinterpret_cast<const TQ*>(p.q) + (int64_t)b * p.q_sb + (int64_t)h * p.q_sh + (int64_t)t * p.q_st + lane * kN;
   const int64_t k0 = (kPaged ? 0 : (int64_t)b * p.k_sb) + (int64_t)hkv * p.k_sh + lane * kN;
@@ -180,7 +183,7 @@ __device__ __noinline__ void careful_row(const Params& p, const Seen& seen, int2
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < kN; ++i) f[i] = to_float(static_cast<const T*>(cache)[o + i]);
+      for (int i = 0; i < kN; ++i) f[i] = to_float(static_cast<const TV*>(cache)[o + i]);
     }
   };
   const uint8_t *k_scales = nullptr, *v_scales = nullptr;
@@ -224,14 +227,14 @@ window_tile_kernel(const Params p, const __grid_constant__ CUtensorMap k_map, co
                    const int box_rows) {
   using Shape = TileShape<T, D>;
   using TQ = typename Storage<T>::Query;
-  using TM = std::conditional_t<kIsFp4<T>, __half, T>;                 // of the contractions
+  using TM = std::conditional_t<kHalfQueries<T>, __half, T>;                 // of the contractions
   constexpr int kStages = Shape::kStages;
   constexpr float kShift = std::is_same<TM, __half>::value ? 6.f : 0.f;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t s_bar[3 * kStages + 4];
   __shared__ uint32_t s_tmem;
   __shared__ int64_t s_row[2][kTileRows];                              // where a row starts in q and in out
-  __shared__ float s_unit[kIsFp4<T> ? kTileRows : 1];                  // 4-bit: what a row's scores are to be multiplied with
+  __shared__ float s_unit[kHalfQueries<T> ? kTileRows : 1];            // 4-bit: what a row's scores are to be multiplied with
   __shared__ int s_dead, s_asked;                                      // the block has given up; copies asked for
   const uint32_t base = (smem_at(smem_raw) + 1023) & ~1023u;
   uint8_t* const smem = smem_raw + (base - smem_at(smem_raw));
@@ -417,7 +420,7 @@ window_tile_kernel(const Params p, const __grid_constant__ CUtensorMap k_map, co
       w[y] = make_uint4(0, 0, 0, 0);
       if (r < rows) w[y] = *reinterpret_cast<const uint4*>(reinterpret_cast<const TQ*>(p.q) + s_row[0][r] + i * 8);
     }
-    if constexpr (kIsFp4<T>) {
+    if constexpr (kHalfQueries<T>) {
 #pragma unroll
       for (int y = 0; y < 32 / kAtOnce; ++y) {
         uint32_t x[4] = {w[y].x, w[y].y, w[y].z, w[y].w};
@@ -534,7 +537,7 @@ window_tile_kernel(const Params p, const __grid_constant__ CUtensorMap k_map, co
     const int window_lo = p.window == 0 ? 0 : pos - p.window + 1;
     const int32_t* table = kPaged ? p.page_table + (int64_t)b * p.page_table_stride : nullptr;
     float m = neg_inf(), l = 0.f, unit = p.scale_log2;
-    if constexpr (kIsFp4<T>) unit = s_unit[threadIdx.x];
+    if constexpr (kHalfQueries<T>) unit = s_unit[threadIdx.x];
     int n = 0;                                               // tiles so far
     for (int it = range.x; it < range.y; ++it) {
       const int j0 = seen.position(it);
@@ -753,8 +756,9 @@ inline bool tile_map(CUtensorMap* map, const void* base, int32_t dtype, int D, i
 template <typename T, int D, typename Params>
 static cudaError_t launch_tiles(const Params& p, const CUtensorMap& k_map, const CUtensorMap& v_map, int box_rows, cudaStream_t st) {
   const dim3 grid((unsigned)((p.group * p.n_q + kTileRows - 1) / kTileRows * p.n_splits), (unsigned)p.H_kv, (unsigned)p.B);
-  auto kernel = p.page_table ? (p.out_f32 ? window_tile_kernel<T, D, true, true, Params> : window_tile_kernel<T, D, true, false, Params>)
-                             : (p.out_f32 ? window_tile_kernel<T, D, false, true, Params> : window_tile_kernel<T, D, false, false, Params>);
+  auto kernel = p.out_f32 ? window_tile_kernel<T, D, true, true, Params> : window_tile_kernel<T, D, true, false, Params>;
+  if constexpr (!kIsFp4AsHalf<T>)                            // (those are in pages)
+    if (!p.page_table) kernel = p.out_f32 ? window_tile_kernel<T, D, false, true, Params> : window_tile_kernel<T, D, false, false, Params>;
   constexpr int kSmem = TileShape<T, D>::kSmem;
   const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (err != cudaSuccess) return err;
