@@ -21,3 +21,49 @@ def test_bits_do_not_depend_on_the_workspace(D, page, out_dtype):
         got = [p.call(ctx, new, window, sinks, out_dtype, less=less) for less in (0, 1)]
         assert np.array_equal(got[0][0], got[1][0]) and np.array_equal(got[0][1], got[1][1]) and got[0][3] == got[1][3] == 0
         check_tokens(p, got[0], ctx, new, window, sinks, out_dtype, tiles=True)
+
+
+@pytest.mark.parametrize("page,n_q", [(0, 400), (16, 150)])
+@pytest.mark.parametrize("out_dtype", [BF16, F32])
+def test_nan_scales_through_the_conversion(page, n_q, out_dtype):
+    """More than 768 rows a K/V head, 256 in pages: a NaN scale reaches the tokens that see its row, nothing else."""
+    T = n_q + 100
+    p = Fp4Tokens(1, 4, 2, T, 64, n_q, page=page)
+    ctx, first = T - 10, T - 10 - n_q                        # of positions first ... ctx - 1
+    assert 2 * n_q > (256 if page else 768)
+    row = (lambda j: (int(p.cache.table[0, j // page]), j % page)) if page else None
+
+    def put(name, j, scale, h=slice(None), part=slice(None)):
+        x = p.cache.parts[name]
+        if page:
+            x[row(j)[0], row(j)[1], h, part] = scale
+        else:
+            x[0, h, j, part] = scale
+
+    want = p.call([ctx], None, window=60, out_dtype=out_dtype)
+    for j in (first - 65, ctx, T - 1):                       # before every window; behind the context
+        for name in ("k_scales", "v_scales"):
+            put(name, j, 0xff)
+    got = p.call([ctx], None, window=60, out_dtype=out_dtype)
+    assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
+    put("v_scales", first + 50, 0x7f, 1, 3)                  # tokens 50 ... 109 see it
+    got = p.call([ctx], None, window=60, out_dtype=out_dtype)[0]
+    assert np.isnan(got[0, 2:, 50:110, 48:]).all() and np.isfinite(got[0, 2:, 50:110, :48]).all()
+    assert np.isfinite(got[0, 2:, :50]).all() and np.isfinite(got[0, 2:, 110:]).all() and np.array_equal(got[0, :2], want[0][0, :2])
+    put("k_scales", first + 20, 0x7f, 0, 1)                  # scores of tokens 20 ... 79 of the other head
+    got, lse = p.call([ctx], None, window=60, out_dtype=out_dtype)[:2]
+    assert np.isnan(got[0, :2, 20:80]).all() and np.isnan(lse[0, :2, 20:80]).all()
+    assert np.isfinite(got[0, :2, :20]).all() and np.isfinite(got[0, :2, 80:]).all() and np.isfinite(lse[0, :2, 80:]).all()
+
+
+@pytest.mark.parametrize("page", [0, 16])
+def test_scales_of_every_size_through_the_conversion(page):
+    """One position a token sees: its row of V, every code and scale, times a weight of 22 bits over one of 24."""
+    n_q = 400 if not page else 150
+    p = Fp4Tokens(1, 2, 1, n_q, 64, n_q, page=page)
+    scales = (torch.arange(n_q * 4) * 37 % 256).to(torch.uint8).view(1, 1, n_q, 4)
+    scales[(scales & 127) == 127] = 3
+    p.cache.put("v_scales", scales)
+    out = p.call([n_q], None, window=1)[0]
+    v = p.cache.values("v")
+    assert (np.abs(out[0] - v[0]) <= 2.0 ** -21 * np.abs(v[0])).all()
