@@ -77,6 +77,7 @@ class Blocks(C.Structure):
 
 class Append(C.Structure):
     """ssa_append (see include/ssa.h)."""
+    made_for, strides = None, ()                             # (requests, heads, query heads, D) that make_append was given
     _fields_ = [("n_q", C.c_int32), ("rotary_dims", C.c_int32), ("interleaved", C.c_int32), ("n_positions", C.c_int32),
                 ("k_factor", C.c_float), ("v_factor", C.c_float), ("q_stride_t", C.c_int64),
                 *((f"{n}_stride_{d}", C.c_int64) for n in ("qo", "kn", "vn") for d in "bht"),
@@ -649,11 +650,14 @@ def attn_blocks(desc, blocks, q, k_cache, v_cache, ctx_lens, index, counts, out,
 def make_append(k_new, v_new, q=None, q_out=None, cos_sin=None, interleaved: bool = False, positions=None, q_lens=None,
                 paging: Paging | None = None, k_factor: float = 1.0, v_factor: float = 1.0) -> Append:
     """ssa_append for k_new, v_new [B,H_kv,n_q,D], q and q_out [B,H,n_q,D] (any strides), cos_sin[positions, rotary dimensions]
-    (fp32: cosines, then sines) and positions[B,n_q] (int32).  cos_sin, positions and q_lens must stay alive."""
+    (fp32: cosines, then sines) and positions[B,n_q] (int32).  cos_sin, positions and q_lens must stay alive.  cache_append takes it
+    with rows of these shapes and strides."""
     B, _, n_q, D = k_new.shape
     for x in (k_new, v_new, q, q_out):
         if x is not None and (x.shape[0] != B or x.shape[2] != n_q or x.shape[3] != D or x.stride(3) != 1 or x.dtype != k_new.dtype):
             raise ValueError("new rows are [B, heads, n_q, D] of one type, the head dimension contiguous")
+    if v_new.shape[1] != k_new.shape[1] or (q is None) != (q_out is None) or (q is not None and q_out.shape[1] != q.shape[1]):
+        raise ValueError("keys and values are of as many heads, and so are queries and their places")
     _check_lens(q_lens, B, k_new.device)
     a = Append()
     a.n_q, a.interleaved, a.k_factor, a.v_factor = int(n_q), int(bool(interleaved)), float(k_factor), float(v_factor)
@@ -672,13 +676,32 @@ def make_append(k_new, v_new, q=None, q_out=None, cos_sin=None, interleaved: boo
     a.q_lens = None if q_lens is None else q_lens.data_ptr()
     if paging is not None:
         a.paging = C.pointer(paging)
+    a.made_for = B, int(k_new.shape[1]), None if q is None else int(q.shape[1]), D
+    a.strides = tuple(x is not None and x.stride() for x in (k_new, v_new, q, q_out))
     return a
+
+
+def _check_append(desc, append, new):
+    """That the rows (keys, values, queries, their places) are those that make_append was given, and those that the descriptor counts."""
+    if append.made_for is None:                              # (a structure that the caller has filled)
+        return
+    B, H_kv, H, D = append.made_for
+    if B < desc.B or H_kv != desc.H_kv or D != desc.D or (new[2] is not None and H != desc.H):
+        raise ValueError(f"rows of {B} requests, {H_kv} heads and {H} query heads of {D} for {desc.B}, {desc.H_kv}, {desc.H} and {desc.D}")
+    for x, of, heads in zip(new, append.strides, (H_kv, H_kv, H, H)):    # (of one token, its dimension may be left out; what has one
+        if x is not None and (of is False or x.shape[1] != heads or       # element in a dimension may have any stride there)
+                              any(n > 1 and y != z for n, y, z in zip((B, heads, append.n_q), x.stride()[: x.dim() - 1], of))):
+            raise ValueError("rows of other strides than make_append was given")
 
 
 def cache_append(desc, append, k_new, v_new, ctx_lens, k_cache, v_cache, q=None, q_out=None, k_scales=None, v_scales=None,
                  dev_status=None, stream=None, check=True):
     """ssa_cache_append: the step's keys and values into the cache, rotated by position, and its queries rotated into q_out."""
     _check_type(desc, k_new)
+    # (almost always the very strides and numbers that make_append has seen: looked at one by one only where not)
+    if append.made_for != (desc.B, desc.H_kv, desc.H, desc.D) or append.strides != (
+            k_new.stride(), v_new.stride(), q is not None and q.stride(), q is not None and q_out.stride()):
+        _check_append(desc, append, (k_new, v_new, q, q_out))
     rc = _call.cache_append(desc, append, k_new, v_new, ctx_lens, k_cache, v_cache, q, q_out, k_scales, v_scales, dev_status,
                             _stream(stream))
     return _check("ssa_cache_append", rc, check)

@@ -1,0 +1,54 @@
+"""What the calls that fill a cache and read its blocks refuse of tensors that do not go with their structures (no GPU)."""
+import pytest
+import torch
+
+from paper_2404_09336_b200 import ssa
+
+
+def rows(B=2, heads=2, n_q=3, D=128):
+    return torch.zeros(B, heads, n_q, D, dtype=torch.bfloat16)
+
+
+def cache(B=2, H_kv=2, T=64, D=128):
+    return torch.zeros(B, H_kv, T, D, dtype=torch.bfloat16)
+
+
+def refuses(desc, a, k, v, q=None, q_out=None):
+    with pytest.raises(ValueError, match="rows of"):
+        ssa.cache_append(desc, a, k, v, None, None, None, q, q_out, stream=0)
+
+
+def test_rows_of_other_head_counts():
+    k, q = rows(), rows(heads=8)
+    for bad in (dict(v_new=rows(heads=1)), dict(v_new=rows(heads=8)), dict(q=q, q_out=rows(heads=4)), dict(q=q), dict(q_out=q)):
+        with pytest.raises(ValueError, match="heads"):
+            ssa.make_append(**{**dict(k_new=k, v_new=k), **bad})
+
+
+def test_rows_that_the_descriptor_does_not_count():
+    q = rows(heads=8)
+    desc = ssa.make_desc(q[:, :, 0], cache(), cache(), q[:, :, 0])
+    good = ssa.make_append(rows(), rows(), q, q)
+    with pytest.raises(ssa.SsaError):                        # (refused by the library: there are no lengths)
+        ssa.cache_append(desc, good, rows(), rows(), None, None, None, q, q, stream=0)
+    for k, x in ((rows(heads=1), q), (rows(heads=4), q), (rows(D=64), rows(heads=8, D=64)), (rows(), rows(heads=4)), (rows(B=1), rows(B=1, heads=8))):
+        refuses(desc, ssa.make_append(k, k, x, x), k, k, x, x)
+    k = rows(heads=1)
+    refuses(desc, ssa.make_append(k, k), k, k)
+    # (queries that are not rotated need not be the descriptor's)
+    with pytest.raises(ssa.SsaError):
+        ssa.cache_append(desc, ssa.make_append(rows(), rows()), rows(), rows(), None, None, None, stream=0)
+
+
+def test_rows_of_other_strides_than_the_structure_has():
+    q, apart = rows(heads=8), rows().transpose(1, 2).contiguous().transpose(1, 2)
+    desc = ssa.make_desc(q[:, :, 0], cache(), cache(), q[:, :, 0])
+    good = ssa.make_append(rows(), rows(), q, q)
+    refuses(desc, good, apart, rows(), q, q)
+    refuses(desc, good, rows(), apart, q, q)
+    refuses(desc, good, rows(), rows(), q, rows(heads=4))
+    refuses(desc, ssa.make_append(rows(), rows()), rows(), rows(), q, q)
+    one = ssa.make_desc(q[:1, :, 0], cache(1, 1), cache(1, 1), q[:1, :, 0])
+    k = rows(1, 1)
+    with pytest.raises(ssa.SsaError):                        # one request, one head: strides between them do not matter
+        ssa.cache_append(one, ssa.make_append(k, k), k.as_strided(k.shape, (7, 5, 128, 1)), k, None, None, None, stream=0)
