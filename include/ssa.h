@@ -697,7 +697,8 @@ int32_t ssa_block_select(const ssa_attn_desc* desc, const ssa_blocks* blocks, co
  * absolute 2^-38 of it), over a 4-bit cache with BF16 outputs as one fp16 part;
  * scores and sums are fp32.
  * Errors: those of ssa_attn_window, SSA_ERR_CAPACITY (budget <= 0, or a list of
- * 2^31 positions and more) and SSA_ERR_UNSUPPORTED (block_size).
+ * 2^31 positions and more) and SSA_ERR_UNSUPPORTED (block_size; an o_stride_t of
+ * zero between several tokens).
  */
 size_t ssa_attn_blocks_workspace_bytes(const ssa_attn_desc* desc, const ssa_blocks* blocks);
 int32_t ssa_attn_blocks(const ssa_attn_desc* desc, const ssa_blocks* blocks, const void* q, const void* k_cache,

@@ -89,6 +89,7 @@ int32_t ssa_attn_blocks(const ssa_attn_desc* desc, const ssa_blocks* blocks, con
     return SSA_ERR_ALIGN;
   BlocksPlan pl;
   if (!plan_blocks(desc, blocks, &pl)) return SSA_ERR_SHAPE;
+  if (blocks->n_q > 1 && blocks->o_stride_t == 0) return SSA_ERR_UNSUPPORTED;      // (tokens would share a row of out)
   if (!workspace || workspace_bytes < pl.total_bytes) return SSA_ERR_WORKSPACE;
   ListParams p = {};
   fill_params(p, desc, blocks->n_q, blocks->q_stride_t, blocks->o_stride_t, blocks->q_lens, blocks->paging, q, k_cache, v_cache,

@@ -596,6 +596,15 @@ def _check_bounds(desc, blocks, bounds):
     B, H_kv, n, _, D = bounds.size()
     if B < desc.B or H_kv < desc.H_kv or n * blocks.block_size < desc.max_ctx or D != desc.D:
         raise ValueError(f"bounds have room for {desc.B} requests, {desc.H_kv} heads and the blocks of {desc.max_ctx} positions")
+    of_b, of_h = bounds.stride()[:2]
+    if (of_b != blocks.bounds_stride_b and desc.B > 1) or (of_h != blocks.bounds_stride_h and desc.H_kv > 1):
+        raise ValueError("bounds of other strides than make_blocks was given")
+
+
+def _check_tokens(blocks, x, of_t):
+    """x[B,H,n_q,D] (of one token [B,H,D] too) has its tokens as far apart as make_blocks was told."""
+    if blocks.n_q > 1 and x is not None and (x.dim() != 4 or x.stride(2) != of_t):
+        raise ValueError("q and out of other strides than make_blocks was given")
 
 
 _INT32, _FLOAT32 = torch.int32, torch.float32
@@ -624,6 +633,7 @@ def block_select(desc, blocks, q, bounds, ctx_lens, index, counts, scores=None, 
     _check_bounds(desc, blocks, bounds)
     _check_type(desc, bounds)
     _check_type(desc, q)
+    _check_tokens(blocks, q, blocks.q_stride_t)
     rows = _check_lists(desc, blocks, index, counts)
     if scores is not None:
         n = -(-desc.max_ctx // max(1, blocks.block_size))
@@ -642,6 +652,8 @@ def attn_blocks(desc, blocks, q, k_cache, v_cache, ctx_lens, index, counts, out,
     """ssa_attn_blocks: every token over the blocks of its list; out (and lse[B,H,n_q]) are written."""
     _check_lists(desc, blocks, index, counts)
     _check_type(desc, q)
+    _check_tokens(blocks, q, blocks.q_stride_t)
+    _check_tokens(blocks, out, blocks.o_stride_t)
     rc = _call.attn_blocks(desc, blocks, q, k_cache, v_cache, k_scales, v_scales, ctx_lens, index, counts, out, lse, workspace,
                            dev_status, _stream(stream))
     return _check("ssa_attn_blocks", rc, check)

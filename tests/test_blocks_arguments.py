@@ -52,3 +52,38 @@ def test_rows_of_other_strides_than_the_structure_has():
     k = rows(1, 1)
     with pytest.raises(ssa.SsaError):                        # one request, one head: strides between them do not matter
         ssa.cache_append(one, ssa.make_append(k, k), k.as_strided(k.shape, (7, 5, 128, 1)), k, None, None, None, stream=0)
+
+
+def chosen(n_q=3):
+    q, b = rows(heads=8, n_q=n_q), torch.zeros(2, 2, 2, 2, 128, dtype=torch.bfloat16)
+    desc = ssa.make_desc(q[:, :, 0], cache(), cache(), q[:, :, 0])
+    return q, b, desc, torch.zeros(2, 2, n_q, 4, dtype=torch.int32), torch.zeros(2, 2, n_q, dtype=torch.int32)
+
+
+def test_blocks_made_without_the_tensors_that_a_call_takes():
+    q, b, desc, index, counts = chosen()
+    with pytest.raises(ValueError, match="bounds of other strides"):
+        ssa.block_select(desc, ssa.make_blocks(3, 32, 4, q=q), q, b, None, index, counts, stream=0)
+    with pytest.raises(ValueError, match="bounds of other strides"):
+        ssa.block_bounds(desc, ssa.make_blocks(3, 32, 4, bounds=torch.zeros(2, 3, 2, 2, 128).bfloat16()[:, :2]), None, None, b, stream=0)
+    for k, x, out in ((ssa.make_blocks(3, 32, 4, bounds=b), q, q), (ssa.make_blocks(3, 32, 4, q=q, bounds=b), q[:, :, 0], q)):
+        with pytest.raises(ValueError, match="q and out"):
+            ssa.block_select(desc, k, x, b, None, index, counts, stream=0)
+    apart = q.transpose(1, 2).contiguous().transpose(1, 2)
+    for k, x, out in ((ssa.make_blocks(3, 32, 4), q, q), (ssa.make_blocks(3, 32, 4, q=q), q, q), (ssa.make_blocks(3, 32, 4, q=q, out=q), q, apart),
+                      (ssa.make_blocks(3, 32, 4, q=q, out=q), apart, q)):
+        with pytest.raises(ValueError, match="q and out"):
+            ssa.attn_blocks(desc, k, x, None, None, None, index, counts, out, stream=0)
+    # one token: as the runner calls them
+    q, b, desc, index, counts = chosen(1)
+    for f in (lambda: ssa.block_select(desc, ssa.make_blocks(1, 32, 4, bounds=b), q[:, :, 0], b, None, index, counts, stream=0),
+              lambda: ssa.attn_blocks(desc, ssa.make_blocks(1, 32, 4), q[:, :, 0], None, None, None, index, counts, q[:, :, 0], stream=0)):
+        with pytest.raises(ssa.SsaError):
+            f()
+
+
+def test_tokens_that_share_a_row_of_out():
+    from test_blocks_abi import attend, desc, good_blocks
+    before, k = ssa.launch_count(), good_blocks()
+    k.o_stride_t = 0
+    assert attend(desc(), k) == ssa.ERR_UNSUPPORTED and ssa.launch_count() == before
