@@ -668,9 +668,10 @@ int32_t ssa_block_bounds(const ssa_attn_desc* desc, const ssa_blocks* blocks, co
  *   counts dev int32 [B*H_kv*n_q]: min(m, budget)
  *   scores dev float [B*H_kv*n_q, n] or NULL: entries [0, m) of the row
  * Scores are summed in 64 bits and rounded to 32 once, so that lists do not depend
- * on the order of summation; an infinite bound against queries all of the other
- * sign makes a NaN.  (Bounds of a block hold all its keys, those behind the
- * token's own position among them.)
+ * on the order of summation.  Infinite bounds count as the formula has them (zero
+ * times an infinity is zero); a block without rows, of +inf and -inf, scores -inf.
+ * (Bounds of a block hold all its keys, those behind the token's own position among
+ * them.)
  *   desc     host; the fields of k, v and out are checked but not used, but for
  *            H_kv; q and bounds (dev) have the queries' type for kv_dtype
  * Errors: SSA_ERR_NULL, SSA_ERR_SHAPE, SSA_ERR_UNSUPPORTED, SSA_ERR_DTYPE,

@@ -3,7 +3,7 @@
 //
 //   min_j, max_j   per dimension, over the keys of block j
 //   score_j = sum_h sum_d max(q_hd min_jd, q_hd max_jd) = sum_d N_d min_jd + P_d max_jd,  N_d = sum_h min(q_hd, 0), P_d likewise
-// so that the heads of a group cost no more than one.
+// so that the heads of a group cost no more than one.  (With infinite bounds too, as long as nothing times an infinity is nothing.)
 #include <algorithm>
 #include <type_traits>
 
@@ -221,7 +221,23 @@ block_select_kernel(const SelectParams p, const int ranks) {
   double weight[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) weight[e] = s_weight[lane % kLanes * 8 + e];
-  auto score = [&](int j0, const uint4 (&x)[kDeep]) {
+  // Infinite bounds of which the queries, all of the other sign, want nothing become zero.
+  auto drop = [&](uint32_t& w, double lo, double hi) {
+    constexpr uint32_t kInf = std::is_same<TQ, __half>::value ? 0x7c00u : 0x7f80u;
+    if (lo == 0 && (w & 0x7fffu) == kInf) w &= 0xffff0000u;
+    if (hi == 0 && (w & 0x7fff0000u) == kInf << 16) w &= 0xffffu;
+  };
+  bool careful = false, odd = false;
+  auto score = [&](int j0, uint4 (&x)[kDeep]) {
+    if (careful) {
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i) {
+        drop(x[i].x, weight[0], weight[1]);
+        drop(x[i].y, weight[2], weight[3]);
+        drop(x[i].z, weight[4], weight[5]);
+        drop(x[i].w, weight[6], weight[7]);
+      }
+    }
     double sum[kDeep];
 #pragma unroll
     for (int i = 0; i < kDeep; ++i) {
@@ -236,17 +252,24 @@ block_select_kernel(const SelectParams p, const int ranks) {
     const float total = (float)sums_of<kLanes>(sum, lane, which);
     const int j = place(j0, which);
     if (j < m && lane % (kLanes / kDeep) == 0) {
+      odd |= total != total;
       if (p.scores) p.scores[r * p.n_blocks + j] = total;
       if (rank == 0) s_key[j] = order_key(total);
       else store_to(&s_key[j], 0, order_key(total));
     }
   };
+again:
 #pragma unroll 1
   for (int j0 = rank * kStep; j0 < m; j0 += 2 * ranks * kStep) {
     ask(j0 + ranks * kStep, m, w[1]);
     score(j0, w[0]);
     ask(j0 + 2 * ranks * kStep, m, w[0]);
     if (j0 + ranks * kStep < m) score(j0 + ranks * kStep, w[1]);
+  }
+  if (!careful && __any_sync(~0u, odd)) {                    // a warp that met a NaN scores its blocks once more
+    careful = true;
+    ask(rank * kStep, m, w[0]);
+    goto again;
   }
   if (ranks > 1) cluster_sync();
   else __syncthreads();
