@@ -891,7 +891,7 @@ int32_t ssa_decode_attn_sparse_noalloc(const ssa_attn_desc* desc, const void* q,
  * Optional timing hook for harnesses (no counterpart in the paper): the next
  * attention call made by the calling thread records `ev_begin` immediately
  * before and `ev_end` immediately after its main (split-KV) kernel on the
- * call's stream, then forgets them.  Both are cudaEvent_t passed as void*;
+ * call's stream (and what it converts a 4-bit cache with), then forgets them.  Both are cudaEvent_t passed as void*;
  * passing NULLs clears the hook.  Has no effect on results.
  */
 void ssa_set_kernel_events(void* ev_begin, void* ev_end);

@@ -76,6 +76,9 @@ static int32_t launch_expanded(const Fp4Params& p, const Fp4Expanded& x, cudaStr
   if (!tile_map(&maps[0], x.k, SSA_F16, D, x.head_rows, D, p.H_kv, head, 1, 0, page) ||
       !tile_map(&maps[1], x.v, SSA_F16, D, x.head_rows, D, p.H_kv, head, 1, 0, page))
     return SSA_ERR_CUDA;
+  cudaEvent_t begin, end;
+  take_kernel_events(&begin, &end);
+  if (begin) cudaEventRecord(begin, st);                     // (what the tiles read is part of their time)
   const dim3 grid((unsigned)x.most_tiles, (unsigned)p.H_kv, (unsigned)p.B);
   if (launch_pdl(p.page_table ? fp4_expand_kernel<D, true> : fp4_expand_kernel<D, false>, grid, dim3(kExpandThreads), st, p, x) != cudaSuccess)
     return SSA_ERR_CUDA;
@@ -85,9 +88,6 @@ static int32_t launch_expanded(const Fp4Params& p, const Fp4Expanded& x, cudaStr
   t.page_table = x.table; t.page_table_stride = x.table_stride; t.page_shift = x.page_shift;
   t.n_pages = (int)(x.head_rows >> x.page_shift);
   t.k_sb = t.v_sb = 0; t.k_sh = t.v_sh = head; t.k_st = t.v_st = D;
-  cudaEvent_t begin, end;
-  take_kernel_events(&begin, &end);
-  if (begin) cudaEventRecord(begin, st);
   if (launch_tiles<Fp4AsHalf, D>(t, maps[0], maps[1], page, st) != cudaSuccess) return SSA_ERR_CUDA;
   if (end) cudaEventRecord(end, st);
   note_launches(1);

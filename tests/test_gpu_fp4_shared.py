@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from budget_util import DEV
 from cache_util import Fp4Tokens, check_tokens
 from paper_2404_09336_b200 import ssa
 
@@ -67,3 +68,27 @@ def test_scales_of_every_size_through_the_conversion(page):
     out = p.call([n_q], None, window=1)[0]
     v = p.cache.values("v")
     assert (np.abs(out[0] - v[0]) <= 2.0 ** -21 * np.abs(v[0])).all()
+
+
+def test_timing_events_bracket_the_conversion():
+    """Many rows that are converted for few that attend to them, nothing to join: between the events lies all of the call."""
+    B, T = 100, 2048
+    p = Fp4Tokens(B, 264, 1, T, 128, 1, page=256)
+    out, ctx = torch.zeros_like(p.q), torch.full((B,), T, dtype=torch.int32, device=DEV)
+    c, share = p.cache, []
+    desc, win = c.desc(p.q, out), ssa.make_window(p.q, out, paging=c.paging())
+    ws = torch.empty(ssa.attn_window_fp4_workspace_bytes(desc, win), dtype=torch.uint8, device=DEV)
+    for _ in range(20):
+        a, b, y, z = (torch.cuda.Event(enable_timing=True) for _ in range(4))
+        for e in (b, y):
+            e.record()                                       # (made by then)
+        torch.cuda.synchronize()
+        ssa.set_kernel_events(b, y)
+        before = ssa.launch_count()
+        a.record()
+        ssa.attn_window_fp4(desc, win, p.q, c.parts["k"], c.parts["v"], c.scales("k"), c.scales("v"), ctx, out, None, ws)
+        z.record()
+        torch.cuda.synchronize()
+        assert ssa.launch_count() - before == 2              # conversion, tiles
+        share.append(b.elapsed_time(y) / a.elapsed_time(z))
+    assert max(share) > 0.85, share                          # (the tiles alone: 0.7)
