@@ -595,9 +595,12 @@ int32_t ssa_cache_compact(const ssa_attn_desc* desc, const ssa_paging* paging, v
  * below the largest are off by an absolute 2^-38 of it, in tiles of many rows
  * 2^-31.  Above 768 rows per K/V head (tokens x grouped heads), 256 of a paged
  * cache (pages of eight rows and more), the part of the cache that the tokens see is
- * converted to fp16 once, exactly, in the workspace.  The size has room for that; a
- * call given less converts it in every block of 128 rows, if the rest fits, and
- * refuses otherwise: the results are the same.  A scale that is NaN
+ * converted to fp16 once, exactly, in the workspace: 4*D bytes for each position that
+ * the tokens of a request see and each K/V head, 512 MB at a time (requests, or heads of
+ * one, in turn).  The size has room for that; a call given less takes fewer at a time,
+ * or, where not even one head fits, converts in every block of 128 rows, and is refused
+ * where the partial results do not fit (a few dozen MB): results are the same but for
+ * the order of sums over the parts of a long context.  A scale that is NaN
  * makes its 16 values NaN.
  */
 size_t ssa_attn_window_fp4_workspace_bytes(const ssa_attn_desc* desc, const ssa_window* window);

@@ -6,7 +6,8 @@ namespace ssa {
 // ---- the seen part of a 4-bit cache in fp16 ---------------------------------------------------------------------------------
 // Every block of 128 query rows that works on tiles converts the K and V rows that it sees.  Where many share them (prompt chunks)
 // they are converted once instead, into pages of the workspace that the tiles then read: products of a code and a scale have six
-// significant bits and are multiples of 2^-10 up to 2688, so that nothing is rounded, and outputs are those of tiles that convert.  HBM bounds it: 2.56 bytes a value.  8 requests' chunks of up to 509
+// significant bits and are multiples of 2^-10 up to 2688, so that nothing is rounded, and outputs are those of tiles that convert.
+// They take 512 MB of the workspace at most: requests, or K/V heads of one, go through it in turn.  HBM bounds it: 2.56 bytes a value.  8 requests' chunks of up to 509
 // tokens within a window of 4096, 8 K/V heads: some 36 us (5.4 TB/s), and 166 for the tiles; 49 with 16 bytes of codes to a thread,
 // whose stores then lie 64 bytes apart.
 constexpr int kExpandThreads = 256;
@@ -69,31 +70,49 @@ fp4_expand_kernel(const Fp4Params p, const Fp4Expanded x) {
 }
 
 template <int D>
-static int32_t launch_expanded(const Fp4Params& p, const Fp4Expanded& x, cudaStream_t st) {
+static int32_t launch_expanded(const Fp4Params& all, const Fp4Expanded& x, cudaStream_t st) {
   const int page = 1 << x.page_shift;
   const int64_t head = x.head_rows * D;
   CUtensorMap maps[2];
-  if (!tile_map(&maps[0], x.k, SSA_F16, D, x.head_rows, D, p.H_kv, head, 1, 0, page) ||
-      !tile_map(&maps[1], x.v, SSA_F16, D, x.head_rows, D, p.H_kv, head, 1, 0, page))
+  if (!tile_map(&maps[0], x.k, SSA_F16, D, x.head_rows, D, x.heads, head, 1, 0, page) ||
+      !tile_map(&maps[1], x.v, SSA_F16, D, x.head_rows, D, x.heads, head, 1, 0, page))
     return SSA_ERR_CUDA;
   cudaEvent_t begin, end;
   take_kernel_events(&begin, &end);
   if (begin) cudaEventRecord(begin, st);                     // (what the tiles read is part of their time)
-  const dim3 grid((unsigned)x.most_tiles, (unsigned)p.H_kv, (unsigned)p.B);
-  if (launch_pdl(p.page_table ? fp4_expand_kernel<D, true> : fp4_expand_kernel<D, false>, grid, dim3(kExpandThreads), st, p, x) != cudaSuccess)
-    return SSA_ERR_CUDA;
-  note_launches(1);
-  WindowParams t = p;
-  t.k = x.k; t.v = x.v;
-  t.page_table = x.table; t.page_table_stride = x.table_stride; t.page_shift = x.page_shift;
-  t.n_pages = (int)(x.head_rows >> x.page_shift);
-  t.k_sb = t.v_sb = 0; t.k_sh = t.v_sh = head; t.k_st = t.v_st = D;
-  if (launch_tiles<Fp4AsHalf, D>(t, maps[0], maps[1], page, st) != cudaSuccess) return SSA_ERR_CUDA;
-  if (end) cudaEventRecord(end, st);
-  note_launches(1);
-  if (p.n_splits == 1) return SSA_OK;
-  if (launch_join<__nv_bfloat16, D>(t, st) != cudaSuccess) return SSA_ERR_CUDA;
-  note_launches(1);
+  for (int b0 = 0; b0 < all.B; b0 += x.requests)
+    for (int h0 = 0; h0 < all.H_kv; h0 += x.heads) {         // (in parts only where they are one request's: rows of lse lie side by side)
+      Fp4Params p = all;
+      p.B = std::min(x.requests, all.B - b0);
+      p.H_kv = std::min(x.heads, all.H_kv - h0);
+      p.H = p.H_kv * p.group;
+      const int64_t first = (int64_t)h0 * p.group, k0 = (p.page_table ? 0 : b0 * p.k_sb) + h0 * p.k_sh, v0 = (p.page_table ? 0 : b0 * p.v_sb) + h0 * p.v_sh;
+      p.q = static_cast<const __nv_bfloat16*>(all.q) + b0 * p.q_sb + first * p.q_sh;
+      p.out = static_cast<char*>(all.out) + (b0 * p.o_sb + first * p.o_sh) * (p.out_f32 ? 4 : 2);
+      if (p.lse) p.lse += ((int64_t)b0 * all.H + first) * p.n_q;
+      p.ctx_lens += b0;
+      if (p.q_lens) p.q_lens += b0;
+      if (p.page_table) p.page_table += (int64_t)b0 * p.page_table_stride;
+      p.k = static_cast<const uint8_t*>(all.k) + k0 / 2;
+      p.v = static_cast<const uint8_t*>(all.v) + v0 / 2;
+      p.k_scales += k0 / kScaleDims;
+      p.v_scales += v0 / kScaleDims;
+      const dim3 grid((unsigned)x.most_tiles, (unsigned)p.H_kv, (unsigned)p.B);
+      if (launch_pdl(p.page_table ? fp4_expand_kernel<D, true> : fp4_expand_kernel<D, false>, grid, dim3(kExpandThreads), st, p, x) != cudaSuccess)
+        return SSA_ERR_CUDA;
+      note_launches(1);
+      WindowParams t = p;
+      t.k = x.k; t.v = x.v;
+      t.page_table = x.table; t.page_table_stride = x.table_stride; t.page_shift = x.page_shift;
+      t.n_pages = (int)(x.head_rows >> x.page_shift);
+      t.k_sb = t.v_sb = 0; t.k_sh = t.v_sh = head; t.k_st = t.v_st = D;
+      if (launch_tiles<Fp4AsHalf, D>(t, maps[0], maps[1], page, st) != cudaSuccess) return SSA_ERR_CUDA;
+      if (end) cudaEventRecord(end, st);                     // (the last one counts)
+      note_launches(1);
+      if (p.n_splits == 1) continue;
+      if (launch_join<__nv_bfloat16, D>(t, st) != cudaSuccess) return SSA_ERR_CUDA;
+      note_launches(1);
+    }
   return SSA_OK;
 }
 

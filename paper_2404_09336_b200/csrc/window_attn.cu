@@ -157,35 +157,63 @@ static bool plan_window(const ssa_attn_desc* d, const ssa_window* w, bool mass, 
   return row_tiles * pl->n_splits <= 0x7fffffffll;
 }
 
-// Where the rows of a 4-bit cache that the tokens see have places in fp16; bytes of all of it, 0 where the call has no use for that.
-// Few blocks of 128 rows convert what they see themselves.
-static size_t plan_expanded(const ssa_attn_desc* d, const ssa_window* w, Fp4Expanded* x) {
+// Most bytes of converted rows that a call has in its workspace at a time.  (A 4-bit cache is held for its size: all rows at once would
+// take 3.6 times that.)  Parts of a call are few blocks for the GPU: 32 chunks of 512 tokens over 16384 positions, 32 heads over 8, take
+// 4333 us with all 2 GB, 4198 with 1 GB, 4633 with 512 MB, 4749 with 256; 32 K/V heads of 8 requests 1669, 1745, 1790 and 2076; 4 chunks
+// of 128 over 131072 positions 1799, 1819, 1816 and 2036.
+constexpr long long kExpandBytes = 1 << 29;
+
+// Where the rows of a 4-bit cache that the tokens see have places in fp16; bytes of all of it, 0 where the call has no use for that, or a
+// K/V head of a request does not fit most_bytes.  Few blocks of 128 rows convert what they see themselves.
+static size_t plan_expanded(const ssa_attn_desc* d, const ssa_window* w, long long most_bytes, Fp4Expanded* x) {
   const long long rows = (long long)(d->H / d->H_kv) * w->n_q;
   if (rows <= (w->paging ? kExpandRowsPaged : kExpandRows)) return 0;
   const long long all = (d->max_ctx + kTileKeys - 1ll) / kTileKeys;
   const long long seen = ((long long)w->sinks + kTileKeys - 1) / kTileKeys + ((long long)w->window + w->n_q + kTileKeys - 1) / kTileKeys + 1;
-  const long long tiles = w->window == 0 ? all : std::min(all, seen);
-  if (tiles * d->B * kTileKeys > 0x7fffffffll) return 0;
+  const long long tiles = w->window == 0 ? all : std::min(all, seen), fit = most_bytes / (tiles * kTileKeys * d->D * 2 * (long long)sizeof(__half));
+  if (fit == 0) return 0;
+  // as many requests as fit, or heads of one, in parts of one size
+  const long long per = std::max(1ll, fit / d->H_kv), parts = (d->B + per - 1) / per;
+  const long long most = std::min<long long>(fit, d->H_kv), head_parts = (d->H_kv + most - 1) / most;
+  x->requests = (int)((d->B + parts - 1) / parts);
+  x->heads = (int)((d->H_kv + head_parts - 1) / head_parts);
   const int page = w->paging ? std::min(w->paging->page_size, kTileKeys) : kTileKeys;
   x->most_tiles = (int)tiles;
-  x->head_rows = tiles * d->B * kTileKeys;
+  x->head_rows = tiles * x->requests * kTileKeys;
   x->page_shift = 0;
   while ((1 << x->page_shift) < page) ++x->page_shift;
   x->table_stride = (int)((d->max_ctx + (long long)page - 1) / page);
-  return up256((size_t)d->B * x->table_stride * sizeof(int32_t)) + 2 * up256((size_t)x->head_rows * d->H_kv * d->D * 2);
+  return up256((size_t)x->requests * x->table_stride * sizeof(int32_t)) + 2 * up256((size_t)x->head_rows * x->heads * d->D * 2);
 }
 
-// Room for either kernel: which one runs may depend on the cache's strides.
+// The part of the call that is served at a time.
+static ssa_attn_desc part_of(const ssa_attn_desc* d, const Fp4Expanded& x) {
+  ssa_attn_desc part = *d;
+  part.B = x.requests;
+  part.H = d->H / d->H_kv * x.heads;
+  part.H_kv = x.heads;
+  return part;
+}
+
+// Room for either kernel: which one runs may depend on the cache's strides (of a 4-bit cache: does not).
 static size_t window_bytes(const ssa_attn_desc* d, const ssa_window* w, bool mass, bool fp4) {
   WindowPlan pl;
   if (!d || !w || check_window(d, w, mass, fp4) != SSA_OK || !plan_window(d, w, mass, false, &pl)) return 0;
   const size_t few = pl.total_bytes;
   if (!tiles_pay(d, w, mass) || !plan_window(d, w, mass, true, &pl)) return few;
-  return std::max(few, pl.total_bytes);
+  return fp4 ? pl.total_bytes : std::max(few, pl.total_bytes);
 }
-static size_t expanded_bytes(const ssa_attn_desc* d, const ssa_window* w) {
-  Fp4Expanded x;
-  return tiles_pay(d, w, false) ? plan_expanded(d, w, &x) : 0;
+// The same for a call that converts once, and where in it the converted rows start, in parts that have room in ws_bytes; 0 where it
+// does not, or the smallest have none.
+static size_t expanded_bytes(const ssa_attn_desc* d, const ssa_window* w, size_t ws_bytes, Fp4Expanded* x, size_t* start) {
+  if (!tiles_pay(d, w, false)) return 0;
+  for (long long most = kExpandBytes;; most /= 2) {
+    const size_t more = plan_expanded(d, w, most, x);
+    if (!more) return 0;
+    const ssa_attn_desc part = part_of(d, *x);               // (whose rows may be split further than the whole call's)
+    *start = std::max(window_bytes(d, w, false, true), window_bytes(&part, w, false, true));
+    if (*start + more <= ws_bytes) return *start + more;
+  }
 }
 
 template <typename T, int D>
@@ -263,13 +291,18 @@ static int32_t run_window(const ssa_attn_desc* d, const ssa_window* w, const voi
     f.k_scales = static_cast<const uint8_t*>(k_scales);
     f.v_scales = static_cast<const uint8_t*>(v_scales);
     Fp4Expanded x;
-    if (const size_t more = tiles ? plan_expanded(d, w, &x) : 0; more && ws_bytes >= window_bytes(d, w, mass, fp4) + more) {
+    size_t start = 0;
+    if (expanded_bytes(d, w, ws_bytes, &x, &start)) {
       // the rows that are seen in fp16, behind the partial results, and the tiles of a cache of such rows in pages
-      char* to = static_cast<char*>(ws) + window_bytes(d, w, mass, fp4);
+      const ssa_attn_desc part = part_of(d, x);
+      if (!plan_window(&part, w, false, true, &pl)) return SSA_ERR_SHAPE;
+      f.n_splits = pl.n_splits;
+      f.ws_acc = reinterpret_cast<float*>(at + pl.ml_bytes);
+      char* to = at + start;
       x.table = reinterpret_cast<int32_t*>(to);
-      to += up256((size_t)d->B * x.table_stride * sizeof(int32_t));
+      to += up256((size_t)x.requests * x.table_stride * sizeof(int32_t));
       x.k = reinterpret_cast<__half*>(to);
-      x.v = reinterpret_cast<__half*>(to + up256((size_t)x.head_rows * d->H_kv * d->D * 2));
+      x.v = reinterpret_cast<__half*>(to + up256((size_t)x.head_rows * x.heads * d->D * 2));
       return launch_expanded(f, x, d->D, st);
     }
     return launch_window_fp4(f, d->D, tiles ? box_rows : 0, st);
@@ -312,7 +345,9 @@ int32_t ssa_attn_mass(const ssa_attn_desc* desc, const ssa_window* window, const
 
 size_t ssa_attn_window_fp4_workspace_bytes(const ssa_attn_desc* desc, const ssa_window* window) {
   const size_t need = ssa::window_bytes(desc, window, false, true);
-  return need ? need + ssa::expanded_bytes(desc, window) : 0;
+  ssa::Fp4Expanded x;
+  size_t start;
+  return need ? std::max(need, ssa::expanded_bytes(desc, window, ~(size_t)0, &x, &start)) : 0;
 }
 
 int32_t ssa_attn_window_fp4(const ssa_attn_desc* desc, const ssa_window* window, const void* q, const void* k_cache,

@@ -837,11 +837,12 @@ inline long long rows_splits(long long n_tiles, long long blocks, int rows, bool
   return splits;
 }
 inline size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-// The seen part of a 4-bit cache as pages of an fp16 one, in the workspace.
+// The seen part of a 4-bit cache as pages of an fp16 one, in the workspace: of so many requests, or K/V heads of one request, at a time.
 struct Fp4Expanded {
-  __half *k, *v;                 // [H_kv][head_rows][D]
-  int32_t* table;                // [B][table_stride]
-  int64_t head_rows;             // B most_tiles 128
+  int requests, heads;
+  __half *k, *v;                 // [heads][head_rows][D]
+  int32_t* table;                // [requests][table_stride]
+  int64_t head_rows;             // requests most_tiles 128
   int most_tiles, table_stride, page_shift;
 };
 // Converts it, and attends to it (defined in fp4_attn.cu).

@@ -1,4 +1,6 @@
 """What the calls that fill a cache and read its blocks refuse of tensors that do not go with their structures (no GPU)."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -87,3 +89,30 @@ def test_tokens_that_share_a_row_of_out():
     before, k = ssa.launch_count(), good_blocks()
     k.o_stride_t = 0
     assert attend(desc(), k) == ssa.ERR_UNSUPPORTED and ssa.launch_count() == before
+
+
+@pytest.mark.parametrize("B,H,H_kv,T,n_q", [(64, 32, 32, 16384, 1024), (16, 32, 8, 131072, 512), (32, 32, 8, 16384, 512), (1, 8, 1, 1 << 20, 200),
+                                            (1, 8, 1, (1 << 20) + 128, 200), (1, 8, 8, 1 << 24, 200)])
+@pytest.mark.parametrize("paged", [False, True])
+def test_workspaces_of_4_bit_chunks_are_bounded(B, H, H_kv, T, n_q, paged):
+    """What converted rows take: 512 MB and a page table of the requests that are served at a time, whatever the cache's size."""
+    d, w = ssa.AttnDesc(), ssa.Window()
+    d.B, d.H, d.H_kv, d.D, d.max_ctx, d.kv_dtype, d.out_dtype = B, H, H_kv, 128, T, ssa.FP4_E2M1, ssa.BF16
+    d.q_stride_b, d.q_stride_h, d.o_stride_b, d.o_stride_h = H * n_q * 128, n_q * 128, H * n_q * 128, n_q * 128
+    for x in "kv":
+        setattr(d, x + "_stride_b", 0 if paged else H_kv * T * 128), setattr(d, x + "_stride_h", 128 if paged else T * 128)
+        setattr(d, x + "_stride_t", H_kv * 128 if paged else 128)
+    w.n_q, w.q_stride_t, w.o_stride_t = n_q, 128, 128
+    if paged:
+        table = torch.zeros(1, dtype=torch.int32)
+        w.paging = C.pointer(ssa.make_paging(table.view(1, 1), 16, 1 << 20))
+        w.paging[0].page_table_stride = T // 16
+    whole = ssa.attn_window_fp4_workspace_bytes(d, w)
+    w.n_q = 32 // (H // H_kv)                                # (few rows: nothing is converted)
+    few = ssa.attn_window_fp4_workspace_bytes(d, w)
+    assert 0 < few < 1 << 27 and whole > 0
+    # partial results: max and sum of every row; and rows of the parts of a context, of as many rows as keep the GPU busy
+    rest = B * H * n_q * 8 + (64 << 20)
+    converts = T <= 1 << 20                                  # (a head of 2^20 positions is 512 MB)
+    assert whole <= rest + converts * ((1 << 29) + B * T // 4)
+    assert not converts or whole > 1 << 28

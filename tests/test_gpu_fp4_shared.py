@@ -11,16 +11,38 @@ pytestmark = pytest.mark.gpu
 BF16, F32 = torch.bfloat16, torch.float32
 
 
+def least_room(p, *args):
+    """Most bytes that the call may have less than it asks for (calls with less still are refused before anything is launched)."""
+    desc, win = p.cache.desc(p.q, p.q), ssa.make_window(p.q, p.q, *args[2:4], None, p.cache.paging())
+    taken, refused = 0, ssa.attn_window_fp4_workspace_bytes(desc, win)
+    while refused - taken > 1:
+        less = (taken + refused) // 2
+        try:
+            p.call(*args, less=less)
+            taken = less
+        except ssa.SsaError:
+            refused = less
+    return taken
+
+
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("page", [0, 8, 64])
 @pytest.mark.parametrize("out_dtype", [BF16, F32])
 def test_bits_do_not_depend_on_the_workspace(D, page, out_dtype):
-    """Weights keep the bits of the calls of fewer rows, whether the call has room to convert once or converts in every block."""
+    """Weights keep the bits of the calls of fewer rows, whether the call has room to convert once, in parts, or converts in every
+    block."""
     n = 70 if page else 200
     p = Fp4Tokens(2, 8, 2, 900, D, n, page=page, spread=2.0)
     for ctx, new, window, sinks in (([900, 641], None, 0, 0), ([877, 300], [n, n - 30], 150, 9)):
-        got = [p.call(ctx, new, window, sinks, out_dtype, less=less) for less in (0, 1)]
-        assert np.array_equal(got[0][0], got[1][0]) and np.array_equal(got[0][1], got[1][1]) and got[0][3] == got[1][3] == 0
+        got, launches = [], []
+        for less in (0, 1, least_room(p, ctx, new, window, sinks, out_dtype)):
+            before = ssa.launch_count()
+            got.append(p.call(ctx, new, window, sinks, out_dtype, less=less))
+            launches.append(ssa.launch_count() - before)
+        # conversion, tiles, a join perhaps; parts of a request, or of a head, each; no conversion
+        assert launches[0] in (2, 3) and launches[1] >= 2 * launches[0] and launches[2] == launches[0] - 1, launches
+        for x in got:
+            assert np.array_equal(x[0], got[0][0]) and np.array_equal(x[1], got[0][1]) and x[3] == 0
         check_tokens(p, got[0], ctx, new, window, sinks, out_dtype, tiles=True)
 
 
@@ -92,3 +114,44 @@ def test_timing_events_bracket_the_conversion():
         assert ssa.launch_count() - before == 2              # conversion, tiles
         share.append(b.elapsed_time(y) / a.elapsed_time(z))
     assert max(share) > 0.85, share                          # (the tiles alone: 0.7)
+
+
+def in_parts(p, T, ctx, new, window, sinks, out_dtype, less=0):
+    """The call as one of a cache with room for T positions, of which there are as many as p has."""
+    c, was, table = p.cache, p.cache.T, None
+    if c.page:
+        table = torch.full((p.B, T // c.page), -1, dtype=torch.int32)
+        table[:, : c.table.shape[1]] = c.table
+    c.T = T
+    try:
+        return p.call(ctx, new, window, sinks, out_dtype, table=table, less=less)
+    finally:
+        c.T = was
+
+
+@pytest.mark.parametrize("B,T", [(5, 1 << 18), (2, 1 << 20), (3, 1 << 21), (2, 1 << 22)])
+@pytest.mark.parametrize("page", [0, 16])
+def test_requests_and_heads_in_turn(B, T, page):
+    """Room for 512 MB of converted rows: 64, 256, 512 and 1024 MB a K/V head here, three heads.  Requests two at a time, and one left;
+    heads two at a time; each by itself; none at all."""
+    n_q = 150 if page else 400
+    p = Fp4Tokens(B, 6, 3, n_q + 90, 64, n_q, page=page)
+    ctx, new = [n_q + 90, n_q + 3, 40, 0, n_q][:B], [n_q, n_q - 1, 40, 0, 5][:B]
+    for out_dtype, window, sinks in ((F32, 0, 0), (BF16, 0, 0)):
+        want = p.call(ctx, new, window, sinks, out_dtype)
+        check_tokens(p, want, ctx, new, window, sinks, out_dtype, tiles=True)
+        before = ssa.launch_count()
+        got = in_parts(p, T, ctx, new, window, sinks, out_dtype)
+        launches = ssa.launch_count() - before
+        assert launches >= {1 << 18: 2 * 3, 1 << 20: 2 * 2 * B, 1 << 21: 2 * 3 * B, 1 << 22: 1}[T]
+        assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1]) and got[3] == want[3] == 0
+
+
+@pytest.mark.parametrize("page", [0, 64])
+def test_parts_that_are_split(page):
+    """One K/V head at a time is few blocks for the GPU: long contexts are cut, and joined part by part."""
+    n_q = 300 if page else 800
+    p = Fp4Tokens(2, 2, 2, 6000, 64, n_q, page=page)
+    for ctx, new, out_dtype in (([6000, 4100], None, F32), ([5999, 900], [n_q, 7], BF16)):
+        got = in_parts(p, 1 << 21, ctx, new, 0, 0, out_dtype)
+        check_tokens(p, got, ctx, new, 0, 0, out_dtype, tiles=True)
