@@ -113,10 +113,10 @@ static int32_t check_window(const ssa_attn_desc* d, const ssa_window* w, bool ma
   return w->paging ? check_paging(w->paging, d->max_ctx) : SSA_OK;
 }
 
-// Rows of a K/V head up to which the kernel for few rows serves a 4-bit cache: with 32 it takes 91, 57, 102 and 36 us, the tiles 98, 48,
-// 106 and 32 (8 requests of 4100 to 16384 positions, those within a window of 4096, 32 requests of up to 4096, one of 16384; 8 K/V
-// heads); with 24 rows 69, 42, 70 and 16 against 105, 48, 99 and 25, with 48 154, 73, 150 and 43 against 111, 48, 100 and 29.
-constexpr int kFewRowsFp4 = 32;
+// kFewRows holds for a 4-bit cache too: with 24 rows the kernel for few rows takes 85, 52, 81 and 42 us, the tiles 124, 54, 116 and 40 (8
+// requests of 4100 to 16384 positions, those within a window of 4096, 32 requests of up to 4096, one of 16384; 8 K/V heads, L2 cold), in
+// pages of 16 89, 56, 91 and 42 against 163, 66, 155 and 44; with 25 to 32 rows 122, 71, 119 and 54 against 124, 56, 117 and 40, in pages
+// 133, 78, 133 and 56 against 163, 66, 155 and 44.
 // Rows above which it is converted once for all of them, instead of by every block of 128 rows: for the same requests that takes 199,
 // 94, 197 and 40 us with 256 rows, 280, 116, 214 and 54 with 512, 314, 121, 277 and 65 with 768, each block for itself 176, 79, 160 and
 // 40, then 283, 117, 199 and 61, then 336, 119, 276 and 66.  In pages each piece of a row costs a block more instructions: 212, 99, 213
@@ -126,7 +126,7 @@ constexpr int kExpandRows = 768, kExpandRowsPaged = 256;
 // Whether the tiles of 128 rows serve a call.
 static bool tiles_pay(const ssa_attn_desc* d, const ssa_window* w, bool mass) {
   return !mass && d->kv_dtype != SSA_FP8_E4M3 &&
-         (long long)(d->H / d->H_kv) * w->n_q > (d->kv_dtype == SSA_FP4_E2M1 ? kFewRowsFp4 : kFewRows) &&
+         (long long)(d->H / d->H_kv) * w->n_q > kFewRows &&
          (!w->paging || w->paging->page_size >= 8);          // (a box of a copy is eight rows at least, or a lane's run of 4-bit ones)
 }
 
