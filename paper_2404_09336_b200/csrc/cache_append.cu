@@ -213,9 +213,11 @@ static cudaError_t launch_append(const AppendParams& p, cudaStream_t st) {
     const dim3 grid((unsigned)((p.n_q + x.tokens - 1) / x.tokens), (unsigned)((x.slots * x.tokens + kRows - 1) / kRows), (unsigned)p.B);
     return launch_pdl(kernel, grid, dim3(kAppendThreads), st, x);
   };
-  // Where there are rows for more threads than the GPU holds, three a thread: cosines are made ready once for them, and more of them
-  // are under way.
-  const bool many = rows >= 3 && (long long)rows * p.n_q * p.B > 6ll * sm_count() * kRows;
+  // Where rows take more blocks than the GPU holds at a time (12 to an SM), three a thread: cosines are made ready once for them, and more
+  // of them are under way.  One against three, L2 cold: 32 heads over 8 of 128, 6 blocks to an SM 8.2 against 9.2 us (4 bits 8.3 against
+  // 10.3), 10 blocks 9.2 against 10.2, 24 both 12.3; 8 heads of 64, 8 blocks 8.2 against 10.2, 24 13.2 against 12.3, 48 18.4 against 16.4;
+  // 4 x 4096 tokens, 32 heads of 128, 206 against 155.
+  const bool many = rows >= 3 && (long long)rows * p.n_q * p.B > 12ll * sm_count() * kRows;
   if (p.page_table) return many ? launch(cache_append_kernel<T, D, true, 3>, 3) : launch(cache_append_kernel<T, D, true, 1>, 1);
   return many ? launch(cache_append_kernel<T, D, false, 3>, 3) : launch(cache_append_kernel<T, D, false, 1>, 1);
 }
