@@ -77,7 +77,7 @@ class Blocks(C.Structure):
 
 class Append(C.Structure):
     """ssa_append (see include/ssa.h)."""
-    made_for, strides = None, ()                             # (requests, heads, query heads, D) that make_append was given
+    made_for, strides = None, ()                             # (requests, heads, query heads or False, D) that make_append was given
     _fields_ = [("n_q", C.c_int32), ("rotary_dims", C.c_int32), ("interleaved", C.c_int32), ("n_positions", C.c_int32),
                 ("k_factor", C.c_float), ("v_factor", C.c_float), ("q_stride_t", C.c_int64),
                 *((f"{n}_stride_{d}", C.c_int64) for n in ("qo", "kn", "vn") for d in "bht"),
@@ -688,7 +688,7 @@ def make_append(k_new, v_new, q=None, q_out=None, cos_sin=None, interleaved: boo
     a.q_lens = None if q_lens is None else q_lens.data_ptr()
     if paging is not None:
         a.paging = C.pointer(paging)
-    a.made_for = B, int(k_new.shape[1]), None if q is None else int(q.shape[1]), D
+    a.made_for = B, int(k_new.shape[1]), q is not None and int(q.shape[1]), D
     a.strides = tuple(x is not None and x.stride() for x in (k_new, v_new, q, q_out))
     return a
 
@@ -699,7 +699,7 @@ def _check_append(desc, append, new):
         return
     B, H_kv, H, D = append.made_for
     if B < desc.B or H_kv != desc.H_kv or D != desc.D or (new[2] is not None and H != desc.H):
-        raise ValueError(f"rows of {B} requests, {H_kv} heads and {H} query heads of {D} for {desc.B}, {desc.H_kv}, {desc.H} and {desc.D}")
+        raise ValueError(f"rows of {B} requests, {H_kv} heads and {H or 0} query heads of {D} for {desc.B}, {desc.H_kv}, {desc.H} and {desc.D}")
     for x, of, heads in zip(new, append.strides, (H_kv, H_kv, H, H)):    # (of one token, its dimension may be left out; what has one
         if x is not None and (of is False or x.shape[1] != heads or       # element in a dimension may have any stride there)
                               any(n > 1 and y != z for n, y, z in zip((B, heads, append.n_q), x.stride()[: x.dim() - 1], of))):
@@ -711,7 +711,7 @@ def cache_append(desc, append, k_new, v_new, ctx_lens, k_cache, v_cache, q=None,
     """ssa_cache_append: the step's keys and values into the cache, rotated by position, and its queries rotated into q_out."""
     _check_type(desc, k_new)
     # (almost always the very strides and numbers that make_append has seen: looked at one by one only where not)
-    if append.made_for != (desc.B, desc.H_kv, desc.H, desc.D) or append.strides != (
+    if append.made_for != (desc.B, desc.H_kv, q is not None and desc.H, desc.D) or append.strides != (
             k_new.stride(), v_new.stride(), q is not None and q.stride(), q is not None and q_out.stride()):
         _check_append(desc, append, (k_new, v_new, q, q_out))
     rc = _call.cache_append(desc, append, k_new, v_new, ctx_lens, k_cache, v_cache, q, q_out, k_scales, v_scales, dev_status,

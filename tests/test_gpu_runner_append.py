@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from oracle import budget_oracle as BO
+from oracle import cache_oracle as CO
 from paper_2404_09336_b200 import inputs, ssa
 from paper_2404_09336_b200.runner import DecodeStep
 
@@ -123,3 +124,60 @@ def test_captured_appends_fill_a_cache_up():
     for a, b in zip((*eager.k_store, *eager.v_store, *eager.fp4, eager.bounds, eager.q), (*captured.k_store, *captured.v_store, *captured.fp4, captured.bounds, captured.q)):
         assert torch.equal(a, b)
     assert int(eager.status) == int(captured.status) == ssa.DEV_BAD_COUNT
+
+
+def over_4_bits(ds, b, h):
+    n = int(ds.ctx_lens[b])
+    K, V = (CO.fp4_values(ds.fp4[i][b, h, :n].cpu().numpy(), ds.fp4[2 + i][b, h, :n].cpu().numpy()) for i in (0, 1))
+    return CO.attention(ds.q[b, h][None].double().cpu().numpy(), K, V, np.arange(n), ds.wl.D ** -0.5)[0][0]
+
+
+def test_a_compacted_cache_is_attended_to_in_4_bits():
+    ds = made()
+    ds.enable_fp4()
+    before = ds.ctx_lens.tolist()
+    ds.attend_mass()
+    ds.select_heaviest(70, sinks=2, recent=5)
+    ds.compact()
+    ds.attend_fp4()
+    torch.cuda.synchronize()
+    assert ds.ctx_lens.tolist() == [min(70, n) for n in before] and min(before) > 70
+    for b in range(3):
+        for h in range(4):
+            assert np.abs(ds.out[b, h].cpu().numpy() - over_4_bits(ds, b, h)).max() < 1e-4
+
+
+def test_captured_4_bit_steps():
+    """Graphs of a token appended and attended to in 4 bits, and of other calls in the same workspace, replayed in turn: each output is
+    what an eager runner gives, and the oracle."""
+    eager, captured = made(), made()
+    for ds in (eager, captured):
+        ds.ctx_lens.sub_(30)
+        ds.enable_fp4()
+        ds.enable_blocks(32, 5)
+        ds.attend_fp4()
+        ds.attend_blocks()
+    xs = rows(eager, 5)
+    k = xs[0].clone()
+    torch.cuda.synchronize()
+    step, other = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(step):
+        captured.append(k, k, k)
+        captured.attend_fp4()
+        got = captured.out.clone()
+    with torch.cuda.graph(other):
+        captured.attend_window(9)
+        captured.select_blocks()
+        captured.attend_blocks()
+    for x in xs:
+        k.copy_(x)
+        step.replay()
+        other.replay()
+        eager.append(x, x, x)
+        eager.attend_fp4()
+        torch.cuda.synchronize()
+        assert torch.equal(got, eager.out) and not torch.equal(got, captured.out)
+    for b in range(3):
+        for h in range(4):
+            assert np.abs(got[b, h].cpu().numpy() - over_4_bits(eager, b, h)).max() < 1e-4
+    assert int(captured.status) == int(eager.status) == 0
