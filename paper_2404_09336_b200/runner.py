@@ -302,15 +302,20 @@ class DecodeStep:
         with self._on(stream):
             k, v = (torch.zeros(B, H, T, D // 2, dtype=torch.uint8, device=dev) for _ in range(2))
             k_scales, v_scales = (torch.zeros(B, H, T, D // 16, dtype=torch.uint8, device=dev) for _ in range(2))
-            self._filled = torch.full_like(self.ctx_lens, T) # contexts whose newest T positions are all there are
+            # rows at a time, as many as a call takes, and contexts of which they are the newest
+            most = (1 << 24) // self.q.shape[1]
+            self._filled = [(t, torch.full_like(self.ctx_lens, min(t + most, T))) for t in range(0, T, most)]
         self.fp4 = k, v, k_scales, v_scales
         self.desc_fp4 = ssa.make_desc_fp4(self.q, k, v, k_scales, v_scales, self.out, T)
         return self._fill_fp4(stream)
 
     def _fill_fp4(self, stream):
         k, v, k_scales, v_scales = self.fp4
-        return ssa.cache_append(self.desc_fp4, ssa.make_append(self.k, self.v), self.k, self.v, self._filled, k, v, None, None,
-                                k_scales, v_scales, self.status, stream)
+        most = (1 << 24) // self.q.shape[1]
+        for t, ends in self._filled:
+            rows = self.k[:, :, t:t + most], self.v[:, :, t:t + most]
+            ssa.cache_append(self.desc_fp4, ssa.make_append(*rows), *rows, ends, k, v, None, None, k_scales, v_scales, self.status, stream)
+        return ssa.OK
 
     def attend_fp4(self, window: int = 0, sinks: int = 0, stream=None):
         """The step's token over its context (or window), read from the 4-bit cache."""

@@ -181,3 +181,18 @@ def test_captured_4_bit_steps():
         for h in range(4):
             assert np.abs(got[b, h].cpu().numpy() - over_4_bits(eager, b, h)).max() < 1e-4
     assert int(captured.status) == int(eager.status) == 0
+
+
+def test_a_4_bit_copy_made_in_parts(monkeypatch):
+    """As many query heads as make a call take fewer rows than the cache has: the copy is that of one call."""
+    ds = DecodeStep(inputs.make_config(2, B=2, H=2), out_dtype=torch.float32, query_heads=1 << 14)
+    ds.enable_fp4()
+    whole = [x.clone() for x in ds.fp4]
+    assert len(ds._filled) == 1
+    few = DecodeStep(inputs.make_config(2, B=2, H=2), out_dtype=torch.float32, query_heads=3 << 13)      # 682 rows at a time
+    few.enable_fp4()
+    torch.cuda.synchronize()
+    assert len(few._filled) == 2 and all(torch.equal(a, b) for a, b in zip(few.fp4, whole)) and int(few.status) == 0
+    for b in range(2):
+        want = CO.to_fp4(few.k[b].float().cpu().numpy())
+        assert np.array_equal(few.fp4[0][b].cpu().numpy(), want[0]) and np.array_equal(few.fp4[2][b].cpu().numpy(), want[1])

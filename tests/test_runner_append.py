@@ -58,3 +58,19 @@ def test_full_contexts_stay_as_they_are(made):               # noqa: F811
         assert ds._new_lens.tolist() == stored
     assert (ds.mass[0] == 7).all() and ds.mass[1, T - 1] == 0 and (ds.mass[1, : T - 1] == 7).all()
     assert not ds.mass[2, 5:7].any() and (ds.mass[2, :5] == 7).all() and (ds.mass[2, 7:] == 7).all()
+
+
+def test_a_4_bit_copy_of_more_rows_than_a_call_takes(made, monkeypatch):  # noqa: F811
+    """H n_q <= 2^24 in a call: long contexts of many query heads are copied in parts."""
+    ds = small(query_heads=4096)
+    T = ds.wl.max_ctx                                        # 2^10: all at once
+    ds.enable_fp4()
+    assert [a["append"].n_q for _, a in made] == [T]
+    ds.q, ds.out = (x.new_zeros(ds.wl.B, 1 << 16, ds.wl.D) for x in (ds.q, ds.out))      # as if there were 16 times as many heads
+    made.clear()
+    ds.enable_fp4()
+    parts = [(int(a["ctx_lens"][0]) - a["append"].n_q, int(a["ctx_lens"][0])) for _, a in made]
+    assert parts == [(t, t + 256) for t in range(0, T, 256)]
+    for (t, z), (_, a) in zip(parts, made):
+        assert a["append"].n_q * (1 << 16) <= 1 << 24 and torch.equal(a["k_new"], ds.k[:, :, t:z]) and a["k_new"].data_ptr() == ds.k[:, :, t:z].data_ptr()
+        assert a["k_cache"] is ds.fp4[0] and a["v_scales"] is ds.fp4[3]
