@@ -233,7 +233,7 @@ class DecodeStep:
         if hasattr(self, "bounds"):
             self.refresh_bounds(stream=stream)
         if hasattr(self, "fp4"):
-            self._fill_fp4(stream)
+            self._fill_fp4(self.fp4, stream)
         return ssa.OK
 
     # ---- filling the cache ----------------------------------------------------------------
@@ -269,19 +269,27 @@ class DecodeStep:
 
     # ---- blocks that the queries select ------------------------------------------------------
     def enable_blocks(self, block_size: int = 64, budget: int = 32, sinks: int = 1, recent: int = 1, stream=None):
-        """Bounds of every block of the cache, and room for the lists of attention over the `budget` blocks that score best."""
+        """Bounds of every block of the cache, and room for the lists of attention over the `budget` blocks that score best.  (Asked for
+        once more, e.g. with other blocks: graphs captured before go on using what they were captured with.)"""
         B, H, D, T, dev = self.wl.B, self.wl.H, self.wl.D, self.wl.max_ctx, self.device
         with self._on(stream):
-            self.bounds = torch.zeros(B, H, -(-T // block_size), 2, D, dtype=self.q.dtype, device=dev)
-            self.block_lists = (torch.full((B, H, 1, budget), -7, dtype=torch.int32, device=dev),
-                                torch.zeros((B, H, 1), dtype=torch.int32, device=dev))
-        self.blocks = ssa.make_blocks(1, block_size, budget, sinks, recent, self.q.unsqueeze(2), self.out.unsqueeze(2), self.bounds)
-        return self.refresh_bounds(stream=stream)
+            bounds = torch.zeros(B, H, -(-T // block_size), 2, D, dtype=self.q.dtype, device=dev)
+            lists = (torch.full((B, H, 1, budget), -7, dtype=torch.int32, device=dev),
+                     torch.zeros((B, H, 1), dtype=torch.int32, device=dev))
+        blocks = ssa.make_blocks(1, block_size, budget, sinks, recent, self.q.unsqueeze(2), self.out.unsqueeze(2), bounds)
+        self._refresh(blocks, bounds, None, stream)          # (refused: nothing has changed)
+        if hasattr(self, "bounds"):
+            self._outgrown += [self.bounds, self.block_lists]
+        self.bounds, self.block_lists, self.blocks = bounds, lists, blocks
+        return ssa.OK
+
+    def _refresh(self, blocks, bounds, newest, stream):
+        which = ssa.make_blocks(newest or self.wl.max_ctx, blocks.block_size, blocks.budget, bounds=bounds)
+        return ssa.block_bounds(self.desc, which, self.k, self.ctx_lens, bounds, None, self.status, stream)
 
     def refresh_bounds(self, newest=None, stream=None):
         """Bounds of the blocks of the newest positions (None: of all)."""
-        which = ssa.make_blocks(newest or self.wl.max_ctx, self.blocks.block_size, self.blocks.budget, bounds=self.bounds)
-        return ssa.block_bounds(self.desc, which, self.k, self.ctx_lens, self.bounds, None, self.status, stream)
+        return self._refresh(self.blocks, self.bounds, newest, stream)
 
     def select_blocks(self, stream=None):
         """self.block_lists: for every K/V head the blocks that the step's queries rank first."""
@@ -295,22 +303,26 @@ class DecodeStep:
 
     # ---- the cache in 4 bits -------------------------------------------------------------------
     def enable_fp4(self, stream=None):
-        """A copy of the cache in 4-bit values (codes and scales of K and of V)."""
+        """A copy of the cache in 4-bit values (codes and scales of K and of V).  Asked for once more, it is made anew in its place."""
         B, H, D, T, dev = self.wl.B, self.wl.H, self.wl.D, self.wl.max_ctx, self.device
         if self.q.dtype != torch.bfloat16:
             raise ValueError("queries over a 4-bit cache are bf16")
+        fp4 = getattr(self, "fp4", None)
         with self._on(stream):
-            k, v = (torch.zeros(B, H, T, D // 2, dtype=torch.uint8, device=dev) for _ in range(2))
-            k_scales, v_scales = (torch.zeros(B, H, T, D // 16, dtype=torch.uint8, device=dev) for _ in range(2))
+            if fp4 is None:
+                fp4 = (*(torch.zeros(B, H, T, D // 2, dtype=torch.uint8, device=dev) for _ in range(2)),
+                       *(torch.zeros(B, H, T, D // 16, dtype=torch.uint8, device=dev) for _ in range(2)))
             # rows at a time, as many as a call takes, and contexts of which they are the newest
             most = (1 << 24) // self.q.shape[1]
-            self._filled = [(t, torch.full_like(self.ctx_lens, min(t + most, T))) for t in range(0, T, most)]
-        self.fp4 = k, v, k_scales, v_scales
-        self.desc_fp4 = ssa.make_desc_fp4(self.q, k, v, k_scales, v_scales, self.out, T)
-        return self._fill_fp4(stream)
+            filled = [(t, torch.full_like(self.ctx_lens, min(t + most, T))) for t in range(0, T, most)]
+        self._outgrown.append(getattr(self, "_filled", None))
+        self.desc_fp4, self._filled = ssa.make_desc_fp4(self.q, *fp4, self.out, T), filled
+        rc = self._fill_fp4(fp4, stream)
+        self.fp4 = fp4
+        return rc
 
-    def _fill_fp4(self, stream):
-        k, v, k_scales, v_scales = self.fp4
+    def _fill_fp4(self, fp4, stream):
+        k, v, k_scales, v_scales = fp4
         most = (1 << 24) // self.q.shape[1]
         for t, ends in self._filled:
             rows = self.k[:, :, t:t + most], self.v[:, :, t:t + most]

@@ -1,5 +1,8 @@
 """DecodeStep.append: what a token that is appended finds and leaves in the runner's own buffers (no GPU: the library's calls are
 recorded)."""
+import gc
+import weakref
+
 import pytest
 import torch
 
@@ -74,3 +77,39 @@ def test_a_4_bit_copy_of_more_rows_than_a_call_takes(made, monkeypatch):  # noqa
     for (t, z), (_, a) in zip(parts, made):
         assert a["append"].n_q * (1 << 16) <= 1 << 24 and torch.equal(a["k_new"], ds.k[:, :, t:z]) and a["k_new"].data_ptr() == ds.k[:, :, t:z].data_ptr()
         assert a["k_cache"] is ds.fp4[0] and a["v_scales"] is ds.fp4[3]
+
+
+def test_blocks_that_are_refused_leave_none(made, monkeypatch):          # noqa: F811
+    ds = small()
+
+    def refuse(*a, **kw):
+        raise ssa.SsaError("ssa_block_bounds", 9)
+    with monkeypatch.context() as m:
+        m.setattr(ssa, "block_bounds", refuse)
+        with pytest.raises(ssa.SsaError):
+            ds.enable_blocks(48, 8)
+    made.clear()
+    ds.append(*rows(ds))
+    assert [n for n, _ in made] == ["cache_append"]
+    ds.enable_blocks(64, 8)
+    was = ds.bounds, ds.block_lists, ds.blocks
+    with monkeypatch.context() as m:
+        m.setattr(ssa, "block_bounds", refuse)
+        with pytest.raises(ssa.SsaError):
+            ds.enable_blocks(32, 2)
+    assert ds.bounds is was[0] and ds.block_lists is was[1] and ds.blocks is was[2]
+
+
+def test_what_graphs_were_captured_with_stays(made):         # noqa: F811
+    """Blocks asked for once more have buffers of their own beside the first, a 4-bit copy is made anew in its place."""
+    ds = small()
+    ds.enable_blocks(64, 8)
+    ds.enable_fp4()
+    first = [weakref.ref(x) for x in (ds.bounds, *ds.block_lists, *ds.fp4, ds._filled[0][1])]
+    places = [x.data_ptr() for x in ds.fp4]
+    made.clear()
+    ds.enable_blocks(32, 4)
+    ds.enable_fp4()
+    gc.collect()
+    assert all(x() is not None for x in first) and [x.data_ptr() for x in ds.fp4] == places
+    assert ds.bounds is not first[0]() and [n for n, _ in made] == ["block_bounds", "cache_append"]
