@@ -422,7 +422,7 @@ int32_t ssa_block_bounds(const ssa_attn_desc* desc, const ssa_blocks* blocks, co
   p.page_table_stride = pg ? pg->page_table_stride : 0; p.n_pages = pg ? pg->n_pages : 0; p.page_shift = pg ? shift_of(pg->page_size) : 0;
   // the newest n_q positions lie in that many blocks
   const long long n = (desc->max_ctx + blocks->block_size - 1ll) / blocks->block_size;
-  const long long touched = std::min(n, (blocks->n_q + blocks->block_size - 2ll) / blocks->block_size + 1);
+  const long long touched = std::min(n, (blocks->n_q - 2ll + blocks->block_size) / blocks->block_size + 1);
   const dim3 grid((unsigned)touched, (unsigned)desc->H_kv, (unsigned)desc->B);
   cudaStream_t st = (cudaStream_t)stream;
   const bool wide = desc->D == 128;

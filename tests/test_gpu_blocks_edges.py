@@ -1,4 +1,4 @@
-"""ssa_block_select over infinite bounds: the formula's scores, and the lists that follow from them."""
+"""ssa_block_bounds and ssa_block_select at their edges: infinite bounds, blocks without rows, as many tokens as 32 bits hold."""
 import numpy as np
 import pytest
 import torch
@@ -84,6 +84,15 @@ def test_a_zero_query_wants_nothing_of_an_infinity():
     check(c, 1024, 6)
     c.q[:] = 0
     check(c, 1024, 6)
+
+
+@pytest.mark.parametrize("n_q", [411, 2 ** 31 - 200, 2 ** 31 - 1])
+def test_bounds_of_more_tokens_than_there_are(n_q):
+    """As many as 32 bits hold: all blocks are made anew."""
+    c = Cache(2, 2, 411, 64, "bf16")
+    got, status = bounds_of(c, 2, [411, 100], None, n_q, 64)
+    want, _ = bounds_of(c, 2, [411, 100], None, 411, 64)
+    assert status == 0 and np.array_equal(got, want) and (got[0] != 5).any()
 
 
 def test_an_infinite_key_in_a_cache():
