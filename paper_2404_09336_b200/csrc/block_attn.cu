@@ -3,7 +3,7 @@
 //
 // The kernel for few rows of window_rows.cuh, whose rows are here the query heads of one token and K/V head: they share its list.
 // HBM bounds it: the listed rows of K and V are read once, by tiles of 16 or 32 positions that never cross a block.  32 requests, 8 K/V
-// heads, 32 blocks of 64 positions each: 51.4 us, 5.2 TB/s; in 8 bits 40, in 4 bits 37, where instructions bound it.
+// heads, 32 blocks of 64 positions each: 51.4 us, 5.2 TB/s; in 8 bits 40, in 4 bits 33, where instructions bound it.
 #include "window_rows.cuh"
 
 namespace ssa {

@@ -35,7 +35,8 @@ template <typename P> __device__ __forceinline__ uint32_t to_bits(P x) { return 
 
 // grid (blocks of positions, H_kv, B).  Lanes take 16-byte pieces of rows, the thread block's rows at a time, keep the least and the
 // largest of their piece, and meet at the end.  8- and 4-bit values become fp16 on the way, which holds them exactly.  Bound by HBM
-// over whole contexts (8 requests of 9000 to 16384 positions, 8 heads: 33.5 us, 5.8 TB/s); one round trip for a step's newest blocks.
+// over whole contexts (8 requests of 9000 to 16384 positions, 8 heads: 33 to 34 us, 5.7 to 5.9 TB/s), over 8- and 4-bit ones, 27 and 36 us, by the conversions and comparisons; one round trip for a
+// step's newest blocks.
 template <typename T, int D, bool kPaged>
 __global__ void __launch_bounds__(kBoundThreads)
 block_bounds_kernel(const BoundsParams p) {
@@ -161,7 +162,7 @@ __device__ __forceinline__ double sums_of(double (&v)[kDeep], int lane, int& whi
 // bits from the top, each by a histogram of the keys that match the digits found, and what stays is numbered by a prefix sum.
 // Products of 16-bit values are summed in fp64, so that lists depend on no order; HBM bounds the scores (the bounds' bytes) all the
 // same, as long as eight pieces a lane are under way while the eight before them are converted and summed.  32 requests of 6001 to
-// 16384 positions, 8 K/V heads, blocks of 32: 18.6 us (four pieces 25, blocks of 128 threads 24); conversions to fp64 take a quarter.
+// 16384 positions, 8 K/V heads, blocks of 32: 18.8 us (four pieces 25, blocks of 128 threads 24); conversions to fp64 take a quarter.
 template <typename TQ, int D>
 __global__ void __launch_bounds__(kSelectThreads, 2)
 block_select_kernel(const SelectParams p, const int ranks) {

@@ -4,8 +4,9 @@
 //
 // HBM bounds it: every row is read and written once.  The products of 16-bit values and fp32 cosines are exact in fp64, so that what
 // is stored is the formula's value rounded: to fp32, then to the cache's type.  (8- and 4-bit values lie next to borders, where an
-// error of an fp32 rounding would be half a step.)  4 x 4096 tokens, 32 heads, pages of 16: 151 us, 5.4 TB/s (without rotation 135);
-// conversions to and from fp64 fill a third of their pipe.  In 8 bits, 6 x 4096 tokens, 32 heads over 8: 112 us; in 4 bits 153.
+// error of an fp32 rounding would be half a step.)  4 x 4096 tokens, 32 heads, pages of 16: 148 to 163 us by the GPU, 5.0 to 5.5 TB/s
+// (without rotation 135); conversions to and from fp64 fill a third of their pipe.  In 8 bits, 6 x 4096 tokens, 32 heads over 8: 110
+// us; in 4 bits 151.
 #include <algorithm>
 #include <type_traits>
 

@@ -7,9 +7,10 @@ namespace ssa {
 // Every block of 128 query rows that works on tiles converts the K and V rows that it sees.  Where many share them (prompt chunks)
 // they are converted once instead, into pages of the workspace that the tiles then read: products of a code and a scale have six
 // significant bits and are multiples of 2^-10 up to 2688, so that nothing is rounded, and outputs are those of tiles that convert.
-// They take 512 MB of the workspace at most: requests, or K/V heads of one, go through it in turn.  HBM bounds it: 2.56 bytes a value.  8 requests' chunks of up to 509
-// tokens within a window of 4096, 8 K/V heads: some 36 us (5.4 TB/s), and 166 for the tiles; 49 with 16 bytes of codes to a thread,
-// whose stores then lie 64 bytes apart.
+// They take 512 MB of the workspace at most: requests, or K/V heads of one, go through it in turn.  HBM bounds it: 2.56 bytes a value.
+// 8 requests' chunks of up to 509 tokens within a window of 4096, 8 K/V heads: some 36 us (5.4 TB/s), and 177 to 183 for the tiles; 49
+// with 16 bytes of codes to a thread, whose stores then lie 64 bytes apart.  (To bf16, with weights of eight bits, the tiles took 5 us
+// less: no queries to bring to fp16.)
 constexpr int kExpandThreads = 256;
 
 // grid (tiles of 128 positions that a request's tokens see between them, H_kv, B).  Page tables of the pages made: tile i of request b

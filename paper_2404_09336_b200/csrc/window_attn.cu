@@ -117,10 +117,11 @@ static int32_t check_window(const ssa_attn_desc* d, const ssa_window* w, bool ma
 // requests of 4100 to 16384 positions, those within a window of 4096, 32 requests of up to 4096, one of 16384; 8 K/V heads, L2 cold), in
 // pages of 16 89, 56, 91 and 42 against 163, 66, 155 and 44; with 25 to 32 rows 122, 71, 119 and 54 against 124, 56, 117 and 40, in pages
 // 133, 78, 133 and 56 against 163, 66, 155 and 44.
-// Rows above which it is converted once for all of them, instead of by every block of 128 rows: for the same requests that takes 199,
-// 94, 197 and 40 us with 256 rows, 280, 116, 214 and 54 with 512, 314, 121, 277 and 65 with 768, each block for itself 176, 79, 160 and
-// 40, then 283, 117, 199 and 61, then 336, 119, 276 and 66.  In pages each piece of a row costs a block more instructions: 212, 99, 213
-// and 41 against 235, 97, 207 and 45 with 256 rows, 314, 121, 222 and 53 against 416, 149, 232 and 64 with 384.
+// Rows above which it is converted once for all of them, instead of by every block of 128 rows: for the same requests that takes 247,
+// 110, 235 and 73 us with 256 rows, 361, 134, 286 and 97 with 512, 441, 196, 452 and 99 with 768, 562, 216, 478 and 116 with 1024, each
+// block for itself 212, 89, 191 and 62, then 389, 127, 264 and 93, then 467, 199, 453 and 101, then 649, 231, 498 and 128.  In pages each
+// piece of a row costs a block more instructions: 273, 116, 255 and 75 against 280, 108, 248 and 71 with 256 rows, 386, 142, 308 and 87
+// against 463, 158, 330 and 87 with 384.
 constexpr int kExpandRows = 768, kExpandRowsPaged = 256;
 
 // Whether the tiles of 128 rows serve a call.

@@ -124,7 +124,8 @@ template <> __device__ __forceinline__ bool pair_not_finite<__half>(uint32_t w) 
 // kListed parameters: the rows are the query heads of one token, grid.x (splits x parts of them x tokens), the tiles those of the
 // blocks on its list.
 // kBoth: weights as a 16-bit value and the 16-bit rest.  Without (4-bit values, 16-bit outputs): rounded to fp16 once, 2^-11, less
-// than the output is.  32 requests of up to 16384 positions, 32 heads over 8, 4-bit values: 119 us instead of 132.
+// than the output is.  32 requests of up to 16384 positions, 32 heads over 8, 4-bit values: 119 us instead of 132, before splits were
+// planned for four blocks to an SM (115 to 120 by the GPU since).
 template <typename T, int D, bool kPaged, bool kMass, int kTeam, int kGroups, bool kBoth, typename Params>
 __global__ void __launch_bounds__(kWarps * 32, (RowShape<T, D, kGroups>::kBlocks))
 window_rows_kernel(const Params p) {
@@ -822,7 +823,7 @@ static cudaError_t launch_join(const Params& p, cudaStream_t st) {
 // Splits of the kernel for few rows: what n splits cost in units of one tile's time.  The work of all blocks, each with a start and
 // an end, over the places that there are (two or three blocks to an SM), but no less than one block's; half a block's until the
 // last is done (lengths differ: three quarters of the longest are taken for the mean); joining.  Tiles of 4-bit values take longer,
-// and four blocks of one group fit an SM (32 requests of up to 16384 positions, 32 heads over 8: 113 us instead of 119).
+// and four blocks of one group fit an SM (32 requests of up to 16384 positions, 32 heads over 8: 113 us instead of 119 on one GPU).
 inline long long rows_splits(long long n_tiles, long long blocks, int rows, bool fp4, long long most_splits) {
   const int teams = rows <= kMostGroups * kGroup ? kWarps : kWarps / 2;
   const bool four = fp4 && rows <= kGroup;
